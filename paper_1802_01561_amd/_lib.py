@@ -1,4 +1,4 @@
-"""ctypes declarations of the libvtrace C ABI (include/vtrace.h).
+"""ctypes declarations of the libvtrace C ABI (include/vtrace.h and vtrace_tokens.h).
 
 Loading fails loudly when the library has not been built: there is no
 fallback implementation anywhere in this package.
@@ -70,6 +70,20 @@ SIGNATURES = {
     "vtrace_error_flag": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_int32), _P]),
 }
 
+# Every symbol include/vtrace_tokens.h declares.
+_I = ctypes.c_int
+TOKEN_SIGNATURES = {
+    "vtrace_vocab_workspace_bytes": (ctypes.c_size_t, [_I64] * 4),
+    "vtrace_vocab_log_probs": (_I, [_I64] * 4 + [_P] * 8 + [ctypes.c_size_t, _P]),
+    "vtrace_vocab_grad_workspace_bytes": (ctypes.c_size_t, [_I64] * 4 + [_I]),
+    "vtrace_vocab_grad": (_I, [_I64] * 4 + [_I] + [_P] * 12 + [ctypes.c_size_t, _P]),
+    "vtrace_log_prob_workspace_bytes": (ctypes.c_size_t, [_I64] * 2),
+    "vtrace_log_prob_loss_grad": (_I, [_I64] * 2 + [_P] * 8 + [_F] * 5 + [ctypes.POINTER(Variant)] + [_P] * 7
+                                  + [ctypes.c_size_t, _P]),
+    "vtrace_clip_grad_norm": (_I, [_I64] + [_P] * 4 + [_F] + [_P] * 2 + [ctypes.c_size_t, _P]),
+}
+CLIP_WORKSPACE_BYTES = 33024  # VTRACE_CLIP_WORKSPACE_BYTES
+
 _lib = None
 
 
@@ -88,7 +102,7 @@ def lib():
             raise RuntimeError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_1802_01561_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in {**SIGNATURES, **TOKEN_SIGNATURES}.items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

@@ -1,0 +1,350 @@
+// The vocabulary layer: workspaces, launches, and the small kernels around the tiles
+// (vocab_logits.hip, vocab_products.hip) and the few-step kernel (vocab_stream.hip).
+#include "vocab_impl.hpp"
+
+namespace vtrace {
+namespace {
+
+constexpr int kListThreads = 1024;
+constexpr int kListItems = 8;  // tokens per thread and pass
+
+// active[0 .. count) = the steps with a token, in order.  One workgroup: a pass over
+// 8192 tokens counts, scans and writes.
+__global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
+  constexpr int kWaves = kListThreads / kWave;
+  __shared__ int s_count[2][kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int total = 0;
+  int flip = 0;
+  for (int64_t base = 0; base < a.N; base += kListThreads * kListItems, flip ^= 1) {
+    const int64_t first = base + static_cast<int64_t>(threadIdx.x) * kListItems;
+    int32_t token[kListItems];
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < kListItems; ++j) {
+      token[j] = first + j < a.N ? a.tokens[first + j] : kNoToken;
+      mine += token[j] != kNoToken;
+    }
+    int upto = mine;  // of this wave's lanes up to this one
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int x = __shfl_up(upto, o, kWave);
+      if (lane >= o) upto += x;
+    }
+    if (lane == kWave - 1) s_count[flip][wave] = upto;
+    __syncthreads();
+    int at = total + upto - mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int n = s_count[flip][w];
+      if (w < wave) at += n;
+      total += n;
+    }
+#pragma unroll
+    for (int j = 0; j < kListItems; ++j) {
+      if (token[j] != kNoToken) a.active[at++] = static_cast<int32_t>(first + j);
+    }
+  }
+  if (threadIdx.x == 0) *a.active_count = total;
+}
+
+// Joins the pieces' statistics: 16 steps a workgroup, 32 threads over the pieces of
+// each.  The kernel also writes the zeros of the steps without a token.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinRows = 16;
+template <bool kListed, bool kDot>
+__global__ __launch_bounds__(kJoinThreads) void vocab_join_kernel(VocabArgs a) {
+  constexpr int kParts = kJoinThreads / kJoinRows;
+  __shared__ float s_top[kParts][kJoinRows];
+  __shared__ double s_sum[kParts][kJoinRows], s_dot[kParts][kJoinRows];
+  const int r = threadIdx.x % kJoinRows, part = threadIdx.x / kJoinRows;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kJoinRows + r;
+  if constexpr (kListed) {
+    if (part == 0 && row < a.N && a.tokens[row] == kNoToken) {
+      a.log_probs[row] = 0.0f;
+      a.log_sums[row] = 0.0f;
+      if constexpr (kDot) a.entropy[row] = 0.0f;
+    }
+  }
+  const int64_t rows = kListed ? *a.active_count : a.N;
+  const bool in = row < rows;
+  float top = -INFINITY;
+  if (in) {
+#pragma unroll 8
+    for (int64_t j = part; j < a.pieces; j += kParts)
+      top = fmaxf(top, a.part_sum[j * a.row_pitch + row] == 0.0f ? -INFINITY : a.part_max[j * a.row_pitch + row]);
+  }
+  s_top[part][r] = top;
+  __syncthreads();
+#pragma unroll 8
+  for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_top[q][r]);
+  // Nothing but -inf logits (or NaN ones, which the sums carry).
+  const float c = top == -INFINITY ? 0.0f : top;
+  double sum = 0.0, dot = 0.0;
+  if (in) {
+#pragma unroll 4
+    for (int64_t j = part; j < a.pieces; j += kParts) {
+      const double d = static_cast<double>(a.part_max[j * a.row_pitch + row]) - static_cast<double>(c);
+      const double p = static_cast<double>(a.part_sum[j * a.row_pitch + row]);
+      const double e = exp2_f64(p == 0.0 ? 0.0 : d);
+      sum += e * p;
+      if constexpr (kDot) dot += e * (static_cast<double>(a.part_dot[j * a.row_pitch + row]) + p * d);
+    }
+  }
+  s_sum[part][r] = sum;
+  if constexpr (kDot) s_dot[part][r] = dot;
+  __syncthreads();
+  if (part != 0 || !in) return;
+  sum = 0.0;
+  dot = 0.0;
+#pragma unroll 8
+  for (int q = 0; q < kParts; ++q) {
+    sum += s_sum[q][r];
+    if constexpr (kDot) dot += s_dot[q][r];
+  }
+  constexpr double kLn2 = 0.6931471805599453;
+  const int64_t step = kListed ? a.active[row] : row;
+  const int32_t token = a.tokens[step];
+  if (!kListed && token == kNoToken) {
+    a.log_probs[step] = 0.0f;
+    a.log_sums[step] = 0.0f;
+    if constexpr (kDot) a.entropy[step] = 0.0f;
+    return;
+  }
+  const double log_s = log(sum);
+  const double lse = log_s + static_cast<double>(c) / static_cast<double>(kLog2eF);
+  const bool valid = token >= 0 && token < a.V;
+  if (!valid) raise_error_flag(a.error_flag);
+  a.log_sums[step] = static_cast<float>(lse);
+  a.log_probs[step] = valid ? static_cast<float>(static_cast<double>(a.token_logit[row]) - lse) : NAN;
+  if constexpr (kDot) a.entropy[step] = static_cast<float>(log_s - kLn2 * (dot / sum));
+}
+
+// vtrace_vocab_grad's operands by active step: hidden states side by side with zeros
+// behind each row's end and behind the last row (up to a whole step of 64), and the
+// scalars that the tiles' epilogue needs.  A wave a row; the same waves clear
+// d_hidden of the steps without a token.
+constexpr int kGatherThreads = 256;
+__global__ __launch_bounds__(kGatherThreads) void vocab_gather_kernel(VocabArgs a) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t row = (static_cast<int64_t>(blockIdx.x) * kGatherThreads + threadIdx.x) / kWave;
+  const int64_t count = *a.active_count;
+  const v4u zero = {0u, 0u, 0u, 0u};
+  if (row < a.N && a.tokens[row] == kNoToken) {
+    const int64_t bytes = a.H * (a.grad_bf16 ? 2 : 4);
+    char* const out = static_cast<char*>(a.d_hidden) + row * bytes;
+    for (int64_t i = lane * 16; i < bytes; i += kWave * 16) *reinterpret_cast<v4u*>(out + i) = zero;
+  }
+  if (row >= a.row_pitch) return;
+  const int64_t step = row < count ? a.active[row] : 0;
+  if (row < (count + kTileK - 1) / kTileK * kTileK) {
+    const uint16_t* const in = a.hidden + step * a.H;
+    uint16_t* const out = a.x + row * a.x_pitch;
+    for (int64_t i = lane * 8; i < a.x_pitch; i += kWave * 8)
+      *reinterpret_cast<v4u*>(out + i) =
+          row < count && i < a.H ? *reinterpret_cast<const v4u*>(in + i) : zero;
+  }
+  if (lane != 0) return;
+  float lse = 0.0f, c0 = 0.0f, c1 = 0.0f, d_lp = 0.0f;
+  int32_t token = kNoToken;
+  if (row < count) {
+    token = a.tokens[step];
+    lse = a.in_log_sums[step];
+    d_lp = a.d_log_probs[step];
+    if (token < 0 || token >= a.V) {
+      raise_error_flag(a.error_flag);
+      d_lp = NAN;
+    }
+    // G = p (c0 + c1 log p) + d_lp 1[v = a].
+    c0 = -d_lp;
+    if (a.d_entropy != nullptr) {
+      c1 = -a.d_entropy[step];
+      c0 += c1 * a.in_entropy[step];
+    }
+  }
+  const int64_t P = a.row_pitch;
+  a.row_scalars[row] = lse;
+  a.row_scalars[P + row] = c0;
+  a.row_scalars[2 * P + row] = c1;
+  a.row_scalars[3 * P + row] = d_lp;
+  a.row_scalars[4 * P + row] = __int_as_float(token);
+}
+
+// d_hidden of the active steps from the splits' sums.
+constexpr int kFinishThreads = 256;
+template <typename Out>
+__global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs a) {
+  const int64_t quads = a.H / 4;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
+  const int64_t row = i / quads, h = (i % quads) * 4;
+  if (row >= *a.active_count) return;
+  f32x4 x = *reinterpret_cast<const f32x4*>(a.h_partials + row * a.H + h);
+  for (int k = 1; k < a.splits; ++k)
+    x += *reinterpret_cast<const f32x4*>(a.h_partials + (k * a.row_pitch + row) * a.H + h);
+  Out* const out = static_cast<Out*>(a.d_hidden) + static_cast<int64_t>(a.active[row]) * a.H + h;
+  if constexpr (sizeof(Out) == 4) {
+    *reinterpret_cast<f32x4*>(out) = x;
+  } else {
+    v2u w;
+    w.x = pack_bf16x2(x[0], x[1]);
+    w.y = pack_bf16x2(x[2], x[3]);
+    *reinterpret_cast<v2u*>(out) = w;
+  }
+}
+
+// d_bias of one piece: the sums of 64 steps each, in order.
+__global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a, int64_t v_begin) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
+  if (i >= a.g_pitch || v_begin + i >= a.V) return;
+  const int64_t blocks = (static_cast<int64_t>(*a.active_count) + kWaveN - 1) / kWaveN;
+  double sum = 0.0;
+#pragma unroll 8
+  for (int64_t b = 0; b < blocks; ++b) sum += static_cast<double>(a.bias_partials[b * a.g_pitch + i]);
+  a.d_bias[v_begin + i] = static_cast<float>(sum);
+}
+
+int64_t round_up(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
+unsigned blocks_of(int64_t n, int64_t k) { return static_cast<unsigned>((n + k - 1) / k); }
+
+constexpr size_t kHeaderCountOffset = 8;  // behind the counter and the error flag
+
+// Pieces of a workspace, each on a 256-byte boundary.
+struct Carver {
+  uintptr_t base;  // an integer: sizes are asked for without a workspace
+  size_t at = kWsHeaderBytes;
+  explicit Carver(void* ws) : base(reinterpret_cast<uintptr_t>(ws)) {}
+  template <typename T>
+  T* take(int64_t n) {
+    T* const p = reinterpret_cast<T*>(base + at);
+    at = static_cast<size_t>(round_up(static_cast<int64_t>(at) + n * static_cast<int64_t>(sizeof(T)), 256));
+    return p;
+  }
+};
+
+void header(VocabArgs* a, void* ws) {
+  a->error_flag = reinterpret_cast<unsigned int*>(reinterpret_cast<uintptr_t>(ws) + kWsFlagOffset);
+  a->active_count = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderCountOffset);
+}
+
+size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
+  header(a, ws);
+  Carver c(ws);
+  a->row_pitch = p.row_pitch;
+  a->pieces = p.pieces;
+  a->active = c.take<int32_t>(a->N);
+  a->part_max = c.take<float>(p.pieces * p.row_pitch);
+  a->part_sum = c.take<float>(p.pieces * p.row_pitch);
+  a->part_dot = c.take<float>(p.pieces * p.row_pitch);
+  a->token_logit = c.take<float>(p.row_pitch);
+  return c.at;
+}
+
+size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
+  header(a, ws);
+  Carver c(ws);
+  a->row_pitch = p.row_pitch;
+  a->x_pitch = p.x_pitch;
+  a->g_pitch = p.g_pitch;
+  a->splits = p.splits;
+  a->active = c.take<int32_t>(a->N);
+  a->row_scalars = c.take<float>(5 * p.row_pitch);
+  a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
+  a->g = c.take<uint16_t>((a->grad_bf16 ? 1 : 2) * p.row_pitch * p.g_pitch);
+  a->bias_partials = c.take<float>(p.row_pitch / kWaveN * p.g_pitch);
+  a->h_partials = c.take<float>(p.splits * p.row_pitch * a->H);
+  return c.at;
+}
+
+// The kernel for few steps, against tiles of 256 steps.
+constexpr int64_t kStreamMostSteps = 64;
+
+// G of one piece takes at most this much (or one tile's columns): it is written and read
+// twice within the 256 MB Infinity Cache.
+constexpr int64_t kMostPieceBytes = int64_t(256) << 20;
+// Workgroups that d_hidden's product is split up to.
+constexpr int64_t kWantedTiles = 512;
+
+}  // namespace
+
+VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
+  VocabPlan p = {};
+  (void)H;
+  p.stream = N <= kStreamMostSteps;
+  if (p.stream) {
+    p.row_pitch = N <= 16 ? 16 : N <= 32 ? 32 : 64;
+    // 64 tokens a workgroup while that fills the GPU twice, else 16.
+    p.pieces = V >= 64 * 512 ? (V + 63) / 64 : (V + 15) / 16;
+  } else {
+    p.row_pitch = round_up(N, kTile);
+    p.pieces = 2 * ((V + kTile - 1) / kTile);
+  }
+  VocabArgs a = {};
+  a.N = N;
+  p.bytes = carve_log_probs(&a, p, nullptr);
+  return p;
+}
+
+VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
+  VocabPlan p = {};
+  p.row_pitch = round_up(N, kTile);
+  p.x_pitch = round_up(H, kTileK);
+  const int64_t all = round_up(V, kTile);
+  const int64_t fit = kMostPieceBytes / (p.row_pitch * (grad_bf16 ? 2 : 4)) / kTile * kTile;
+  const int64_t most = fit < kTile ? kTile : fit;
+  const int64_t pieces = (all + most - 1) / most;
+  p.g_pitch = round_up((all + pieces - 1) / pieces, kTile);
+  const int64_t tiles = (p.row_pitch / kTile) * ((H + kTile - 1) / kTile);
+  int64_t splits = kWantedTiles / tiles;
+  if (splits > p.g_pitch / (8 * kTileK)) splits = p.g_pitch / (8 * kTileK);
+  p.splits = static_cast<int>(splits < 1 ? 1 : splits);
+  VocabArgs a = {};
+  a.N = N;
+  a.H = H;
+  a.grad_bf16 = grad_bf16;
+  p.bytes = carve_grad(&a, p, nullptr);
+  return p;
+}
+
+void attach_vocab_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) { carve_log_probs(a, p, ws); }
+void attach_vocab_grad(VocabArgs* a, const VocabPlan& p, void* ws) { carve_grad(a, p, ws); }
+
+hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
+  hipError_t e;
+  if (!p.stream) {
+    hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  e = p.stream ? launch_vocab_stream(a, st) : launch_vocab_stats(a, st);
+  if (e != hipSuccess) return e;
+  const dim3 grid(blocks_of(a.N, kJoinRows)), block(kJoinThreads);
+  if (p.stream && a.entropy) hipLaunchKernelGGL((vocab_join_kernel<false, true>), grid, block, 0, st, a);
+  else if (p.stream) hipLaunchKernelGGL((vocab_join_kernel<false, false>), grid, block, 0, st, a);
+  else if (a.entropy) hipLaunchKernelGGL((vocab_join_kernel<true, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((vocab_join_kernel<true, false>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_grad(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
+  hipError_t e;
+  hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(vocab_gather_kernel, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)), dim3(kGatherThreads), 0,
+                     st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  for (int64_t v0 = 0; v0 < a.V; v0 += p.g_pitch) {
+    if ((e = launch_vocab_logit_grads(a, v0, st)) != hipSuccess) return e;
+    if ((e = launch_vocab_d_weight(a, v0, st)) != hipSuccess) return e;
+    if ((e = launch_vocab_d_hidden(a, v0, v0 == 0, st)) != hipSuccess) return e;
+    if (a.d_bias != nullptr) {
+      hipLaunchKernelGGL(vocab_bias_kernel, dim3(blocks_of(p.g_pitch, kFinishThreads)), dim3(kFinishThreads), 0, st, a,
+                         v0);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  const dim3 grid(blocks_of(a.N * (a.H / 4), kFinishThreads)), block(kFinishThreads);
+  if (a.grad_bf16) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(vocab_finish_kernel<float>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace vtrace

@@ -1,0 +1,429 @@
+"""The vocabulary layer's log-probabilities and gradients on the GPU against the fp64
+oracle.
+
+Tolerances, from u = 2^-24 (a float32 rounding) and 2^-8 (half a bfloat16 step):
+a logit is H exact products and a bias summed in float32, within
+  tau = (sqrt(H) + 8) u * (sum |x w| + |b|)
+of itself (the framework's bound for such sums).  A log-sum moves by at most the largest
+tau, by its terms' relative errors (an exponential, the rounding of its argument, at most
+32 + 8 float32 additions: 64 u together) and by its own rounding.  G's terms carry the
+same, and then 2^-8 (bfloat16 outputs) or 2^-16 (the pair: 2^-8 of the first's 2^-8) as
+operands; sums of K products add (sqrt(K) + 8) u.  Each is multiplied out below over the
+magnitudes of the terms.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1802_01561_amd as vt
+from oracle import tokens as ot
+
+pytestmark = pytest.mark.gpu
+
+U, HALF_BF16 = 2.0 ** -24, 2.0 ** -8
+
+
+def _batch(seed, T, B, H, V, *, bias=False, none=0.0, scale=2.0):
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn(V, H, generator=g) * scale / H ** 0.5).bfloat16()
+    tokens = torch.randint(0, V, (T, B), generator=g)
+    x = (torch.randn(T, B, H, generator=g) + 2.0 * torch.rand(T, B, 1, generator=g) * w[tokens].float()).bfloat16()
+    tokens = torch.where(torch.rand(T, B, generator=g) < none, vt.NO_TOKEN, tokens).int()
+    b = torch.randn(V, generator=g) if bias else None
+    keep = (tokens >= 0).float()
+    d_lp, d_h = torch.randn(T, B, generator=g) * keep, 0.1 * torch.randn(T, B, generator=g) * keep
+    return x, w, b, tokens, d_lp, d_h
+
+
+def _flat(x, w, b, tokens):
+    f = lambda t: None if t is None else t.double().numpy()  # noqa: E731
+    return f(x).reshape(-1, x.shape[-1]), f(w), f(b), tokens.numpy().reshape(-1)
+
+
+def _tau(x, w, b):
+    m = np.abs(x) @ np.abs(w).T
+    if b is not None:
+        m = m + np.where(np.isfinite(b), np.abs(b), 0.0)
+    return ((np.sqrt(x.shape[1]) + 8.0) * U * m).max(axis=1)
+
+
+def _gpu(*t):
+    return [None if x is None else x.cuda() for x in t]
+
+
+def _within(name, got, expect, bound):
+    got = np.asarray(got, dtype=np.float64).reshape(expect.shape)
+    bad = ~(np.abs(got - expect) <= bound)
+    if bad.any():
+        i = np.unravel_index(np.argmax(np.where(bad, np.abs(got - expect) / np.maximum(bound, 1e-300), 0)), bad.shape)
+        raise AssertionError(f"{name}: {int(bad.sum())} of {bad.size} outside; worst {i}: {got[i]!r} expected {expect[i]!r} "
+                             f"bound {np.broadcast_to(bound, bad.shape)[i]!r}")
+
+
+def _poison(ws):
+    """Nothing that an earlier call left in the workspace (behind its header) may matter."""
+    ws.tensor[256:].fill_(0xFF)
+    return ws
+
+
+def _check_log_probs(x, w, b, tokens, out):
+    f = _flat(x, w, b, tokens)
+    o = ot.vocab_log_probs(*f)
+    tau = _tau(np.where(f[3][:, None] == vt.NO_TOKEN, 0.0, f[0]), f[1], f[2])
+    use = f[3] != vt.NO_TOKEN
+    lse = np.where(use, tau + U * (64.0 + np.abs(o.log_sums)), 0.0)
+    _within("log_sums", out.log_sums.cpu(), o.log_sums, lse)
+    _within("log_probs", out.log_probs.cpu(), o.log_probs, np.where(use, 2.0 * tau + U * (64.0 + 2.0 * np.abs(o.log_probs)
+                                                                                       + np.abs(o.log_sums)), 0.0))
+    if out.entropy is not None:
+        # sum p log p: each p within tau_p of itself, each log p within tau + u |log p|
+        spread = np.sum(np.exp(o.log_pi) * np.abs(np.where(np.isfinite(o.log_pi), o.log_pi, 0.0) + o.entropy[:, None]), axis=1)
+        tol = (2.0 * tau + 64.0 * U) * (1.0 + spread) + U * (o.entropy + 64.0)
+        _within("entropy", out.entropy.cpu(), o.entropy, np.where(use, tol, 0.0))
+    return o
+
+
+FORWARD = [(1, 1, 8, 1), (1, 1, 64, 5), (3, 5, 72, 300), (16, 1, 256, 1000), (17, 1, 64, 33000), (4, 8, 136, 257),
+           (64, 1, 64, 40001), (65, 1, 64, 255), (13, 9, 200, 513), (129, 2, 128, 256), (83, 13, 1000, 1021), (300, 3, 8, 2000)]
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("T,B,H,V", FORWARD)
+def test_log_probs(T, B, H, V, bias):
+    x, w, b, tokens, _, _ = _batch(T * 7 + V, T, B, H, V, bias=bias, none=0.2)
+    xd, wd, bd, td = _gpu(x, w, b, tokens)
+    ws = _poison(vt.VocabWorkspace(T, B, V, H))
+    out = vt.vtrace_vocab_log_probs(xd, wd, bd, td, workspace=ws)
+    _check_log_probs(x, w, b, tokens, out)
+    plain = vt.vtrace_vocab_log_probs(xd, wd, bd, td, with_entropy=False)
+    assert plain.entropy is None
+    _check_log_probs(x, w, b, tokens, plain)
+    assert vt.vtrace_error_flag(ws) == 0
+
+
+@pytest.mark.parametrize("N", [3, 40, 200])
+def test_log_probs_special_rows(N):
+    """Steps without a token hold anything; ruled-out tokens; tokens outside the vocabulary."""
+    H, V = 72, 700
+    x, w, b, tokens, _, _ = _batch(N, N, 1, H, V, bias=True)
+    tokens[0] = vt.NO_TOKEN
+    x[0] = float("nan")
+    b[100:400], b[500], b[501], b[502] = -float("inf"), -1.7e38, -torch.finfo(torch.float32).max, -2e37
+    ruled_out = b < -1e37
+    b64 = torch.where(ruled_out, torch.tensor(-float("inf")), b)
+    tokens = torch.where(tokens >= 0, torch.where(ruled_out[tokens.long().clamp(min=0)], 3, tokens), tokens).int()
+    tokens[2] = V  # outside
+    ws = _poison(vt.VocabWorkspace(N, 1, V, H))
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, b, tokens), workspace=ws)
+    assert torch.isnan(out.log_probs[2]).all() and vt.vtrace_error_flag(ws) == 1
+    assert out.log_probs[0, 0] == 0 and out.log_sums[0, 0] == 0 and out.entropy[0, 0] == 0
+    valid = torch.ones(N, dtype=torch.bool)
+    valid[2] = False
+    pick = lambda o: vt.VocabLogProbs(*(t[valid.cuda()] for t in o))  # noqa: E731
+    _check_log_probs(x[valid], w, b64, tokens[valid], pick(out))
+    # a token that is ruled out has probability 0
+    tokens[2] = 500
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, b, tokens))
+    assert out.log_probs[2, 0] == -float("inf") and torch.isfinite(out.log_sums[2, 0])
+
+
+@pytest.mark.parametrize("N", [5, 100])
+def test_log_probs_of_nothing(N):
+    H, V = 64, 300
+    x, w, _, tokens, _, _ = _batch(1, N, 1, H, V)
+    none = torch.full_like(tokens, vt.NO_TOKEN)
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, None, none))
+    assert not any(t.any() for t in out)
+    # every token ruled out
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, torch.full((V,), -float("inf")), tokens))
+    assert torch.isneginf(out.log_sums).all() and torch.isnan(out.log_probs).all() and torch.isnan(out.entropy).all()
+    # one step with a NaN: its own outputs alone
+    x[1] = float("nan")
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, None, tokens))
+    bad = torch.isnan(out.log_probs).cpu()
+    assert bad[1].all() and bad.sum() == 1
+
+
+@pytest.mark.parametrize("N", [4, 90])
+def test_log_probs_of_large_and_peaked_logits(N):
+    H, V = 64, 1500
+    x, w, b, tokens, _, _ = _batch(2, N, 1, H, V, scale=40.0)
+    _check_log_probs(x, w, b, tokens, vt.vtrace_vocab_log_probs(*_gpu(x, w, b, tokens)))
+    b = torch.full((V,), 3e4)
+    b[7:] = -3e4
+    tokens[:] = 3
+    _check_log_probs(x, w, b, tokens, vt.vtrace_vocab_log_probs(*_gpu(x, w, b, tokens)))
+
+
+def _check_grad(x, w, b, tokens, d_lp, d_h, out, dtype):
+    f = _flat(x, w, b, tokens)
+    g = lambda t: None if t is None else t.double().numpy().reshape(-1)  # noqa: E731
+    o = ot.vocab_grad(*f, g(d_lp), g(d_h))
+    fwd = ot.vocab_log_probs(*f)
+    use = f[3] != vt.NO_TOKEN
+    rows = np.where(use[:, None], f[0], 0.0)
+    tau = _tau(rows, f[1], f[2])
+    log_pi = np.where(np.isfinite(fwd.log_pi), fwd.log_pi, 0.0)
+    p = np.exp(fwd.log_pi)
+    c1 = np.abs(g(d_h)) if d_h is not None else np.zeros(len(use))
+    # p (c0 + c1 log p) + d 1[a]: p within tau + u (|log p| + |log-sum| + 4) of itself, the factor within its roundings
+    slope = np.abs(g(d_lp))[:, None] + c1[:, None] * (np.abs(log_pi) + fwd.entropy[:, None])
+    rel = tau[:, None] + U * (np.abs(log_pi) + np.abs(fwd.log_sums)[:, None] + 8.0)
+    d_g = np.where(use[:, None], p * (slope * (rel + 4.0 * U) + c1[:, None] * rel), 0.0) + U * np.abs(o.g)
+    wide = dtype == torch.float32
+    operand, stored = (HALF_BF16 ** 2, U) if wide else (HALF_BF16, HALF_BF16)
+    mag = np.abs(o.g)
+    N, V = mag.shape
+
+    def bound(sum_of, k, value):
+        return (sum_of(d_g) + (operand + (np.sqrt(k) + 8.0) * U) * sum_of(mag + d_g)) * (1.0 + stored) + stored * np.abs(value)
+
+    _within("d_hidden", out.d_hidden.float().cpu(), o.d_hidden, bound(lambda m: m @ np.abs(f[1]), V, o.d_hidden) + 1e-37)
+    _within("d_weight", out.d_weight.float().cpu(), o.d_weight, bound(lambda m: m.T @ np.abs(rows), N, o.d_weight) + 1e-37)
+    if out.d_bias is not None:
+        _within("d_bias", out.d_bias.cpu(), o.d_bias,
+                d_g.sum(0) + 80.0 * U * (mag + d_g).sum(0) + U * np.abs(o.d_bias) + 1e-37)
+    idle = torch.from_numpy(~use).view(tokens.shape)
+    assert not out.d_hidden[idle.cuda()].any()
+
+
+def _grad_inputs(x, w, b, tokens):
+    """What the forward call returned, here the oracle's rounded to float32."""
+    o = ot.vocab_log_probs(*_flat(x, w, b, tokens))
+    return [torch.from_numpy(v).float().view(tokens.shape) for v in (o.log_sums, o.entropy)]
+
+
+GRAD = [(1, 1, 8, 1), (1, 1, 64, 5), (5, 3, 72, 300), (20, 2, 256, 1000), (64, 1, 64, 255), (65, 1, 320, 257), (13, 9, 200, 513),
+        (257, 1, 264, 600), (83, 13, 1000, 777), (300, 3, 8, 2000)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bias,entropy,none", [(False, False, 0.0), (True, True, 0.3)])
+@pytest.mark.parametrize("T,B,H,V", GRAD)
+def test_grad(T, B, H, V, bias, entropy, none, dtype):
+    x, w, b, tokens, d_lp, d_h = _batch(T * 5 + V, T, B, H, V, bias=bias, none=none)
+    ls, ent = _grad_inputs(x, w, b, tokens)
+    d_h = d_h if entropy else None
+    ws = _poison(vt.VocabWorkspace(T, B, V, H, grad_dtype=dtype))
+    args = _gpu(x, w, b, tokens, ls, ent, d_lp, d_h)
+    out = vt.vtrace_vocab_grad(*args, grad_dtype=dtype, workspace=ws)
+    assert (out.d_bias is not None) == bias and out.d_hidden.dtype == out.d_weight.dtype == dtype
+    _check_grad(x, w, b, tokens, d_lp, d_h, out, dtype)
+    again = vt.vtrace_vocab_grad(*args, grad_dtype=dtype, workspace=ws)
+    assert all(p is None or torch.equal(p, q) for p, q in zip(out, again))
+    assert vt.vtrace_error_flag(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_grad_special_rows(dtype):
+    """What steps without a token hold reaches nothing; ruled-out tokens get no gradient."""
+    T, B, H, V = 90, 3, 72, 700
+    x, w, b, tokens, d_lp, d_h = _batch(11, T, B, H, V, bias=True, none=0.4)
+    b[100:400], b[650] = -float("inf"), -torch.finfo(torch.float32).max
+    ruled_out = b < -1e37
+    tokens = torch.where(ruled_out[tokens.long().clamp(min=0)] & (tokens >= 0), 3, tokens).int()
+    b64 = torch.where(ruled_out, torch.tensor(-float("inf")), b)
+    ls, ent = _grad_inputs(x, w, b64, tokens)
+    idle = tokens == vt.NO_TOKEN
+    clean = [x, ls, ent, d_lp, d_h]
+    dirty = [t.clone() for t in clean]
+    for t in dirty:
+        t[idle] = float("nan")
+    out = vt.vtrace_vocab_grad(*_gpu(dirty[0], w, b, tokens, *dirty[1:]), grad_dtype=dtype)
+    _check_grad(x, w, b64, tokens, d_lp, d_h, out, dtype)
+    assert not out.d_weight[ruled_out.cuda()].any() and not out.d_bias[ruled_out.cuda()].any()
+    # no step with a token at all
+    out = vt.vtrace_vocab_grad(*_gpu(dirty[0], w, b, torch.full_like(tokens, vt.NO_TOKEN), *dirty[1:]), grad_dtype=dtype)
+    assert not any(t.any() for t in out)
+    # a token outside the vocabulary: its step, the layer, and the flag
+    tokens[5, 1] = -7
+    ws = vt.VocabWorkspace(T, B, V, H, grad_dtype=dtype)
+    out = vt.vtrace_vocab_grad(*_gpu(dirty[0], w, b, tokens, *clean[1:]), grad_dtype=dtype, workspace=ws)
+    bad = torch.isnan(out.d_hidden).all(-1).cpu()
+    assert bad[5, 1] and bad.sum() == 1 and torch.isnan(out.d_weight[0]).all() and vt.vtrace_error_flag(ws) == 1
+
+
+def test_the_same_token_in_every_step():
+    x, w, b, tokens, d_lp, d_h = _batch(12, 150, 2, 64, 400)
+    tokens[:] = 399
+    ls, ent = _grad_inputs(x, w, b, tokens)
+    _check_grad(x, w, b, tokens, d_lp, d_h, vt.vtrace_vocab_grad(*_gpu(x, w, b, tokens, ls, ent, d_lp, d_h)), torch.float32)
+
+
+def test_grad_is_the_difference_quotient():
+    """Of the fp64 objective along random directions, from the kernels' float32 gradients."""
+    x, w, b, tokens, d_lp, d_h = _batch(13, 40, 2, 64, 500, bias=True)
+    ls, ent = _grad_inputs(x, w, b, tokens)
+    out = vt.vtrace_vocab_grad(*_gpu(x, w, b, tokens, ls, ent, d_lp, d_h))
+    fx, fw, fb, ft = _flat(x, w, b, tokens)
+    g, h = d_lp.double().numpy().reshape(-1), d_h.double().numpy().reshape(-1)
+
+    def objective(x, w, b):
+        o = ot.vocab_log_probs(x, w, b, ft)
+        return np.sum(g * o.log_probs) + np.sum(h * o.entropy)
+
+    r = np.random.default_rng(1)
+    for i, (arr, grad) in enumerate([(fx, out.d_hidden.cpu().double().numpy().reshape(fx.shape)),
+                                     (fw, out.d_weight.cpu().double().numpy()), (fb, out.d_bias.cpu().double().numpy())]):
+        d = r.normal(size=arr.shape)
+        eps = 1e-5
+        args = [fx, fw, fb]
+        up, down = list(args), list(args)
+        up[i], down[i] = arr + eps * d, arr - eps * d
+        q = (objective(*up) - objective(*down)) / (2 * eps)
+        # float32 gradients: 2^-16 of the terms' magnitudes; the quotient itself to eps^2
+        assert abs(q - np.sum(grad * d)) <= 2.0 ** -14 * np.sum(np.abs(grad * d)) + 1e-6
+
+
+def test_pieces_of_the_vocabulary_and_splits():
+    """A G of 2.2 GB (float32 outputs: a pair): several pieces, the last one odd.  The
+    reference is the same formulas in float64 on the GPU."""
+    T, B, H, V = 1030, 2, 64, 65537 + 70
+    x, w, _, tokens, d_lp, d_h = _batch(14, T, B, H, V)
+    xd, wd, td, gd, hd = (t.cuda() for t in (x, w, tokens, d_lp, d_h))
+    fwd = vt.vtrace_vocab_log_probs(xd, wd, None, td)
+    out = vt.vtrace_vocab_grad(xd, wd, None, td, fwd.log_sums, fwd.entropy, gd, hd)
+    X, W = xd.view(-1, H).double(), wd.double()
+    z = X @ W.t()
+    lse = torch.logsumexp(z, 1)
+    lp = z - lse.unsqueeze(1)
+    p = lp.exp()
+    a = td.view(-1, 1).long()
+    # as in _check_log_probs
+    tau = ((H ** 0.5 + 8.0) * U * (X.abs() @ W.abs().t())).amax(1)
+    assert ((fwd.log_sums.view(-1).double() - lse).abs() <= tau + U * (64.0 + lse.abs())).all()
+    e = -(p * lp).sum(1)
+    g, h = gd.view(-1, 1).double(), hd.view(-1, 1).double()
+    G = -g * p - h * p * (lp + e.unsqueeze(1))
+    G.scatter_add_(1, a, g)
+    # G's terms from the kernels' own log-sums and entropies: their errors enter as p's relative one
+    rel = (2.0 * tau + U * 128.0).unsqueeze(1) + U * (lp.abs() + 8.0)
+    dG = p * (g.abs() + h.abs() * (lp.abs() + e.unsqueeze(1) + 1.0)) * rel * 2.0
+    mag = G.abs() + dG
+    for got, ref, terms, k in ((out.d_hidden.view(-1, H), G @ W, (dG + (2.0 ** -16 + (V ** 0.5 + 8) * U) * mag) @ W.abs(), V),
+                               (out.d_weight, G.t().contiguous() @ X,
+                                (dG + (2.0 ** -16 + ((T * B) ** 0.5 + 8) * U) * mag).t().contiguous() @ X.abs(), T * B)):
+        assert ((got.double() - ref).abs() <= terms + U * ref.abs()).all()
+
+
+def test_offsets_beyond_32_bits():
+    """A layer of 4.8 GB: the last tokens lie beyond 2^32 bytes."""
+    H, V = 4096, 590000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.empty((V, H), dtype=torch.bfloat16, device="cuda")
+    for at in range(0, V, 1 << 16):
+        n = min(1 << 16, V - at)
+        w[at:at + n] = (torch.randn((n, H), generator=g, device="cuda") * 0.03).bfloat16()
+    for N in (3, 70):
+        x = torch.randn((N, 1, H), generator=g, device="cuda").bfloat16()
+        tokens = torch.randint(V - 1000, V, (N, 1), generator=g, device="cuda").int()
+        tokens[0] = 0
+        out = vt.vtrace_vocab_log_probs(x, w, None, tokens)
+        z = torch.cat([x.view(N, H).double() @ w[at:at + (1 << 16)].double().t() for at in range(0, V, 1 << 16)], 1)
+        lse = torch.logsumexp(z, 1)
+        tau = (H ** 0.5 + 8.0) * U * (x.view(N, H).double().abs().sum(1) * w.abs().max().double())
+        za = z.gather(1, tokens.long()).squeeze(1)
+        assert ((out.log_sums.view(-1).double() - lse).abs() <= tau + U * (64 + lse.abs())).all()
+        assert ((out.log_probs.view(-1).double() - (za - lse)).abs() <= 2 * tau + U * (64 + 4 * lse.abs())).all()
+        if N == 70:
+            d = torch.ones((N, 1), device="cuda")
+            grad = vt.vtrace_vocab_grad(x, w, None, tokens, out.log_sums, None, d, grad_dtype=torch.bfloat16)
+            for v in (0, 12345, V - 1, int(tokens[5]), int(tokens[69])):
+                G = (tokens.view(-1) == v).double() - torch.exp(z[:, v] - lse)
+                ref = G @ x.view(N, H).double()
+                bound = (HALF_BF16 + 1e-4) * (G.abs() @ x.view(N, H).double().abs()) + HALF_BF16 * ref.abs() + 1e-37
+                assert ((grad.d_weight[v].double() - ref).abs() <= bound * 1.01).all()
+            del grad
+
+
+def test_captured_calls_replay():
+    """Forward, gradients and clipping captured into one graph, replayed on new inputs between eager calls."""
+    T, B, H, V = 90, 2, 64, 1000
+    x, w, b, tokens, d_lp, d_h = _gpu(*_batch(15, T, B, H, V, bias=True, none=0.2))
+    fw, gw, cw = vt.VocabWorkspace(T, B, V, H), vt.VocabWorkspace(T, B, V, H, grad_dtype=torch.float32), vt.ClipWorkspace()
+
+    def step():
+        o = vt.vtrace_vocab_log_probs(x, w, b, tokens, workspace=fw)
+        g = vt.vtrace_vocab_grad(x, w, b, tokens, o.log_sums, o.entropy, d_lp, d_h, workspace=gw)
+        n = vt.vtrace_clip_grad_norm(list(g), 0.5, workspace=cw)
+        return [*o, *g, n]
+
+    step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in (21, 22, 23):
+        new = _batch(seed, T, B, H, V, bias=True, none=0.3)
+        for t, n in zip((x, w, b, tokens, d_lp, d_h), new):
+            t.copy_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        for p, q in zip(got, step()):
+            assert torch.equal(p, q)
+
+
+def test_other_streams_and_strided_inputs():
+    T, B, H, V = 50, 3, 64, 900
+    x, w, b, tokens, d_lp, d_h = _gpu(*_batch(16, T, B, H, V, bias=True))
+    base = vt.vtrace_vocab_log_probs(x, w, b, tokens)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o = vt.vtrace_vocab_log_probs(x, w, b, tokens, stream=s)
+    g = vt.vtrace_vocab_grad(x, w, b, tokens, o.log_sums, o.entropy, d_lp, d_h, stream=s)
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(base, o))
+    assert all(torch.equal(p, q) for p, q in zip(g, vt.vtrace_vocab_grad(x, w, b, tokens, *base[1:], d_lp, d_h)))
+    with pytest.raises(ValueError, match="contiguous"):
+        vt.vtrace_vocab_log_probs(x.transpose(0, 1), w, b, tokens.t())
+    with pytest.raises(ValueError, match="contiguous"):
+        vt.vtrace_vocab_log_probs(x, w.t().contiguous().t(), b, tokens)
+    with pytest.raises(ValueError, match="expected"):
+        vt.vtrace_vocab_log_probs(x, w.cpu(), b, tokens)
+    with pytest.raises(TypeError):
+        vt.vtrace_vocab_log_probs(x.float(), w, b, tokens)
+    with pytest.raises(TypeError, match="VocabWorkspace"):
+        vt.vtrace_vocab_log_probs(x, w, b, tokens, workspace=vt.ClipWorkspace())
+    with pytest.raises(vt.VtraceError, match="WORKSPACE"):
+        vt.vtrace_vocab_log_probs(x, w, b, tokens, workspace=vt.VocabWorkspace(1, 1, V, H))
+    with pytest.raises(vt.VtraceError, match="SHAPE"):
+        vt.vtrace_vocab_log_probs(x[..., :60].contiguous(), w[:, :60].contiguous(), b, tokens,
+                                  workspace=vt.VocabWorkspace(T, B, V, H))
+
+
+def test_nothing_is_written_outside_the_outputs():
+    T, B, H, V = 77, 1, 72, 300
+    x, w, b, tokens, d_lp, d_h = _gpu(*_batch(17, T, B, H, V, bias=True, none=0.2))
+
+    def guarded(shape, dtype):
+        n = int(np.prod(shape))
+        whole = torch.full((n + 1024,), 7.0, dtype=dtype, device="cuda")
+        return whole, whole[512:512 + n].view(shape)
+
+    def intact(whole):
+        return (whole[:512] == 7).all() and (whole[-512:] == 7).all()
+
+    for N in (T, 9):
+        cut = [t[:N].contiguous() for t in (x, tokens, d_lp, d_h)]
+        outs = [guarded((N, B), torch.float32) for _ in range(3)]
+        ws, wv = guarded((vt.vtrace_vocab_workspace_bytes(N, B, V, H),), torch.uint8)
+        work = vt.VocabWorkspace(N, B, V, H)
+        work.tensor = wv
+        wv.zero_()
+        o = vt.vtrace_vocab_log_probs(cut[0], w, b, cut[1], out=vt.VocabLogProbs(*(v for _, v in outs)), workspace=work)
+        assert all(intact(t) for t, _ in outs) and intact(ws)
+        for dtype in (torch.float32, torch.bfloat16):
+            grads = [guarded((N, B, H), dtype), guarded((V, H), dtype), guarded((V,), torch.float32)]
+            ws, wv = guarded((vt.vtrace_vocab_grad_workspace_bytes(N, B, V, H, dtype),), torch.uint8)
+            work = vt.VocabWorkspace(N, B, V, H, grad_dtype=dtype)
+            work.tensor = wv
+            wv.zero_()
+            vt.vtrace_vocab_grad(cut[0], w, b, cut[1], o.log_sums, o.entropy, cut[2], cut[3], grad_dtype=dtype,
+                                 out=vt.VocabGrad(*(v for _, v in grads)), workspace=work)
+            assert all(intact(t) for t, _ in grads) and intact(ws)
