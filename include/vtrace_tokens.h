@@ -122,7 +122,7 @@ vtrace_status vtrace_vocab_grad(
  *   vs, pg_advantages  optional [T,B] float32
  *   workspace    vtrace_log_prob_workspace_bytes(T,B) bytes, 16-byte aligned, cleared
  *                once by vtrace_workspace_init
- * T*B <= 2^40, B <= 2^27.  Ratios, recursion and loss sums are float64.
+ * T*B <= 2^40, B <= 2^22.  Ratios, recursion and loss sums are float64.
  */
 size_t vtrace_log_prob_workspace_bytes(int64_t T, int64_t B);
 

@@ -118,6 +118,12 @@ class _FastCall:
         self.targets, self.loss, self.head = (
             ctypes.cast(f, ctypes.c_void_p).value
             for f in (L.vtrace_targets_ex, L.vtrace_loss_grad_ex, L.vtrace_head_loss_grad))
+        self.call_vocab_log_probs, self.call_vocab_grad, self.call_log_prob_loss, self.call_clip = (
+            _fast_call.vocab_log_probs, _fast_call.vocab_grad, _fast_call.log_prob_loss, _fast_call.clip)
+        self.vocab_log_probs, self.vocab_grad, self.log_prob_loss, self.clip = (
+            ctypes.cast(f, ctypes.c_void_p).value
+            for f in (L.vtrace_vocab_log_probs, L.vtrace_vocab_grad, L.vtrace_log_prob_loss_grad,
+                      L.vtrace_clip_grad_norm))
         self.device, self.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 

@@ -21,9 +21,19 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kSteps = 8;      // consecutive steps of a thread
+constexpr int kSteps = 4;       // consecutive steps of a thread
 constexpr int kMostLanes = 16;  // of a workgroup
 constexpr int64_t kWantedGroups = 1024;
+constexpr double kLog2e = 1.4426950408889634;
+
+// Raw buffers: loads beyond the end give 0, stores there are dropped.
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+constexpr int kRawBufferFlags = 0x00020000;
+constexpr uint32_t kOutOfRange = 0x80000000u;
+__device__ __forceinline__ Rsrc make_rsrc(const void* base, int64_t bytes) {
+  const int64_t n = bytes < 0x7fffffff ? bytes : 0x7fffffff;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(n), kRawBufferFlags);
+}
 
 struct Map {
   double a, b;  // x -> a x + b
@@ -74,7 +84,10 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
   const int64_t id = xcd_tile(blockIdx.x, groups * args.chunks);
   const int64_t chunk = id / groups;
   const int q = threadIdx.x / kLanes;
-  const int64_t b = (id % groups) * kLanes + threadIdx.x % kLanes;
+  const uint32_t l = threadIdx.x % kLanes;
+  const int64_t b0 = (id % groups) * kLanes;
+  const int64_t b = b0 + l;
+  const uint32_t stride = static_cast<uint32_t>(a.B);
   const bool lane_ok = b < a.B;
   int64_t n = 0;  // steps of this lane
   double boot = 0.0;
@@ -87,6 +100,15 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
     boot = static_cast<double>(a.bootstrap_value[b]);
   }
   const double lam = a.lambda, rho_bar = a.rho_bar, c_bar = a.c_bar;
+  const bool weighted = a.correction == kCorrVtrace, weighted_pg = weighted || a.correction == kCorrOneStepIs;
+  // variant_weights with the choices made once.
+  auto weights = [&](double ratio) {
+    const double rho = clip_above(ratio, rho_bar);
+    return StepWeights{weighted ? rho : 1.0, lam * (weighted ? clip_above(ratio, c_bar) : 1.0), weighted_pg ? rho : 1.0};
+  };
+  auto step_of = [](const StepWeights& w, double diff, float g, bool in) {  // x -> delta + gamma c x
+    return Map{in ? static_cast<double>(g) * w.c_v : 0.0, in ? w.rho_v * diff : 0.0};
+  };
 
   double x_end = 0.0;  // x at the first step behind the tile
   if (kFinish && args.chunks > 1) {
@@ -111,67 +133,81 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
   Map composite = {1.0, 0.0};
   double sum_pg = 0.0, sum_base = 0.0, sum_ent = 0.0;
   for (int64_t tile = last_tile - 1; tile >= first_tile; --tile) {
-    const int64_t t0 = tile * kTileSteps + static_cast<int64_t>(q) * kSteps;
-    const int64_t at = t0 * a.B + b;
+    const int64_t t0 = tile * kTileSteps + q * kSteps;
+    // The tile's place in the arrays (uniform), and this thread's steps in it.  A step that
+    // is not a lane's own is read and written out of range: it reads 0 and writes nothing.
+    const int64_t corner = tile * kTileSteps * a.B + b0;
+    const int64_t left = 4 * (a.T * a.B - corner);
+    auto array = [&](const void* p) { return make_rsrc(p ? static_cast<const float*>(p) + corner : p, p ? left : 0); };
+    auto read = [](Rsrc p, uint32_t o) { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(p, o, 0, 0)); };
+    const uint32_t at = 4 * (static_cast<uint32_t>(q * kSteps) * stride + l);
+    const Rsrc p_lp = array(args.target), p_lm = array(args.behaviour), p_r = array(a.rewards), p_g = array(a.discounts),
+               p_v = array(a.values);
     float lp[kSteps], lm[kSteps], r[kSteps], gm[kSteps], v[kSteps + 1];
+    uint32_t off[kSteps];
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-      const bool in = t0 + j < n;
-      const int64_t i = at + j * a.B;
-      lp[j] = in ? args.target[i] : 0.0f;
-      lm[j] = in ? args.behaviour[i] : 0.0f;
-      r[j] = in ? a.rewards[i] : 0.0f;
-      gm[j] = in ? a.discounts[i] : 0.0f;
-      v[j] = in ? a.values[i] : 0.0f;
+      off[j] = t0 + j < n ? at + 4 * j * stride : kOutOfRange;
+      lp[j] = read(p_lp, off[j]);
+      lm[j] = read(p_lm, off[j]);
+      r[j] = read(p_r, off[j]);
+      gm[j] = read(p_g, off[j]);
+      v[j] = read(p_v, off[j]);
     }
-    v[kSteps] = t0 + kSteps < n ? a.values[at + kSteps * a.B] : 0.0f;
-    double delta[kSteps], decay[kSteps];
-    StepWeights w[kSteps];
+    v[kSteps] = read(p_v, t0 + kSteps < n ? at + 4 * kSteps * stride : kOutOfRange);
+    if (a.reward_transform != 0) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) r[j] = transform_reward(r[j], a.reward_transform);
+    }
+    // Of each step: the ratio, and the temporal difference before its weight.
+    double ratio[kSteps], diff[kSteps];
     Map mine = {1.0, 0.0};
 #pragma unroll
     for (int j = kSteps - 1; j >= 0; --j) {
       const bool in = t0 + j < n;
-      const double ratio = exp2_f64((static_cast<double>(lp[j]) - static_cast<double>(lm[j])) * 1.4426950408889634);
-      w[j] = variant_weights(a.correction, clip_above(ratio, rho_bar), lam * clip_above(ratio, c_bar), lam, true);
+      ratio[j] = exp2_f64((static_cast<double>(lp[j]) - static_cast<double>(lm[j])) * kLog2e);
       const double v_next = t0 + j + 1 == n ? boot : static_cast<double>(v[j + 1]);
-      const double reward = transform_reward(r[j], a.reward_transform), g = gm[j], V = v[j];
-      delta[j] = in ? w[j].rho_v * (reward + g * v_next - V) : 0.0;
-      decay[j] = in ? g * w[j].c_v : 0.0;
-      mine = after({decay[j], delta[j]}, mine);
+      diff[j] = static_cast<double>(r[j]) + gm[j] * v_next - v[j];
+      mine = after(step_of(weights(ratio[j]), diff[j], gm[j], in), mine);
     }
     Map all;
     const Map behind = s_scan.behind(mine, &all);
     if constexpr (!kFinish) {
       composite = after(all, composite);
     } else {
+      const Rsrc o_lp = array(args.d_log_probs), o_v = array(a.d_values), o_h = array(args.d_entropy), o_vs = array(a.vs),
+                 o_adv = array(a.pg_adv), p_h = array(args.entropy);
+      auto write = [](Rsrc p, uint32_t o, float value) {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), p, o, 0, 0);
+      };
+      float entropy[kSteps];
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) entropy[j] = read(p_h, off[j]);
       double x = fma(behind.a, x_end, behind.b);
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {
-        const int64_t t = t0 + j;
-        const bool in = t < n;
-        const double v_next = t + 1 == n ? boot : static_cast<double>(v[j + 1]);
-        const double V = v[j], g = gm[j], reward = transform_reward(r[j], a.reward_transform);
-        const double q_next = a.q_estimate == kQBaseline ? v_next : v_next + x;
-        const double adv = in ? w[j].rho_pg * (reward + g * q_next - V) : 0.0;
-        x = fma(decay[j], x, delta[j]);
-        if (t >= a.T || !lane_ok) continue;
-        const int64_t i = at + j * a.B;
-        double d_lp = -adv, log_p = lp[j];
+        const bool in = t0 + j < n;
+        const StepWeights w = weights(ratio[j]);
+        const double behind_x = a.q_estimate == kQBaseline ? 0.0 : x;
+        const double adv = in ? w.rho_pg * fma(static_cast<double>(gm[j]), behind_x, diff[j]) : 0.0;
+        const Map m = step_of(w, diff[j], gm[j], in);
+        x = fma(m.a, x, m.b);
+        double d_lp = adv, log_p = lp[j];
         if (a.correction == kCorrEpsilon) {
-          const double p = exp2_f64(log_p * 1.4426950408889634), eps = a.epsilon;
+          const double p = exp2_f64(log_p * kLog2e), eps = a.epsilon;
           d_lp *= p / (p + eps);
           log_p = log(p + eps);
         }
-        args.d_log_probs[i] = in ? static_cast<float>(d_lp) : 0.0f;
-        a.d_values[i] = in ? static_cast<float>(-a.baseline_cost * x) : 0.0f;
-        if (args.d_entropy) args.d_entropy[i] = in ? -a.entropy_cost : 0.0f;
-        if (a.vs) a.vs[i] = in ? static_cast<float>(V + x) : 0.0f;
-        if (a.pg_adv) a.pg_adv[i] = static_cast<float>(adv);
-        if (in) {
-          sum_pg -= adv * log_p;
-          sum_base += 0.5 * x * x;
-          if (args.entropy) sum_ent -= static_cast<double>(args.entropy[i]);
-        }
+        sum_pg -= in ? adv * log_p : 0.0;
+        sum_base += 0.5 * x * x;
+        sum_ent -= static_cast<double>(entropy[j]);
+        // Steps behind a lane's last get zeros.
+        const uint32_t o = t0 + j < a.T && lane_ok ? at + 4 * j * stride : kOutOfRange;
+        write(o_lp, o, in ? static_cast<float>(-d_lp) : 0.0f);
+        write(o_v, o, in ? static_cast<float>(-a.baseline_cost * x) : 0.0f);
+        write(o_h, o, in ? -a.entropy_cost : 0.0f);
+        write(o_vs, o, in ? static_cast<float>(v[j] + x) : 0.0f);
+        write(o_adv, o, static_cast<float>(adv));
       }
       x_end = fma(all.a, x_end, all.b);
     }
@@ -187,15 +223,20 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
   }
 }
 
-int lanes_of(int64_t B) {
+// Lanes of a workgroup: as many as there are, up to 16; fewer (down to 4) where the unroll
+// then fits one tile, so that one launch does.
+int lanes_of(int64_t T, int64_t B) {
   int n = 1;
   while (n < kMostLanes && n < B) n *= 2;
+  if (B < kMostLanes * kWantedGroups)
+    for (int m = n; m >= 4; m /= 2)
+      if (T <= kThreads / m * kSteps) return m;
   return n;
 }
 
 // Chunks: as many as give kWantedGroups workgroups, none shorter than a tile.
 void split_time(int64_t T, int64_t B, int64_t* chunks, int64_t* chunk_tiles, int64_t* groups) {
-  const int64_t lanes = lanes_of(B), steps = kThreads / lanes * kSteps;
+  const int64_t lanes = lanes_of(T, B), steps = kThreads / lanes * kSteps;
   const int64_t tiles = (T + steps - 1) / steps;
   *groups = (B + lanes - 1) / lanes;
   int64_t want = (kWantedGroups + *groups - 1) / *groups;
@@ -238,7 +279,7 @@ void attach_log_prob_workspace(LogProbArgs* a, void* ws) {
 }
 
 hipError_t launch_log_prob_loss(const LogProbArgs& a, hipStream_t st) {
-  switch (lanes_of(a.step.B)) {
+  switch (lanes_of(a.step.T, a.step.B)) {
     case 1: return launch<1>(a, st);
     case 2: return launch<2>(a, st);
     case 4: return launch<4>(a, st);

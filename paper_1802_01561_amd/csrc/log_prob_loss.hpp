@@ -10,7 +10,8 @@
 
 namespace vtrace {
 
-constexpr int64_t kLogProbMaxLanes = int64_t(1) << 27;
+// A tile's steps are addressed with 31-bit byte offsets.
+constexpr int64_t kLogProbMaxLanes = int64_t(1) << 22;
 
 struct LogProbArgs {
   // T, B, the inputs and outputs that a loss call shares, and the workspace's counter

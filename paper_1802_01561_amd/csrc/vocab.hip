@@ -48,48 +48,71 @@ __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
   if (threadIdx.x == 0) *a.active_count = total;
 }
 
-// Joins the pieces' statistics: 16 steps a workgroup, 32 threads over the pieces of
-// each.  The kernel also writes the zeros of the steps without a token.
+// A step's outputs from the joined statistics: sums of 2^d and of 2^d d, d = z log2 e - c.
+template <bool kDot>
+__device__ __forceinline__ void store_step(const VocabArgs& a, int64_t step, int64_t row, double c, double sum,
+                                           double dot) {
+  constexpr double kLn2 = 0.6931471805599453;
+  const int32_t token = a.tokens[step];
+  const double log_s = log(sum);
+  const double lse = log_s + c / static_cast<double>(kLog2eF);
+  const bool valid = token >= 0 && token < a.V;
+  if (!valid) raise_error_flag(a.error_flag);
+  a.log_sums[step] = static_cast<float>(lse);
+  a.log_probs[step] = valid ? static_cast<float>(static_cast<double>(a.token_logit[row]) - lse) : NAN;
+  if constexpr (kDot) a.entropy[step] = static_cast<float>(log_s - kLn2 * (dot / sum));
+}
+template <bool kDot>
+__device__ __forceinline__ void store_no_step(const VocabArgs& a, int64_t step) {
+  a.log_probs[step] = 0.0f;
+  a.log_sums[step] = 0.0f;
+  if constexpr (kDot) a.entropy[step] = 0.0f;
+}
+
+// One piece's statistics, added to sums about c.  An empty piece (nothing but -inf
+// logits) has the sum 0 and no maximum.
+template <bool kDot>
+__device__ __forceinline__ void add_piece(const VocabArgs& a, int64_t o, float c, double& sum, double& dot) {
+  const float p = a.part_sum[o];
+  const float d = p == 0.0f ? 0.0f : a.part_max[o] - c;
+  const double e = static_cast<double>(__builtin_amdgcn_exp2f(d)) * static_cast<double>(p);
+  sum += e;
+  if constexpr (kDot) {
+    const double ratio = static_cast<double>(__builtin_amdgcn_exp2f(d));
+    dot += fma(e, static_cast<double>(d), ratio * static_cast<double>(a.part_dot[o]));
+  }
+}
+__device__ __forceinline__ float piece_top(const VocabArgs& a, int64_t o) {
+  return a.part_sum[o] == 0.0f ? -INFINITY : a.part_max[o];
+}
+
+// Joins the pieces' statistics of the tiles: 16 steps a workgroup, 32 threads over the
+// pieces of each.  The kernel also writes the zeros of the steps without a token.
 constexpr int kJoinThreads = 512;
 constexpr int kJoinRows = 16;
-template <bool kListed, bool kDot>
+template <bool kDot>
 __global__ __launch_bounds__(kJoinThreads) void vocab_join_kernel(VocabArgs a) {
   constexpr int kParts = kJoinThreads / kJoinRows;
   __shared__ float s_top[kParts][kJoinRows];
   __shared__ double s_sum[kParts][kJoinRows], s_dot[kParts][kJoinRows];
   const int r = threadIdx.x % kJoinRows, part = threadIdx.x / kJoinRows;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kJoinRows + r;
-  if constexpr (kListed) {
-    if (part == 0 && row < a.N && a.tokens[row] == kNoToken) {
-      a.log_probs[row] = 0.0f;
-      a.log_sums[row] = 0.0f;
-      if constexpr (kDot) a.entropy[row] = 0.0f;
-    }
-  }
-  const int64_t rows = kListed ? *a.active_count : a.N;
-  const bool in = row < rows;
+  if (part == 0 && row < a.N && a.tokens[row] == kNoToken) store_no_step<kDot>(a, row);
+  const bool in = row < *a.active_count;
   float top = -INFINITY;
   if (in) {
 #pragma unroll 8
-    for (int64_t j = part; j < a.pieces; j += kParts)
-      top = fmaxf(top, a.part_sum[j * a.row_pitch + row] == 0.0f ? -INFINITY : a.part_max[j * a.row_pitch + row]);
+    for (int64_t j = part; j < a.pieces; j += kParts) top = fmaxf(top, piece_top(a, j * a.row_pitch + row));
   }
   s_top[part][r] = top;
   __syncthreads();
 #pragma unroll 8
   for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_top[q][r]);
-  // Nothing but -inf logits (or NaN ones, which the sums carry).
   const float c = top == -INFINITY ? 0.0f : top;
   double sum = 0.0, dot = 0.0;
   if (in) {
-#pragma unroll 4
-    for (int64_t j = part; j < a.pieces; j += kParts) {
-      const double d = static_cast<double>(a.part_max[j * a.row_pitch + row]) - static_cast<double>(c);
-      const double p = static_cast<double>(a.part_sum[j * a.row_pitch + row]);
-      const double e = exp2_f64(p == 0.0 ? 0.0 : d);
-      sum += e * p;
-      if constexpr (kDot) dot += e * (static_cast<double>(a.part_dot[j * a.row_pitch + row]) + p * d);
-    }
+#pragma unroll 8
+    for (int64_t j = part; j < a.pieces; j += kParts) add_piece<kDot>(a, j * a.row_pitch + row, c, sum, dot);
   }
   s_sum[part][r] = sum;
   if constexpr (kDot) s_dot[part][r] = dot;
@@ -102,22 +125,35 @@ __global__ __launch_bounds__(kJoinThreads) void vocab_join_kernel(VocabArgs a) {
     sum += s_sum[q][r];
     if constexpr (kDot) dot += s_dot[q][r];
   }
-  constexpr double kLn2 = 0.6931471805599453;
-  const int64_t step = kListed ? a.active[row] : row;
-  const int32_t token = a.tokens[step];
-  if (!kListed && token == kNoToken) {
-    a.log_probs[step] = 0.0f;
-    a.log_sums[step] = 0.0f;
-    if constexpr (kDot) a.entropy[step] = 0.0f;
+  store_step<kDot>(a, a.active[row], row, c, sum, dot);
+}
+
+// The same for few steps: a workgroup a step.
+constexpr int kJoinFewThreads = 256;
+template <bool kDot>
+__global__ __launch_bounds__(kJoinFewThreads) void vocab_join_few_kernel(VocabArgs a) {
+  __shared__ float s_top[kJoinFewThreads / kWave];
+  __shared__ double s_red[3 * (kJoinFewThreads / kWave)];
+  const int64_t row = blockIdx.x;
+  if (a.tokens[row] == kNoToken) {
+    if (threadIdx.x == 0) store_no_step<kDot>(a, row);
     return;
   }
-  const double log_s = log(sum);
-  const double lse = log_s + static_cast<double>(c) / static_cast<double>(kLog2eF);
-  const bool valid = token >= 0 && token < a.V;
-  if (!valid) raise_error_flag(a.error_flag);
-  a.log_sums[step] = static_cast<float>(lse);
-  a.log_probs[step] = valid ? static_cast<float>(static_cast<double>(a.token_logit[row]) - lse) : NAN;
-  if constexpr (kDot) a.entropy[step] = static_cast<float>(log_s - kLn2 * (dot / sum));
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int64_t j = threadIdx.x; j < a.pieces; j += kJoinFewThreads) top = fmaxf(top, piece_top(a, row * a.pieces + j));
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+  if (threadIdx.x % kWave == 0) s_top[threadIdx.x / kWave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kJoinFewThreads / kWave; ++q) top = fmaxf(top, s_top[q]);
+  const float c = top == -INFINITY ? 0.0f : top;
+  double sum = 0.0, dot = 0.0, unused = 0.0;
+#pragma unroll 4
+  for (int64_t j = threadIdx.x; j < a.pieces; j += kJoinFewThreads) add_piece<kDot>(a, row * a.pieces + j, c, sum, dot);
+  block_sum3<kJoinFewThreads>(sum, dot, unused, s_red);
+  if (threadIdx.x == 0) store_step<kDot>(a, row, row, c, sum, dot);
 }
 
 // vtrace_vocab_grad's operands by active step: hidden states side by side with zeros
@@ -178,8 +214,9 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
   const int64_t row = i / quads, h = (i % quads) * 4;
   if (row >= *a.active_count) return;
-  f32x4 x = *reinterpret_cast<const f32x4*>(a.h_partials + row * a.H + h);
-  for (int k = 1; k < a.splits; ++k)
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (int k = 0; k < a.splits; ++k)
     x += *reinterpret_cast<const f32x4*>(a.h_partials + (k * a.row_pitch + row) * a.H + h);
   Out* const out = static_cast<Out*>(a.d_hidden) + static_cast<int64_t>(a.active[row]) * a.H + h;
   if constexpr (sizeof(Out) == 4) {
@@ -231,6 +268,8 @@ size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
   Carver c(ws);
   a->row_pitch = p.row_pitch;
   a->pieces = p.pieces;
+  a->tile_tokens = p.tile_tokens;
+  a->narrow = p.narrow;
   a->active = c.take<int32_t>(a->N);
   a->part_max = c.take<float>(p.pieces * p.row_pitch);
   a->part_sum = c.take<float>(p.pieces * p.row_pitch);
@@ -255,8 +294,15 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   return c.at;
 }
 
-// The kernel for few steps, against tiles of 256 steps.
+// The kernels for few steps against tiles of 256 steps (H = 4096, V = 131072: 128 steps 266
+// us, 129 in tiles 288; 256 in tiles 304), and between those two: the streaming kernel up to
+// 16 steps, and up to 64 on layers of at most 32 MB (24 steps, H = 512, V = 4000 9.2 us
+// against 13.9; 20, 256, 32768 12.0 against 14.2; 64, 1024, 8000 15.1 against 21.5; but 32,
+// 1024, 50000 36 against 28).
+constexpr int64_t kMostFewSteps = 128;
 constexpr int64_t kStreamMostSteps = 64;
+constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
+constexpr int64_t kCus = 256;
 
 // G of one piece takes at most this much (or one tile's columns): it is written and read
 // twice within the 256 MB Infinity Cache.
@@ -268,12 +314,24 @@ constexpr int64_t kWantedTiles = 512;
 
 VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
   VocabPlan p = {};
-  (void)H;
-  p.stream = N <= kStreamMostSteps;
-  if (p.stream) {
-    p.row_pitch = N <= 16 ? 16 : N <= 32 ? 32 : 64;
-    // 64 tokens a workgroup while that fills the GPU twice, else 16.
-    p.pieces = V >= 64 * 512 ? (V + 63) / 64 : (V + 15) / 16;
+  p.few = N <= kMostFewSteps;
+  if (p.few) {
+    p.row_pitch = N;
+    p.narrow = N > kStreamMostSteps || (N > 16 && V * H > kStreamMostLayer);
+    if (p.narrow) {
+      // As few rounds over the workgroups that fit the GPU as tiles of 128 or 256 tokens
+      // allow, each as even as rows of 16 are.
+      const int64_t slots = N <= 64 ? 2 * kCus : kCus, most = N <= 64 ? 128 : 256;
+      const int64_t rounds = (V + most * slots - 1) / (most * slots);
+      p.tile_tokens = static_cast<int>(round_up((V + rounds * slots - 1) / (rounds * slots), 16));
+      const int64_t tiles = (V + p.tile_tokens - 1) / p.tile_tokens;
+      p.pieces = tiles < slots ? tiles : slots;
+    } else {
+      // Tokens of a workgroup: as many as leave about a workgroup or two a CU.
+      p.tile_tokens = V >= 64 * 2 * kCus ? 64 : V >= 24 * kCus ? 32 : 16;
+      const int64_t tiles = (V + p.tile_tokens - 1) / p.tile_tokens;
+      p.pieces = tiles < 4 * kCus ? tiles : 4 * kCus;
+    }
   } else {
     p.row_pitch = round_up(N, kTile);
     p.pieces = 2 * ((V + kTile - 1) / kTile);
@@ -310,17 +368,18 @@ void attach_vocab_grad(VocabArgs* a, const VocabPlan& p, void* ws) { carve_grad(
 
 hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
   hipError_t e;
-  if (!p.stream) {
+  if (!p.few) {
     hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  e = p.stream ? launch_vocab_stream(a, st) : launch_vocab_stats(a, st);
+  e = p.few ? launch_vocab_few(a, st) : launch_vocab_stats(a, st);
   if (e != hipSuccess) return e;
+  const dim3 few(static_cast<unsigned>(a.N)), few_block(kJoinFewThreads);
   const dim3 grid(blocks_of(a.N, kJoinRows)), block(kJoinThreads);
-  if (p.stream && a.entropy) hipLaunchKernelGGL((vocab_join_kernel<false, true>), grid, block, 0, st, a);
-  else if (p.stream) hipLaunchKernelGGL((vocab_join_kernel<false, false>), grid, block, 0, st, a);
-  else if (a.entropy) hipLaunchKernelGGL((vocab_join_kernel<true, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((vocab_join_kernel<true, false>), grid, block, 0, st, a);
+  if (p.few && a.entropy) hipLaunchKernelGGL(vocab_join_few_kernel<true>, few, few_block, 0, st, a);
+  else if (p.few) hipLaunchKernelGGL(vocab_join_few_kernel<false>, few, few_block, 0, st, a);
+  else if (a.entropy) hipLaunchKernelGGL(vocab_join_kernel<true>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(vocab_join_kernel<false>, grid, block, 0, st, a);
   return hipGetLastError();
 }
 

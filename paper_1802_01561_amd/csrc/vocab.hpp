@@ -39,13 +39,16 @@ struct VocabArgs {
   unsigned int* error_flag;
   int32_t* active_count;  // in the header
   int32_t* active;        // [N] the active steps
-  // log_probs: statistics of vocabulary pieces, [pieces, row_pitch] each
+  // log_probs: statistics of vocabulary pieces, [pieces, row_pitch] each ([N, pieces] from
+  // the kernel for few steps)
   float* part_max;        // log2 units
   float* part_sum;
   float* part_dot;        // or null
   float* token_logit;     // [row_pitch]
   int64_t row_pitch;
   int64_t pieces;
+  int tile_tokens;        // of the kernels for few steps
+  bool narrow;            // the one for 17 to 128 steps
   // grad
   float* row_scalars;     // [5, row_pitch]: log-sum, c0, c1, d_log_probs, token (as int)
   uint16_t* x;            // [row_pitch, x_pitch] the active steps' hidden states, zeros around
@@ -58,8 +61,10 @@ struct VocabArgs {
 };
 
 struct VocabPlan {
-  bool stream;     // log_probs: the kernel for few steps
+  bool few;        // log_probs: the kernels for few steps
   int64_t pieces;  // log_probs: statistics per step
+  int tile_tokens;
+  bool narrow;
   int64_t row_pitch, x_pitch, g_pitch;
   int splits;
   size_t bytes;
@@ -73,7 +78,7 @@ hipError_t launch_vocab_grad(const VocabArgs& a, const VocabPlan& p, hipStream_t
 
 // The launches of one translation unit each.
 hipError_t launch_vocab_stats(const VocabArgs& a, hipStream_t s);
-hipError_t launch_vocab_stream(const VocabArgs& a, hipStream_t s);
+hipError_t launch_vocab_few(const VocabArgs& a, hipStream_t s);
 hipError_t launch_vocab_logit_grads(const VocabArgs& a, int64_t v0, hipStream_t s);
 hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t s);
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t s);

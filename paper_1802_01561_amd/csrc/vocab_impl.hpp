@@ -55,16 +55,25 @@ __device__ __forceinline__ Rsrc make_rsrc(const void* base, int64_t left) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(n), kRawBufferFlags);
 }
 
+// 16 bytes a lane, straight into LDS: a wave's 64 vectors one after the other.
+__device__ __forceinline__ void copy_to_lds(Rsrc r, char* lds, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)lds, 16, offset, 0, 0, 0);
+}
+
 __device__ __forceinline__ int swizzle_of(int r) { return (r & 3) | ((r >> 1) & 4); }
 
-// Copies one operand's 256 x 64 tiles to LDS, step after step along k.  `base` and
+// Copies one operand's tiles of kRows x 64 to LDS (by kWaves waves), step after step along k.  `base` and
 // `left` (bytes to the array's end) move with the steps; vectors outside the operand
 // are asked for beyond the end and arrive as zeros.
+template <int kRows = kTile, int kWaves = kGemmThreads / kWave>
 struct Loader {
+  static constexpr int kCopyRows = 8 * kWaves;            // "along": of one copy by all threads
+  static constexpr int kCopies = kRows / kCopyRows;       // of a thread and step
+  static constexpr int kCopyBytes = 1024 * kWaves;
   const char* base;
   int64_t left;
   int64_t step;       // bytes per step of 64 k
-  uint32_t off[4];
+  uint32_t off[kCopies];
   // "along" only: the lane's first k of a step, and where k ends.
   int lane_k, k, k_end;
   // After `first` steps the operand starts again at `again` (the low parts of G).
@@ -95,14 +104,15 @@ struct Loader {
     const int c = (lane % 8) ^ swizzle_of(r0);
     lane_k = c * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t o = row_offset(i * 64 + r0);
+    for (int i = 0; i < kCopies; ++i) {
+      const uint32_t o = row_offset(i * kCopyRows + r0);
       off[i] = o == kOutOfRange ? o : o + c * 16;
     }
   }
   // k outermost: rows of `pitch` elements, the tile's columns from `p`, `width` of them in the array.
   __device__ __forceinline__ void across(const void* p, int64_t bytes, int64_t pitch, int64_t width, int wave,
                                          int lane) {
+    static_assert(kRows == kTile && kWaves == 8, "rows of 512 bytes in LDS, 16 a copy");
     start(p, bytes);
     step = kTileK * 2 * pitch;
     k_end = 0x7fffffff;
@@ -111,7 +121,7 @@ struct Loader {
     const int slot = lane % 32;
     const int c = (((slot >> 1) ^ swizzle_of(r0)) << 1) | (slot & 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kCopies; ++i)
       off[i] = c * 8 < width ? static_cast<uint32_t>((i * 16 + r0) * pitch * 2) + c * 16 : kOutOfRange;
   }
   __device__ __forceinline__ void copy(char* lds, int wave) {
@@ -124,9 +134,8 @@ struct Loader {
     // The last step of an operand whose k is no multiple of 64 ends inside a row.
     const bool cut = k + kTileK > k_end && k + lane_k >= k_end;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(lds + i * 8192 + wave * 1024), 16,
-                                               cut ? kOutOfRange : off[i], 0, 0, 0);
+    for (int i = 0; i < kCopies; ++i)
+      copy_to_lds(r, lds + i * kCopyBytes + wave * 1024, cut ? kOutOfRange : off[i]);
     base += step;
     left -= step;
     k += kTileK;
@@ -182,7 +191,7 @@ __device__ __forceinline__ void stage_barrier() {
 // barrier when its own copies into this stage have arrived and its reads of the other
 // are done, so after the barrier this stage is whole and the other free.
 template <bool kAAcross, bool kBAcross>
-__device__ __forceinline__ void contract(Loader& la, Loader& lb, int steps, char* lds, int wave, int lane,
+__device__ __forceinline__ void contract(Loader<>& la, Loader<>& lb, int steps, char* lds, int wave, int lane,
                                          f32x4 (&acc)[kMT][kNT]) {
   const int s = lane % 16, g = lane / 16;
   Reader<kAAcross, !kAAcross, kMT> ra;
@@ -235,13 +244,13 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 // Where a token's logit starts: its bias.  Behind the vocabulary's end, and for a bias
-// so low that the logit's scaling could overflow, the token is ruled out.
+// so low that the logit's scaling could overflow, the token is ruled out.  (Without a bias
+// the buffer is empty and reads 0.)
 constexpr float kRuledOut = -1e37f;
 __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
-  if (v >= a.V) return -INFINITY;
-  if (a.bias == nullptr) return 0.0f;
-  const float b = a.bias[v];
-  return b < kRuledOut ? -INFINITY : b;
+  const Rsrc bias = make_rsrc(a.bias, a.bias ? a.V * 4 : 0);
+  const float b = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bias, static_cast<uint32_t>(v) * 4, 0, 0));
+  return v >= a.V || b < kRuledOut ? -INFINITY : b;
 }
 // A token ruled out adds p log p = 0, not 0 * -inf.
 constexpr float kLeastLog = -1e30f;

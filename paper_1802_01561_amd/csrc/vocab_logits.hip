@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_logits_kernel(VocabArgs
   const int s = lane % 16, g = lane / 16;
   const int wm = (wave % 2) * kWaveM, wn = (wave / 2) * kWaveN;
 
-  Loader lw, lx;
+  Loader<> lw, lx;
   const int64_t H = a.H;
   lw.along(a.weight + v0 * H, (a.V - v0) * H * 2, static_cast<int>(H), wave, lane, [&](int r) -> uint32_t {
     return v0 + r < a.V ? static_cast<uint32_t>(r * H * 2) : kOutOfRange;

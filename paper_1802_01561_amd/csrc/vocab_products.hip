@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_weight_kernel(VocabAr
   const int64_t rows = active_rows64(a);
   const int once = static_cast<int>(rows / kTileK);
   const int64_t part = a.row_pitch * a.g_pitch;  // elements of G's high parts
-  Loader lx, lg;
+  Loader<> lx, lg;
   lx.across(a.x + h0, (rows * a.x_pitch - h0) * 2, a.x_pitch, a.x_pitch - h0, wave, lane);
   lg.across(a.g + vt, (rows * a.g_pitch - vt) * 2, a.g_pitch, a.g_pitch - vt, wave, lane);
   if (!a.grad_bf16) {
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_hidden_kernel(VocabAr
   const int once = static_cast<int>(to - from);
   const int64_t part = a.row_pitch * a.g_pitch;
   const int64_t v0 = v_begin + from * kTileK;
-  Loader lw, lg;
+  Loader<> lw, lg;
   const uint16_t* const w = a.weight + v0 * a.H + h0;
   const int64_t w_left = ((a.V - v0) * a.H - h0) * 2;
   lw.across(w, w_left, a.H, a.H - h0, wave, lane);
@@ -115,25 +115,22 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_hidden_kernel(VocabAr
   }
 }
 
-template <typename... Params, typename... Args>
-hipError_t launch(void (*kernel)(Params...), int64_t tiles, hipStream_t st, Args... args) {
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tiles)), dim3(kGemmThreads), 0, st, args...);
-  return hipGetLastError();
-}
-
 int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
 
 }  // namespace
 
 hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st) {
   const int64_t v = a.V - v0 < a.g_pitch ? a.V - v0 : a.g_pitch;
-  const int64_t tiles = tiles_of(a.H) * tiles_of(v);
-  return a.grad_bf16 ? launch(&vocab_d_weight_kernel<uint16_t>, tiles, st, a, v0)
-                     : launch(&vocab_d_weight_kernel<float>, tiles, st, a, v0);
+  const dim3 grid(static_cast<unsigned>(tiles_of(a.H) * tiles_of(v))), block(kGemmThreads);
+  if (a.grad_bf16) hipLaunchKernelGGL(vocab_d_weight_kernel<uint16_t>, grid, block, 0, st, a, v0);
+  else hipLaunchKernelGGL(vocab_d_weight_kernel<float>, grid, block, 0, st, a, v0);
+  return hipGetLastError();
 }
 
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t st) {
-  return launch(&vocab_d_hidden_kernel, tiles_of(a.H) * tiles_of(a.N) * a.splits, st, a, v0, first ? 1 : 0);
+  const dim3 grid(static_cast<unsigned>(tiles_of(a.H) * tiles_of(a.N) * a.splits)), block(kGemmThreads);
+  hipLaunchKernelGGL(vocab_d_hidden_kernel, grid, block, 0, st, a, v0, first ? 1 : 0);
+  return hipGetLastError();
 }
 
 }  // namespace vtrace

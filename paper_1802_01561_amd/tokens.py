@@ -15,7 +15,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from ._lib import CLIP_WORKSPACE_BYTES, VTRACE_BF16, VTRACE_F32, check, lib
-from .binding import _allocating_on, _p, _require, _variant
+from .binding import _allocating_on, _fast_call, _fast_variant, _p, _require, _variant
 
 __all__ = [
     "NO_TOKEN",
@@ -33,6 +33,10 @@ __all__ = [
     "vtrace_vocab_log_probs",
     "vtrace_vocab_workspace_bytes",
 ]
+
+# The ordinary call (plain tensors, a workspace, the current stream of the current device) is
+# checked and marshalled, and its outputs allocated, in native code (csrc/fast_call.cpp),
+# which declines whatever is not exactly that.
 
 # The token of a step that takes no part (a prompt, the padding behind a sequence).
 NO_TOKEN = -1
@@ -121,6 +125,18 @@ def _workspace(given, kind, device, *args, **kw):
     return given
 
 
+def _native_out(out, kind, required: int) -> bool:
+    """Whether native code takes these outputs: none, or all that are required."""
+    return out is None or (type(out) is kind and all(t is not None for t in out[:required]))
+
+
+def _outputs(result, out=None, kind=tuple):
+    """The outputs of a call that native code took, or its error."""
+    if type(result) is int:
+        check(result)
+    return out if out is not None else result if kind is tuple else kind._make(result)
+
+
 def vtrace_vocab_workspace_bytes(T: int, B: int, V: int, H: int) -> int:
     return lib().vtrace_vocab_workspace_bytes(T, B, V, H)
 
@@ -166,6 +182,15 @@ def vtrace_vocab_log_probs(hidden, vocab_weight, vocab_bias, tokens, *,
 
     ``tokens`` [T,B] int32; NO_TOKEN marks steps that take no part (their outputs are 0).
     With ``out``, its entropy decides instead of ``with_entropy``."""
+    if stream is None and type(workspace) is VocabWorkspace and _native_out(out, VocabLogProbs, 2):
+        fast = _fast_call(hidden)
+        if fast:
+            device = fast.device()
+            r = fast.call_vocab_log_probs(
+                fast.vocab_log_probs, hidden, vocab_weight, vocab_bias, tokens, out is None and with_entropy,
+                *(out or (None, None, None)), workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return _outputs(r, out, VocabLogProbs)
     T, B, V, H, dev = _vocab_inputs(hidden, vocab_weight, vocab_bias, tokens)
     with _On(dev, stream) as s:
         workspace = _workspace(workspace, VocabWorkspace, dev, T, B, V, H, stream=stream)
@@ -197,6 +222,16 @@ def vtrace_vocab_grad(hidden, vocab_weight, vocab_bias, tokens, log_sums, entrop
     ``log_sums`` and (with d_entropy) ``entropy`` are vtrace_vocab_log_probs' outputs;
     ``grad_dtype`` (float32 or bfloat16) is the type of d_hidden and d_weight."""
     code = _grad_dtype_code(grad_dtype)
+    if stream is None and type(workspace) is VocabWorkspace and _native_out(out, VocabGrad, 2):
+        fast = _fast_call(hidden)
+        if fast:
+            device = fast.device()
+            r = fast.call_vocab_grad(
+                fast.vocab_grad, hidden, vocab_weight, vocab_bias, tokens, log_sums, entropy, d_log_probs, d_entropy,
+                grad_dtype is torch.bfloat16, *(out or (None, None, None)), out is None and vocab_bias is not None,
+                workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return _outputs(r, out, VocabGrad)
     T, B, V, H, dev = _vocab_inputs(hidden, vocab_weight, vocab_bias, tokens)
     if d_entropy is not None and entropy is None:
         raise ValueError("d_entropy needs entropy")
@@ -242,6 +277,18 @@ def vtrace_log_prob_loss_grad(target_log_probs, behaviour_log_probs, entropy, re
 
     ``entropy`` [T,B] is the policy's (None: no entropy loss and no d_entropy); the
     variant arguments are as in vtrace_loss_grad."""
+    if stream is None and type(workspace) is LogProbWorkspace and _native_out(out, LogProbLossGrad, 3):
+        fast = _fast_call(target_log_probs)
+        known = fast and _fast_variant(correction, q_estimate, epsilon, "log_probs", reward_transform, torch.float32)
+        if known:
+            device = fast.device()
+            r = fast.call_log_prob_loss(
+                fast.log_prob_loss, target_log_probs, behaviour_log_probs, entropy, rewards, discounts, values,
+                bootstrap_value, lengths, rho_bar, c_bar, lam, baseline_cost, entropy_cost, known[1],
+                *(out or (None,) * 6), out is None and entropy is not None, out is None and with_vs,
+                out is None and with_pg_advantages, workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return _outputs(r, out, LogProbLossGrad)
     variant = _variant(correction, q_estimate, epsilon, "log_probs", reward_transform)
     if not isinstance(target_log_probs, torch.Tensor):
         raise TypeError("target_log_probs must be a torch.Tensor")
@@ -289,6 +336,14 @@ def vtrace_clip_grad_norm(gradients: Sequence[torch.Tensor], max_norm: Optional[
     if max_norm is None and out is not None:
         raise ValueError("out needs max_norm")
     first = gradients[0]
+    if stream is None and type(workspace) is ClipWorkspace:
+        fast = _fast_call(first)
+        if fast:
+            device = fast.device()
+            r = fast.call_clip(fast.clip, gradients, gradients if out is None else list(out), max_norm is not None,
+                               max_norm, norm, workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return _outputs(r)[0]
     if not isinstance(first, torch.Tensor):
         raise TypeError("gradients must be torch.Tensors")
     dev = first.device
