@@ -6,8 +6,8 @@
 //   logits    m: token, n: step, k: hidden unit   (both operands have k innermost)
 //   d_weight  m: hidden unit, n: token, k: step   (both have k outermost)
 //   d_hidden  m: hidden unit, n: step, k: token   (A outermost, B innermost)
-// A workgroup of eight waves computes a 256 x 256 tile in steps of 64 along k; wave
-// (wm, wn) = (wave % 2, wave / 2) holds a 128 x 64 piece in registers, as 8 x 4 tiles
+// A workgroup of four waves computes a 256 x 256 tile in steps of 64 along k; wave
+// (wm, wn) = (wave % 2, wave / 2) holds a 128 x 128 piece in registers, as 8 x 8 tiles
 // of a 16x16x32 MFMA.  The next step's operands are copied from memory straight into
 // the other half of LDS while this one's are multiplied.
 //
@@ -31,11 +31,11 @@ namespace {
 
 constexpr int kTile = 256;
 constexpr int kTileK = 64;
-constexpr int kGemmThreads = 512;
+constexpr int kGemmThreads = 256;
 constexpr int kOperandBytes = kTile * kTileK * 2;
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kGemmLds = 2 * kStageBytes;
-constexpr int kWaveM = 128, kWaveN = 64;
+constexpr int kWaveM = 128, kWaveN = 128;
 constexpr int kMT = kWaveM / 16, kNT = kWaveN / 16;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -47,12 +47,18 @@ typedef __attribute__((address_space(3))) void LdsVoid;
 
 constexpr int kRawBufferFlags = 0x00020000;      // raw buffer, 32-bit elements, no swizzle
 constexpr uint32_t kOutOfRange = 0x80000000u;    // at or beyond the end of every descriptor: reads 0
-constexpr int64_t kMostRecords = 0x7fffffff;
 constexpr float kLog2eF = 1.44269504088896340736f;
 
+// A descriptor of `left` bytes from base on (none if negative), held in scalar registers:
+// every wave of a workgroup forms the same one.
 __device__ __forceinline__ Rsrc make_rsrc(const void* base, int64_t left) {
-  const int64_t n = left < 0 ? 0 : (left < kMostRecords ? left : kMostRecords);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(n), kRawBufferFlags);
+  const int beyond = static_cast<int>(left >> 31);  // 32-bit comparisons stay on the scalar unit
+  const int n = beyond == 0 ? static_cast<int>(left) : beyond < 0 ? 0 : 0x7fffffff;
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0,
+                                           __builtin_amdgcn_readfirstlane(n), kRawBufferFlags);
 }
 
 // 16 bytes a lane, straight into LDS: a wave's 64 vectors one after the other.
@@ -76,6 +82,7 @@ struct Loader {
   uint32_t off[kCopies];
   // "along" only: the lane's first k of a step, and where k ends.
   int lane_k, k, k_end;
+  bool cut;
   // After `first` steps the operand starts again at `again` (the low parts of G).
   int done, first;
   const char* again;
@@ -112,34 +119,43 @@ struct Loader {
   // k outermost: rows of `pitch` elements, the tile's columns from `p`, `width` of them in the array.
   __device__ __forceinline__ void across(const void* p, int64_t bytes, int64_t pitch, int64_t width, int wave,
                                          int lane) {
-    static_assert(kRows == kTile && kWaves == 8, "rows of 512 bytes in LDS, 16 a copy");
+    static_assert(kRows == kTile, "rows of 512 bytes in LDS");
     start(p, bytes);
     step = kTileK * 2 * pitch;
     k_end = 0x7fffffff;
     lane_k = 0;
-    const int r0 = wave * 2 + lane / 32;
     const int slot = lane % 32;
-    const int c = (((slot >> 1) ^ swizzle_of(r0)) << 1) | (slot & 1);
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i)
-      off[i] = c * 8 < width ? static_cast<uint32_t>((i * 16 + r0) * pitch * 2) + c * 16 : kOutOfRange;
+    for (int i = 0; i < kCopies; ++i) {
+      const int r = i * 2 * kWaves + wave * 2 + lane / 32;
+      const int c = (((slot >> 1) ^ swizzle_of(r)) << 1) | (slot & 1);
+      off[i] = c * 8 < width ? static_cast<uint32_t>(r * pitch * 2) + c * 16 : kOutOfRange;
+    }
   }
-  __device__ __forceinline__ void copy(char* lds, int wave) {
+  // One step's copies: the descriptor, then each of them.  Behind the last step they may go
+  // on with `more` false: nothing is read, zeros arrive.
+  __device__ __forceinline__ Rsrc begin(bool more = true) {
     if (done == first) {
       base = again;
       left = again_left;
       k = 0;
     }
-    const Rsrc r = make_rsrc(base, left);
+    const Rsrc r = make_rsrc(base, more ? left : 0);
     // The last step of an operand whose k is no multiple of 64 ends inside a row.
-    const bool cut = k + kTileK > k_end && k + lane_k >= k_end;
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i)
-      copy_to_lds(r, lds + i * kCopyBytes + wave * 1024, cut ? kOutOfRange : off[i]);
+    cut = k + kTileK > k_end && k + lane_k >= k_end;
     base += step;
     left -= step;
     k += kTileK;
     ++done;
+    return r;
+  }
+  __device__ __forceinline__ void copy(Rsrc r, char* lds, int wave, int i) const {
+    copy_to_lds(r, lds + i * kCopyBytes + wave * 1024, cut ? kOutOfRange : off[i]);
+  }
+  __device__ __forceinline__ void copy(char* lds, int wave) {
+    const Rsrc r = begin();
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) copy(r, lds, wave, i);
   }
 };
 
@@ -187,43 +203,88 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// acc += A B over `steps` steps of 64 k.  kSteps of the two stages: a wave passes the
-// barrier when its own copies into this stage have arrived and its reads of the other
-// are done, so after the barrier this stage is whole and the other free.
+// c += a b.  As an instruction of our own so that the accumulators stay in the accumulation
+// registers: the compiler's allocation moves them to and fro (three moves an MFMA).  It knows
+// nothing of its latency: see settle().
+__device__ __forceinline__ void mfma(f32x4& c, bf16x8 a, bf16x8 b) {
+  asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+
+// What a wave does between two barriers: it multiplies the second half of a step (a1, b1)
+// and reads the first half of the next from `from`, multiplies that and reads the second,
+// while its copies of the step after go to `to`.  The two stages do not overlap, and
+// __restrict says so: the compiler otherwise waits for every copy in flight before a read.
+template <bool kAAcross, bool kBAcross>
+struct Contraction {
+  Reader<kAAcross, !kAAcross, kMT> ra;
+  Reader<kBAcross, false, kNT> rb;
+  bf16x8 a0[kMT], b0[kNT], a1[kMT], b1[kNT];
+
+  // Two of a half's 16 fragments.
+  __device__ __forceinline__ void read(const char* from, int kk, int i, bf16x8 (&a)[kMT], bf16x8 (&b)[kNT]) {
+    if (i < kNT / 2) {
+      b[2 * i] = rb.read(from + kOperandBytes, 2 * i, kk);
+      b[2 * i + 1] = rb.read(from + kOperandBytes, 2 * i + 1, kk);
+    } else {
+      a[2 * i - kNT] = ra.read(from, 2 * i - kNT, kk);
+      a[2 * i - kNT + 1] = ra.read(from, 2 * i - kNT + 1, kk);
+    }
+  }
+  template <bool kFirst>
+  __device__ __forceinline__ void step(char* __restrict to, const char* __restrict from, Loader<>& la, Loader<>& lb,
+                                       bool more, int wave, f32x4 (&acc)[kMT][kNT]) {
+    const Rsrc da = la.begin(more), db = lb.begin(more);
+#pragma unroll
+    for (int m = 0; m < kMT; ++m) {
+      read(from, 0, m, a0, b0);
+      la.copy(da, to, wave, m);
+      lb.copy(db, to + kOperandBytes, wave, m);
+      if constexpr (!kFirst) {
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a1[m], b1[n]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int m = 0; m < kMT; ++m) {
+      read(from, 1, m, a1, b1);
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a0[m], b0[n]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// acc += A B over `steps` steps of 64 k.  A step's two halves of 32 k take turns in
+// registers: while one is multiplied the other is read.  A wave passes the barrier when it
+// has read all of a step and its copies of the next have arrived, so behind it the next
+// stage is whole and this one free.
 template <bool kAAcross, bool kBAcross>
 __device__ __forceinline__ void contract(Loader<>& la, Loader<>& lb, int steps, char* lds, int wave, int lane,
                                          f32x4 (&acc)[kMT][kNT]) {
-  const int s = lane % 16, g = lane / 16;
-  Reader<kAAcross, !kAAcross, kMT> ra;
-  Reader<kBAcross, false, kNT> rb;
-  ra.start((wave % 2) * kWaveM, s, g);
-  rb.start((wave / 2) * kWaveN, s, g);
-  if (steps > 0) {
-    la.copy(lds, wave);
-    lb.copy(lds + kOperandBytes, wave);
-  }
-  for (int it = 0; it < steps; ++it) {
-    char* cur = lds + (it & 1) * kStageBytes;
-    char* next = lds + ((it & 1) ^ 1) * kStageBytes;
+  if (steps <= 0) return;
+  Contraction<kAAcross, kBAcross> c;
+  c.ra.start((wave % 2) * kWaveM, lane % 16, lane / 16);
+  c.rb.start((wave / 2) * kWaveN, lane % 16, lane / 16);
+  la.copy(lds, wave);
+  lb.copy(lds + kOperandBytes, wave);
+  stage_barrier();
+  c.template step<true>(lds + kStageBytes, lds, la, lb, 1 < steps, wave, acc);
+  for (int it = 1; it < steps; ++it) {
     stage_barrier();
-    if (it + 1 < steps) {
-      la.copy(next, wave);
-      lb.copy(next + kOperandBytes, wave);
-    }
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8 a[kMT], b[kNT];
-#pragma unroll
-      for (int m = 0; m < kMT; ++m) a[m] = ra.read(cur, m, kk);
-#pragma unroll
-      for (int n = 0; n < kNT; ++n) b[n] = rb.read(cur + kOperandBytes, n, kk);
-#pragma unroll
-      for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int n = 0; n < kNT; ++n)
-          acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[m], b[n], acc[m][n], 0, 0, 0);
-    }
+    c.template step<false>(lds + ((it + 1) & 1) * kStageBytes, lds + (it & 1) * kStageBytes, la, lb, it + 1 < steps, wave,
+                           acc);
   }
+#pragma unroll
+  for (int m = 0; m < kMT; ++m)
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) mfma(acc[m][n], c.a1[m], c.b1[n]);
+  // The last copies (of nothing) have ended, and the last products are written.
+  __builtin_amdgcn_s_waitcnt(kWaitAll);
+  asm volatile("s_nop 15\n\ts_nop 15"
+               : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]), "+a"(acc[7][4]), "+a"(acc[7][5]),
+                 "+a"(acc[7][6]), "+a"(acc[7][7]));
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Sums (or maxima) over the four lane groups, the same in all of them.

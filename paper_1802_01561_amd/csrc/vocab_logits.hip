@@ -19,7 +19,7 @@ namespace {
 enum { kStats = 0, kStatsDot = 1, kGrad = 2, kGradDot = 3 };
 
 template <int kMode>
-__global__ __launch_bounds__(kGemmThreads, 2) void vocab_logits_kernel(VocabArgs a, int64_t v_begin, int64_t v_count) {
+__global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs a, int64_t v_begin, int64_t v_count) {
   __shared__ __align__(1024) char lds[kGemmLds];
   const int64_t count = *a.active_count;
   const int64_t tiles_n = (count + kTile - 1) / kTile;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_logits_kernel(VocabArgs
       }
     }
     if (a.d_bias != nullptr) {
-      // d_bias: this wave's 64 steps, summed over the 16 lanes of a group.
+      // d_bias: this wave's 128 steps, summed over the 16 lanes of a group.
 #pragma unroll
       for (int m = 0; m < kMT; ++m)
 #pragma unroll
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_logits_kernel(VocabArgs
 #pragma unroll
           for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
           if (s == 0)
-            a.bias_partials[(at.wide * 4 + wave / 2) * a.g_pitch + vt + wm + 32 * (m / 2) + 8 * g + 4 * (m % 2) + i] = x;
+            a.bias_partials[(at.wide * (kTile / kWaveN) + wave / 2) * a.g_pitch + vt + wm + 32 * (m / 2) + 8 * g + 4 * (m % 2) + i] = x;
         }
     }
   }

@@ -24,7 +24,7 @@ __device__ __forceinline__ void store4(Out* p, f32x4 x) {
 }
 
 template <typename Out>
-__global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_weight_kernel(VocabArgs a, int64_t v_begin) {
+__global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabArgs a, int64_t v_begin) {
   __shared__ __align__(1024) char lds[kGemmLds];
   const int64_t tiles_h = (a.H + kTile - 1) / kTile;
   const int64_t v_left = a.V - v_begin < a.g_pitch ? a.V - v_begin : a.g_pitch;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_weight_kernel(VocabAr
 
 // d_hidden's tiles are few where there are few steps: k (the piece) is split over
 // `splits` workgroups, each with float32 sums of its own that grow over the pieces.
-__global__ __launch_bounds__(kGemmThreads, 2) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
+__global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
   __shared__ __align__(1024) char lds[kGemmLds];
   const int64_t count = *a.active_count;
   const int64_t tiles_h = (a.H + kTile - 1) / kTile;
