@@ -156,54 +156,60 @@ __global__ __launch_bounds__(kJoinFewThreads) void vocab_join_few_kernel(VocabAr
   if (threadIdx.x == 0) store_step<kDot>(a, row, row, c, sum, dot);
 }
 
-// vtrace_vocab_grad's operands by active step: hidden states side by side with zeros
-// behind each row's end and behind the last row (up to a whole step of 64), and the
-// scalars that the tiles' epilogue needs.  A wave a row; the same waves clear
-// d_hidden of the steps without a token.
+// The tiles' operands by active step: hidden states side by side with zeros behind each
+// row's end and behind the last row (up to a whole tile), the tokens, and (kGrad) the
+// scalars that the gradient's epilogue needs.  A wave a row; in kGrad the same waves clear
+// d_hidden of the steps without a token.  (The copy takes 14 us of the largest step's 10 ms,
+// and makes every operand of the products one of plain rows.)
+//
+// With l = log-sum, lp = log p and G = p (c + d_h' lp) + d_lp 1[v = a] (c = -d_lp - d_h
+// entropy, d_h' = -d_h), the epilogue has p = 2^(z K - l2), K the float32 log2 e and l2 the
+// rounded l log2 e; what the rounding of l2 does to p is a factor of each step's own, and
+// goes into c0 and c1 here.  Rows behind the last get an l2 that makes p 0.
 constexpr int kGatherThreads = 256;
+template <bool kGrad>
 __global__ __launch_bounds__(kGatherThreads) void vocab_gather_kernel(VocabArgs a) {
   const int lane = threadIdx.x % kWave;
   const int64_t row = (static_cast<int64_t>(blockIdx.x) * kGatherThreads + threadIdx.x) / kWave;
   const int64_t count = *a.active_count;
   const v4u zero = {0u, 0u, 0u, 0u};
-  if (row < a.N && a.tokens[row] == kNoToken) {
+  if (kGrad && row < a.N && a.tokens[row] == kNoToken) {
     const int64_t bytes = a.H * (a.grad_bf16 ? 2 : 4);
     char* const out = static_cast<char*>(a.d_hidden) + row * bytes;
     for (int64_t i = lane * 16; i < bytes; i += kWave * 16) *reinterpret_cast<v4u*>(out + i) = zero;
   }
-  if (row >= a.row_pitch) return;
+  if (row >= (count + kTile - 1) / kTile * kTile) return;
   const int64_t step = row < count ? a.active[row] : 0;
-  if (row < (count + kTileK - 1) / kTileK * kTileK) {
-    const uint16_t* const in = a.hidden + step * a.H;
-    uint16_t* const out = a.x + row * a.x_pitch;
-    for (int64_t i = lane * 8; i < a.x_pitch; i += kWave * 8)
-      *reinterpret_cast<v4u*>(out + i) =
-          row < count && i < a.H ? *reinterpret_cast<const v4u*>(in + i) : zero;
-  }
+  const uint16_t* const in = a.hidden + step * a.H;
+  uint16_t* const out = a.x + row * a.x_pitch;
+  for (int64_t i = lane * 8; i < a.x_pitch; i += kWave * 8)
+    *reinterpret_cast<v4u*>(out + i) = row < count && i < a.H ? *reinterpret_cast<const v4u*>(in + i) : zero;
   if (lane != 0) return;
-  float lse = 0.0f, c0 = 0.0f, c1 = 0.0f, d_lp = 0.0f;
-  int32_t token = kNoToken;
+  const int32_t token = row < count ? a.tokens[step] : kNoToken;
+  a.row_tokens[row] = token;
+  if constexpr (!kGrad) return;
+  float4v scalars = {1e30f, 0.0f, 0.0f, 0.0f};
   if (row < count) {
-    token = a.tokens[step];
-    lse = a.in_log_sums[step];
-    d_lp = a.d_log_probs[step];
+    constexpr double kLn2 = 0.6931471805599453;
+    float d_lp = a.d_log_probs[step];
     if (token < 0 || token >= a.V) {
       raise_error_flag(a.error_flag);
       d_lp = NAN;
     }
-    // G = p (c0 + c1 log p) + d_lp 1[v = a].
-    c0 = -d_lp;
+    const double lse = a.in_log_sums[step], exact = lse / kLn2;
+    const float l2 = static_cast<float>(exact);
+    const double factor = __builtin_isfinite(lse) ? 1.0 + (static_cast<double>(l2) - exact) * kLn2 : 1.0;
+    double c0 = -static_cast<double>(d_lp), c1 = 0.0;
     if (a.d_entropy != nullptr) {
-      c1 = -a.d_entropy[step];
-      c0 += c1 * a.in_entropy[step];
+      c1 = -static_cast<double>(a.d_entropy[step]);
+      c0 += c1 * static_cast<double>(a.in_entropy[step]);
     }
+    scalars[0] = l2;
+    scalars[1] = static_cast<float>(c0 * factor);
+    scalars[2] = static_cast<float>(c1 * factor * kLn2);
+    scalars[3] = d_lp;
   }
-  const int64_t P = a.row_pitch;
-  a.row_scalars[row] = lse;
-  a.row_scalars[P + row] = c0;
-  a.row_scalars[2 * P + row] = c1;
-  a.row_scalars[3 * P + row] = d_lp;
-  a.row_scalars[4 * P + row] = __int_as_float(token);
+  a.row_scalars[row] = scalars;
 }
 
 // d_hidden of the active steps from the splits' sums.
@@ -229,7 +235,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
   }
 }
 
-// d_bias of one piece: the sums of 64 steps each, in order.
+// d_bias of one piece: the sums of 128 steps each, in order.
 __global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a, int64_t v_begin) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
   if (i >= a.g_pitch || v_begin + i >= a.V) return;
@@ -275,6 +281,11 @@ size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->part_sum = c.take<float>(p.pieces * p.row_pitch);
   a->part_dot = c.take<float>(p.pieces * p.row_pitch);
   a->token_logit = c.take<float>(p.row_pitch);
+  if (!p.few) {
+    a->x_pitch = p.x_pitch;
+    a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
+    a->row_tokens = c.take<int32_t>(p.row_pitch);
+  }
   return c.at;
 }
 
@@ -286,7 +297,8 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->g_pitch = p.g_pitch;
   a->splits = p.splits;
   a->active = c.take<int32_t>(a->N);
-  a->row_scalars = c.take<float>(5 * p.row_pitch);
+  a->row_scalars = c.take<float4v>(p.row_pitch);
+  a->row_tokens = c.take<int32_t>(p.row_pitch);
   a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
   a->g = c.take<uint16_t>((a->grad_bf16 ? 1 : 2) * p.row_pitch * p.g_pitch);
   a->bias_partials = c.take<float>(p.row_pitch / kWaveN * p.g_pitch);
@@ -302,7 +314,6 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
 constexpr int64_t kMostFewSteps = 128;
 constexpr int64_t kStreamMostSteps = 64;
 constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
-constexpr int64_t kCus = 256;
 
 // G of one piece takes at most this much (or one tile's columns): it is written and read
 // twice within the 256 MB Infinity Cache.
@@ -334,6 +345,7 @@ VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
     }
   } else {
     p.row_pitch = round_up(N, kTile);
+    p.x_pitch = round_up(H, kTileK);
     p.pieces = 2 * ((V + kTile - 1) / kTile);
   }
   VocabArgs a = {};
@@ -371,6 +383,9 @@ hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStr
   if (!p.few) {
     hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(vocab_gather_kernel<false>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
+                       dim3(kGatherThreads), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   e = p.few ? launch_vocab_few(a, st) : launch_vocab_stats(a, st);
   if (e != hipSuccess) return e;
@@ -387,8 +402,8 @@ hipError_t launch_vocab_grad(const VocabArgs& a, const VocabPlan& p, hipStream_t
   hipError_t e;
   hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(vocab_gather_kernel, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)), dim3(kGatherThreads), 0,
-                     st, a);
+  hipLaunchKernelGGL(vocab_gather_kernel<true>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
+                     dim3(kGatherThreads), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t v0 = 0; v0 < a.V; v0 += p.g_pitch) {
     if ((e = launch_vocab_logit_grads(a, v0, st)) != hipSuccess) return e;

@@ -8,6 +8,8 @@
 
 namespace vtrace {
 
+typedef float float4v __attribute__((ext_vector_type(4)));
+
 constexpr int64_t kVocabMaxTokens = int64_t(1) << 24;
 constexpr int64_t kVocabMaxHidden = 32768;
 // Hidden states are addressed with 31-bit byte offsets.
@@ -49,13 +51,15 @@ struct VocabArgs {
   int64_t pieces;
   int tile_tokens;        // of the kernels for few steps
   bool narrow;            // the one for 17 to 128 steps
-  // grad
-  float* row_scalars;     // [5, row_pitch]: log-sum, c0, c1, d_log_probs, token (as int)
-  uint16_t* x;            // [row_pitch, x_pitch] the active steps' hidden states, zeros around
+  // tiles: the active steps' hidden states, zeros around, and tokens
+  uint16_t* x;            // [row_pitch, x_pitch]
   int64_t x_pitch;
+  int32_t* row_tokens;    // [row_pitch]
+  // grad
+  float4v* row_scalars;   // [row_pitch]: log-sum (log2 units), c0, c1, d_log_probs
   uint16_t* g;            // [1 or 2, row_pitch, g_pitch] G of one piece: high (and low) parts
   int64_t g_pitch;        // tokens of a piece, a multiple of the tile
-  float* bias_partials;   // [row_pitch / 64, g_pitch]
+  float* bias_partials;   // [row_pitch / 128, g_pitch]
   float* h_partials;      // [splits, row_pitch, H]
   int splits;
 };

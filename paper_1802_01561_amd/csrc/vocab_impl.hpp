@@ -68,69 +68,65 @@ __device__ __forceinline__ void copy_to_lds(Rsrc r, char* lds, uint32_t offset) 
 
 __device__ __forceinline__ int swizzle_of(int r) { return (r & 3) | ((r >> 1) & 4); }
 
-// Copies one operand's tiles of kRows x 64 to LDS (by kWaves waves), step after step along k.  `base` and
-// `left` (bytes to the array's end) move with the steps; vectors outside the operand
-// are asked for beyond the end and arrive as zeros.
+// Copies one operand's tiles of kRows x 64 to LDS (by kWaves waves), step after step along k.
+// A lane's places in a tile are fixed once, along() or across(); aim() points the tile at an
+// array, `base` and `left` (bytes to its end) moving with the steps.  Rows behind the array's
+// end arrive as zeros.  Columns behind a row's end hold what comes next in memory: they are
+// columns of the result that nobody stores.
 template <int kRows = kTile, int kWaves = kGemmThreads / kWave>
 struct Loader {
   static constexpr int kCopyRows = 8 * kWaves;            // "along": of one copy by all threads
   static constexpr int kCopies = kRows / kCopyRows;       // of a thread and step
   static constexpr int kCopyBytes = 1024 * kWaves;
-  const char* base;
-  int64_t left;
   int64_t step;       // bytes per step of 64 k
   uint32_t off[kCopies];
-  // "along" only: the lane's first k of a step, and where k ends.
-  int lane_k, k, k_end;
-  bool cut;
+  int lane_k;         // "along": the lane's first k of a step
+  const char* base;
+  int64_t left;
+  int k, k_end;       // "along": where the step begins, and where k ends
+  uint32_t cut;       // kOutOfRange, to be added to an offset, where this lane's k lie behind k_end
   // After `first` steps the operand starts again at `again` (the low parts of G).
   int done, first;
   const char* again;
   int64_t again_left;
 
-  __device__ __forceinline__ void start(const void* p, int64_t bytes) {
-    base = static_cast<const char*>(p);
-    left = bytes;
-    done = 0;
-    first = -1;
-    k = 0;
-  }
-  __device__ __forceinline__ void restart_after(int steps, const void* p, int64_t bytes) {
-    first = steps;
-    again = static_cast<const char*>(p);
-    again_left = bytes;
-  }
-
-  // k innermost: row_offset(r) is row r's byte offset from `p`, or kOutOfRange.
-  template <typename F>
-  __device__ __forceinline__ void along(const void* p, int64_t bytes, int ks, int wave, int lane, F row_offset) {
-    start(p, bytes);
+  // k innermost, rows of `pitch` elements; rows from `rows` on are not read.
+  __device__ __forceinline__ void along(int64_t pitch, int rows, int wave, int lane) {
     step = kTileK * 2;
-    k_end = ks;
     const int r0 = wave * 8 + lane / 8;
     const int c = (lane % 8) ^ swizzle_of(r0);
     lane_k = c * 8;
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      const uint32_t o = row_offset(i * kCopyRows + r0);
-      off[i] = o == kOutOfRange ? o : o + c * 16;
+      const int r = i * kCopyRows + r0;
+      off[i] = r < rows ? static_cast<uint32_t>(r * pitch * 2) + c * 16 : kOutOfRange;
     }
   }
-  // k outermost: rows of `pitch` elements, the tile's columns from `p`, `width` of them in the array.
-  __device__ __forceinline__ void across(const void* p, int64_t bytes, int64_t pitch, int64_t width, int wave,
-                                         int lane) {
+  // k outermost, rows of `pitch` elements.
+  __device__ __forceinline__ void across(int64_t pitch, int wave, int lane) {
     static_assert(kRows == kTile, "rows of 512 bytes in LDS");
-    start(p, bytes);
     step = kTileK * 2 * pitch;
-    k_end = 0x7fffffff;
     lane_k = 0;
     const int slot = lane % 32;
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int r = i * 2 * kWaves + wave * 2 + lane / 32;
       const int c = (((slot >> 1) ^ swizzle_of(r)) << 1) | (slot & 1);
-      off[i] = c * 8 < width ? static_cast<uint32_t>(r * pitch * 2) + c * 16 : kOutOfRange;
+      off[i] = static_cast<uint32_t>(r * pitch * 2) + c * 16;
     }
+  }
+  __device__ __forceinline__ void aim(const void* p, int64_t bytes, int ks = 0x7fffffff) {
+    base = static_cast<const char*>(p);
+    left = bytes;
+    k = 0;
+    k_end = ks;
+    done = 0;
+    first = -1;
+  }
+  __device__ __forceinline__ void restart_after(int steps, const void* p, int64_t bytes) {
+    first = steps;
+    again = static_cast<const char*>(p);
+    again_left = bytes;
   }
   // One step's copies: the descriptor, then each of them.  Behind the last step they may go
   // on with `more` false: nothing is read, zeros arrive.
@@ -142,7 +138,7 @@ struct Loader {
     }
     const Rsrc r = make_rsrc(base, more ? left : 0);
     // The last step of an operand whose k is no multiple of 64 ends inside a row.
-    cut = k + kTileK > k_end && k + lane_k >= k_end;
+    cut = k + kTileK > k_end && k + lane_k >= k_end ? kOutOfRange : 0u;
     base += step;
     left -= step;
     k += kTileK;
@@ -150,7 +146,7 @@ struct Loader {
     return r;
   }
   __device__ __forceinline__ void copy(Rsrc r, char* lds, int wave, int i) const {
-    copy_to_lds(r, lds + i * kCopyBytes + wave * 1024, cut ? kOutOfRange : off[i]);
+    copy_to_lds(r, lds + i * kCopyBytes + wave * 1024, off[i] | cut);
   }
   __device__ __forceinline__ void copy(char* lds, int wave) {
     const Rsrc r = begin();
@@ -205,9 +201,17 @@ __device__ __forceinline__ void stage_barrier() {
 
 // c += a b.  As an instruction of our own so that the accumulators stay in the accumulation
 // registers: the compiler's allocation moves them to and fro (three moves an MFMA).  It knows
-// nothing of its latency: see settle().
+// nothing of its latency: contract() waits for the last.
 __device__ __forceinline__ void mfma(f32x4& c, bf16x8 a, bf16x8 b) {
   asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+
+// An accumulator's element, read where it is used: by itself the compiler moves all of a
+// tile's into vector registers at once, which do not hold them.
+__device__ __forceinline__ float element(const f32x4& c, int i) {
+  float x;
+  asm("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(c[i]));
+  return x;
 }
 
 // What a wave does between two barriers: it multiplies the second half of a step (a1, b1)
@@ -230,7 +234,6 @@ struct Contraction {
       a[2 * i - kNT + 1] = ra.read(from, 2 * i - kNT + 1, kk);
     }
   }
-  template <bool kFirst>
   __device__ __forceinline__ void step(char* __restrict to, const char* __restrict from, Loader<>& la, Loader<>& lb,
                                        bool more, int wave, f32x4 (&acc)[kMT][kNT]) {
     const Rsrc da = la.begin(more), db = lb.begin(more);
@@ -239,10 +242,8 @@ struct Contraction {
       read(from, 0, m, a0, b0);
       la.copy(da, to, wave, m);
       lb.copy(db, to + kOperandBytes, wave, m);
-      if constexpr (!kFirst) {
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a1[m], b1[n]);
-      }
+      for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a1[m], b1[n]);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -255,32 +256,56 @@ struct Contraction {
   }
 };
 
-// acc += A B over `steps` steps of 64 k.  A step's two halves of 32 k take turns in
-// registers: while one is multiplied the other is read.  A wave passes the barrier when it
-// has read all of a step and its copies of the next have arrived, so behind it the next
-// stage is whole and this one free.
-template <bool kAAcross, bool kBAcross>
-__device__ __forceinline__ void contract(Loader<>& la, Loader<>& lb, int steps, char* lds, int wave, int lane,
-                                         f32x4 (&acc)[kMT][kNT]) {
-  if (steps <= 0) return;
+// A tile's contraction: where its operands start, and how many steps of 64 k it has (at
+// least one; 0: there is no tile).
+struct Job {
+  Loader<> a, b;
+  int steps = 0;
+
+  __device__ __forceinline__ void copy(char* stage, int wave) {
+    a.copy(stage, wave);
+    b.copy(stage + kOperandBytes, wave);
+  }
+};
+
+// acc += A B over the job's steps.  A step's two halves of 32 k take turns in registers:
+// while one is multiplied the other is read.  A wave passes the barrier when it has read
+// all of a step and its copies of the next have arrived, so behind it the next stage is
+// whole and this one free.
+//
+// The first step's copies are under way when this is called (to stage `parity`).  With the
+// last step's products go the copies of the next tile's first: next() makes `job` that
+// tile's, and what follows the contraction hides their
+// latency.
+template <bool kAAcross, bool kBAcross, typename Next>
+__device__ __forceinline__ void contract(Job& job, char* lds, int& parity, int wave, int lane, f32x4 (&acc)[kMT][kNT],
+                                         Next next) {
+  const int steps = job.steps;
   Contraction<kAAcross, kBAcross> c;
   c.ra.start((wave % 2) * kWaveM, lane % 16, lane / 16);
   c.rb.start((wave / 2) * kWaveN, lane % 16, lane / 16);
-  la.copy(lds, wave);
-  lb.copy(lds + kOperandBytes, wave);
-  stage_barrier();
-  c.template step<true>(lds + kStageBytes, lds, la, lb, 1 < steps, wave, acc);
-  for (int it = 1; it < steps; ++it) {
+  // The first step finds no second half before it: zeros (64 products, against a branch
+  // around each of them).
+#pragma unroll
+  for (int i = 0; i < kMT; ++i) c.a1[i] = bf16x8{};
+#pragma unroll
+  for (int i = 0; i < kNT; ++i) c.b1[i] = bf16x8{};
+  int it = 0;
+  do {
     stage_barrier();
-    c.template step<false>(lds + ((it + 1) & 1) * kStageBytes, lds + (it & 1) * kStageBytes, la, lb, it + 1 < steps, wave,
-                           acc);
-  }
+    bool more = true;
+    if (it + 1 == steps) {
+      next();
+      more = job.steps > 0;
+    }
+    c.step(lds + (parity ^ 1) * kStageBytes, lds + parity * kStageBytes, job.a, job.b, more, wave, acc);
+    parity ^= 1;
+  } while (++it < steps);
 #pragma unroll
   for (int m = 0; m < kMT; ++m)
 #pragma unroll
     for (int n = 0; n < kNT; ++n) mfma(acc[m][n], c.a1[m], c.b1[n]);
-  // The last copies (of nothing) have ended, and the last products are written.
-  __builtin_amdgcn_s_waitcnt(kWaitAll);
+  // The last products are written.
   asm volatile("s_nop 15\n\ts_nop 15"
                : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]), "+a"(acc[7][4]), "+a"(acc[7][5]),
                  "+a"(acc[7][6]), "+a"(acc[7][7]));
@@ -305,10 +330,12 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 // Where a token's logit starts: its bias.  Behind the vocabulary's end, and for a bias
-// so low that the logit's scaling could overflow, the token is ruled out.  (Without a bias
-// the buffer is empty and reads 0.)
+// so low that the logit's scaling could overflow, the token is ruled out.  (A buffer without
+// a bias is empty and reads 0.)
 constexpr float kRuledOut = -1e37f;
+template <bool kBias = true>
 __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
+  if constexpr (!kBias) return v >= a.V ? -INFINITY : 0.0f;
   const Rsrc bias = make_rsrc(a.bias, a.bias ? a.V * 4 : 0);
   const float b = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bias, static_cast<uint32_t>(v) * 4, 0, 0));
   return v >= a.V || b < kRuledOut ? -INFINITY : b;
@@ -316,19 +343,35 @@ __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
 // A token ruled out adds p log p = 0, not 0 * -inf.
 constexpr float kLeastLog = -1e30f;
 
-// A workgroup's tile: `wide` x `deep` tiles, the id numbered so that workgroups that
-// run together on one XCD share operands in its L2 (groups of 8 tiles along `wide`,
-// then along `deep`).
-struct TileAt {
-  int64_t wide, deep;
+// Workgroups of a launch over tiles: one a CU (they fill its LDS), each with every
+// kCus-th tile.
+constexpr int kCus = 256;
+inline unsigned workgroups_of(int64_t tiles) { return static_cast<unsigned>(tiles < kCus ? tiles : kCus); }
+
+// The tiles of this workgroup, one after the other.  The 256 that are worked on at a time are
+// consecutive numbers, and those of one XCD are too.
+struct Tiles {
+  int total, at;
+
+  __device__ __forceinline__ explicit Tiles(int64_t n) : total(static_cast<int>(n)) {
+    at = static_cast<int>(xcd_tile(blockIdx.x, gridDim.x));
+  }
+  __device__ __forceinline__ bool any() const { return at < total; }
+  __device__ __forceinline__ void next() { at += gridDim.x; }
 };
-__device__ __forceinline__ TileAt tile_at(int64_t id, int64_t wide, int64_t deep) {
-  constexpr int64_t kGroup = 8;
-  const int64_t per = kGroup * deep;
-  const int64_t grp = id / per, in = id % per;
-  const int64_t first = grp * kGroup;
-  const int64_t n = wide - first < kGroup ? wide - first : kGroup;
-  return {first + in % n, in / n};
+
+// Tile number `id` of `wide` x `deep`: consecutive numbers share operands in an XCD's L2
+// (8 tiles along `wide`, then along `deep`).
+struct TileAt {
+  int wide, deep;
+};
+__device__ __forceinline__ TileAt tile_at(int id, int wide, int deep) {
+  constexpr int kGroup = 8;
+  const unsigned per = kGroup * deep;
+  const unsigned grp = static_cast<unsigned>(id) / per, in = static_cast<unsigned>(id) % per;
+  const int first = grp * kGroup;
+  const unsigned n = wide - first < kGroup ? wide - first : kGroup;
+  return {first + static_cast<int>(in % n), static_cast<int>(in / n)};
 }
 
 }  // namespace

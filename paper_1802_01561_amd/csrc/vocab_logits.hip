@@ -18,62 +18,104 @@ namespace {
 
 enum { kStats = 0, kStatsDot = 1, kGrad = 2, kGradDot = 3 };
 
-template <int kMode>
+// The token that lane (s, g) holds in accumulator (m, i), of its wave's 128 and behind 8 g.
+__device__ __forceinline__ constexpr int token_at(int m, int i) { return 32 * (m / 2) + 4 * (m % 2) + i; }
+
+template <int kMode, bool kBias>
 __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs a, int64_t v_begin, int64_t v_count) {
-  __shared__ __align__(1024) char lds[kGemmLds];
-  const int64_t count = *a.active_count;
-  const int64_t tiles_n = (count + kTile - 1) / kTile;
-  const int64_t tiles_v = (v_count + kTile - 1) / kTile;
-  if (static_cast<int64_t>(blockIdx.x) >= tiles_n * tiles_v) return;
-  const TileAt at = tile_at(xcd_tile(blockIdx.x, tiles_n * tiles_v), tiles_n, tiles_v);
-  const int64_t n0 = at.wide * kTile;
-  const int64_t vt = at.deep * kTile;    // in this launch's piece
-  const int64_t v0 = v_begin + vt;       // in the vocabulary
+  // The stages, then two tiles' tokens and scalars: one array, since what the compiler makes of
+  // several loses what __restrict says of the stages.
+  constexpr int kTokens = kTile * sizeof(int32_t), kScalars = kMode >= kGrad ? kTile * sizeof(float4v) : 0;
+  __shared__ __align__(1024) char lds[kGemmLds + 2 * (kTokens + kScalars)];
+  int32_t* const s_tokens = reinterpret_cast<int32_t*>(lds + kGemmLds);
+  float4v* const s_scalars = reinterpret_cast<float4v*>(lds + kGemmLds + 2 * kTokens);
+  const int count = *a.active_count;
+  const int tiles_n = (count + kTile - 1) / kTile;
+  const int tiles_v = static_cast<int>((v_count + kTile - 1) / kTile);
+  Tiles tiles(static_cast<int64_t>(tiles_n) * tiles_v);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int s = lane % 16, g = lane / 16;
   const int wm = (wave % 2) * kWaveM, wn = (wave / 2) * kWaveN;
-
-  Loader<> lw, lx;
   const int64_t H = a.H;
-  lw.along(a.weight + v0 * H, (a.V - v0) * H * 2, static_cast<int>(H), wave, lane, [&](int r) -> uint32_t {
-    return v0 + r < a.V ? static_cast<uint32_t>(r * H * 2) : kOutOfRange;
-  });
-  if constexpr (kMode >= kGrad) {
-    lx.along(a.x + n0 * a.x_pitch, kTile * a.x_pitch * 2, static_cast<int>(a.x_pitch), wave, lane,
-             [&](int r) -> uint32_t { return static_cast<uint32_t>(r * a.x_pitch * 2); });
-  } else {
-    lx.along(a.hidden, a.N * H * 2, static_cast<int>(H), wave, lane, [&](int r) -> uint32_t {
-      return n0 + r < count ? static_cast<uint32_t>(static_cast<int64_t>(a.active[n0 + r]) * H * 2) : kOutOfRange;
-    });
-  }
 
-  // Lane (s, g) holds tokens v(m, i) = 32 (m / 2) + 8 g + 4 (m % 2) + i of steps 16 n + s.
+  // Rows behind the vocabulary's end lie behind the array's.
+  Job job;
+  job.a.along(H, kTile, wave, lane);
+  job.b.along(a.x_pitch, kTile, wave, lane);
+  TileAt at;
+  auto start = [&] {
+    job.steps = 0;
+    if (!tiles.any()) return;
+    at = tile_at(tiles.at, tiles_n, tiles_v);
+    const int64_t n0 = static_cast<int64_t>(at.wide) * kTile, v0 = v_begin + static_cast<int64_t>(at.deep) * kTile;
+    job.steps = static_cast<int>(a.x_pitch / kTileK);
+    job.a.aim(a.weight + v0 * H, (a.V - v0) * H * 2, static_cast<int>(H));
+    job.b.aim(a.x + n0 * a.x_pitch, kTile * a.x_pitch * 2);
+  };
+  int parity = 0, turn = 0;
+  start();
+  if (job.steps > 0) job.copy(lds, wave);
+  while (tiles.any()) {
+  const int64_t n0 = static_cast<int64_t>(at.wide) * kTile;
+  const int64_t vt = static_cast<int64_t>(at.deep) * kTile;  // in this launch's piece
+  const int64_t v0 = v_begin + vt;                           // in the vocabulary
+  const int tile_wide = at.wide, tile_deep = at.deep;
+  // What follows from the lane's number is formed in each tile: kept from tile to tile it
+  // would take the registers that the contraction needs.
+  int here = lane;
+  asm volatile("" : "+v"(here));
+  const int s = here % 16, g = here / 16;
+  // Accumulator (m, n) of lane (s, g) holds tokens 8 g + token_at(m, 0..3) of step 16 n + s;
+  // it starts as start_of_logit.
+  const int64_t first = v0 + wm;
+  const int own = static_cast<int>(a.V - first < kTile ? a.V - first : kTile) - 8 * g;
+  const Rsrc bias = make_rsrc(a.bias + first, kBias && a.bias ? (a.V - first) * 4 : 0);
   f32x4 acc[kMT][kNT];
 #pragma unroll
   for (int m = 0; m < kMT; ++m) {
     f32x4 b;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t v = v0 + wm + 32 * (m / 2) + 8 * g + 4 * (m % 2) + i;
-      b[i] = start_of_logit(a, v);
+      const int t = token_at(m, i);
+      if constexpr (kBias) {
+        const float x = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bias, 32 * g + 4 * t, 0, 0));
+        b[i] = t >= own || x < kRuledOut ? -INFINITY : x;
+      } else {
+        b[i] = t >= own ? -INFINITY : 0.0f;
+      }
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) acc[m][n] = b;
   }
-  const int steps = static_cast<int>((H + kTileK - 1) / kTileK);
-  contract<false, false>(lw, lx, steps, lds, wave, lane, acc);
+  // What the epilogue needs of each step, by way of LDS (registers would hold it through the
+  // contraction).  Two of them: a wave may be in its next tile while another ends this one.
+  turn ^= kTile;
+  s_tokens[turn + threadIdx.x] = a.row_tokens[n0 + threadIdx.x];
+  if constexpr (kMode >= kGrad) s_scalars[turn + threadIdx.x] = a.row_scalars[n0 + threadIdx.x];
+  contract<false, false>(job, lds, parity, wave, lane, acc, [&] {
+    tiles.next();
+    start();
+  });
 
+  // A step's token, counted from this lane's first (what token_at gives, where it has it).
+  auto taken_of = [&](int32_t token) {
+    return token < 0 || token < first || token >= first + kWaveM ? -1 : static_cast<int>(token - first) - 8 * g;
+  };
   if constexpr (kMode < kGrad) {
-    const int64_t piece = at.deep * 2 + wave % 2;
+    const int64_t piece = tile_deep * 2 + wave % 2;
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
       const int64_t row = n0 + wn + 16 * n + s;
+      const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
+      float z[kMT][4];
       float top = -INFINITY;
 #pragma unroll
       for (int m = 0; m < kMT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[m][n][i]);
+        for (int i = 0; i < 4; ++i) {
+          z[m][i] = element(acc[m][n], i);
+          top = fmaxf(top, z[m][i]);
+        }
       top = group_max(top);
       const float c = top == -INFINITY ? 0.0f : top * kLog2eF;
       float sum = 0.0f, dot = 0.0f;
@@ -81,7 +123,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
       for (int m = 0; m < kMT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float d = fmaf(acc[m][n][i], kLog2eF, -c);
+          const float d = fmaf(z[m][i], kLog2eF, -c);
           const float e = __builtin_amdgcn_exp2f(d);
           sum += e;
           if constexpr (kMode == kStatsDot) dot = fmaf(e, fmaxf(d, kLeastLog), dot);
@@ -95,91 +137,111 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
         if constexpr (kMode == kStatsDot) a.part_dot[o] = dot;
       }
       // The taken token's logit, where this lane holds it.
-      const int32_t token = row < count ? a.tokens[a.active[row]] : kNoToken;
-      const int64_t in = token - (v0 + wm);
-      if (__any(token >= 0 && in >= 0 && in < kWaveM)) {
+      if (__any(taken >= 0)) {
+        float logit = 0.0f;
+        bool mine = false;
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (in == 32 * (m / 2) + 8 * g + 4 * (m % 2) + i) a.token_logit[row] = acc[m][n][i];
+          for (int i = 0; i < 4; ++i) {
+            logit = taken == token_at(m, i) ? z[m][i] : logit;
+            mine |= taken == token_at(m, i);
+          }
+        if (mine) a.token_logit[row] = logit;
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   } else {
     const int64_t P = a.row_pitch;
     float col[kMT][4];
+    if constexpr (kBias) {
 #pragma unroll
-    for (int m = 0; m < kMT; ++m)
+      for (int m = 0; m < kMT; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) col[m][i] = 0.0f;
-    const bool edge = n0 + kTile > count;
+        for (int i = 0; i < 4; ++i) col[m][i] = 0.0f;
+    }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
       const int64_t row = n0 + wn + 16 * n + s;
-      const float lse = a.row_scalars[row], c0 = a.row_scalars[P + row];
-      const float c1 = kMode == kGradDot ? a.row_scalars[2 * P + row] : 0.0f;
-      const float d_lp = a.row_scalars[3 * P + row];
-      const int32_t token = __float_as_int(a.row_scalars[4 * P + row]);
-      const int64_t in = token - (v0 + wm);
-      const bool here = __any(token >= 0 && in >= 0 && in < kWaveM);
+      // G = p (c0 + c1 log2 p) + d_lp 1[v = a] with p = 2^(z log2 e - l2): see the gather kernel.
+      const float4v scalars = s_scalars[turn + wn + 16 * n + s];
+      const float l2 = scalars[0], c0 = scalars[1], c1 = scalars[2], d_lp = scalars[3];
+      const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
+      float grad[kMT][4];
 #pragma unroll
       for (int m = 0; m < kMT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float lp = acc[m][n][i] - lse;
-          const float p = __builtin_amdgcn_exp2f(lp * kLog2eF);
-          float d = kMode == kGradDot ? p * fmaf(c1, fmaxf(lp, kLeastLog), c0) : p * c0;
-          if (edge && row >= count) d = 0.0f;
-          if (here && in == 32 * (m / 2) + 8 * g + 4 * (m % 2) + i) d += d_lp;
-          acc[m][n][i] = d;
-          col[m][i] += d;
+          const float d = fmaf(element(acc[m][n], i), kLog2eF, -l2);
+          const float p = __builtin_amdgcn_exp2f(d);
+          grad[m][i] = kMode == kGradDot ? p * fmaf(c1, fmaxf(d, kLeastLog), c0) : p * c0;
         }
+      if (__any(taken >= 0)) {
+#pragma unroll
+        for (int m = 0; m < kMT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) grad[m][i] += taken == token_at(m, i) ? d_lp : 0.0f;
+      }
+      if constexpr (kBias) {
+#pragma unroll
+        for (int m = 0; m < kMT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) col[m][i] += grad[m][i];
+      }
       uint16_t* out = a.g + row * a.g_pitch + vt + wm + 8 * g;
       uint16_t* out_low = out + P * a.g_pitch;
 #pragma unroll
       for (int p = 0; p < kMT / 2; ++p) {
+        const float* const x = grad[2 * p];
+        const float* const y = grad[2 * p + 1];
         v4u hi;
-        const f32x4 x = acc[2 * p][n], y = acc[2 * p + 1][n];
         hi.x = pack_bf16x2(x[0], x[1]);
         hi.y = pack_bf16x2(x[2], x[3]);
         hi.z = pack_bf16x2(y[0], y[1]);
         hi.w = pack_bf16x2(y[2], y[3]);
         *reinterpret_cast<v4u*>(out + 32 * p) = hi;
         if (!a.grad_bf16) {
-          auto low = [](float f, unsigned h) { return f - __uint_as_float(h << 16); };
-          auto low2 = [&](float f0, float f1, unsigned h) {
-            return pack_bf16x2(low(f0, h & 0xffffu), low(f1, h >> 16));
+          auto low = [](float f0, float f1, unsigned h) {
+            return pack_bf16x2(f0 - __uint_as_float(h << 16), f1 - __uint_as_float(h & 0xffff0000u));
           };
           v4u lo;
-          lo.x = low2(x[0], x[1], hi.x);
-          lo.y = low2(x[2], x[3], hi.y);
-          lo.z = low2(y[0], y[1], hi.z);
-          lo.w = low2(y[2], y[3], hi.w);
+          lo.x = low(x[0], x[1], hi.x);
+          lo.y = low(x[2], x[3], hi.y);
+          lo.z = low(y[0], y[1], hi.z);
+          lo.w = low(y[2], y[3], hi.w);
           *reinterpret_cast<v4u*>(out_low + 32 * p) = lo;
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (a.d_bias != nullptr) {
-      // d_bias: this wave's 128 steps, summed over the 16 lanes of a group.
+    if constexpr (kBias) {
+      if (a.d_bias != nullptr) {
+        // d_bias: this wave's 128 steps, summed over the 16 lanes of a group.
 #pragma unroll
-      for (int m = 0; m < kMT; ++m)
+        for (int m = 0; m < kMT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = col[m][i];
+          for (int i = 0; i < 4; ++i) {
+            float x = col[m][i];
 #pragma unroll
-          for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
-          if (s == 0)
-            a.bias_partials[(at.wide * (kTile / kWaveN) + wave / 2) * a.g_pitch + vt + wm + 32 * (m / 2) + 8 * g + 4 * (m % 2) + i] = x;
-        }
+            for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
+            if (s == 0)
+              a.bias_partials[(tile_wide * (kTile / kWaveN) + wave / 2) * a.g_pitch + vt + wm + 8 * g + token_at(m, i)] = x;
+          }
+      }
     }
   }
+  }
+  __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
 template <int kMode>
 hipError_t launch(const VocabArgs& a, int64_t v0, int64_t v_count, hipStream_t st) {
-  const int64_t tiles = (a.row_pitch / kTile) * ((v_count + kTile - 1) / kTile);
-  hipLaunchKernelGGL(vocab_logits_kernel<kMode>, dim3(static_cast<unsigned>(tiles)), dim3(kGemmThreads), 0, st, a, v0,
-                     v_count);
+  const dim3 grid(workgroups_of(a.row_pitch / kTile * ((v_count + kTile - 1) / kTile))), block(kGemmThreads);
+  // d_bias without a bias: as if there were one of zeros.
+  if (a.bias != nullptr || a.d_bias != nullptr)
+    hipLaunchKernelGGL((vocab_logits_kernel<kMode, true>), grid, block, 0, st, a, v0, v_count);
+  else
+    hipLaunchKernelGGL((vocab_logits_kernel<kMode, false>), grid, block, 0, st, a, v0, v_count);
   return hipGetLastError();
 }
 

@@ -11,6 +11,10 @@ __device__ __forceinline__ int64_t active_rows64(const VocabArgs& a) {
   return (static_cast<int64_t>(*a.active_count) + kTileK - 1) / kTileK * kTileK;
 }
 
+__device__ __forceinline__ f32x4 load4(Rsrc r, uint32_t offset) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0));
+}
+
 template <typename Out>
 __device__ __forceinline__ void store4(Out* p, f32x4 x) {
   if constexpr (sizeof(Out) == 4) {
@@ -26,93 +30,144 @@ __device__ __forceinline__ void store4(Out* p, f32x4 x) {
 template <typename Out>
 __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabArgs a, int64_t v_begin) {
   __shared__ __align__(1024) char lds[kGemmLds];
-  const int64_t tiles_h = (a.H + kTile - 1) / kTile;
+  const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
   const int64_t v_left = a.V - v_begin < a.g_pitch ? a.V - v_begin : a.g_pitch;
-  const int64_t tiles_v = (v_left + kTile - 1) / kTile;
-  const TileAt at = tile_at(xcd_tile(blockIdx.x, tiles_h * tiles_v), tiles_h, tiles_v);
-  const int64_t h0 = at.wide * kTile, vt = at.deep * kTile;
+  const int tiles_v = static_cast<int>((v_left + kTile - 1) / kTile);
+  Tiles tiles(static_cast<int64_t>(tiles_h) * tiles_v);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-
-  const int64_t rows = active_rows64(a);
-  const int once = static_cast<int>(rows / kTileK);
-  const int64_t part = a.row_pitch * a.g_pitch;  // elements of G's high parts
-  Loader<> lx, lg;
-  lx.across(a.x + h0, (rows * a.x_pitch - h0) * 2, a.x_pitch, a.x_pitch - h0, wave, lane);
-  lg.across(a.g + vt, (rows * a.g_pitch - vt) * 2, a.g_pitch, a.g_pitch - vt, wave, lane);
-  if (!a.grad_bf16) {
-    lx.restart_after(once, a.x + h0, (rows * a.x_pitch - h0) * 2);
-    lg.restart_after(once, a.g + part + vt, (rows * a.g_pitch - vt) * 2);
-  }
-  f32x4 acc[kMT][kNT] = {};
-  contract<true, true>(lx, lg, a.grad_bf16 ? once : 2 * once, lds, wave, lane, acc);
-
   const int s = lane % 16, g = lane / 16;
-  Out* const d_weight = static_cast<Out*>(a.d_weight);
+  const int64_t rows = active_rows64(a);
+  const int once = rows == 0 ? 1 : static_cast<int>(rows / kTileK);  // no rows: a step of nothing
+  const int64_t part = a.row_pitch * a.g_pitch;  // elements of G's high parts
+
+  Job job;
+  job.a.across(a.x_pitch, wave, lane);
+  job.b.across(a.g_pitch, wave, lane);
+  TileAt at;
+  auto start = [&] {
+    job.steps = 0;
+    if (!tiles.any()) return;
+    at = tile_at(tiles.at, tiles_h, tiles_v);
+    const int64_t h0 = static_cast<int64_t>(at.wide) * kTile, vt = static_cast<int64_t>(at.deep) * kTile;
+    job.a.aim(a.x + h0, (rows * a.x_pitch - h0) * 2);
+    job.b.aim(a.g + vt, (rows * a.g_pitch - vt) * 2);
+    job.steps = once;
+    if (!a.grad_bf16) {
+      job.a.restart_after(once, a.x + h0, (rows * a.x_pitch - h0) * 2);
+      job.b.restart_after(once, a.g + part + vt, (rows * a.g_pitch - vt) * 2);
+      job.steps = 2 * once;
+    }
+  };
+  int parity = 0;
+  start();
+  if (job.steps > 0) job.copy(lds, wave);
+  while (tiles.any()) {
+    const int64_t h0 = static_cast<int64_t>(at.wide) * kTile, vt = static_cast<int64_t>(at.deep) * kTile;
+    f32x4 acc[kMT][kNT] = {};
+    contract<true, true>(job, lds, parity, wave, lane, acc, [&] {
+      tiles.next();
+      start();
+    });
+    Out* const d_weight = static_cast<Out*>(a.d_weight);
 #pragma unroll
-  for (int n = 0; n < kNT; ++n) {
-    const int64_t v = v_begin + vt + (wave / 2) * kWaveN + 16 * n + s;
-    if (v >= a.V) continue;
+    for (int n = 0; n < kNT; ++n) {
+      const int64_t v = v_begin + vt + (wave / 2) * kWaveN + 16 * n + s;
+      if (v >= a.V) continue;
 #pragma unroll
-    for (int m = 0; m < kMT; ++m) {
-      const int64_t h = h0 + (wave % 2) * kWaveM + 16 * m + 4 * g;
-      if (h < a.H) store4(d_weight + v * a.H + h, acc[m][n]);
+      for (int m = 0; m < kMT; ++m) {
+        const int64_t h = h0 + (wave % 2) * kWaveM + 16 * m + 4 * g;
+        if (h < a.H) store4(d_weight + v * a.H + h, acc[m][n]);
+      }
     }
   }
+  __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-// d_hidden's tiles are few where there are few steps: k (the piece) is split over
-// `splits` workgroups, each with float32 sums of its own that grow over the pieces.
+// d_hidden's tiles are few where there are few steps: k (the piece) is split into `splits`
+// parts, each with float32 sums of its own that grow over the pieces.
 __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
   __shared__ __align__(1024) char lds[kGemmLds];
-  const int64_t count = *a.active_count;
-  const int64_t tiles_h = (a.H + kTile - 1) / kTile;
-  const int64_t tiles_n = (count + kTile - 1) / kTile;
-  const int64_t tiles = tiles_h * tiles_n;
-  if (static_cast<int64_t>(blockIdx.x) >= tiles * a.splits) return;
-  const int64_t id = xcd_tile(blockIdx.x, tiles * a.splits);
-  const int split = static_cast<int>(id / tiles);
-  const TileAt at = tile_at(id % tiles, tiles_n, tiles_h);
-  const int64_t h0 = at.deep * kTile, n0 = at.wide * kTile;
+  const int count = *a.active_count;
+  const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
+  const int tiles_n = (count + kTile - 1) / kTile;
+  const int per_split = tiles_h * tiles_n;
+  Tiles tiles(static_cast<int64_t>(per_split) * a.splits);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-
-  const int64_t v_left = a.V - v_begin < a.g_pitch ? a.V - v_begin : a.g_pitch;
-  const int64_t steps = (v_left + kTileK - 1) / kTileK;
-  const int64_t from = steps * split / a.splits, to = steps * (split + 1) / a.splits;
-  const int once = static_cast<int>(to - from);
-  const int64_t part = a.row_pitch * a.g_pitch;
-  const int64_t v0 = v_begin + from * kTileK;
-  Loader<> lw, lg;
-  const uint16_t* const w = a.weight + v0 * a.H + h0;
-  const int64_t w_left = ((a.V - v0) * a.H - h0) * 2;
-  lw.across(w, w_left, a.H, a.H - h0, wave, lane);
-  const uint16_t* const gp = a.g + n0 * a.g_pitch + from * kTileK;
-  const int64_t g_left = ((a.row_pitch - n0) * a.g_pitch - from * kTileK) * 2;
-  lg.along(gp, g_left, 0x7fffffff, wave, lane,
-           [&](int r) -> uint32_t { return static_cast<uint32_t>(r * a.g_pitch * 2); });
-  if (!a.grad_bf16) {
-    lw.restart_after(once, w, w_left);
-    lg.restart_after(once, gp + part, g_left);
-  }
-  f32x4 acc[kMT][kNT] = {};
-  contract<true, false>(lw, lg, a.grad_bf16 ? once : 2 * once, lds, wave, lane, acc);
-
   const int s = lane % 16, g = lane / 16;
+  const int64_t v_left = a.V - v_begin < a.g_pitch ? a.V - v_begin : a.g_pitch;
+  const int all_steps = static_cast<int>((v_left + kTileK - 1) / kTileK);
+  const int64_t part = a.row_pitch * a.g_pitch;
+
+  Job job;
+  job.a.across(a.H, wave, lane);
+  job.b.along(a.g_pitch, kTile, wave, lane);
+  TileAt at;
+  int split = 0;
+  auto start = [&] {
+    job.steps = 0;
+    if (!tiles.any()) return;
+    split = tiles.at / per_split;
+    at = tile_at(tiles.at % per_split, tiles_n, tiles_h);
+    const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
+    const int64_t from = static_cast<int64_t>(all_steps) * split / a.splits;
+    const int64_t to = static_cast<int64_t>(all_steps) * (split + 1) / a.splits;
+    const int once = to == from ? 1 : static_cast<int>(to - from);  // nothing left: a step of nothing
+    const int64_t v0 = v_begin + from * kTileK;
+    const uint16_t* const w = a.weight + v0 * a.H + h0;
+    const int64_t w_left = to == from ? 0 : ((a.V - v0) * a.H - h0) * 2;
+    const uint16_t* const gp = a.g + n0 * a.g_pitch + from * kTileK;
+    const int64_t g_left = ((a.row_pitch - n0) * a.g_pitch - from * kTileK) * 2;
+    job.a.aim(w, w_left);
+    job.b.aim(gp, g_left);
+    job.steps = once;
+    if (!a.grad_bf16) {
+      job.a.restart_after(once, w, w_left);
+      job.b.restart_after(once, gp + part, g_left);
+      job.steps = 2 * once;
+    }
+  };
+  int parity = 0;
+  start();
+  if (job.steps > 0) job.copy(lds, wave);
+  while (tiles.any()) {
+    const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
+    float* const sums = a.h_partials + split * a.row_pitch * a.H;
+    f32x4 acc[kMT][kNT] = {};
+    contract<true, false>(job, lds, parity, wave, lane, acc, [&] {
+      tiles.next();
+      start();
+    });
+    // Later pieces add to what the earlier ones left: the next step's row is fetched while
+    // this one's is added to.
+    const Rsrc out = make_rsrc(sums + n0 * a.H, (count - n0) * a.H * 4);
+    const Rsrc before = make_rsrc(sums + n0 * a.H, first ? 0 : (count - n0) * a.H * 4);
+    const int64_t h = h0 + (wave % 2) * kWaveM + 4 * g;
+    auto place = [&](int n, int m) -> uint32_t {
+      const int row = (wave / 2) * kWaveN + 16 * n + s;
+      return h + 16 * m < a.H ? static_cast<uint32_t>((row * a.H + h + 16 * m) * 4) : kOutOfRange;
+    };
+    f32x4 was[2][kMT];
 #pragma unroll
-  for (int n = 0; n < kNT; ++n) {
-    const int64_t row = n0 + (wave / 2) * kWaveN + 16 * n + s;
-    if (row >= count) continue;
-    float* const out = a.h_partials + (split * a.row_pitch + row) * a.H;
+    for (int m = 0; m < kMT; ++m) was[0][m] = load4(before, place(0, m));
 #pragma unroll
-    for (int m = 0; m < kMT; ++m) {
-      const int64_t h = h0 + (wave % 2) * kWaveM + 16 * m + 4 * g;
-      if (h >= a.H) continue;
-      f32x4 x = acc[m][n];
-      if (!first) x += *reinterpret_cast<const f32x4*>(out + h);
-      *reinterpret_cast<f32x4*>(out + h) = x;
+    for (int n = 0; n < kNT; ++n) {
+      if (n + 1 < kNT) {
+#pragma unroll
+        for (int m = 0; m < kMT; ++m) was[(n + 1) % 2][m] = load4(before, place(n + 1, m));
+      }
+#pragma unroll
+      for (int m = 0; m < kMT; ++m) {
+        f32x4 x = was[n % 2][m];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += element(acc[m][n], i);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, x), out, place(n, m), 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
+  __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
 int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
@@ -121,14 +176,14 @@ int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
 
 hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st) {
   const int64_t v = a.V - v0 < a.g_pitch ? a.V - v0 : a.g_pitch;
-  const dim3 grid(static_cast<unsigned>(tiles_of(a.H) * tiles_of(v))), block(kGemmThreads);
+  const dim3 grid(workgroups_of(tiles_of(a.H) * tiles_of(v))), block(kGemmThreads);
   if (a.grad_bf16) hipLaunchKernelGGL(vocab_d_weight_kernel<uint16_t>, grid, block, 0, st, a, v0);
   else hipLaunchKernelGGL(vocab_d_weight_kernel<float>, grid, block, 0, st, a, v0);
   return hipGetLastError();
 }
 
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(tiles_of(a.H) * tiles_of(a.N) * a.splits)), block(kGemmThreads);
+  const dim3 grid(workgroups_of(tiles_of(a.H) * tiles_of(a.N) * a.splits)), block(kGemmThreads);
   hipLaunchKernelGGL(vocab_d_hidden_kernel, grid, block, 0, st, a, v0, first ? 1 : 0);
   return hipGetLastError();
 }

@@ -172,17 +172,15 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void vocab_narrow_kernel(VocabArg
 
   Loader<kTileTokens, kWaves> lw;
   Loader<kRows, kWaves> lx;
+  lw.along(H, tokens, wave, lane);
+  lx.along(H, static_cast<int>(a.N), wave, lane);
   int64_t load_tile = blockIdx.x;
   int load_step = 0;
   auto start_tile = [&] {
     const int64_t v0 = load_tile * tokens;
     const bool any = load_tile < tiles;
-    lw.along(a.weight + v0 * H, (a.V - v0) * H * 2, static_cast<int>(H), wave, lane, [&](int r) -> uint32_t {
-      return any && r < tokens && v0 + r < a.V ? static_cast<uint32_t>(r * H * 2) : kOutOfRange;
-    });
-    lx.along(a.hidden, a.N * H * 2, static_cast<int>(H), wave, lane, [&](int r) -> uint32_t {
-      return any && r < a.N ? static_cast<uint32_t>(r * H * 2) : kOutOfRange;
-    });
+    lw.aim(a.weight + v0 * H, any ? (a.V - v0) * H * 2 : 0, static_cast<int>(H));
+    lx.aim(a.hidden, any ? a.N * H * 2 : 0, static_cast<int>(H));
   };
   // Behind the last tile everything is out of range: the number of copies in flight stays
   // the same, and with it what a wait for the oldest means.
