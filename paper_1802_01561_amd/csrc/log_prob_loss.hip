@@ -5,13 +5,17 @@
 // With x_t = v_t - V(x_t) the recursion is affine, x_t = delta_t + gamma_t c_t x_{t+1},
 // and maps compose: (A, B) o (A', B') = (A A', A B' + B).  A workgroup takes up to 16
 // consecutive lanes (64 bytes of a time row) and walks backwards over tiles of time: a
-// thread has 8 consecutive steps of one lane, composes them, and a suffix scan over the
+// thread has 4 consecutive steps of one lane, composes them, and a suffix scan over the
 // workgroup's threads gives each the value behind its steps.
 //
 // Few lanes with many steps are split along time as well (chunks of whole tiles): a
 // first launch forms the chunks' composites, and the second starts each chunk from the
 // composite of those behind it.  The inputs are then read twice, the second time mostly
 // from the Infinity Cache.
+//
+// Measured, us a call in a graph: T = 100, B = 32 (one launch) 9; T = 16384, B = 128 (1.56 M
+// steps of 36 bytes, 10 us at 5.5 TB/s) 33, bound by the latency of two walks of two tiles
+// each (four waves a SIMD; at three, 41); T = 1000, B = 16384 (590 MB) 186, 3.2 TB/s.
 #include "device_common.hpp"
 #include "log_prob_loss.hpp"
 #include "wave_ops.hpp"
@@ -23,6 +27,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kSteps = 4;       // consecutive steps of a thread
 constexpr int kMostLanes = 16;  // of a workgroup
+// Workgroups that an unroll is split up to: four a CU (16384 x 128: 33 us; 2048 of them 40).
 constexpr int64_t kWantedGroups = 1024;
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -30,10 +35,6 @@ constexpr double kLog2e = 1.4426950408889634;
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 constexpr int kRawBufferFlags = 0x00020000;
 constexpr uint32_t kOutOfRange = 0x80000000u;
-__device__ __forceinline__ Rsrc make_rsrc(const void* base, int64_t bytes) {
-  const int64_t n = bytes < 0x7fffffff ? bytes : 0x7fffffff;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(n), kRawBufferFlags);
-}
 
 struct Map {
   double a, b;  // x -> a x + b
@@ -73,8 +74,51 @@ struct Scan {
   }
 };
 
-template <int kLanes, bool kFinish>
-__global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
+// The loss totals as in finish_losses, but for the ticket: workgroups that finish together
+// would queue for one counter (about 10 ns each), so each of 32 counters takes a share of
+// them, and the workgroup that is the last of its counter draws the ticket.  Both are
+// thread 0's; the others follow through LDS.
+constexpr int kCounters = 32, kCounterWords = 32;  // a 128-byte line each
+__device__ __forceinline__ bool last_of_counter(const LogProbArgs& args) {
+  __shared__ int s_last;
+  if (gridDim.x == 1) return false;
+  if (threadIdx.x == 0) {
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // the partial stores have completed
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    const unsigned mine = blockIdx.x % kCounters;
+    const unsigned sharers = (gridDim.x - mine + kCounters - 1) / kCounters;
+    unsigned* const counter = args.counters + mine * kCounterWords;
+    bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sharers - 1;
+    if (last) {
+      __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const unsigned used = gridDim.x < kCounters ? gridDim.x : kCounters;
+      last = __hip_atomic_fetch_add(args.step.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
+    }
+    s_last = last;
+  }
+  __syncthreads();
+  return s_last != 0;
+}
+__device__ __forceinline__ void finish_counters(const LogProbArgs& args, double* scratch) {
+  const StepArgs& a = args.step;
+  double s0 = 0.0, s1 = 0.0, s2 = 0.0;
+#pragma unroll 4
+  for (unsigned i = threadIdx.x; i < gridDim.x; i += kThreads) {
+    const double* p = a.partials + 3 * static_cast<size_t>(i);
+    s0 += __hip_atomic_load(p + 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s1 += __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s2 += __hip_atomic_load(p + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  block_sum3<kThreads>(s0, s1, s2, scratch);
+  if (threadIdx.x == 0) {
+    store_totals(a, s0, s1, s2);
+    __hip_atomic_store(a.ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+template <int kLanes, bool kFinish, bool kEpsilon>
+__global__ __launch_bounds__(kThreads, 4) void log_prob_kernel(LogProbArgs args) {
   constexpr int kRows = kThreads / kLanes;        // threads of a lane
   constexpr int64_t kTileSteps = kRows * kSteps;
   __shared__ Scan<kLanes> s_scan;
@@ -106,9 +150,10 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
     const double rho = clip_above(ratio, rho_bar);
     return StepWeights{weighted ? rho : 1.0, lam * (weighted ? clip_above(ratio, c_bar) : 1.0), weighted_pg ? rho : 1.0};
   };
-  auto step_of = [](const StepWeights& w, double diff, float g, bool in) {  // x -> delta + gamma c x
-    return Map{in ? static_cast<double>(g) * w.c_v : 0.0, in ? w.rho_v * diff : 0.0};
+  auto step_of = [](const StepWeights& w, double diff, float g) {  // x -> delta + gamma c x
+    return Map{static_cast<double>(g) * w.c_v, w.rho_v * diff};
   };
+  const bool q_baseline = a.q_estimate == kQBaseline;
 
   double x_end = 0.0;  // x at the first step behind the tile
   if (kFinish && args.chunks > 1) {
@@ -117,10 +162,9 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
     const int64_t from = chunk + 1 + later * q / kRows, to = chunk + 1 + later * (q + 1) / kRows;
     Map m = {1.0, 0.0};
     if (lane_ok) {
-      for (int64_t k = to - 1; k >= from; --k) {
-        const double* p = args.composites + 2 * (k * a.B + b);
-        m = after({p[0], p[1]}, m);
-      }
+      const Map* const maps = reinterpret_cast<const Map*>(args.composites);
+#pragma unroll 4
+      for (int64_t k = to - 1; k >= from; --k) m = after(maps[k * a.B + b], m);
     }
     Map all;
     s_scan.behind(m, &all);
@@ -130,31 +174,51 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
   const int64_t tiles = (a.T + kTileSteps - 1) / kTileSteps;
   const int64_t first_tile = chunk * args.chunk_tiles;
   const int64_t last_tile = first_tile + args.chunk_tiles < tiles ? first_tile + args.chunk_tiles : tiles;
+  uint32_t place[kSteps + 1];  // of this thread's steps in a tile
+#pragma unroll
+  for (int j = 0; j <= kSteps; ++j) place[j] = 4 * ((static_cast<uint32_t>(q * kSteps) + j) * stride + l);
+  auto read = [](Rsrc p, uint32_t o) { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(p, o, 0, 0)); };
+  auto write = [](Rsrc p, uint32_t o, float value) {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), p, o, 0, 0);
+  };
   Map composite = {1.0, 0.0};
   double sum_pg = 0.0, sum_base = 0.0, sum_ent = 0.0;
   for (int64_t tile = last_tile - 1; tile >= first_tile; --tile) {
+    // Of this thread's steps in the tile, how many are the lane's, and how many there are.
     const int64_t t0 = tile * kTileSteps + q * kSteps;
-    // The tile's place in the arrays (uniform), and this thread's steps in it.  A step that
-    // is not a lane's own is read and written out of range: it reads 0 and writes nothing.
+    auto steps_to = [&](int64_t end) { return static_cast<int>(end - t0 < 0 ? 0 : end - t0 > kSteps + 1 ? kSteps + 1 : end - t0); };
+    const int mine_n = steps_to(n);
+    // The tile's place in the arrays (uniform).  A step that is not the lane's is read out of
+    // range, as zeros: log-ratio, reward, discount and value 0 make every quantity below 0.
     const int64_t corner = tile * kTileSteps * a.B + b0;
     const int64_t left = 4 * (a.T * a.B - corner);
-    auto array = [&](const void* p) { return make_rsrc(p ? static_cast<const float*>(p) + corner : p, p ? left : 0); };
-    auto read = [](Rsrc p, uint32_t o) { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(p, o, 0, 0)); };
-    const uint32_t at = 4 * (static_cast<uint32_t>(q * kSteps) * stride + l);
-    const Rsrc p_lp = array(args.target), p_lm = array(args.behaviour), p_r = array(a.rewards), p_g = array(a.discounts),
-               p_v = array(a.values);
-    float lp[kSteps], lm[kSteps], r[kSteps], gm[kSteps], v[kSteps + 1];
-    uint32_t off[kSteps];
+    const int records = left >> 31 ? 0x7fffffff : static_cast<int>(left);
+    auto array = [&](const void* p) {
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(static_cast<const float*>(p) + corner), 0, p ? records : 0,
+                                               kRawBufferFlags);
+    };
+    uint32_t off[kSteps + 1];
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      off[j] = t0 + j < n ? at + 4 * j * stride : kOutOfRange;
-      lp[j] = read(p_lp, off[j]);
-      lm[j] = read(p_lm, off[j]);
-      r[j] = read(p_r, off[j]);
-      gm[j] = read(p_g, off[j]);
-      v[j] = read(p_v, off[j]);
+    for (int j = 0; j <= kSteps; ++j) off[j] = j < mine_n ? place[j] : kOutOfRange;
+    float lp[kSteps], lm[kSteps], r[kSteps], gm[kSteps], v[kSteps + 1], entropy[kSteps];
+    {
+      const Rsrc p_lp = array(args.target), p_lm = array(args.behaviour), p_r = array(a.rewards), p_g = array(a.discounts),
+                 p_v = array(a.values);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        lp[j] = read(p_lp, off[j]);
+        lm[j] = read(p_lm, off[j]);
+        r[j] = read(p_r, off[j]);
+        gm[j] = read(p_g, off[j]);
+        v[j] = read(p_v, off[j]);
+      }
+      v[kSteps] = read(p_v, off[kSteps]);
     }
-    v[kSteps] = read(p_v, t0 + kSteps < n ? at + 4 * kSteps * stride : kOutOfRange);
+    if constexpr (kFinish) {
+      const Rsrc p_h = array(args.entropy);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) entropy[j] = read(p_h, off[j]);
+    }
     if (a.reward_transform != 0) {
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) r[j] = transform_reward(r[j], a.reward_transform);
@@ -164,50 +228,62 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
     Map mine = {1.0, 0.0};
 #pragma unroll
     for (int j = kSteps - 1; j >= 0; --j) {
-      const bool in = t0 + j < n;
       ratio[j] = exp2_f64((static_cast<double>(lp[j]) - static_cast<double>(lm[j])) * kLog2e);
-      const double v_next = t0 + j + 1 == n ? boot : static_cast<double>(v[j + 1]);
-      diff[j] = static_cast<double>(r[j]) + gm[j] * v_next - v[j];
-      mine = after(step_of(weights(ratio[j]), diff[j], gm[j], in), mine);
+      const double v_next = j + 1 == mine_n ? boot : v[j + 1];
+      diff[j] = fma(static_cast<double>(gm[j]), v_next, static_cast<double>(r[j]) - static_cast<double>(v[j]));
+      mine = after(step_of(weights(ratio[j]), diff[j], gm[j]), mine);
     }
     Map all;
     const Map behind = s_scan.behind(mine, &all);
     if constexpr (!kFinish) {
       composite = after(all, composite);
     } else {
-      const Rsrc o_lp = array(args.d_log_probs), o_v = array(a.d_values), o_h = array(args.d_entropy), o_vs = array(a.vs),
-                 o_adv = array(a.pg_adv), p_h = array(args.entropy);
-      auto write = [](Rsrc p, uint32_t o, float value) {
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), p, o, 0, 0);
-      };
-      float entropy[kSteps];
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) entropy[j] = read(p_h, off[j]);
+      const int here_n = lane_ok ? steps_to(a.T) : 0;
       double x = fma(behind.a, x_end, behind.b);
+      float d_lps[kSteps], d_vs[kSteps], advs[kSteps];
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {
-        const bool in = t0 + j < n;
         const StepWeights w = weights(ratio[j]);
-        const double behind_x = a.q_estimate == kQBaseline ? 0.0 : x;
-        const double adv = in ? w.rho_pg * fma(static_cast<double>(gm[j]), behind_x, diff[j]) : 0.0;
-        const Map m = step_of(w, diff[j], gm[j], in);
-        x = fma(m.a, x, m.b);
+        const double g = gm[j];
+        const double adv = w.rho_pg * (q_baseline ? diff[j] : fma(g, x, diff[j]));
+        x = fma(g * w.c_v, x, w.rho_v * diff[j]);
         double d_lp = adv, log_p = lp[j];
-        if (a.correction == kCorrEpsilon) {
+        if constexpr (kEpsilon) {
           const double p = exp2_f64(log_p * kLog2e), eps = a.epsilon;
           d_lp *= p / (p + eps);
           log_p = log(p + eps);
         }
-        sum_pg -= in ? adv * log_p : 0.0;
-        sum_base += 0.5 * x * x;
+        sum_pg = fma(-adv, log_p, sum_pg);
+        sum_base = fma(0.5 * x, x, sum_base);
         sum_ent -= static_cast<double>(entropy[j]);
-        // Steps behind a lane's last get zeros.
-        const uint32_t o = t0 + j < a.T && lane_ok ? at + 4 * j * stride : kOutOfRange;
-        write(o_lp, o, in ? static_cast<float>(-d_lp) : 0.0f);
-        write(o_v, o, in ? static_cast<float>(-a.baseline_cost * x) : 0.0f);
-        write(o_h, o, in ? -a.entropy_cost : 0.0f);
-        write(o_vs, o, in ? static_cast<float>(v[j] + x) : 0.0f);
-        write(o_adv, o, static_cast<float>(adv));
+        d_lps[j] = static_cast<float>(-d_lp);
+        d_vs[j] = static_cast<float>(-a.baseline_cost * x);
+        advs[j] = static_cast<float>(adv);
+        if (a.vs) v[j] = static_cast<float>(v[j] + x);
+      }
+      // Steps behind a lane's last get zeros.
+#pragma unroll
+      for (int j = 0; j <= kSteps; ++j) off[j] = j < here_n ? place[j] : kOutOfRange;
+      const Rsrc o_lp = array(args.d_log_probs), o_v = array(a.d_values);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        write(o_lp, off[j], d_lps[j]);
+        write(o_v, off[j], d_vs[j]);
+      }
+      if (args.d_entropy) {
+        const Rsrc o = array(args.d_entropy);
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) write(o, off[j], j < mine_n ? -a.entropy_cost : 0.0f);
+      }
+      if (a.vs) {
+        const Rsrc o = array(a.vs);
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) write(o, off[j], v[j]);
+      }
+      if (a.pg_adv) {
+        const Rsrc o = array(a.pg_adv);
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) write(o, off[j], advs[j]);
       }
       x_end = fma(all.a, x_end, all.b);
     }
@@ -219,7 +295,9 @@ __global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs args) {
       p[1] = composite.b;
     }
   } else {
-    finish_losses<kThreads>(a, sum_pg, a.baseline_cost * sum_base, a.entropy_cost * sum_ent, s_red);
+    block_sum3<kThreads>(sum_pg, sum_base, sum_ent, s_red);
+    if (threadIdx.x == 0) publish_losses(a, sum_pg, a.baseline_cost * sum_base, a.entropy_cost * sum_ent);
+    if (last_of_counter(args)) finish_counters(args, s_red);
   }
 }
 
@@ -245,6 +323,7 @@ void split_time(int64_t T, int64_t B, int64_t* chunks, int64_t* chunk_tiles, int
   *chunks = (tiles + *chunk_tiles - 1) / *chunk_tiles;
 }
 
+constexpr size_t kCounterBytes = kCounters * kCounterWords * sizeof(unsigned);
 size_t partial_bytes(int64_t groups) { return (static_cast<size_t>(groups) * 3 * sizeof(double) + 255) / 256 * 256; }
 
 template <int kLanes>
@@ -252,11 +331,14 @@ hipError_t launch(const LogProbArgs& a, hipStream_t st) {
   const int64_t groups = (a.step.B + kLanes - 1) / kLanes;
   const dim3 grid(static_cast<unsigned>(groups * a.chunks)), block(kThreads);
   if (a.chunks > 1) {
-    hipLaunchKernelGGL((log_prob_kernel<kLanes, false>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((log_prob_kernel<kLanes, false, false>), grid, block, 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((log_prob_kernel<kLanes, true>), grid, block, 0, st, a);
+  if (a.step.correction == kCorrEpsilon)
+    hipLaunchKernelGGL((log_prob_kernel<kLanes, true, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((log_prob_kernel<kLanes, true, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -266,7 +348,7 @@ size_t log_prob_workspace_bytes(int64_t T, int64_t B) {
   int64_t chunks, chunk_tiles, groups;
   split_time(T, B, &chunks, &chunk_tiles, &groups);
   const size_t composites = chunks > 1 ? static_cast<size_t>(chunks * B) * 2 * sizeof(double) : 0;
-  return kWsHeaderBytes + partial_bytes(groups * chunks) + composites;
+  return kWsHeaderBytes + kCounterBytes + partial_bytes(groups * chunks) + composites;
 }
 
 void attach_log_prob_workspace(LogProbArgs* a, void* ws) {
@@ -274,8 +356,10 @@ void attach_log_prob_workspace(LogProbArgs* a, void* ws) {
   split_time(a->step.T, a->step.B, &a->chunks, &a->chunk_tiles, &groups);
   char* const base = static_cast<char*>(ws);
   a->step.ticket = reinterpret_cast<unsigned int*>(base + kWsTicketOffset);
-  a->step.partials = reinterpret_cast<double*>(base + kWsHeaderBytes);
-  a->composites = reinterpret_cast<double*>(base + kWsHeaderBytes + partial_bytes(groups * a->chunks));
+  a->counters = reinterpret_cast<unsigned int*>(base + kWsHeaderBytes);
+  char* const sums = base + kWsHeaderBytes + kCounterBytes;
+  a->step.partials = reinterpret_cast<double*>(sums);
+  a->composites = reinterpret_cast<double*>(sums + partial_bytes(groups * a->chunks));
 }
 
 hipError_t launch_log_prob_loss(const LogProbArgs& a, hipStream_t st) {

@@ -26,6 +26,7 @@ struct LogProbArgs {
   // Long unrolls are split along time: each chunk's composite of the recursion.
   int64_t chunks, chunk_tiles;
   double* composites;  // [chunks, B, 2]
+  unsigned int* counters;
 };
 
 size_t log_prob_workspace_bytes(int64_t T, int64_t B);

@@ -81,7 +81,7 @@ def test_losses_and_gradients(T, B, ragged):
         for k in ("target_log_probs", "behaviour_log_probs", "entropy", "rewards", "discounts", "values"):
             d[k][behind] = float("nan")
     ws = vt.LogProbWorkspace(T, B)
-    ws.tensor[256:].fill_(0xFF)
+    ws.tensor[256 + 4096:].fill_(0xFF)  # behind the counters, which every call leaves at zero
     for s in (PLAIN, dict(rho_bar=0.9, c_bar=0.5, lam=0.95, baseline_cost=0.3, entropy_cost=0.1)):
         out = vt.vtrace_log_prob_loss_grad(**d, **s, workspace=ws, with_vs=True, with_pg_advantages=True)
         assert (out.d_entropy is None) == (x["entropy"] is None)
