@@ -142,7 +142,7 @@ vtrace_status vtrace_log_prob_loss_grad(
  *
  *   count       0 .. 2^16 gradients; gradients, outputs, sizes and dtypes are HOST
  *               arrays of that length, read during the call
- *   gradients   device pointers to sizes[i] >= 0 contiguous elements of dtypes[i]
+ *   gradients   device pointers to sizes[i] (0 .. 2^36) contiguous elements of dtypes[i]
  *               (VTRACE_F32 or VTRACE_BF16), element-aligned (NULL if sizes[i] is 0)
  *   outputs     where the clipped gradients go, of the same sizes and types.  An output may be
  *               its own gradient (clipping in place); it may not overlap anything
@@ -157,7 +157,7 @@ vtrace_status vtrace_log_prob_loss_grad(
  * a NaN anywhere makes the norm and every output NaN, an infinite norm gives 0
  * for finite elements and NaN for infinite ones.
  */
-#define VTRACE_CLIP_WORKSPACE_BYTES 33024
+#define VTRACE_CLIP_WORKSPACE_BYTES 20736
 
 vtrace_status vtrace_clip_grad_norm(
     int64_t count, const void* const* gradients, void* const* outputs, const int64_t* sizes,

@@ -82,7 +82,7 @@ TOKEN_SIGNATURES = {
                                   + [ctypes.c_size_t, _P]),
     "vtrace_clip_grad_norm": (_I, [_I64] + [_P] * 4 + [_F] + [_P] * 2 + [ctypes.c_size_t, _P]),
 }
-CLIP_WORKSPACE_BYTES = 33024  # VTRACE_CLIP_WORKSPACE_BYTES
+CLIP_WORKSPACE_BYTES = 20736  # VTRACE_CLIP_WORKSPACE_BYTES
 
 _lib = None
 

@@ -9,7 +9,9 @@
 namespace vtrace {
 
 constexpr int64_t kClipMostTensors = 1 << 16;
-constexpr int kClipMostBlocks = 4096;
+// Of one gradient: its chunks are a launch's workgroups.
+constexpr int64_t kClipMostElements = int64_t(1) << 36;
+constexpr int kClipMostBlocks = 2048;
 
 // One gradient of a call.
 struct ClipItem {

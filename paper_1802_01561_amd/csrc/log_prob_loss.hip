@@ -18,6 +18,7 @@
 // each (four waves a SIMD; at three, 41); T = 1000, B = 16384 (590 MB) 186, 3.2 TB/s.
 #include "device_common.hpp"
 #include "log_prob_loss.hpp"
+#include "tickets.hpp"
 #include "wave_ops.hpp"
 
 namespace vtrace {
@@ -74,34 +75,8 @@ struct Scan {
   }
 };
 
-// The loss totals as in finish_losses, but for the ticket: workgroups that finish together
-// would queue for one counter (about 10 ns each), so each of 32 counters takes a share of
-// them, and the workgroup that is the last of its counter draws the ticket.  Both are
-// thread 0's; the others follow through LDS.
-constexpr int kCounters = 32, kCounterWords = 32;  // a 128-byte line each
-__device__ __forceinline__ bool last_of_counter(const LogProbArgs& args) {
-  __shared__ int s_last;
-  if (gridDim.x == 1) return false;
-  if (threadIdx.x == 0) {
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // the partial stores have completed
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    const unsigned mine = blockIdx.x % kCounters;
-    const unsigned sharers = (gridDim.x - mine + kCounters - 1) / kCounters;
-    unsigned* const counter = args.counters + mine * kCounterWords;
-    bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sharers - 1;
-    if (last) {
-      __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const unsigned used = gridDim.x < kCounters ? gridDim.x : kCounters;
-      last = __hip_atomic_fetch_add(args.step.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
-    }
-    s_last = last;
-  }
-  __syncthreads();
-  return s_last != 0;
-}
-__device__ __forceinline__ void finish_counters(const LogProbArgs& args, double* scratch) {
-  const StepArgs& a = args.step;
+// The loss totals, by the last workgroup.
+__device__ __forceinline__ void add_totals(const StepArgs& a, double* scratch) {
   double s0 = 0.0, s1 = 0.0, s2 = 0.0;
 #pragma unroll 4
   for (unsigned i = threadIdx.x; i < gridDim.x; i += kThreads) {
@@ -111,10 +86,7 @@ __device__ __forceinline__ void finish_counters(const LogProbArgs& args, double*
     s2 += __hip_atomic_load(p + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   block_sum3<kThreads>(s0, s1, s2, scratch);
-  if (threadIdx.x == 0) {
-    store_totals(a, s0, s1, s2);
-    __hip_atomic_store(a.ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  if (threadIdx.x == 0) store_totals(a, s0, s1, s2);
 }
 
 template <int kLanes, bool kFinish, bool kEpsilon>
@@ -297,7 +269,7 @@ __global__ __launch_bounds__(kThreads, 4) void log_prob_kernel(LogProbArgs args)
   } else {
     block_sum3<kThreads>(sum_pg, sum_base, sum_ent, s_red);
     if (threadIdx.x == 0) publish_losses(a, sum_pg, a.baseline_cost * sum_base, a.entropy_cost * sum_ent);
-    if (last_of_counter(args)) finish_counters(args, s_red);
+    if (gridDim.x > 1 && last_workgroup(a.ticket, args.counters)) add_totals(a, s_red);
   }
 }
 
@@ -323,7 +295,6 @@ void split_time(int64_t T, int64_t B, int64_t* chunks, int64_t* chunk_tiles, int
   *chunks = (tiles + *chunk_tiles - 1) / *chunk_tiles;
 }
 
-constexpr size_t kCounterBytes = kCounters * kCounterWords * sizeof(unsigned);
 size_t partial_bytes(int64_t groups) { return (static_cast<size_t>(groups) * 3 * sizeof(double) + 255) / 256 * 256; }
 
 template <int kLanes>

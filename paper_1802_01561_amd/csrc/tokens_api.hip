@@ -188,7 +188,7 @@ vtrace_status vtrace_clip_grad_norm(int64_t count, const void* const* gradients,
   if (!workspace) return VTRACE_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return VTRACE_ERR_ALIGN;
   if (workspace_bytes < vtrace::clip_workspace_bytes()) return VTRACE_ERR_WORKSPACE;
-  static_assert(VTRACE_CLIP_WORKSPACE_BYTES == 256 + 8 * vtrace::kClipMostBlocks, "header states the size");
+  static_assert(VTRACE_CLIP_WORKSPACE_BYTES == 256 + 4096 + 8 * vtrace::kClipMostBlocks, "header states the size");
   try {
     // What is read and what is written, to find outputs that overlap anything.
     struct Range {
@@ -206,7 +206,7 @@ vtrace_status vtrace_clip_grad_norm(int64_t count, const void* const* gradients,
       ranges.push_back({w, w + workspace_bytes, true, -2});
     }
     for (int64_t i = 0; i < count; ++i) {
-      if (sizes[i] < 0 || sizes[i] > vtrace::kMaxElements) return VTRACE_ERR_SHAPE;
+      if (sizes[i] < 0 || sizes[i] > vtrace::kClipMostElements) return VTRACE_ERR_SHAPE;
       if (dtypes[i] != VTRACE_F32 && dtypes[i] != VTRACE_BF16) return VTRACE_ERR_DTYPE;
       if (sizes[i] == 0) continue;
       const uintptr_t bytes = dtypes[i] == VTRACE_F32 ? 4 : 2;

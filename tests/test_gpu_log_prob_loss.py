@@ -196,7 +196,7 @@ CLIP = [([1], [F]), ([1], [H]), ([5, 0, 3], [F, H, H]), ([16384, 16385, 16383, 1
 @pytest.mark.parametrize("sizes,dtypes", CLIP)
 def test_clip(sizes, dtypes, shift):
     ws = vt.ClipWorkspace()
-    ws.tensor[256:].fill_(0xFF)
+    ws.tensor[256 + 4096:].fill_(0xFF)
     grads = _grads(len(sizes), sizes, dtypes, shift)
     for max_norm in (0.25, 1e6):
         outs = _grads(9, sizes, dtypes, shift if max_norm < 1 else 0)  # alike and other alignments
