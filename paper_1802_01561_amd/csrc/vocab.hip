@@ -5,11 +5,27 @@
 namespace vtrace {
 namespace {
 
+// Tiles that d_hidden's product is split up to (two rounds of the CUs).
+constexpr int kMostSplitTiles = 512;
+
 constexpr int kListThreads = 1024;
 constexpr int kListItems = 8;  // tokens per thread and pass
 
+// The time of d_hidden's product with `splits` parts, in units of a step of 64 k (1.56 us,
+// all CUs): every CU has `rounds` tiles one after the other, each of them with its share
+// of a piece's steps, stores what 8 steps take, and in the end the parts are added.
+__device__ __forceinline__ float split_cost(const VocabArgs& a, int tiles, int rows, int steps, int splits) {
+  const int passes = a.grad_bf16 ? 1 : 2;
+  const int rounds = (tiles * splits + kCus - 1) / kCus, share = (steps + splits - 1) / splits;
+  const float bytes = static_cast<float>(splits) * static_cast<float>(rows) * static_cast<float>(a.H) * 4.0f;
+  return static_cast<float>(a.pieces) * static_cast<float>(rounds) * static_cast<float>(share * passes + 8) + bytes * (1.0f / 8e6f);
+}
+
 // active[0 .. count) = the steps with a token, in order.  One workgroup: a pass over
-// 8192 tokens counts, scans and writes.
+// 8192 tokens counts, scans and writes.  For the gradient it also chooses the number of
+// parts of d_hidden's product, which depends on the count: the cheapest of the numbers with
+// which the tiles fit the workspace.
+template <bool kGrad>
 __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
   constexpr int kWaves = kListThreads / kWave;
   __shared__ int s_count[2][kWaves];
@@ -46,6 +62,32 @@ __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
     }
   }
   if (threadIdx.x == 0) *a.active_count = total;
+  if constexpr (kGrad) {
+    __shared__ float s_cost[kWaves];
+    __shared__ int s_splits[kWaves];
+    const int tiles_n = (total + kTile - 1) / kTile;
+    const int tiles = tiles_n * static_cast<int>((a.H + kTile - 1) / kTile);
+    const int steps = static_cast<int>(a.g_pitch / kTileK);
+    int splits = threadIdx.x + 1;
+    float cost = splits <= steps && (splits == 1 || tiles * splits <= kMostSplitTiles)
+                     ? split_cost(a, tiles, tiles_n * kTile, steps, splits)
+                     : INFINITY;
+    auto take = [&](float c, int k) {
+      if (c < cost || (c == cost && k < splits)) cost = c, splits = k;
+    };
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+      const float c = __shfl_xor(cost, o, kWave);
+      const int k = __shfl_xor(splits, o, kWave);
+      take(c, k);
+    }
+    if (lane == 0) s_cost[wave] = cost, s_splits[wave] = splits;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < kWaves; ++w) take(s_cost[w], s_splits[w]);
+      *a.splits = splits;
+    }
+  }
 }
 
 // A step's outputs from the joined statistics: sums of 2^d and of 2^d d, d = z log2 e - c.
@@ -221,9 +263,10 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
   const int64_t row = i / quads, h = (i % quads) * 4;
   if (row >= *a.active_count) return;
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int splits = *a.splits;
+  const int64_t rows = (static_cast<int64_t>(*a.active_count) + kTile - 1) / kTile * kTile;
 #pragma unroll 8
-  for (int k = 0; k < a.splits; ++k)
-    x += *reinterpret_cast<const f32x4*>(a.h_partials + (k * a.row_pitch + row) * a.H + h);
+  for (int k = 0; k < splits; ++k) x += *reinterpret_cast<const f32x4*>(a.h_partials + (k * rows + row) * a.H + h);
   Out* const out = static_cast<Out*>(a.d_hidden) + static_cast<int64_t>(a.active[row]) * a.H + h;
   if constexpr (sizeof(Out) == 4) {
     *reinterpret_cast<f32x4*>(out) = x;
@@ -249,7 +292,8 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a,
 int64_t round_up(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 unsigned blocks_of(int64_t n, int64_t k) { return static_cast<unsigned>((n + k - 1) / k); }
 
-constexpr size_t kHeaderCountOffset = 8;  // behind the counter and the error flag
+// Behind the counter and the error flag.
+constexpr size_t kHeaderCountOffset = 8, kHeaderSplitsOffset = 12;
 
 // Pieces of a workspace, each on a 256-byte boundary.
 struct Carver {
@@ -295,14 +339,15 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->row_pitch = p.row_pitch;
   a->x_pitch = p.x_pitch;
   a->g_pitch = p.g_pitch;
-  a->splits = p.splits;
+  a->pieces = p.pieces;
+  a->splits = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderSplitsOffset);
   a->active = c.take<int32_t>(a->N);
   a->row_scalars = c.take<float4v>(p.row_pitch);
   a->row_tokens = c.take<int32_t>(p.row_pitch);
   a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
   a->g = c.take<uint16_t>((a->grad_bf16 ? 1 : 2) * p.row_pitch * p.g_pitch);
   a->bias_partials = c.take<float>(p.row_pitch / kWaveN * p.g_pitch);
-  a->h_partials = c.take<float>(p.splits * p.row_pitch * a->H);
+  a->h_partials = c.take<float>(p.split_rows * a->H);
   return c.at;
 }
 
@@ -318,8 +363,6 @@ constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
 // G of one piece takes at most this much (or one tile's columns): it is written and read
 // twice within the 256 MB Infinity Cache.
 constexpr int64_t kMostPieceBytes = int64_t(256) << 20;
-// Workgroups that d_hidden's product is split up to.
-constexpr int64_t kWantedTiles = 512;
 
 }  // namespace
 
@@ -363,10 +406,11 @@ VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
   const int64_t most = fit < kTile ? kTile : fit;
   const int64_t pieces = (all + most - 1) / most;
   p.g_pitch = round_up((all + pieces - 1) / pieces, kTile);
-  const int64_t tiles = (p.row_pitch / kTile) * ((H + kTile - 1) / kTile);
-  int64_t splits = kWantedTiles / tiles;
-  if (splits > p.g_pitch / (8 * kTileK)) splits = p.g_pitch / (8 * kTileK);
-  p.splits = static_cast<int>(splits < 1 ? 1 : splits);
+  p.pieces = pieces;
+  // d_hidden's tiles, whatever the number of active steps: those of one part, or as many as
+  // it is split into at most.
+  const int64_t split_rows = kMostSplitTiles / ((H + kTile - 1) / kTile) * kTile;
+  p.split_rows = split_rows > p.row_pitch ? split_rows : p.row_pitch;
   VocabArgs a = {};
   a.N = N;
   a.H = H;
@@ -381,7 +425,7 @@ void attach_vocab_grad(VocabArgs* a, const VocabPlan& p, void* ws) { carve_grad(
 hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
   hipError_t e;
   if (!p.few) {
-    hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
+    hipLaunchKernelGGL(vocab_list_kernel<false>, dim3(1), dim3(kListThreads), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(vocab_gather_kernel<false>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
                        dim3(kGatherThreads), 0, st, a);
@@ -400,7 +444,7 @@ hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStr
 
 hipError_t launch_vocab_grad(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
   hipError_t e;
-  hipLaunchKernelGGL(vocab_list_kernel, dim3(1), dim3(kListThreads), 0, st, a);
+  hipLaunchKernelGGL(vocab_list_kernel<true>, dim3(1), dim3(kListThreads), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(vocab_gather_kernel<true>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
                      dim3(kGatherThreads), 0, st, a);

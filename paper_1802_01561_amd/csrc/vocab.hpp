@@ -48,7 +48,7 @@ struct VocabArgs {
   float* part_dot;        // or null
   float* token_logit;     // [row_pitch]
   int64_t row_pitch;
-  int64_t pieces;
+  int64_t pieces;         // grad: of the vocabulary
   int tile_tokens;        // of the kernels for few steps
   bool narrow;            // the one for 17 to 128 steps
   // tiles: the active steps' hidden states, zeros around, and tokens
@@ -60,17 +60,17 @@ struct VocabArgs {
   uint16_t* g;            // [1 or 2, row_pitch, g_pitch] G of one piece: high (and low) parts
   int64_t g_pitch;        // tokens of a piece, a multiple of the tile
   float* bias_partials;   // [row_pitch / 128, g_pitch]
-  float* h_partials;      // [splits, row_pitch, H]
-  int splits;
+  float* h_partials;      // [*splits, count rounded up to tiles, H]
+  int32_t* splits;        // in the header: parts of d_hidden's product
 };
 
 struct VocabPlan {
   bool few;        // log_probs: the kernels for few steps
-  int64_t pieces;  // log_probs: statistics per step
+  int64_t pieces;  // log_probs: statistics per step; grad: of the vocabulary
   int tile_tokens;
   bool narrow;
   int64_t row_pitch, x_pitch, g_pitch;
-  int splits;
+  int64_t split_rows;
   size_t bytes;
 };
 VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H);

@@ -85,14 +85,15 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabAr
 }
 
 // d_hidden's tiles are few where there are few steps: k (the piece) is split into `splits`
-// parts, each with float32 sums of its own that grow over the pieces.
+// parts, each with float32 sums of its own that grow over the pieces (how many parts is
+// chosen on the device: vocab_list_kernel).
 __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
   __shared__ __align__(1024) char lds[kGemmLds];
   const int count = *a.active_count;
   const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
   const int tiles_n = (count + kTile - 1) / kTile;
-  const int per_split = tiles_h * tiles_n;
-  Tiles tiles(static_cast<int64_t>(per_split) * a.splits);
+  const int per_split = tiles_h * tiles_n, splits = *a.splits;
+  Tiles tiles(static_cast<int64_t>(per_split) * splits);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, g = lane / 16;
@@ -111,8 +112,8 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
     split = tiles.at / per_split;
     at = tile_at(tiles.at % per_split, tiles_n, tiles_h);
     const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
-    const int64_t from = static_cast<int64_t>(all_steps) * split / a.splits;
-    const int64_t to = static_cast<int64_t>(all_steps) * (split + 1) / a.splits;
+    const int64_t from = static_cast<int64_t>(all_steps) * split / splits;
+    const int64_t to = static_cast<int64_t>(all_steps) * (split + 1) / splits;
     const int once = to == from ? 1 : static_cast<int>(to - from);  // nothing left: a step of nothing
     const int64_t v0 = v_begin + from * kTileK;
     const uint16_t* const w = a.weight + v0 * a.H + h0;
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   if (job.steps > 0) job.copy(lds, wave);
   while (tiles.any()) {
     const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
-    float* const sums = a.h_partials + split * a.row_pitch * a.H;
+    float* const sums = a.h_partials + static_cast<int64_t>(split) * tiles_n * kTile * a.H;
     f32x4 acc[kMT][kNT] = {};
     contract<true, false>(job, lds, parity, wave, lane, acc, [&] {
       tiles.next();
@@ -183,7 +184,7 @@ hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st)
 }
 
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t st) {
-  const dim3 grid(workgroups_of(tiles_of(a.H) * tiles_of(a.N) * a.splits)), block(kGemmThreads);
+  const dim3 grid(kCus), block(kGemmThreads);
   hipLaunchKernelGGL(vocab_d_hidden_kernel, grid, block, 0, st, a, v0, first ? 1 : 0);
   return hipGetLastError();
 }
