@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
 __global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a, int64_t v_begin) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
   if (i >= a.g_pitch || v_begin + i >= a.V) return;
-  const int64_t blocks = (static_cast<int64_t>(*a.active_count) + kWaveN - 1) / kWaveN;
+  const int64_t blocks = (static_cast<int64_t>(*a.active_count) + kBiasSteps - 1) / kBiasSteps;
   double sum = 0.0;
 #pragma unroll 8
   for (int64_t b = 0; b < blocks; ++b) sum += static_cast<double>(a.bias_partials[b * a.g_pitch + i]);
@@ -326,6 +326,7 @@ size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->part_dot = c.take<float>(p.pieces * p.row_pitch);
   a->token_logit = c.take<float>(p.row_pitch);
   if (!p.few) {
+    a->small_logits = p.small_logits;
     a->x_pitch = p.x_pitch;
     a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
     a->row_tokens = c.take<int32_t>(p.row_pitch);
@@ -339,6 +340,8 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->row_pitch = p.row_pitch;
   a->x_pitch = p.x_pitch;
   a->g_pitch = p.g_pitch;
+  a->small_logits = p.small_logits;
+  a->small_weight = p.small_weight;
   a->pieces = p.pieces;
   a->splits = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderSplitsOffset);
   a->active = c.take<int32_t>(a->N);
@@ -346,7 +349,7 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->row_tokens = c.take<int32_t>(p.row_pitch);
   a->x = c.take<uint16_t>(p.row_pitch * p.x_pitch);
   a->g = c.take<uint16_t>((a->grad_bf16 ? 1 : 2) * p.row_pitch * p.g_pitch);
-  a->bias_partials = c.take<float>(p.row_pitch / kWaveN * p.g_pitch);
+  a->bias_partials = c.take<float>(p.row_pitch / kBiasSteps * p.g_pitch);
   a->h_partials = c.take<float>(p.split_rows * a->H);
   return c.at;
 }
@@ -363,6 +366,20 @@ constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
 // G of one piece takes at most this much (or one tile's columns): it is written and read
 // twice within the 256 MB Infinity Cache.
 constexpr int64_t kMostPieceBytes = int64_t(256) << 20;
+
+// Whether a product m x n over `steps` steps of 64 k is done in tiles of 128 rather than of
+// 256.  A round of tiles of 256 (one a CU) takes 1.56 us a step and 13 us, one of tiles of
+// 128 (two a CU, half as many products) 1.2 and 6.  640 steps, H = 256, V = 32768: logits 40
+// us in two rounds, 32 in three small ones; d_weight (float32) 47 in one half empty, 29 in a
+// small one.  3200 steps, H = 1024: 261 in seven, 303 in thirteen small ones.
+bool small_tiles_pay(int64_t m, int64_t n, int64_t steps) {
+  auto rounds = [&](int size, int64_t resident) {
+    const int64_t tiles = tiles_of(m, size) * tiles_of(n, size);
+    return static_cast<double>((tiles + resident - 1) / resident);
+  };
+  const double k = static_cast<double>(steps);
+  return rounds(kSmallTile, kResident<kSmallTile>) * (1.2 * k + 6.0) < rounds(kTile, kResident<kTile>) * (1.56 * k + 13.0);
+}
 
 }  // namespace
 
@@ -389,7 +406,8 @@ VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
   } else {
     p.row_pitch = round_up(N, kTile);
     p.x_pitch = round_up(H, kTileK);
-    p.pieces = 2 * ((V + kTile - 1) / kTile);
+    p.small_logits = small_tiles_pay(N, V, p.x_pitch / kTileK);
+    p.pieces = 2 * tiles_of(V, p.small_logits ? kSmallTile : kTile);
   }
   VocabArgs a = {};
   a.N = N;
@@ -407,6 +425,8 @@ VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
   const int64_t pieces = (all + most - 1) / most;
   p.g_pitch = round_up((all + pieces - 1) / pieces, kTile);
   p.pieces = pieces;
+  p.small_logits = small_tiles_pay(N, p.g_pitch, p.x_pitch / kTileK);
+  p.small_weight = small_tiles_pay(H, p.g_pitch, tiles_of(N, kTileK) * (grad_bf16 ? 1 : 2));
   // d_hidden's tiles, whatever the number of active steps: those of one part, or as many as
   // it is split into at most.
   const int64_t split_rows = kMostSplitTiles / ((H + kTile - 1) / kTile) * kTile;

@@ -15,6 +15,8 @@ constexpr int64_t kVocabMaxHidden = 32768;
 // Hidden states are addressed with 31-bit byte offsets.
 constexpr int64_t kVocabMaxHiddenElements = (int64_t(1) << 30) - 1;
 constexpr int32_t kNoToken = -1;
+// Steps of one partial sum of d_bias.
+constexpr int kBiasSteps = 64;
 
 // Everything the kernels of one call need.  N = T B steps; "active" steps are
 // those whose token is not kNoToken, numbered in their order.
@@ -37,6 +39,7 @@ struct VocabArgs {
   void* d_weight;            // [V,H]
   float* d_bias;             // [V] or null
   int grad_bf16;
+  bool small_logits, small_weight;  // tiles of 128 instead of 256
   // workspace pieces
   unsigned int* error_flag;
   int32_t* active_count;  // in the header
@@ -59,7 +62,7 @@ struct VocabArgs {
   float4v* row_scalars;   // [row_pitch]: log-sum (log2 units), c0, c1, d_log_probs
   uint16_t* g;            // [1 or 2, row_pitch, g_pitch] G of one piece: high (and low) parts
   int64_t g_pitch;        // tokens of a piece, a multiple of the tile
-  float* bias_partials;   // [row_pitch / 128, g_pitch]
+  float* bias_partials;   // [row_pitch / kBiasSteps, g_pitch]
   float* h_partials;      // [*splits, count rounded up to tiles, H]
   int32_t* splits;        // in the header: parts of d_hidden's product
 };
@@ -69,6 +72,7 @@ struct VocabPlan {
   int64_t pieces;  // log_probs: statistics per step; grad: of the vocabulary
   int tile_tokens;
   bool narrow;
+  bool small_logits, small_weight;
   int64_t row_pitch, x_pitch, g_pitch;
   int64_t split_rows;
   size_t bytes;

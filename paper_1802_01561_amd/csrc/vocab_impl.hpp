@@ -29,18 +29,19 @@
 namespace vtrace {
 namespace {
 
-constexpr int kTile = 256;
+constexpr int kTile = 256, kSmallTile = 128;
 constexpr int kTileK = 64;
 constexpr int kGemmThreads = 256;
-constexpr int kOperandBytes = kTile * kTileK * 2;
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kGemmLds = 2 * kStageBytes;
-constexpr int kWaveM = 128, kWaveN = 128;
-constexpr int kMT = kWaveM / 16, kNT = kWaveN / 16;
+// Of a tile of kSize x kSize: an operand's bytes of a step, and two steps of both.
+constexpr int operand_bytes(int size) { return size * kTileK * 2; }
+constexpr int tile_lds(int size) { return 4 * operand_bytes(size); }
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+// A wave's quarter of a tile.
+template <int kSize>
+using Accumulators = f32x4[kSize / 32][kSize / 32];
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 typedef __attribute__((address_space(3))) void LdsVoid;
@@ -104,13 +105,13 @@ struct Loader {
   }
   // k outermost, rows of `pitch` elements.
   __device__ __forceinline__ void across(int64_t pitch, int wave, int lane) {
-    static_assert(kRows == kTile, "rows of 512 bytes in LDS");
+    constexpr int kSlots = kRows / 8, kWaveRows = kWave / kSlots;
     step = kTileK * 2 * pitch;
     lane_k = 0;
-    const int slot = lane % 32;
+    const int slot = lane % kSlots;
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      const int r = i * 2 * kWaves + wave * 2 + lane / 32;
+      const int r = (i * kWaves + wave) * kWaveRows + lane / kSlots;
       const int c = (((slot >> 1) ^ swizzle_of(r)) << 1) | (slot & 1);
       off[i] = static_cast<uint32_t>(r * pitch * 2) + c * 16;
     }
@@ -159,7 +160,7 @@ struct Loader {
 // of a stage.  kTransposed: "across".  kPaired ("along"): tiles 2p and 2p + 1 together
 // give lane group g the rows 32p + 8g .. 32p + 8g + 7 in its accumulators, four of each
 // (so that eight consecutive results are one 16-byte store).
-template <bool kTransposed, bool kPaired, int kTiles>
+template <bool kTransposed, bool kPaired, int kTiles, int kRows = kTile>
 struct Reader {
   int at[kTransposed ? kTiles : 2];
 
@@ -168,7 +169,7 @@ struct Reader {
       const int k = 8 * g + s / 4;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
-        at[t] = k * (kTile * 2) + (((first_row / 16 + t) ^ swizzle_of(k)) * 32) + (s % 4) * 8;
+        at[t] = k * (kRows * 2) + (((first_row / 16 + t) ^ swizzle_of(k)) * 32) + (s % 4) * 8;
     } else {
       const int r = first_row + (kPaired ? 8 * (s / 4) + s % 4 : s);
 #pragma unroll
@@ -178,9 +179,9 @@ struct Reader {
   __device__ __forceinline__ bf16x8 read(const char* lds, int tile, int kk) const {
     if constexpr (kTransposed) {
       typedef __attribute__((address_space(3))) s16x4* LdsVec;
-      const char* p = lds + at[tile] + kk * (32 * kTile * 2);
+      const char* p = lds + at[tile] + kk * (32 * kRows * 2);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)p);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)(p + 4 * kTile * 2));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)(p + 4 * kRows * 2));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       const int row = kPaired ? 32 * (tile / 2) + 4 * (tile % 2) : 16 * tile;
@@ -218,13 +219,14 @@ __device__ __forceinline__ float element(const f32x4& c, int i) {
 // and reads the first half of the next from `from`, multiplies that and reads the second,
 // while its copies of the step after go to `to`.  The two stages do not overlap, and
 // __restrict says so: the compiler otherwise waits for every copy in flight before a read.
-template <bool kAAcross, bool kBAcross>
+template <bool kAAcross, bool kBAcross, int kSize>
 struct Contraction {
-  Reader<kAAcross, !kAAcross, kMT> ra;
-  Reader<kBAcross, false, kNT> rb;
+  static constexpr int kMT = kSize / 32, kNT = kSize / 32, kOperandBytes = operand_bytes(kSize);
+  Reader<kAAcross, !kAAcross, kMT, kSize> ra;
+  Reader<kBAcross, false, kNT, kSize> rb;
   bf16x8 a0[kMT], b0[kNT], a1[kMT], b1[kNT];
 
-  // Two of a half's 16 fragments.
+  // Two of a half's fragments.
   __device__ __forceinline__ void read(const char* from, int kk, int i, bf16x8 (&a)[kMT], bf16x8 (&b)[kNT]) {
     if (i < kNT / 2) {
       b[2 * i] = rb.read(from + kOperandBytes, 2 * i, kk);
@@ -234,8 +236,8 @@ struct Contraction {
       a[2 * i - kNT + 1] = ra.read(from, 2 * i - kNT + 1, kk);
     }
   }
-  __device__ __forceinline__ void step(char* __restrict to, const char* __restrict from, Loader<>& la, Loader<>& lb,
-                                       bool more, int wave, f32x4 (&acc)[kMT][kNT]) {
+  __device__ __forceinline__ void step(char* __restrict to, const char* __restrict from, Loader<kSize>& la,
+                                       Loader<kSize>& lb, bool more, int wave, Accumulators<kSize>& acc) {
     const Rsrc da = la.begin(more), db = lb.begin(more);
 #pragma unroll
     for (int m = 0; m < kMT; ++m) {
@@ -258,13 +260,14 @@ struct Contraction {
 
 // A tile's contraction: where its operands start, and how many steps of 64 k it has (at
 // least one; 0: there is no tile).
+template <int kSize>
 struct Job {
-  Loader<> a, b;
+  Loader<kSize> a, b;
   int steps = 0;
 
   __device__ __forceinline__ void copy(char* stage, int wave) {
     a.copy(stage, wave);
-    b.copy(stage + kOperandBytes, wave);
+    b.copy(stage + operand_bytes(kSize), wave);
   }
 };
 
@@ -275,15 +278,15 @@ struct Job {
 //
 // The first step's copies are under way when this is called (to stage `parity`).  With the
 // last step's products go the copies of the next tile's first: next() makes `job` that
-// tile's, and what follows the contraction hides their
-// latency.
-template <bool kAAcross, bool kBAcross, typename Next>
-__device__ __forceinline__ void contract(Job& job, char* lds, int& parity, int wave, int lane, f32x4 (&acc)[kMT][kNT],
-                                         Next next) {
+// tile's, and what follows the contraction hides their latency.
+template <bool kAAcross, bool kBAcross, int kSize, typename Next>
+__device__ __forceinline__ void contract(Job<kSize>& job, char* lds, int& parity, int wave, int lane,
+                                         Accumulators<kSize>& acc, Next next) {
+  constexpr int kMT = kSize / 32, kNT = kSize / 32, kStage = 2 * operand_bytes(kSize);
   const int steps = job.steps;
-  Contraction<kAAcross, kBAcross> c;
-  c.ra.start((wave % 2) * kWaveM, lane % 16, lane / 16);
-  c.rb.start((wave / 2) * kWaveN, lane % 16, lane / 16);
+  Contraction<kAAcross, kBAcross, kSize> c;
+  c.ra.start((wave % 2) * (kSize / 2), lane % 16, lane / 16);
+  c.rb.start((wave / 2) * (kSize / 2), lane % 16, lane / 16);
   // The first step finds no second half before it: zeros (64 products, against a branch
   // around each of them).
 #pragma unroll
@@ -298,7 +301,7 @@ __device__ __forceinline__ void contract(Job& job, char* lds, int& parity, int w
       next();
       more = job.steps > 0;
     }
-    c.step(lds + (parity ^ 1) * kStageBytes, lds + parity * kStageBytes, job.a, job.b, more, wave, acc);
+    c.step(lds + (parity ^ 1) * kStage, lds + parity * kStage, job.a, job.b, more, wave, acc);
     parity ^= 1;
   } while (++it < steps);
 #pragma unroll
@@ -306,9 +309,8 @@ __device__ __forceinline__ void contract(Job& job, char* lds, int& parity, int w
 #pragma unroll
     for (int n = 0; n < kNT; ++n) mfma(acc[m][n], c.a1[m], c.b1[n]);
   // The last products are written.
-  asm volatile("s_nop 15\n\ts_nop 15"
-               : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]), "+a"(acc[7][4]), "+a"(acc[7][5]),
-                 "+a"(acc[7][6]), "+a"(acc[7][7]));
+#pragma unroll
+  for (int n = 0; n < kNT; ++n) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[kMT - 1][n]));
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -343,12 +345,17 @@ __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
 // A token ruled out adds p log p = 0, not 0 * -inf.
 constexpr float kLeastLog = -1e30f;
 
-// Workgroups of a launch over tiles: one a CU (they fill its LDS), each with every
-// kCus-th tile.
 constexpr int kCus = 256;
-inline unsigned workgroups_of(int64_t tiles) { return static_cast<unsigned>(tiles < kCus ? tiles : kCus); }
 
-// The tiles of this workgroup, one after the other.  The 256 that are worked on at a time are
+// Workgroups of a launch over tiles of kSize: as many as fit the CUs at a time (a tile of
+// 256 fills a CU's LDS, one of 128 leaves room for another), each with every so many'th.
+template <int kSize>
+constexpr int kResident = kSize == kTile ? kCus : 2 * kCus;
+template <int kSize>
+unsigned workgroups_of(int64_t tiles) { return static_cast<unsigned>(tiles < kResident<kSize> ? tiles : kResident<kSize>); }
+inline int64_t tiles_of(int64_t n, int size) { return (n + size - 1) / size; }
+
+// The tiles of this workgroup, one after the other.  Those that are worked on at a time are
 // consecutive numbers, and those of one XCD are too.
 struct Tiles {
   int total, at;
@@ -373,6 +380,5 @@ __device__ __forceinline__ TileAt tile_at(int id, int wide, int deep) {
   const unsigned n = wide - first < kGroup ? wide - first : kGroup;
   return {first + static_cast<int>(in % n), static_cast<int>(in / n)};
 }
-
 }  // namespace
 }  // namespace vtrace

@@ -18,20 +18,33 @@ namespace {
 
 enum { kStats = 0, kStatsDot = 1, kGrad = 2, kGradDot = 3 };
 
+// The sum over a row of 16 lanes, in all of them.
+template <int kTurn>
+__device__ __forceinline__ float plus_turned(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x120 + kTurn, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  return plus_turned<1>(plus_turned<2>(plus_turned<4>(plus_turned<8>(x))));
+}
+
 // The token that lane (s, g) holds in accumulator (m, i), of its wave's 128 and behind 8 g.
 __device__ __forceinline__ constexpr int token_at(int m, int i) { return 32 * (m / 2) + 4 * (m % 2) + i; }
 
-template <int kMode, bool kBias>
-__global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs a, int64_t v_begin, int64_t v_count) {
+template <int kMode, bool kBias, int kSize>
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_logits_kernel(VocabArgs a, int64_t v_begin, int64_t v_count) {
   // The stages, then two tiles' tokens and scalars: one array, since what the compiler makes of
   // several loses what __restrict says of the stages.
-  constexpr int kTokens = kTile * sizeof(int32_t), kScalars = kMode >= kGrad ? kTile * sizeof(float4v) : 0;
-  __shared__ __align__(1024) char lds[kGemmLds + 2 * (kTokens + kScalars)];
+  constexpr int kMT = kSize / 32, kNT = kSize / 32, kWaveM = kSize / 2, kWaveN = kSize / 2;
+  constexpr int kGemmLds = tile_lds(kSize);
+  constexpr int kTokens = kSize * sizeof(int32_t), kScalars = kMode >= kGrad ? kSize * sizeof(float4v) : 0;
+  constexpr int kStarts = kBias ? kSize * sizeof(float) : 0;
+  __shared__ __align__(1024) char lds[kGemmLds + 2 * (kTokens + kScalars + kStarts)];
   int32_t* const s_tokens = reinterpret_cast<int32_t*>(lds + kGemmLds);
   float4v* const s_scalars = reinterpret_cast<float4v*>(lds + kGemmLds + 2 * kTokens);
+  float* const s_starts = reinterpret_cast<float*>(lds + kGemmLds + 2 * (kTokens + kScalars));
   const int count = *a.active_count;
-  const int tiles_n = (count + kTile - 1) / kTile;
-  const int tiles_v = static_cast<int>((v_count + kTile - 1) / kTile);
+  const int tiles_n = (count + kSize - 1) / kSize;
+  const int tiles_v = static_cast<int>((v_count + kSize - 1) / kSize);
   Tiles tiles(static_cast<int64_t>(tiles_n) * tiles_v);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -39,27 +52,41 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
   const int64_t H = a.H;
 
   // Rows behind the vocabulary's end lie behind the array's.
-  Job job;
-  job.a.along(H, kTile, wave, lane);
-  job.b.along(a.x_pitch, kTile, wave, lane);
+  Job<kSize> job;
+  job.a.along(H, kSize, wave, lane);
+  job.b.along(a.x_pitch, kSize, wave, lane);
   TileAt at;
   auto start = [&] {
     job.steps = 0;
     if (!tiles.any()) return;
     at = tile_at(tiles.at, tiles_n, tiles_v);
-    const int64_t n0 = static_cast<int64_t>(at.wide) * kTile, v0 = v_begin + static_cast<int64_t>(at.deep) * kTile;
+    const int64_t n0 = static_cast<int64_t>(at.wide) * kSize, v0 = v_begin + static_cast<int64_t>(at.deep) * kSize;
     job.steps = static_cast<int>(a.x_pitch / kTileK);
     job.a.aim(a.weight + v0 * H, (a.V - v0) * H * 2, static_cast<int>(H));
-    job.b.aim(a.x + n0 * a.x_pitch, kTile * a.x_pitch * 2);
+    job.b.aim(a.x + n0 * a.x_pitch, kSize * a.x_pitch * 2);
+  };
+  // What a tile needs of each step, and where its logits start, by way of LDS (registers
+  // would hold the former through the contraction): fetched before the stores of the tile
+  // before it, so that nobody waits for those.
+  int32_t token = kNoToken;
+  float4v scalars = {};
+  float start_at = 0.0f;
+  auto fetch = [&] {
+    if (job.steps == 0 || static_cast<int>(threadIdx.x) >= kSize) return;
+    const int64_t n = static_cast<int64_t>(at.wide) * kSize + threadIdx.x;
+    token = a.row_tokens[n];
+    if constexpr (kMode >= kGrad) scalars = a.row_scalars[n];
+    if constexpr (kBias) start_at = start_of_logit(a, v_begin + static_cast<int64_t>(at.deep) * kSize + threadIdx.x);
   };
   int parity = 0, turn = 0;
   start();
   if (job.steps > 0) job.copy(lds, wave);
+  fetch();
   while (tiles.any()) {
-  const int64_t n0 = static_cast<int64_t>(at.wide) * kTile;
-  const int64_t vt = static_cast<int64_t>(at.deep) * kTile;  // in this launch's piece
+  const int64_t n0 = static_cast<int64_t>(at.wide) * kSize;
+  const int64_t vt = static_cast<int64_t>(at.deep) * kSize;  // in this launch's piece
   const int64_t v0 = v_begin + vt;                           // in the vocabulary
-  const int tile_wide = at.wide, tile_deep = at.deep;
+  const int tile_deep = at.deep;
   // What follows from the lane's number is formed in each tile: kept from tile to tile it
   // would take the registers that the contraction needs.
   int here = lane;
@@ -68,34 +95,36 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
   // Accumulator (m, n) of lane (s, g) holds tokens 8 g + token_at(m, 0..3) of step 16 n + s;
   // it starts as start_of_logit.
   const int64_t first = v0 + wm;
-  const int own = static_cast<int>(a.V - first < kTile ? a.V - first : kTile) - 8 * g;
-  const Rsrc bias = make_rsrc(a.bias + first, kBias && a.bias ? (a.V - first) * 4 : 0);
-  f32x4 acc[kMT][kNT];
+  const int own = static_cast<int>(a.V - first < kSize ? a.V - first : kSize) - 8 * g;
+  // Two of each: a wave may be in its next tile while another ends this one.
+  turn ^= kSize;
+  if (static_cast<int>(threadIdx.x) < kSize) {
+    s_tokens[turn + threadIdx.x] = token;
+    if constexpr (kMode >= kGrad) s_scalars[turn + threadIdx.x] = scalars;
+    if constexpr (kBias) s_starts[turn + threadIdx.x] = start_at;
+  }
+  if constexpr (kBias) {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+  Accumulators<kSize> acc;
 #pragma unroll
   for (int m = 0; m < kMT; ++m) {
     f32x4 b;
+    if constexpr (kBias) {
+      b = *reinterpret_cast<const f32x4*>(s_starts + turn + wm + 8 * g + token_at(m, 0));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = token_at(m, i);
-      if constexpr (kBias) {
-        const float x = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bias, 32 * g + 4 * t, 0, 0));
-        b[i] = t >= own || x < kRuledOut ? -INFINITY : x;
-      } else {
-        b[i] = t >= own ? -INFINITY : 0.0f;
-      }
+      for (int i = 0; i < 4; ++i) b[i] = token_at(m, i) >= own ? -INFINITY : 0.0f;
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) acc[m][n] = b;
   }
-  // What the epilogue needs of each step, by way of LDS (registers would hold it through the
-  // contraction).  Two of them: a wave may be in its next tile while another ends this one.
-  turn ^= kTile;
-  s_tokens[turn + threadIdx.x] = a.row_tokens[n0 + threadIdx.x];
-  if constexpr (kMode >= kGrad) s_scalars[turn + threadIdx.x] = a.row_scalars[n0 + threadIdx.x];
   contract<false, false>(job, lds, parity, wave, lane, acc, [&] {
     tiles.next();
     start();
   });
+  fetch();
+  __builtin_amdgcn_sched_barrier(0);
 
   // A step's token, counted from this lane's first (what token_at gives, where it has it).
   auto taken_of = [&](int32_t token) {
@@ -186,7 +215,10 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) col[m][i] += grad[m][i];
+          for (int i = 0; i < 4; ++i) {
+            col[m][i] += grad[m][i];
+            asm volatile("" : "+v"(col[m][i]));  // here, not later: it would have to keep what it adds
+          }
       }
       uint16_t* out = a.g + row * a.g_pitch + vt + wm + 8 * g;
       uint16_t* out_low = out + P * a.g_pitch;
@@ -215,18 +247,20 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (kBias) {
-      if (a.d_bias != nullptr) {
-        // d_bias: this wave's 128 steps, summed over the 16 lanes of a group.
+      // d_bias: this wave's 128 steps, summed over the 16 lanes of a group; lane s keeps
+      // the sums of accumulators s and s + 16.
+      float keep[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int m = 0; m < kMT; ++m)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = col[m][i];
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
-            if (s == 0)
-              a.bias_partials[(tile_wide * (kTile / kWaveN) + wave / 2) * a.g_pitch + vt + wm + 8 * g + token_at(m, i)] = x;
-          }
+      for (int j = 0; j < 4 * kMT; ++j) {
+        const float x = row_sum(col[j / 4][j % 4]);
+        keep[j / 16] = s == j % 16 ? x : keep[j / 16];
+      }
+      float* const out = a.bias_partials + (n0 + wn) / kBiasSteps * a.g_pitch + vt + wm + 8 * g + token_at(s / 4, s % 4);
+      out[0] = keep[0];
+      if constexpr (kSize == kTile) {
+        out[64] = keep[1];
+        out[a.g_pitch] = 0.0f;
+        out[a.g_pitch + 64] = 0.0f;
       }
     }
   }
@@ -234,15 +268,20 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_logits_kernel(VocabArgs
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-template <int kMode>
-hipError_t launch(const VocabArgs& a, int64_t v0, int64_t v_count, hipStream_t st) {
-  const dim3 grid(workgroups_of(a.row_pitch / kTile * ((v_count + kTile - 1) / kTile))), block(kGemmThreads);
+template <int kMode, int kSize>
+hipError_t launch_tiles(const VocabArgs& a, int64_t v0, int64_t v_count, hipStream_t st) {
+  const dim3 grid(workgroups_of<kSize>(tiles_of(a.N, kSize) * tiles_of(v_count, kSize))), block(kGemmThreads);
   // d_bias without a bias: as if there were one of zeros.
   if (a.bias != nullptr || a.d_bias != nullptr)
-    hipLaunchKernelGGL((vocab_logits_kernel<kMode, true>), grid, block, 0, st, a, v0, v_count);
+    hipLaunchKernelGGL((vocab_logits_kernel<kMode, true, kSize>), grid, block, 0, st, a, v0, v_count);
   else
-    hipLaunchKernelGGL((vocab_logits_kernel<kMode, false>), grid, block, 0, st, a, v0, v_count);
+    hipLaunchKernelGGL((vocab_logits_kernel<kMode, false, kSize>), grid, block, 0, st, a, v0, v_count);
   return hipGetLastError();
+}
+template <int kMode>
+hipError_t launch(const VocabArgs& a, int64_t v0, int64_t v_count, hipStream_t st) {
+  return a.small_logits ? launch_tiles<kMode, kSmallTile>(a, v0, v_count, st)
+                        : launch_tiles<kMode, kTile>(a, v0, v_count, st);
 }
 
 }  // namespace

@@ -16,23 +16,25 @@ __device__ __forceinline__ f32x4 load4(Rsrc r, uint32_t offset) {
 }
 
 template <typename Out>
-__device__ __forceinline__ void store4(Out* p, f32x4 x) {
+__device__ __forceinline__ void store4(Rsrc r, uint32_t offset, const f32x4& x) {
   if constexpr (sizeof(Out) == 4) {
-    *reinterpret_cast<f32x4*>(p) = x;
+    const f32x4 w = {element(x, 0), element(x, 1), element(x, 2), element(x, 3)};
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, w), r, offset, 0, 0);
   } else {
     v2u w;
-    w.x = pack_bf16x2(x[0], x[1]);
-    w.y = pack_bf16x2(x[2], x[3]);
-    *reinterpret_cast<v2u*>(p) = w;
+    w.x = pack_bf16x2(element(x, 0), element(x, 1));
+    w.y = pack_bf16x2(element(x, 2), element(x, 3));
+    __builtin_amdgcn_raw_buffer_store_b64(w, r, offset, 0, 0);
   }
 }
 
-template <typename Out>
-__global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabArgs a, int64_t v_begin) {
-  __shared__ __align__(1024) char lds[kGemmLds];
-  const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
+template <typename Out, int kSize>
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_d_weight_kernel(VocabArgs a, int64_t v_begin) {
+  constexpr int kMT = kSize / 32, kNT = kSize / 32;
+  __shared__ __align__(1024) char lds[tile_lds(kSize)];
+  const int tiles_h = static_cast<int>((a.H + kSize - 1) / kSize);
   const int64_t v_left = a.V - v_begin < a.g_pitch ? a.V - v_begin : a.g_pitch;
-  const int tiles_v = static_cast<int>((v_left + kTile - 1) / kTile);
+  const int tiles_v = static_cast<int>((v_left + kSize - 1) / kSize);
   Tiles tiles(static_cast<int64_t>(tiles_h) * tiles_v);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -41,7 +43,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabAr
   const int once = rows == 0 ? 1 : static_cast<int>(rows / kTileK);  // no rows: a step of nothing
   const int64_t part = a.row_pitch * a.g_pitch;  // elements of G's high parts
 
-  Job job;
+  Job<kSize> job;
   job.a.across(a.x_pitch, wave, lane);
   job.b.across(a.g_pitch, wave, lane);
   TileAt at;
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabAr
     job.steps = 0;
     if (!tiles.any()) return;
     at = tile_at(tiles.at, tiles_h, tiles_v);
-    const int64_t h0 = static_cast<int64_t>(at.wide) * kTile, vt = static_cast<int64_t>(at.deep) * kTile;
+    const int64_t h0 = static_cast<int64_t>(at.wide) * kSize, vt = static_cast<int64_t>(at.deep) * kSize;
     job.a.aim(a.x + h0, (rows * a.x_pitch - h0) * 2);
     job.b.aim(a.g + vt, (rows * a.g_pitch - vt) * 2);
     job.steps = once;
@@ -63,22 +65,24 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabAr
   start();
   if (job.steps > 0) job.copy(lds, wave);
   while (tiles.any()) {
-    const int64_t h0 = static_cast<int64_t>(at.wide) * kTile, vt = static_cast<int64_t>(at.deep) * kTile;
-    f32x4 acc[kMT][kNT] = {};
+    const int64_t h0 = static_cast<int64_t>(at.wide) * kSize, vt = static_cast<int64_t>(at.deep) * kSize;
+    Accumulators<kSize> acc = {};
     contract<true, true>(job, lds, parity, wave, lane, acc, [&] {
       tiles.next();
       start();
     });
-    Out* const d_weight = static_cast<Out*>(a.d_weight);
+    // Rows behind the vocabulary's end lie behind the array's; columns behind a row's end
+    // are pointed there.
+    const int64_t first = (v_begin + vt) * a.H;
+    const Rsrc out = make_rsrc(static_cast<Out*>(a.d_weight) + first, (a.V * a.H - first) * static_cast<int>(sizeof(Out)));
+    const int64_t h = h0 + (wave % 2) * (kSize / 2) + 4 * g;
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-      const int64_t v = v_begin + vt + (wave / 2) * kWaveN + 16 * n + s;
-      if (v >= a.V) continue;
+      const uint32_t row = static_cast<uint32_t>((((wave / 2) * (kSize / 2) + 16 * n + s) * a.H + h) * sizeof(Out));
 #pragma unroll
-      for (int m = 0; m < kMT; ++m) {
-        const int64_t h = h0 + (wave % 2) * kWaveM + 16 * m + 4 * g;
-        if (h < a.H) store4(d_weight + v * a.H + h, acc[m][n]);
-      }
+      for (int m = 0; m < kMT; ++m)
+        store4<Out>(out, h + 16 * m < a.H ? row + 16 * m * static_cast<uint32_t>(sizeof(Out)) : kOutOfRange, acc[m][n]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
@@ -88,7 +92,8 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_weight_kernel(VocabAr
 // parts, each with float32 sums of its own that grow over the pieces (how many parts is
 // chosen on the device: vocab_list_kernel).
 __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
-  __shared__ __align__(1024) char lds[kGemmLds];
+  __shared__ __align__(1024) char lds[tile_lds(kTile)];
+  constexpr int kMT = kTile / 32, kNT = kTile / 32;
   const int count = *a.active_count;
   const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
   const int tiles_n = (count + kTile - 1) / kTile;
@@ -101,7 +106,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   const int all_steps = static_cast<int>((v_left + kTileK - 1) / kTileK);
   const int64_t part = a.row_pitch * a.g_pitch;
 
-  Job job;
+  Job<kTile> job;
   job.a.across(a.H, wave, lane);
   job.b.along(a.g_pitch, kTile, wave, lane);
   TileAt at;
@@ -135,7 +140,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   while (tiles.any()) {
     const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
     float* const sums = a.h_partials + static_cast<int64_t>(split) * tiles_n * kTile * a.H;
-    f32x4 acc[kMT][kNT] = {};
+    Accumulators<kTile> acc = {};
     contract<true, false>(job, lds, parity, wave, lane, acc, [&] {
       tiles.next();
       start();
@@ -144,9 +149,9 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
     // this one's is added to.
     const Rsrc out = make_rsrc(sums + n0 * a.H, (count - n0) * a.H * 4);
     const Rsrc before = make_rsrc(sums + n0 * a.H, first ? 0 : (count - n0) * a.H * 4);
-    const int64_t h = h0 + (wave % 2) * kWaveM + 4 * g;
+    const int64_t h = h0 + (wave % 2) * (kTile / 2) + 4 * g;
     auto place = [&](int n, int m) -> uint32_t {
-      const int row = (wave / 2) * kWaveN + 16 * n + s;
+      const int row = (wave / 2) * (kTile / 2) + 16 * n + s;
       return h + 16 * m < a.H ? static_cast<uint32_t>((row * a.H + h + 16 * m) * 4) : kOutOfRange;
     };
     f32x4 was[2][kMT];
@@ -171,16 +176,20 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
+template <typename Out, int kSize>
+hipError_t launch_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st) {
+  const int64_t v = a.V - v0 < a.g_pitch ? a.V - v0 : a.g_pitch;
+  const dim3 grid(workgroups_of<kSize>(tiles_of(a.H, kSize) * tiles_of(v, kSize))), block(kGemmThreads);
+  hipLaunchKernelGGL((vocab_d_weight_kernel<Out, kSize>), grid, block, 0, st, a, v0);
+  return hipGetLastError();
+}
 
 }  // namespace
 
 hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st) {
-  const int64_t v = a.V - v0 < a.g_pitch ? a.V - v0 : a.g_pitch;
-  const dim3 grid(workgroups_of(tiles_of(a.H) * tiles_of(v))), block(kGemmThreads);
-  if (a.grad_bf16) hipLaunchKernelGGL(vocab_d_weight_kernel<uint16_t>, grid, block, 0, st, a, v0);
-  else hipLaunchKernelGGL(vocab_d_weight_kernel<float>, grid, block, 0, st, a, v0);
-  return hipGetLastError();
+  if (a.grad_bf16)
+    return a.small_weight ? launch_d_weight<uint16_t, kSmallTile>(a, v0, st) : launch_d_weight<uint16_t, kTile>(a, v0, st);
+  return a.small_weight ? launch_d_weight<float, kSmallTile>(a, v0, st) : launch_d_weight<float, kTile>(a, v0, st);
 }
 
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t st) {

@@ -307,6 +307,57 @@ def test_pieces_of_the_vocabulary_and_splits():
         assert ((got.double() - ref).abs() <= terms + U * ref.abs()).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("T,B,H,V", [(130, 4, 520, 19999), (125, 16, 1032, 20003)])
+def test_layers_that_fill_the_gpu(T, B, H, V, bias, dtype):
+    """Enough steps and tokens for the wide tiles, one and several to a workgroup.  The
+    reference is the same formulas in float64 on the GPU, the bounds those of _check_log_probs
+    and _check_grad."""
+    x, w, b, tokens, d_lp, d_h = _gpu(*_batch(31, T, B, H, V, bias=bias, none=0.02))
+    fwd = vt.vtrace_vocab_log_probs(x, w, b, tokens)
+    ws = _poison(vt.VocabWorkspace(T, B, V, H, grad_dtype=dtype))
+    out = vt.vtrace_vocab_grad(x, w, b, tokens, fwd.log_sums, fwd.entropy, d_lp, d_h, grad_dtype=dtype, workspace=ws)
+    use = tokens.view(-1) >= 0
+    X, W = x.view(-1, H).double() * use.unsqueeze(1), w.double()
+    z, m = X @ W.t(), X.abs() @ W.abs().t()
+    if bias:
+        z, m = z + b.double(), m + b.double().abs()
+    tau = ((H ** 0.5 + 8.0) * U * m).amax(1)
+    lse = torch.logsumexp(z, 1)
+    lp = z - lse.unsqueeze(1)
+    p = lp.exp()
+    e = -(p * lp).sum(1)
+    taken = lp.gather(1, tokens.view(-1, 1).clamp(min=0).long()).squeeze(1)
+
+    def within(got, ref, bound):
+        assert ((got.double().view(ref.shape) - ref).abs() <= bound).all()
+
+    within(fwd.log_sums, lse * use, tau + U * (64.0 + lse.abs()))
+    within(fwd.log_probs, taken * use, 2.0 * tau + U * (64.0 + 2.0 * taken.abs() + lse.abs()))
+    spread = (p * (lp + e.unsqueeze(1)).abs()).sum(1)
+    within(fwd.entropy, e * use, (2.0 * tau + 64.0 * U) * (1.0 + spread) + U * (e + 64.0))
+    g, h = (t.view(-1, 1).double() * use.unsqueeze(1) for t in (d_lp, d_h))
+    G = (-g * p - h * p * (lp + e.unsqueeze(1))).scatter_add_(1, tokens.view(-1, 1).clamp(min=0).long(), g)
+    # the kernel's own log-sums and entropies: their errors enter as p's relative one
+    rel = (2.0 * tau + U * 128.0).unsqueeze(1) + U * (lp.abs() + 8.0)
+    dG = p * (g.abs() + h.abs() * (lp.abs() + e.unsqueeze(1) + 1.0)) * rel * 2.0 + U * G.abs()
+    mag = G.abs() + dG
+    operand, stored = (HALF_BF16 ** 2, U) if dtype == torch.float32 else (HALF_BF16, HALF_BF16)
+
+    def bound(sum_of, k, ref):
+        return (sum_of(dG) + (operand + (k ** 0.5 + 8.0) * U) * sum_of(mag)) * (1.0 + stored) + stored * ref.abs() + 1e-37
+
+    ref = G @ W
+    within(out.d_hidden, ref, bound(lambda t: t @ W.abs(), V, ref))
+    ref = G.t().contiguous() @ X
+    within(out.d_weight, ref, bound(lambda t: t.t().contiguous() @ X.abs(), T * B, ref))
+    if bias:
+        ref = G.sum(0)
+        within(out.d_bias, ref, dG.sum(0) + 80.0 * U * mag.sum(0) + U * ref.abs() + 1e-37)
+    assert not out.d_hidden.view(-1, H)[~use].any()
+
+
 def test_offsets_beyond_32_bits():
     """A layer of 4.8 GB: the last tokens lie beyond 2^32 bytes."""
     H, V = 4096, 590000
