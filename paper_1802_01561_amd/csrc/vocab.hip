@@ -5,26 +5,43 @@
 namespace vtrace {
 namespace {
 
-// Tiles that d_hidden's product is split up to (two rounds of the CUs).
-constexpr int kMostSplitTiles = 512;
+// Tiles that d_hidden's product is split up to: two rounds.
+__host__ __device__ constexpr int most_split_tiles(int size) { return 2 * resident_tiles(size); }
+
+__host__ __device__ inline int hidden_tile(const VocabArgs& a) { return a.small_hidden ? kSmallTile : kTile; }
 
 constexpr int kListThreads = 1024;
 constexpr int kListItems = 8;  // tokens per thread and pass
 
-// The time of d_hidden's product with `splits` parts, in units of a step of 64 k (1.56 us,
-// all CUs): every CU has `rounds` tiles one after the other, each of them with its share
-// of a piece's steps, stores what 8 steps take, and in the end the parts are added.
-__device__ __forceinline__ float split_cost(const VocabArgs& a, int tiles, int rows, int steps, int splits) {
-  const int passes = a.grad_bf16 ? 1 : 2;
-  const int rounds = (tiles * splits + kCus - 1) / kCus, share = (steps + splits - 1) / splits;
-  const float bytes = static_cast<float>(splits) * static_cast<float>(rows) * static_cast<float>(a.H) * 4.0f;
-  return static_cast<float>(a.pieces) * static_cast<float>(rounds) * static_cast<float>(share * passes + 8) + bytes * (1.0f / 8e6f);
+// How d_hidden's product is split for `count` active steps, and what it then takes (us):
+// every CU has `rounds` tiles one after the other, each of them with its share of a piece's
+// steps (round_cost), and in the end the parts are added, at 5 TB/s.  Considered are no parts,
+// and as many as fill one round (or half a one) or two.
+struct Split {
+  int parts;
+  double cost;
+};
+__host__ __device__ inline Split best_split(const VocabArgs& a, int count, int size) {
+  const int tiles_n = (count + size - 1) / size, tiles = tiles_n * ((static_cast<int>(a.H) + size - 1) / size);
+  const int steps = static_cast<int>(a.g_pitch / kTileK), resident = resident_tiles(size);
+  Split best = {1, INFINITY};
+  for (int halves = 0; halves <= 4; halves += halves < 2 ? 1 : 2) {
+    int parts = tiles == 0 ? 1 : halves * resident / 2 / tiles;
+    if (parts > steps) parts = steps;
+    if (parts < 1) parts = 1;
+    const int share = (steps + parts - 1) / parts;
+    parts = (steps + share - 1) / share;  // as few as have that share
+    const int rounds = (tiles * parts + resident - 1) / resident;
+    const double bytes = 4.0 * parts * tiles_n * size * static_cast<double>(a.H);
+    const double cost = static_cast<double>(a.pieces) * rounds * round_cost(size, share * (a.grad_bf16 ? 1 : 2)) + bytes / 5e6;
+    if (cost < best.cost) best = {parts, cost};
+  }
+  return best;
 }
 
 // active[0 .. count) = the steps with a token, in order.  One workgroup: a pass over
 // 8192 tokens counts, scans and writes.  For the gradient it also chooses the number of
-// parts of d_hidden's product, which depends on the count: the cheapest of the numbers with
-// which the tiles fit the workspace.
+// parts of d_hidden's product, which depends on the count.
 template <bool kGrad>
 __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
   constexpr int kWaves = kListThreads / kWave;
@@ -62,32 +79,7 @@ __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
     }
   }
   if (threadIdx.x == 0) *a.active_count = total;
-  if constexpr (kGrad) {
-    __shared__ float s_cost[kWaves];
-    __shared__ int s_splits[kWaves];
-    const int tiles_n = (total + kTile - 1) / kTile;
-    const int tiles = tiles_n * static_cast<int>((a.H + kTile - 1) / kTile);
-    const int steps = static_cast<int>(a.g_pitch / kTileK);
-    int splits = threadIdx.x + 1;
-    float cost = splits <= steps && (splits == 1 || tiles * splits <= kMostSplitTiles)
-                     ? split_cost(a, tiles, tiles_n * kTile, steps, splits)
-                     : INFINITY;
-    auto take = [&](float c, int k) {
-      if (c < cost || (c == cost && k < splits)) cost = c, splits = k;
-    };
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      const float c = __shfl_xor(cost, o, kWave);
-      const int k = __shfl_xor(splits, o, kWave);
-      take(c, k);
-    }
-    if (lane == 0) s_cost[wave] = cost, s_splits[wave] = splits;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < kWaves; ++w) take(s_cost[w], s_splits[w]);
-      *a.splits = splits;
-    }
-  }
+  if (kGrad && threadIdx.x == 0) *a.splits = best_split(a, total, hidden_tile(a)).parts;
 }
 
 // A step's outputs from the joined statistics: sums of 2^d and of 2^d d, d = z log2 e - c.
@@ -208,30 +200,82 @@ __global__ __launch_bounds__(kJoinFewThreads) void vocab_join_few_kernel(VocabAr
 // entropy, d_h' = -d_h), the epilogue has p = 2^(z K - l2), K the float32 log2 e and l2 the
 // rounded l log2 e; what the rounding of l2 does to p is a factor of each step's own, and
 // goes into c0 and c1 here.  Rows behind the last get an l2 that makes p 0.
+//
+// kOwnList: up to 8192 steps each workgroup counts the tokens for itself and places its own
+// steps, and the list is a by-product (640 steps: 5 us in place of 9 for two launches).
 constexpr int kGatherThreads = 256;
+constexpr int64_t kOwnListMost = 8192;
 template <bool kGrad>
+__device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t row, int64_t step, bool in, int lane);
+
+template <bool kGrad, bool kOwnList>
 __global__ __launch_bounds__(kGatherThreads) void vocab_gather_kernel(VocabArgs a) {
-  const int lane = threadIdx.x % kWave;
-  const int64_t row = (static_cast<int64_t>(blockIdx.x) * kGatherThreads + threadIdx.x) / kWave;
-  const int64_t count = *a.active_count;
-  const v4u zero = {0u, 0u, 0u, 0u};
-  if (kGrad && row < a.N && a.tokens[row] == kNoToken) {
+  constexpr int kWaves = kGatherThreads / kWave;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+  int64_t count;
+  const bool here = row < a.N, idle = here && a.tokens[row] == kNoToken;
+  if constexpr (kOwnList) {
+    __shared__ int s_before[kWaves], s_all[kWaves];
+    int before = 0, all = 0;  // active steps before this row's, and all of them
+    for (int64_t i = threadIdx.x; i < a.N; i += kGatherThreads) {
+      const bool active = a.tokens[i] != kNoToken;
+      all += active;
+      before += active && i < row - wave;
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+      before += __shfl_xor(before, o, kWave);
+      all += __shfl_xor(all, o, kWave);
+    }
+    if (lane == 0) s_before[wave] = before, s_all[wave] = all;
+    __syncthreads();
+    before = all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      before += s_before[w];
+      all += s_all[w];
+    }
+    for (int w = 0; w < wave; ++w) {
+      const int64_t other = row - wave + w;
+      before += other < a.N && a.tokens[other] != kNoToken;
+    }
+    count = all;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      *a.active_count = all;
+      if constexpr (kGrad) *a.splits = best_split(a, all, hidden_tile(a)).parts;
+    }
+    if (here && !idle) {
+      if (lane == 0) a.active[before] = static_cast<int32_t>(row);
+      gather_row<kGrad>(a, before, row, true, lane);
+    }
+    if (row >= count && row < tiles_of(count, kTile) * kTile) gather_row<kGrad>(a, row, 0, false, lane);
+  } else {
+    count = *a.active_count;
+    if (row < tiles_of(count, kTile) * kTile) gather_row<kGrad>(a, row, row < count ? a.active[row] : 0, row < count, lane);
+  }
+  if (kGrad && idle) {
     const int64_t bytes = a.H * (a.grad_bf16 ? 2 : 4);
     char* const out = static_cast<char*>(a.d_hidden) + row * bytes;
+    const v4u zero = {0u, 0u, 0u, 0u};
     for (int64_t i = lane * 16; i < bytes; i += kWave * 16) *reinterpret_cast<v4u*>(out + i) = zero;
   }
-  if (row >= (count + kTile - 1) / kTile * kTile) return;
-  const int64_t step = row < count ? a.active[row] : 0;
-  const uint16_t* const in = a.hidden + step * a.H;
+}
+
+// Row `row` of the operands, from `step`, or (not `in`) zeros.
+template <bool kGrad>
+__device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t row, int64_t step, bool in, int lane) {
+  const v4u zero = {0u, 0u, 0u, 0u};
+  const uint16_t* const from = a.hidden + step * a.H;
   uint16_t* const out = a.x + row * a.x_pitch;
   for (int64_t i = lane * 8; i < a.x_pitch; i += kWave * 8)
-    *reinterpret_cast<v4u*>(out + i) = row < count && i < a.H ? *reinterpret_cast<const v4u*>(in + i) : zero;
+    *reinterpret_cast<v4u*>(out + i) = in && i < a.H ? *reinterpret_cast<const v4u*>(from + i) : zero;
   if (lane != 0) return;
-  const int32_t token = row < count ? a.tokens[step] : kNoToken;
+  const int32_t token = in ? a.tokens[step] : kNoToken;
   a.row_tokens[row] = token;
   if constexpr (!kGrad) return;
   float4v scalars = {1e30f, 0.0f, 0.0f, 0.0f};
-  if (row < count) {
+  if (in) {
     constexpr double kLn2 = 0.6931471805599453;
     float d_lp = a.d_log_probs[step];
     if (token < 0 || token >= a.V) {
@@ -264,7 +308,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
   if (row >= *a.active_count) return;
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
   const int splits = *a.splits;
-  const int64_t rows = (static_cast<int64_t>(*a.active_count) + kTile - 1) / kTile * kTile;
+  const int64_t rows = tiles_of(*a.active_count, hidden_tile(a)) * hidden_tile(a);
 #pragma unroll 8
   for (int k = 0; k < splits; ++k) x += *reinterpret_cast<const f32x4*>(a.h_partials + (k * rows + row) * a.H + h);
   Out* const out = static_cast<Out*>(a.d_hidden) + static_cast<int64_t>(a.active[row]) * a.H + h;
@@ -342,6 +386,7 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->g_pitch = p.g_pitch;
   a->small_logits = p.small_logits;
   a->small_weight = p.small_weight;
+  a->small_hidden = p.small_hidden;
   a->pieces = p.pieces;
   a->splits = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderSplitsOffset);
   a->active = c.take<int32_t>(a->N);
@@ -368,17 +413,13 @@ constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
 constexpr int64_t kMostPieceBytes = int64_t(256) << 20;
 
 // Whether a product m x n over `steps` steps of 64 k is done in tiles of 128 rather than of
-// 256.  A round of tiles of 256 (one a CU) takes 1.56 us a step and 13 us, one of tiles of
-// 128 (two a CU, half as many products) 1.2 and 6.  640 steps, H = 256, V = 32768: logits 40
-// us in two rounds, 32 in three small ones; d_weight (float32) 47 in one half empty, 29 in a
-// small one.  3200 steps, H = 1024: 261 in seven, 303 in thirteen small ones.
+// 256.
 bool small_tiles_pay(int64_t m, int64_t n, int64_t steps) {
-  auto rounds = [&](int size, int64_t resident) {
-    const int64_t tiles = tiles_of(m, size) * tiles_of(n, size);
-    return static_cast<double>((tiles + resident - 1) / resident);
+  auto cost = [&](int size) {
+    const int64_t tiles = tiles_of(m, size) * tiles_of(n, size), resident = resident_tiles(size);
+    return static_cast<double>((tiles + resident - 1) / resident) * round_cost(size, steps);
   };
-  const double k = static_cast<double>(steps);
-  return rounds(kSmallTile, kResident<kSmallTile>) * (1.2 * k + 6.0) < rounds(kTile, kResident<kTile>) * (1.56 * k + 13.0);
+  return cost(kSmallTile) < cost(kTile);
 }
 
 }  // namespace
@@ -429,12 +470,17 @@ VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
   p.small_weight = small_tiles_pay(H, p.g_pitch, tiles_of(N, kTileK) * (grad_bf16 ? 1 : 2));
   // d_hidden's tiles, whatever the number of active steps: those of one part, or as many as
   // it is split into at most.
-  const int64_t split_rows = kMostSplitTiles / ((H + kTile - 1) / kTile) * kTile;
-  p.split_rows = split_rows > p.row_pitch ? split_rows : p.row_pitch;
   VocabArgs a = {};
   a.N = N;
   a.H = H;
+  a.g_pitch = p.g_pitch;
+  a.pieces = pieces;
   a.grad_bf16 = grad_bf16;
+  const int n = static_cast<int>(N);
+  p.small_hidden = best_split(a, n, kSmallTile).cost < best_split(a, n, kTile).cost;
+  const int size = p.small_hidden ? kSmallTile : kTile;
+  const int64_t split_rows = most_split_tiles(size) / tiles_of(H, size) * size;
+  p.split_rows = split_rows > p.row_pitch ? split_rows : p.row_pitch;
   p.bytes = carve_grad(&a, p, nullptr);
   return p;
 }
@@ -442,14 +488,28 @@ VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
 void attach_vocab_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) { carve_log_probs(a, p, ws); }
 void attach_vocab_grad(VocabArgs* a, const VocabPlan& p, void* ws) { carve_grad(a, p, ws); }
 
+namespace {
+
+template <bool kGrad>
+hipError_t launch_gather(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
+  const dim3 grid(blocks_of(p.row_pitch, kGatherThreads / kWave)), block(kGatherThreads);
+  if (a.N <= kOwnListMost) {
+    hipLaunchKernelGGL((vocab_gather_kernel<kGrad, true>), grid, block, 0, st, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(vocab_list_kernel<kGrad>, dim3(1), dim3(kListThreads), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((vocab_gather_kernel<kGrad, false>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
   hipError_t e;
   if (!p.few) {
-    hipLaunchKernelGGL(vocab_list_kernel<false>, dim3(1), dim3(kListThreads), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(vocab_gather_kernel<false>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
-                       dim3(kGatherThreads), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = launch_gather<false>(a, p, st)) != hipSuccess) return e;
   }
   e = p.few ? launch_vocab_few(a, st) : launch_vocab_stats(a, st);
   if (e != hipSuccess) return e;
@@ -464,11 +524,7 @@ hipError_t launch_vocab_log_probs(const VocabArgs& a, const VocabPlan& p, hipStr
 
 hipError_t launch_vocab_grad(const VocabArgs& a, const VocabPlan& p, hipStream_t st) {
   hipError_t e;
-  hipLaunchKernelGGL(vocab_list_kernel<true>, dim3(1), dim3(kListThreads), 0, st, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(vocab_gather_kernel<true>, dim3(blocks_of(p.row_pitch, kGatherThreads / kWave)),
-                     dim3(kGatherThreads), 0, st, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if ((e = launch_gather<true>(a, p, st)) != hipSuccess) return e;
   for (int64_t v0 = 0; v0 < a.V; v0 += p.g_pitch) {
     if ((e = launch_vocab_logit_grads(a, v0, st)) != hipSuccess) return e;
     if ((e = launch_vocab_d_weight(a, v0, st)) != hipSuccess) return e;

@@ -39,7 +39,7 @@ struct VocabArgs {
   void* d_weight;            // [V,H]
   float* d_bias;             // [V] or null
   int grad_bf16;
-  bool small_logits, small_weight;  // tiles of 128 instead of 256
+  bool small_logits, small_weight, small_hidden;  // tiles of 128 instead of 256
   // workspace pieces
   unsigned int* error_flag;
   int32_t* active_count;  // in the header
@@ -72,7 +72,7 @@ struct VocabPlan {
   int64_t pieces;  // log_probs: statistics per step; grad: of the vocabulary
   int tile_tokens;
   bool narrow;
-  bool small_logits, small_weight;
+  bool small_logits, small_weight, small_hidden;
   int64_t row_pitch, x_pitch, g_pitch;
   int64_t split_rows;
   size_t bytes;

@@ -349,11 +349,17 @@ constexpr int kCus = 256;
 
 // Workgroups of a launch over tiles of kSize: as many as fit the CUs at a time (a tile of
 // 256 fills a CU's LDS, one of 128 leaves room for another), each with every so many'th.
-template <int kSize>
-constexpr int kResident = kSize == kTile ? kCus : 2 * kCus;
-template <int kSize>
-unsigned workgroups_of(int64_t tiles) { return static_cast<unsigned>(tiles < kResident<kSize> ? tiles : kResident<kSize>); }
-inline int64_t tiles_of(int64_t n, int size) { return (n + size - 1) / size; }
+__host__ __device__ constexpr int resident_tiles(int size) { return size == kTile ? kCus : 2 * kCus; }
+__host__ __device__ inline int64_t tiles_of(int64_t n, int size) { return (n + size - 1) / size; }
+inline unsigned workgroups_of(int64_t tiles, int size) {
+  return static_cast<unsigned>(tiles < resident_tiles(size) ? tiles : resident_tiles(size));
+}
+// us of a round of them over `steps` steps of 64 k.  640 steps, H = 256, V = 32768: logits 40
+// us in two rounds of 256, 32 in three of 128; d_weight (float32) 47 in one half empty, 29 in a
+// small one.  3200 steps, H = 1024: 261 in seven, 303 in thirteen small ones.
+__host__ __device__ inline double round_cost(int size, int64_t steps) {
+  return size == kTile ? 1.56 * static_cast<double>(steps) + 13.0 : 1.2 * static_cast<double>(steps) + 6.0;
+}
 
 // The tiles of this workgroup, one after the other.  Those that are worked on at a time are
 // consecutive numbers, and those of one XCD are too.

@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_lo
 
 template <int kMode, int kSize>
 hipError_t launch_tiles(const VocabArgs& a, int64_t v0, int64_t v_count, hipStream_t st) {
-  const dim3 grid(workgroups_of<kSize>(tiles_of(a.N, kSize) * tiles_of(v_count, kSize))), block(kGemmThreads);
+  const dim3 grid(workgroups_of(tiles_of(a.N, kSize) * tiles_of(v_count, kSize), kSize)), block(kGemmThreads);
   // d_bias without a bias: as if there were one of zeros.
   if (a.bias != nullptr || a.d_bias != nullptr)
     hipLaunchKernelGGL((vocab_logits_kernel<kMode, true, kSize>), grid, block, 0, st, a, v0, v_count);

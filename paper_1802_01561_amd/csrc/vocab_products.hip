@@ -90,13 +90,14 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_d_
 
 // d_hidden's tiles are few where there are few steps: k (the piece) is split into `splits`
 // parts, each with float32 sums of its own that grow over the pieces (how many parts is
-// chosen on the device: vocab_list_kernel).
-__global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
-  __shared__ __align__(1024) char lds[tile_lds(kTile)];
-  constexpr int kMT = kTile / 32, kNT = kTile / 32;
+// chosen on the device: best_split).
+template <int kSize>
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_d_hidden_kernel(VocabArgs a, int64_t v_begin, int first) {
+  __shared__ __align__(1024) char lds[tile_lds(kSize)];
+  constexpr int kMT = kSize / 32, kNT = kSize / 32;
   const int count = *a.active_count;
-  const int tiles_h = static_cast<int>((a.H + kTile - 1) / kTile);
-  const int tiles_n = (count + kTile - 1) / kTile;
+  const int tiles_h = static_cast<int>((a.H + kSize - 1) / kSize);
+  const int tiles_n = (count + kSize - 1) / kSize;
   const int per_split = tiles_h * tiles_n, splits = *a.splits;
   Tiles tiles(static_cast<int64_t>(per_split) * splits);
   const int lane = threadIdx.x % kWave;
@@ -106,9 +107,9 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   const int all_steps = static_cast<int>((v_left + kTileK - 1) / kTileK);
   const int64_t part = a.row_pitch * a.g_pitch;
 
-  Job<kTile> job;
+  Job<kSize> job;
   job.a.across(a.H, wave, lane);
-  job.b.along(a.g_pitch, kTile, wave, lane);
+  job.b.along(a.g_pitch, kSize, wave, lane);
   TileAt at;
   int split = 0;
   auto start = [&] {
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
     if (!tiles.any()) return;
     split = tiles.at / per_split;
     at = tile_at(tiles.at % per_split, tiles_n, tiles_h);
-    const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
+    const int64_t h0 = static_cast<int64_t>(at.deep) * kSize, n0 = static_cast<int64_t>(at.wide) * kSize;
     const int64_t from = static_cast<int64_t>(all_steps) * split / splits;
     const int64_t to = static_cast<int64_t>(all_steps) * (split + 1) / splits;
     const int once = to == from ? 1 : static_cast<int>(to - from);  // nothing left: a step of nothing
@@ -138,9 +139,9 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
   start();
   if (job.steps > 0) job.copy(lds, wave);
   while (tiles.any()) {
-    const int64_t h0 = static_cast<int64_t>(at.deep) * kTile, n0 = static_cast<int64_t>(at.wide) * kTile;
-    float* const sums = a.h_partials + static_cast<int64_t>(split) * tiles_n * kTile * a.H;
-    Accumulators<kTile> acc = {};
+    const int64_t h0 = static_cast<int64_t>(at.deep) * kSize, n0 = static_cast<int64_t>(at.wide) * kSize;
+    float* const sums = a.h_partials + static_cast<int64_t>(split) * tiles_n * kSize * a.H;
+    Accumulators<kSize> acc = {};
     contract<true, false>(job, lds, parity, wave, lane, acc, [&] {
       tiles.next();
       start();
@@ -149,9 +150,9 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
     // this one's is added to.
     const Rsrc out = make_rsrc(sums + n0 * a.H, (count - n0) * a.H * 4);
     const Rsrc before = make_rsrc(sums + n0 * a.H, first ? 0 : (count - n0) * a.H * 4);
-    const int64_t h = h0 + (wave % 2) * (kTile / 2) + 4 * g;
+    const int64_t h = h0 + (wave % 2) * (kSize / 2) + 4 * g;
     auto place = [&](int n, int m) -> uint32_t {
-      const int row = (wave / 2) * (kTile / 2) + 16 * n + s;
+      const int row = (wave / 2) * (kSize / 2) + 16 * n + s;
       return h + 16 * m < a.H ? static_cast<uint32_t>((row * a.H + h + 16 * m) * 4) : kOutOfRange;
     };
     f32x4 was[2][kMT];
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void vocab_d_hidden_kernel(VocabAr
 template <typename Out, int kSize>
 hipError_t launch_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st) {
   const int64_t v = a.V - v0 < a.g_pitch ? a.V - v0 : a.g_pitch;
-  const dim3 grid(workgroups_of<kSize>(tiles_of(a.H, kSize) * tiles_of(v, kSize))), block(kGemmThreads);
+  const dim3 grid(workgroups_of(tiles_of(a.H, kSize) * tiles_of(v, kSize), kSize)), block(kGemmThreads);
   hipLaunchKernelGGL((vocab_d_weight_kernel<Out, kSize>), grid, block, 0, st, a, v0);
   return hipGetLastError();
 }
@@ -193,8 +194,10 @@ hipError_t launch_vocab_d_weight(const VocabArgs& a, int64_t v0, hipStream_t st)
 }
 
 hipError_t launch_vocab_d_hidden(const VocabArgs& a, int64_t v0, bool first, hipStream_t st) {
-  const dim3 grid(kCus), block(kGemmThreads);
-  hipLaunchKernelGGL(vocab_d_hidden_kernel, grid, block, 0, st, a, v0, first ? 1 : 0);
+  // How many tiles there are is known on the device: as many workgroups as fit.
+  const dim3 grid(resident_tiles(a.small_hidden ? kSmallTile : kTile)), block(kGemmThreads);
+  if (a.small_hidden) hipLaunchKernelGGL(vocab_d_hidden_kernel<kSmallTile>, grid, block, 0, st, a, v0, first ? 1 : 0);
+  else hipLaunchKernelGGL(vocab_d_hidden_kernel<kTile>, grid, block, 0, st, a, v0, first ? 1 : 0);
   return hipGetLastError();
 }
 

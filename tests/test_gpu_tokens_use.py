@@ -11,9 +11,9 @@ import torch
 import paper_1802_01561_amd as vt
 from oracle import tokens as ot
 from paper_1802_01561_amd._lib import lib
-from tests.test_gpu_log_prob_loss import _batch as _loss_batch
-from tests.test_gpu_log_prob_loss import _dev
-from tests.test_gpu_vocab import _batch, _check_grad, _check_log_probs, _gpu, _grad_inputs
+from test_gpu_log_prob_loss import _batch as _loss_batch
+from test_gpu_log_prob_loss import _dev
+from test_gpu_vocab import _batch, _check_grad, _check_log_probs, _gpu, _grad_inputs
 
 pytestmark = pytest.mark.gpu
 
