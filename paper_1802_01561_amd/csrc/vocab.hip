@@ -408,9 +408,12 @@ constexpr int64_t kMostFewSteps = 128;
 constexpr int64_t kStreamMostSteps = 64;
 constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
 
-// G of one piece takes at most this much (or one tile's columns): it is written and read
-// twice within the 256 MB Infinity Cache.
-constexpr int64_t kMostPieceBytes = int64_t(256) << 20;
+// G is written and read twice within the 256 MB Infinity Cache: as one piece of the
+// vocabulary where it fits, and otherwise in pieces of half of it (or one tile's columns).
+// 4096 steps, H = 4096, V = 131072 (1.07 GB, bfloat16): pieces of 128 MB 9.96 ms, of 96
+// 10.02, of 256 10.30, of 1024 10.48; 3200 steps, H = 1024, V = 32768 (213 MB): one piece 660
+// us, two 685.
+constexpr int64_t kOnePieceBytes = int64_t(256) << 20, kPieceBytes = int64_t(128) << 20;
 
 // Whether a product m x n over `steps` steps of 64 k is done in tiles of 128 rather than of
 // 256.
@@ -461,7 +464,8 @@ VocabPlan plan_vocab_grad(int64_t N, int64_t V, int64_t H, bool grad_bf16) {
   p.row_pitch = round_up(N, kTile);
   p.x_pitch = round_up(H, kTileK);
   const int64_t all = round_up(V, kTile);
-  const int64_t fit = kMostPieceBytes / (p.row_pitch * (grad_bf16 ? 2 : 4)) / kTile * kTile;
+  const int64_t column = p.row_pitch * (grad_bf16 ? 2 : 4);
+  const int64_t fit = (column * all <= kOnePieceBytes ? kOnePieceBytes : kPieceBytes) / column / kTile * kTile;
   const int64_t most = fit < kTile ? kTile : fit;
   const int64_t pieces = (all + most - 1) / most;
   p.g_pitch = round_up((all + pieces - 1) / pieces, kTile);
