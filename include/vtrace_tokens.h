@@ -56,10 +56,12 @@ extern "C" {
  *   workspace      vtrace_vocab_workspace_bytes(T,B,V,H) bytes, 16-byte aligned,
  *                  cleared once by vtrace_workspace_init
  * Numerics: bfloat16 products accumulated in float32 from the bias, exponentials
- * in float32, sums of at most 256 terms in float32 and joined in float64.  Any
+ * in float32, their sums in float32 over the tokens that one wave (or, up to 128
+ * steps, one workgroup: V / 256 tokens or more) takes and joined in float64.  Any
  * other token makes that step's log_probs NaN and raises the workspace's flag
  * (vtrace_error_flag).  A step whose tokens are all ruled out has log_sums
- * -INFINITY and NaN elsewhere; NaN and Inf inputs are propagated.
+ * -INFINITY and NaN elsewhere; NaN and Inf inputs are propagated, also from the
+ * row of a token that is ruled out (0 * NaN): such rows have to hold numbers.
  */
 size_t vtrace_vocab_workspace_bytes(int64_t T, int64_t B, int64_t V, int64_t H);
 
@@ -85,7 +87,8 @@ vtrace_status vtrace_vocab_log_probs(
  *   workspace           vtrace_vocab_grad_workspace_bytes(T,B,V,H,grad_dtype) bytes
  * Everything else as above.  G enters its two products as bfloat16, like a
  * bfloat16 gradient (2^-9 a term), for bfloat16 outputs, and as a bfloat16 pair
- * (high + low part, 2^-17 a term) for float32 ones.  A token that is neither in
+ * (high + low part, 2^-18 a term) for float32 ones; sums over steps and tokens are
+ * float32 (d_bias: 64 or 128 steps, then float64).  A token that is neither in
  * the vocabulary nor VTRACE_NO_TOKEN makes that step's G NaN, and with it
  * d_weight and d_bias.
  */

@@ -17,7 +17,7 @@ namespace {
 using vtrace::aligned;
 using vtrace::as_hip;
 
-// Tiles of 256 steps x 256 tokens that one launch numbers.
+// So that tiles are numbered by 32 bits, and their products and sums fit 64.
 constexpr int64_t kVocabMostSteps = int64_t(1) << 25;
 constexpr int64_t kVocabMostLogits = int64_t(1) << 38;
 

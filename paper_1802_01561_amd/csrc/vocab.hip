@@ -399,8 +399,8 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   return c.at;
 }
 
-// The kernels for few steps against tiles of 256 steps (H = 4096, V = 131072: 128 steps 266
-// us, 129 in tiles 288; 256 in tiles 304), and between those two: the streaming kernel up to
+// The kernels for few steps against tiles (H = 4096, V = 131072: 128 steps 249 us, 129 in
+// tiles 326; H = 512, V = 8000 19.6, 21.7), and between those two: the streaming kernel up to
 // 16 steps, and up to 64 on layers of at most 32 MB (24 steps, H = 512, V = 4000 9.2 us
 // against 13.9; 20, 256, 32768 12.0 against 14.2; 64, 1024, 8000 15.1 against 21.5; but 32,
 // 1024, 50000 36 against 28).

@@ -2,15 +2,18 @@
 // softmax statistics of vtrace_vocab_log_probs, and for G = dL/dz of vtrace_vocab_grad.
 //
 // The tile is z^T: m runs along the vocabulary, n along the steps, so that a lane of
-// the MFMA layout holds 32 logits of each of four steps and the sums over the vocabulary
+// the MFMA layout holds 32 logits of each of eight steps and the sums over the vocabulary
 // are mostly additions inside a lane.  The accumulators start at the bias, and at -inf
 // for the rows behind the vocabulary's end, whose exponentials are 0.
 //
-// Statistics of a step over 128 tokens (a wave's rows): with d = z log2 e - c, c the
+// Statistics of a step over a wave's rows (128 tokens, 64 in the small tiles): with d = z log2 e - c, c the
 // rounded maximum of z log2 e,
 //   sum 2^d and, for the entropy, sum 2^d d.
 // They are exact about c (not about the maximum before rounding), and the pieces are
 // joined in float64 (vocab.hip).
+//
+// Measured: statistics of 8000 ragged steps, H = 4096, V = 131072 (6.66 TFLOP) in 5.33 ms,
+// 1.25 PFLOP/s; G of 4096 steps in eight pieces (4.4 TFLOP, 1.07 GB of G) in 3.46 ms, 1.27.
 #include "vocab_impl.hpp"
 
 namespace vtrace {
