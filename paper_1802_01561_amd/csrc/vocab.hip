@@ -364,6 +364,7 @@ size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->pieces = p.pieces;
   a->tile_tokens = p.tile_tokens;
   a->narrow = p.narrow;
+  a->narrow_per_cu = p.narrow_per_cu;
   a->active = c.take<int32_t>(a->N);
   a->part_max = c.take<float>(p.pieces * p.row_pitch);
   a->part_sum = c.take<float>(p.pieces * p.row_pitch);
@@ -400,13 +401,20 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
 }
 
 // The kernels for few steps against tiles (H = 4096, V = 131072: 128 steps 249 us, 129 in
-// tiles 326; H = 512, V = 8000 19.6, 21.7), and between those two: the streaming kernel up to
-// 16 steps, and up to 64 on layers of at most 32 MB (24 steps, H = 512, V = 4000 9.2 us
-// against 13.9; 20, 256, 32768 12.0 against 14.2; 64, 1024, 8000 15.1 against 21.5; but 32,
-// 1024, 50000 36 against 28).
+// tiles 326; H = 512, V = 8000 19.6, 21.7).
 constexpr int64_t kMostFewSteps = 128;
-constexpr int64_t kStreamMostSteps = 64;
-constexpr int64_t kStreamMostLayer = int64_t(1) << 24;
+// Between those two.  The narrow kernel keeps more of the layer on its way, if its workgroups
+// have tokens enough: 16 steps, H = 4096, V = 32000 46 us against 63 streamed, 1 step, V =
+// 100003 156 against 168 (131072: 212, 208); 32 steps, H = 1024, V = 20000 16.4, 20.8; 64 steps,
+// H = 256, V = 32768 14.0, 16.9.  The streaming kernel starts faster: 16 steps, H = 512, V =
+// 16000 13.2 us narrow, 10.7 streamed; 32 steps, H = 4096, V = 8000 30, 28 and 64 41, 35.
+bool narrow_pays(int64_t N, int64_t V, int64_t H) {
+  return N > 64 || (V >= 12288 && (N > 32 || V * H > int64_t(1) << 24));
+}
+// Its workgroups a CU.  Up to 32 steps and few tokens: one, with more of them and more stages
+// (1 step, H = 8192, V = 20000 70 us, with two 82; H = 512, V = 50000 18.5, 16.7).  More than 64
+// steps: one of eight waves and 256 tokens.
+int narrow_per_cu(int64_t N, int64_t V) { return N > 64 || (N <= 32 && V < 24576) ? 1 : 2; }
 
 // G is written and read twice within the 256 MB Infinity Cache: as one piece of the
 // vocabulary where it fits, and otherwise in pieces of half of it (or one tile's columns).
@@ -432,13 +440,15 @@ VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
   p.few = N <= kMostFewSteps;
   if (p.few) {
     p.row_pitch = N;
-    p.narrow = N > kStreamMostSteps || (N > 16 && V * H > kStreamMostLayer);
+    p.narrow = narrow_pays(N, V, H);
     if (p.narrow) {
       // As few rounds over the workgroups that fit the GPU as tiles of 128 or 256 tokens
-      // allow, each as even as rows of 16 are.
-      const int64_t slots = N <= 64 ? 2 * kCus : kCus, most = N <= 64 ? 128 : 256;
+      // allow, all of them even (48 steps, H = 2048, V = 100003: 92 us, with tiles of whole
+      // 16 tokens 98).
+      p.narrow_per_cu = narrow_per_cu(N, V);
+      const int64_t slots = p.narrow_per_cu * kCus, most = N <= 64 ? 128 : 256;
       const int64_t rounds = (V + most * slots - 1) / (most * slots);
-      p.tile_tokens = static_cast<int>(round_up((V + rounds * slots - 1) / (rounds * slots), 16));
+      p.tile_tokens = static_cast<int>((V + rounds * slots - 1) / (rounds * slots));
       const int64_t tiles = (V + p.tile_tokens - 1) / p.tile_tokens;
       p.pieces = tiles < slots ? tiles : slots;
     } else {

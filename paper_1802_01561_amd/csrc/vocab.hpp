@@ -53,7 +53,8 @@ struct VocabArgs {
   int64_t row_pitch;
   int64_t pieces;         // grad: of the vocabulary
   int tile_tokens;        // of the kernels for few steps
-  bool narrow;            // the one for 17 to 128 steps
+  bool narrow;            // the one of the two that goes through LDS
+  int narrow_per_cu;      // its workgroups a CU
   // tiles: the active steps' hidden states, zeros around, and tokens
   uint16_t* x;            // [row_pitch, x_pitch]
   int64_t x_pitch;
@@ -72,6 +73,7 @@ struct VocabPlan {
   int64_t pieces;  // log_probs: statistics per step; grad: of the vocabulary
   int tile_tokens;
   bool narrow;
+  int narrow_per_cu;
   bool small_logits, small_weight, small_hidden;
   int64_t row_pitch, x_pitch, g_pitch;
   int64_t split_rows;

@@ -1,13 +1,12 @@
 // vtrace_vocab_log_probs for few steps (up to 128): the vocabulary layer is read once, and
 // that is what bounds it.  Two kernels; which one takes a call is chosen in vocab.hip.
 //
-// Up to 16 steps, or a small layer: rows from memory straight into matrix-core operands.
+// Up to 64 steps of a small layer: rows from memory straight into matrix-core operands.
 // A workgroup of four waves takes 16 R tokens and all steps.  The waves share out the
 // hidden units, 64 (a 128-byte line of each row) at a time; their partial logits meet
 // in LDS, where each wave takes some of the 16 x 16 pieces, adds the bias and forms the
-// softmax statistics as in vocab_logits.hip.  Three workgroups a CU hold 96 KB of loads in
-// flight: one step, H = 4096, V = 131072 (1.07 GB) in 204 us, 5.3 TB/s, where plain reads of
-// this pattern reach 4.7 to 5.9 TB/s.
+// softmax statistics as in vocab_logits.hip.  20 steps, H = 256, V = 32768 (17 MB) 8 us and 4
+// for the join.
 #include "vocab_impl.hpp"
 
 namespace vtrace {
@@ -145,22 +144,23 @@ __global__ __launch_bounds__(kStreamThreads) void vocab_stream_kernel(VocabArgs 
   }
 }
 
-// 17 to 128 steps of a large layer: the layer passes through LDS, copied there two or more
+// Up to 128 steps of a large layer: the layer passes through LDS, copied there two or more
 // steps of 64 hidden units ahead, so that the copies take no registers and the hidden
 // states are fetched once for 128 or 256 tokens (in the kernel above they weigh as much as
-// the rows: 48 steps, H = 2048, V = 100003 (410 MB) 131 -> 93 us, 4.4 TB/s; 64 steps,
-// H = 4096, V = 65536 192 -> 125).  Each wave has 32 of the tile's tokens and all steps, and
+// the rows: 48 steps, H = 2048, V = 100003 (410 MB) 131 -> 85 to 92 us, 4.4 to 4.8 TB/s; one step,
+// H = 4096, V = 131072 (1.07 GB) 212 us, 5.1 TB/s, where plain reads of this pattern reach 4.7
+// to 5.9).  Each wave has 32 of the tile's tokens and all steps, and
 // keeps their statistics in registers from tile to tile.  A tile holds as many tokens as
 // share the vocabulary out evenly over the resident workgroups; up to 64 steps these are
-// two a CU of four waves each, whose barriers do not meet (one of eight waves: 104 us).  The
-// copies run on across the tiles: the sequence of (tile, step) is flat.
-template <int kRows, int kWaves, bool kDot>
-__global__ __launch_bounds__(kWaves* kWave, 2) void vocab_narrow_kernel(VocabArgs a) {
+// mostly two a CU of four waves each, whose barriers do not meet (one of eight waves: 104 us
+// instead of 93).  The copies run on across the tiles: the sequence of (tile, step) is flat.
+template <int kRows, int kWaves, int kPerCu, bool kDot>
+__global__ __launch_bounds__(kWaves* kWave, kPerCu* kWaves / 4) void vocab_narrow_kernel(VocabArgs a) {
   constexpr int NT = kRows / 16;
   constexpr int kTileTokens = 32 * kWaves;
   constexpr int kWBytes = kTileTokens * kTileK * 2;
   constexpr int kStage = kWBytes + kRows * kTileK * 2;
-  constexpr int kNarrowStages = 160 * 1024 / (8 / kWaves) / kStage;  // all of LDS, between the CU's workgroups
+  constexpr int kNarrowStages = 160 * 1024 / kPerCu / kStage;  // all of LDS, between the CU's workgroups
   __shared__ __align__(1024) char lds[kNarrowStages * kStage];
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -196,8 +196,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void vocab_narrow_kernel(VocabArg
   };
   constexpr int kCopies = Loader<kTileTokens, kWaves>::kCopies + Loader<kRows, kWaves>::kCopies;
   constexpr int kInFlight = kCopies * (kNarrowStages - 2);
-  static_assert(kInFlight < 16, "vmcnt's low four bits");
-  constexpr int kWaitOldest = kInFlight | 0x0070;  // vmcnt(kInFlight) lgkmcnt(0)
+  static_assert(kInFlight < 64, "vmcnt's six bits");
+  // vmcnt(kInFlight) lgkmcnt(0)
+  constexpr int kWaitOldest = (kInFlight & 15) | (kInFlight >> 4) << 14 | 0x0070;
 
   Reader<false, true, 2> rw;
   Reader<false, false, NT> rx;
@@ -323,18 +324,20 @@ void launch_stream(const VocabArgs& a, hipStream_t st) {
 template <int R, bool kDot>
 void launch_stream_rows(const VocabArgs& a, hipStream_t st) {
   if (a.N <= 16) launch_stream<R, 1, kDot>(a, st);
-  else if (a.N <= 32) launch_stream<R, 2, kDot>(a, st);
-  else launch_stream<R, 4, kDot>(a, st);
+  else if (a.N <= 32 || R == 4) launch_stream<R, 2, kDot>(a, st);  // more steps of so many tokens are narrow
+  else if constexpr (R < 4) launch_stream<R, 4, kDot>(a, st);
 }
-template <int kRows, int kWaves, bool kDot>
+template <int kRows, int kWaves, int kPerCu, bool kDot>
 void launch_narrow(const VocabArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((vocab_narrow_kernel<kRows, kWaves, kDot>), dim3(static_cast<unsigned>(a.pieces)),
+  hipLaunchKernelGGL((vocab_narrow_kernel<kRows, kWaves, kPerCu, kDot>), dim3(static_cast<unsigned>(a.pieces)),
                      dim3(kWaves * kWave), 0, st, a);
 }
 template <bool kDot>
 void launch(const VocabArgs& a, hipStream_t st) {
-  if (a.narrow && a.N <= 64) launch_narrow<64, 4, kDot>(a, st);
-  else if (a.narrow) launch_narrow<128, 8, kDot>(a, st);
+  if (a.narrow && a.N <= 32 && a.narrow_per_cu == 1) launch_narrow<32, 4, 1, kDot>(a, st);
+  else if (a.narrow && a.N <= 32) launch_narrow<32, 4, 2, kDot>(a, st);
+  else if (a.narrow && a.N <= 64) launch_narrow<64, 4, 2, kDot>(a, st);
+  else if (a.narrow) launch_narrow<128, 8, 1, kDot>(a, st);
   else if (a.tile_tokens == 64) launch_stream_rows<4, kDot>(a, st);
   else if (a.tile_tokens == 32) launch_stream_rows<2, kDot>(a, st);
   else launch_stream_rows<1, kDot>(a, st);

@@ -34,9 +34,10 @@ def test_steps_where_another_kernel_takes_over(N, bias):
 
 
 @pytest.mark.parametrize("N,H,V", [(20, 512, 33000), (16, 8, 20001), (33, 520, 33003), (64, 1032, 16400), (100, 8, 70001),
-                                   (128, 328, 66001)])
+                                   (128, 328, 66001), (1, 520, 33003), (16, 1400, 12301), (32, 1032, 16400), (31, 1376, 24575),
+                                   (17, 768, 24576), (40, 72, 12288), (64, 72, 12287), (33, 72, 6144), (64, 8, 300), (2, 136, 140001)])
 def test_layers_where_another_kernel_takes_over(N, H, V):
-    """On both sides of 2^24 elements, of 16, 32 and 64 tokens a workgroup, and of one round."""
+    """On both sides of 2^24 elements, of the bounds on V, of 16, 32 and 64 tokens a workgroup, and of one round."""
     x, w, b, tokens, _, _ = _batch(N + V, N, 1, H, V, bias=True, none=0.1)
     ws = vt.VocabWorkspace(N, 1, V, H)
     ws.tensor[256:].fill_(0xFF)
