@@ -3,8 +3,8 @@
 ``python -m paper_1802_01561_amd.sanitize`` builds a second copy of the library
 whose host code (argument validation, kernel choice, launch set-up) is
 instrumented with ``-fsanitize=address,undefined`` and whose device code is
-built as usual, then runs the C-ABI tests (``tests/test_abi.py``, which need no
-GPU) against it with the sanitizer runtime preloaded into the interpreter.  Any
+built as usual, then runs the C-ABI tests (``tests/test_abi.py`` and
+``tests/test_tokens_abi.py``, which need no GPU) against it with the sanitizer runtime preloaded into the interpreter.  Any
 report ends the run with a non-zero status.  The sanitizers apply to host code
 only: ``-Xarch_host`` keeps them out of the gfx950 code objects.
 """
@@ -42,7 +42,7 @@ def main() -> int:
                ASAN_OPTIONS="detect_leaks=0:abort_on_error=0:halt_on_error=1",
                UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
     cmd = [sys.executable, "-m", "pytest", "-q", "-p", "no:cacheprovider", "-m", "not gpu",
-           os.path.join(REPO_DIR, "tests", "test_abi.py")]
+           os.path.join(REPO_DIR, "tests", "test_abi.py"), os.path.join(REPO_DIR, "tests", "test_tokens_abi.py")]
     print("running:", " ".join(cmd), flush=True)
     return subprocess.run(cmd, env=env, cwd=REPO_DIR).returncode
 
