@@ -21,8 +21,10 @@
 // With f(r) = bits 0, 1 and 3 of r the 64 lanes of each kind of read fall on all banks
 // evenly.
 //
-// Bound by the matrix cores: a step of 64 k takes 1.56 us on all CUs, 1.375 PFLOP/s (large
-// products of the vendor's library 1.45 to 1.49).  A tile costs 7 to 14 us more: filling and
+// A step of 64 k takes 1.56 us on all CUs, 1.375 PFLOP/s (large products of the vendor's
+// library 1.45 to 1.49), with the matrix units busy 60% of it.  What bounds it are the copies,
+// 64 KB a CU and step, 10.7 TB/s from the L2s with 80% hits: without them a timing copy took 25%
+// less, without the reads of LDS too 37%.  A tile costs 7 to 14 us more: filling and
 // draining the pipeline, and its stores, which all CUs make at about the same time (without
 // those of G its kernel takes 836 us instead of 914, without its exponentials 914).  Waiting
 // at the next tile's start for the copies alone and not for the stores behind them, stores
@@ -201,9 +203,13 @@ struct Reader {
 // vmcnt(0) and lgkmcnt(0): the copies into LDS have arrived and this wave's reads are done.
 constexpr int kWaitAll = 0x0070;
 
+// The same but for the last kYounger vector memory operations (they complete in order).
+constexpr int wait_but(int younger) { return (younger & 15) | (younger >> 4) << 14 | kWaitAll; }
+
+template <int kYounger = 0>
 __device__ __forceinline__ void stage_barrier() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(kWaitAll);
+  __builtin_amdgcn_s_waitcnt(wait_but(kYounger));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -223,41 +229,63 @@ __device__ __forceinline__ float element(const f32x4& c, int i) {
   return x;
 }
 
-// What a wave does between two barriers: it multiplies the second half of a step (a1, b1)
-// and reads the first half of the next from `from`, multiplies that and reads the second,
-// while its copies of the step after go to `to`.  The two stages do not overlap, and
-// __restrict says so: the compiler otherwise waits for every copy in flight before a read.
-//
-// The copies are spread over the first half: four at a time instead of two cost 4%, as
-// the path into LDS takes one 16-byte vector a lane at a time.  With both operands "along" a
-// quarter of them goes with the second half (kSpread: logits of 6200 steps, H = 4096, V =
-// 131072 5.42 -> 5.23 ms); d_weight, both "across", took 2% longer so.
+// What a wave does between two barriers.  Of a step's two halves of 32 k one is multiplied
+// while the other is read to registers, and copies go out among the products: the path into
+// LDS takes a 16-byte vector of four lanes at a time, and copies in a bunch hold up the wave
+// (all of a step's within the first quarter, the first half: 11.2, 10.3 ms of the largest
+// gradient).  What is read and what is copied to do not overlap, and __restrict says so: the
+// compiler otherwise waits for every copy in flight before a read.
 template <bool kAAcross, bool kBAcross, int kSize>
 struct Contraction {
   static constexpr int kMT = kSize / 32, kNT = kSize / 32, kOperandBytes = operand_bytes(kSize);
-  static constexpr bool kSpread = !kAAcross && !kBAcross;
   Reader<kAAcross, !kAAcross, kMT, kSize> ra;
   Reader<kBAcross, false, kNT, kSize> rb;
   bf16x8 a0[kMT], b0[kNT], a1[kMT], b1[kNT];
 
+  // The first half finds none before it: zeros (64 products, against a branch around each).
+  __device__ __forceinline__ void start(int wave, int lane) {
+    ra.start((wave % 2) * (kSize / 2), lane % 16, lane / 16);
+    rb.start((wave / 2) * (kSize / 2), lane % 16, lane / 16);
+#pragma unroll
+    for (int i = 0; i < kMT; ++i) a1[i] = bf16x8{};
+#pragma unroll
+    for (int i = 0; i < kNT; ++i) b1[i] = bf16x8{};
+  }
+  // The last half, and the time until the last products are written.
+  __device__ __forceinline__ void end(Accumulators<kSize>& acc) {
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a1[m], b1[n]);
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[kMT - 1][n]));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
   // Two of a half's fragments.
-  __device__ __forceinline__ void read(const char* from, int kk, int i, bf16x8 (&a)[kMT], bf16x8 (&b)[kNT]) {
+  __device__ __forceinline__ void read(const char* from_a, const char* from_b, int kk, int i, bf16x8 (&a)[kMT],
+                                       bf16x8 (&b)[kNT]) {
     if (i < kNT / 2) {
-      b[2 * i] = rb.read(from + kOperandBytes, 2 * i, kk);
-      b[2 * i + 1] = rb.read(from + kOperandBytes, 2 * i + 1, kk);
+      b[2 * i] = rb.read(from_b, 2 * i, kk);
+      b[2 * i + 1] = rb.read(from_b, 2 * i + 1, kk);
     } else {
-      a[2 * i - kNT] = ra.read(from, 2 * i - kNT, kk);
-      a[2 * i - kNT + 1] = ra.read(from, 2 * i - kNT + 1, kk);
+      a[2 * i - kNT] = ra.read(from_a, 2 * i - kNT, kk);
+      a[2 * i - kNT + 1] = ra.read(from_a, 2 * i - kNT + 1, kk);
     }
   }
+  // Both halves of a step: the second half of the step before (a1, b1) and the first of this
+  // one are multiplied, both of this one read from `from`, and the next step copied to `to`.
+  // Operands "along": 12 copies with the first half, 4 with the second, which have less time to
+  // arrive (logits of 6200 steps, H = 4096, V = 131072 5.23 ms; 16 and 0 5.42, 10 and 6 5.40).
+  // "Across" all with the first half (d_weight of the largest gradient 2% faster so).
   __device__ __forceinline__ void step(char* __restrict to, const char* __restrict from, Loader<kSize>& la,
                                        Loader<kSize>& lb, bool more, int wave, Accumulators<kSize>& acc) {
     const Rsrc da = la.begin(more), db = lb.begin(more);
 #pragma unroll
     for (int m = 0; m < kMT; ++m) {
-      read(from, 0, m, a0, b0);
+      read(from, from + kOperandBytes, 0, m, a0, b0);
       la.copy(da, to, wave, m);
-      if constexpr (!kSpread) lb.copy(db, to + kOperandBytes, wave, m);
+      if constexpr (kBAcross) lb.copy(db, to + kOperandBytes, wave, m);
       else if (m % 2 == 0) lb.copy(db, to + kOperandBytes, wave, m / 2);
 #pragma unroll
       for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a1[m], b1[n]);
@@ -265,10 +293,28 @@ struct Contraction {
     }
 #pragma unroll
     for (int m = 0; m < kMT; ++m) {
-      read(from, 1, m, a1, b1);
-      if (kSpread && m < kMT / 2) lb.copy(db, to + kOperandBytes, wave, kMT / 2 + m);
+      read(from, from + kOperandBytes, 1, m, a1, b1);
+      if (!kBAcross && m < kMT / 2) lb.copy(db, to + kOperandBytes, wave, kMT / 2 + m);
 #pragma unroll
       for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a0[m], b0[n]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // The same for half a step, kk: the other half in registers (a, b) is multiplied, this one
+  // read to (na, nb), and a whole step of one operand copied, or (kHalves) two halves.
+  template <bool kHalves>
+  __device__ __forceinline__ void half(char* __restrict to, char* __restrict then_to, const char* __restrict from_a,
+                                       const char* __restrict from_b, const Loader<kSize>& load, Rsrc d, Rsrc then_d,
+                                       int kk, int wave, const bf16x8 (&a)[kMT], const bf16x8 (&b)[kNT],
+                                       bf16x8 (&na)[kMT], bf16x8 (&nb)[kNT], Accumulators<kSize>& acc) {
+#pragma unroll
+    for (int m = 0; m < kMT; ++m) {
+      read(from_a, from_b, kk, m, na, nb);
+      if (!kHalves || m < kMT / 2) load.copy(d, to, wave, m);
+      else load.copy(then_d, then_to, wave, m - kMT / 2);
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) mfma(acc[m][n], a[m], b[n]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -287,28 +333,20 @@ struct Job {
   }
 };
 
-// acc += A B over the job's steps.  A step's two halves of 32 k take turns in registers:
-// while one is multiplied the other is read.  A wave passes the barrier when it has read
-// all of a step and its copies of the next have arrived, so behind it the next stage is
-// whole and this one free.
+// acc += A B over the job's steps, both operands "along" or both "across".  A wave passes the barrier when it
+// has read all of a step and its copies of the next have arrived, so behind it the next stage
+// is whole and this one free.
 //
 // The first step's copies are under way when this is called (to stage `parity`).  With the
 // last step's products go the copies of the next tile's first: next() makes `job` that
 // tile's, and what follows the contraction hides their latency.
-template <bool kAAcross, bool kBAcross, int kSize, typename Next>
+template <bool kAcross, int kSize, typename Next>
 __device__ __forceinline__ void contract(Job<kSize>& job, char* lds, int& parity, int wave, int lane,
                                          Accumulators<kSize>& acc, Next next) {
-  constexpr int kMT = kSize / 32, kNT = kSize / 32, kStage = 2 * operand_bytes(kSize);
+  constexpr int kStage = 2 * operand_bytes(kSize);
   const int steps = job.steps;
-  Contraction<kAAcross, kBAcross, kSize> c;
-  c.ra.start((wave % 2) * (kSize / 2), lane % 16, lane / 16);
-  c.rb.start((wave / 2) * (kSize / 2), lane % 16, lane / 16);
-  // The first step finds no second half before it: zeros (64 products, against a branch
-  // around each of them).
-#pragma unroll
-  for (int i = 0; i < kMT; ++i) c.a1[i] = bf16x8{};
-#pragma unroll
-  for (int i = 0; i < kNT; ++i) c.b1[i] = bf16x8{};
+  Contraction<kAcross, kAcross, kSize> c;
+  c.start(wave, lane);
   int it = 0;
   do {
     stage_barrier();
@@ -320,14 +358,110 @@ __device__ __forceinline__ void contract(Job<kSize>& job, char* lds, int& parity
     c.step(lds + (parity ^ 1) * kStage, lds + parity * kStage, job.a, job.b, more, wave, acc);
     parity ^= 1;
   } while (++it < steps);
+  c.end(acc);
+}
+
+constexpr int kCus = 256;
+
+// Workgroups of a launch over tiles of kSize: as many as fit the CUs at a time (a tile of
+// 256 fills a CU's LDS, one of 128 leaves room for another), each with every so many'th.
+__host__ __device__ constexpr int resident_tiles(int size) { return size == kTile ? kCus : 2 * kCus; }
+__host__ __device__ inline int64_t tiles_of(int64_t n, int size) { return (n + size - 1) / size; }
+inline unsigned workgroups_of(int64_t tiles, int size) {
+  return static_cast<unsigned>(tiles < resident_tiles(size) ? tiles : resident_tiles(size));
+}
+// us of a round of them over `steps` steps of 64 k.  640 steps, H = 256, V = 32768: logits 40
+// us in two rounds of 256, 32 in three of 128; d_weight (float32) 47 in one half empty, 29 in a
+// small one.  3200 steps, H = 1024: 261 in seven, 303 in thirteen small ones.
+__host__ __device__ inline double round_cost(int size, int64_t steps) {
+  return size == kTile ? 1.56 * static_cast<double>(steps) + 13.0 : 1.2 * static_cast<double>(steps) + 6.0;
+}
+
+// The tiles of this workgroup, one after the other.  Those that are worked on at a time are
+// consecutive numbers, and those of one XCD are too.
+struct Tiles {
+  int total, at;
+
+  __device__ __forceinline__ explicit Tiles(int64_t n) : total(static_cast<int>(n)) {
+    at = static_cast<int>(xcd_tile(blockIdx.x, gridDim.x));
+  }
+  __device__ __forceinline__ bool any() const { return at < total; }
+  __device__ __forceinline__ void next() { at += gridDim.x; }
+};
+
+// One operand's copies, tile after tile of this workgroup and ahead of the products: `left`
+// steps (or halves) of its tile are still to come.
+template <int kSize>
+struct Feed {
+  Loader<kSize> load;
+  Tiles tiles;
+  int left = 0;
+
+  __device__ __forceinline__ explicit Feed(const Tiles& t) : tiles(t) {}
+  // The next one's descriptor; start() aims the loader at a tile and returns its steps.  Behind
+  // the last tile nothing is read, and zeros arrive.
+  template <typename Start>
+  __device__ __forceinline__ Rsrc begin(Start start) {
+    if (left == 0) {
+      left = 0x7fffffff;
+      load.aim(nullptr, 0);
+      if (tiles.any()) left = start(*this);
+      tiles.next();
+    }
+    --left;
+    return load.begin();
+  }
+};
+
+// acc += A B over `steps` steps, A "across", so that its halves of a step are apart in LDS, and
+// B "along".  The copies are spread evenly over the products: while the first half of step i is
+// read, those of B's step i + 1 go out, and while the second is, those of A's second half of step
+// i + 1 and first of i + 2 (to where halves were read just before).  Each has half a step of
+// products or more to arrive, and a wave waits for no younger ones.
+//   LDS: two steps of A, then two of B.  In flight when a tile begins: A's first half, B's first
+// step, A's next two halves.
+//   Against one barrier a step, as in contract(): d_hidden of 843 ragged steps, H = 1000, V =
+// 50021 (two products for float32, 98 steps a tile) 203 -> 172 us, where H is a power of two the
+// same.  (d_weight, both operands "across": so 222 -> 213 us there, but 203 -> 215 for 3200 steps,
+// H = 1024, V = 32768 and 1% longer for the largest gradient.)
+template <int kSize, typename StartA, typename StartB>
+__device__ __forceinline__ void contract_halves(int steps, Feed<kSize>& feed_a, Feed<kSize>& feed_b, char* lds,
+                                                int& parity, int wave, int lane, Accumulators<kSize>& acc,
+                                                StartA start_a, StartB start_b) {
+  constexpr int kBytes = operand_bytes(kSize), kCopies = kSize / 32;
+  Contraction<true, false, kSize> c;
+  c.start(wave, lane);
+  int it = 0;
+  do {
+    char* const a = lds + parity * kBytes;
+    char* const b = a + 2 * kBytes;
+    char* const next_a = lds + (parity ^ 1) * kBytes;
+    char* const next_b = next_a + 2 * kBytes;
+    stage_barrier<kCopies>();
+    const Rsrc d = feed_b.begin(start_b);
+    c.template half<false>(next_b, next_b, a, b, feed_b.load, d, d, 0, wave, c.a1, c.b1, c.a0, c.b0, acc);
+    stage_barrier<kCopies + kCopies / 2>();
+    const Rsrc d1 = feed_a.begin(start_a), d2 = feed_a.begin(start_a);
+    c.template half<true>(next_a + kBytes / 2, a, a, b, feed_a.load, d1, d2, 1, wave, c.a0, c.b0, c.a1, c.b1, acc);
+    parity ^= 1;
+  } while (++it < steps);
+  c.end(acc);
+}
+// What is in flight when the first tile begins.
+template <int kSize, typename StartA, typename StartB>
+__device__ __forceinline__ void start_halves(Feed<kSize>& feed_a, Feed<kSize>& feed_b, char* lds, int wave,
+                                             StartA start_a, StartB start_b) {
+  constexpr int kBytes = operand_bytes(kSize), kCopies = kSize / 32;
+  for (int h = 0; h < 3; ++h) {
+    const Rsrc a = feed_a.begin(start_a);
 #pragma unroll
-  for (int m = 0; m < kMT; ++m)
+    for (int i = 0; i < kCopies / 2; ++i) feed_a.load.copy(a, lds + h * (kBytes / 2), wave, i);
+    if (h == 0) {
+      const Rsrc b = feed_b.begin(start_b);
 #pragma unroll
-    for (int n = 0; n < kNT; ++n) mfma(acc[m][n], c.a1[m], c.b1[n]);
-  // The last products are written.
-#pragma unroll
-  for (int n = 0; n < kNT; ++n) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[kMT - 1][n]));
-  __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < kCopies; ++i) feed_b.load.copy(b, lds + 2 * kBytes, wave, i);
+    }
+  }
 }
 
 // Sums (or maxima) over the four lane groups, the same in all of them.
@@ -361,33 +495,6 @@ __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
 // A token ruled out adds p log p = 0, not 0 * -inf.
 constexpr float kLeastLog = -1e30f;
 
-constexpr int kCus = 256;
-
-// Workgroups of a launch over tiles of kSize: as many as fit the CUs at a time (a tile of
-// 256 fills a CU's LDS, one of 128 leaves room for another), each with every so many'th.
-__host__ __device__ constexpr int resident_tiles(int size) { return size == kTile ? kCus : 2 * kCus; }
-__host__ __device__ inline int64_t tiles_of(int64_t n, int size) { return (n + size - 1) / size; }
-inline unsigned workgroups_of(int64_t tiles, int size) {
-  return static_cast<unsigned>(tiles < resident_tiles(size) ? tiles : resident_tiles(size));
-}
-// us of a round of them over `steps` steps of 64 k.  640 steps, H = 256, V = 32768: logits 40
-// us in two rounds of 256, 32 in three of 128; d_weight (float32) 47 in one half empty, 29 in a
-// small one.  3200 steps, H = 1024: 261 in seven, 303 in thirteen small ones.
-__host__ __device__ inline double round_cost(int size, int64_t steps) {
-  return size == kTile ? 1.56 * static_cast<double>(steps) + 13.0 : 1.2 * static_cast<double>(steps) + 6.0;
-}
-
-// The tiles of this workgroup, one after the other.  Those that are worked on at a time are
-// consecutive numbers, and those of one XCD are too.
-struct Tiles {
-  int total, at;
-
-  __device__ __forceinline__ explicit Tiles(int64_t n) : total(static_cast<int>(n)) {
-    at = static_cast<int>(xcd_tile(blockIdx.x, gridDim.x));
-  }
-  __device__ __forceinline__ bool any() const { return at < total; }
-  __device__ __forceinline__ void next() { at += gridDim.x; }
-};
 
 // Tile number `id` of `wide` x `deep`: consecutive numbers share operands in an XCD's L2
 // (8 tiles along `wide`, then along `deep`).

@@ -12,8 +12,8 @@
 // They are exact about c (not about the maximum before rounding), and the pieces are
 // joined in float64 (vocab.hip).
 //
-// Measured: statistics of 8000 ragged steps, H = 4096, V = 131072 (6.66 TFLOP) in 5.33 ms,
-// 1.25 PFLOP/s; G of 4096 steps in eight pieces (4.4 TFLOP, 1.07 GB of G) in 3.46 ms, 1.27.
+// Measured: statistics of 6200 steps, H = 4096, V = 131072 (6.66 TFLOP) in 5.24 ms,
+// 1.27 PFLOP/s; G of 4096 steps in eight pieces (4.4 TFLOP, 1.07 GB of G) in 3.44 ms, 1.28.
 #include "vocab_impl.hpp"
 
 namespace vtrace {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_lo
 #pragma unroll
     for (int n = 0; n < kNT; ++n) acc[m][n] = b;
   }
-  contract<false, false>(job, lds, parity, wave, lane, acc, [&] {
+  contract<false>(job, lds, parity, wave, lane, acc, [&] {
     tiles.next();
     start();
   });

@@ -5,7 +5,7 @@
 // to 2^-18 of itself, for outputs whose own rounding is 2^-24.
 //
 // Measured: 4096 steps, H = 4096, V = 131072, bfloat16, in eight pieces (4.4 TFLOP each)
-// d_weight 3.31 ms, 1.33 PFLOP/s, d_hidden 3.19 ms, 1.38.
+// d_weight 3.31 ms, 1.33 PFLOP/s, d_hidden 3.22 ms, 1.37.
 #include "vocab_impl.hpp"
 
 namespace vtrace {
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_d_
   while (tiles.any()) {
     const int64_t h0 = static_cast<int64_t>(at.wide) * kSize, vt = static_cast<int64_t>(at.deep) * kSize;
     Accumulators<kSize> acc = {};
-    contract<true, true>(job, lds, parity, wave, lane, acc, [&] {
+    contract<true>(job, lds, parity, wave, lane, acc, [&] {
       tiles.next();
       start();
     });
@@ -111,45 +111,48 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_d_
   const int all_steps = static_cast<int>((v_left + kTileK - 1) / kTileK);
   const int64_t part = a.row_pitch * a.g_pitch;
 
-  Job<kSize> job;
-  job.a.across(a.H, wave, lane);
-  job.b.along(a.g_pitch, kSize, wave, lane);
-  TileAt at;
-  int split = 0;
-  auto start = [&] {
-    job.steps = 0;
-    if (!tiles.any()) return;
-    split = tiles.at / per_split;
-    at = tile_at(tiles.at % per_split, tiles_n, tiles_h);
-    const int64_t h0 = static_cast<int64_t>(at.deep) * kSize, n0 = static_cast<int64_t>(at.wide) * kSize;
-    const int64_t from = static_cast<int64_t>(all_steps) * split / splits;
-    const int64_t to = static_cast<int64_t>(all_steps) * (split + 1) / splits;
-    const int once = to == from ? 1 : static_cast<int>(to - from);  // nothing left: a step of nothing
-    const int64_t v0 = v_begin + from * kTileK;
-    const uint16_t* const w = a.weight + v0 * a.H + h0;
-    const int64_t w_left = to == from ? 0 : ((a.V - v0) * a.H - h0) * 2;
-    const uint16_t* const gp = a.g + n0 * a.g_pitch + from * kTileK;
-    const int64_t g_left = ((a.row_pitch - n0) * a.g_pitch - from * kTileK) * 2;
-    job.a.aim(w, w_left);
-    job.b.aim(gp, g_left);
-    job.steps = once;
-    if (!a.grad_bf16) {
-      job.a.restart_after(once, w, w_left);
-      job.b.restart_after(once, gp + part, g_left);
-      job.steps = 2 * once;
-    }
+  struct Part {
+    int64_t h0, n0;
+    int split, from, to;
+  };
+  auto part_of = [&](int id) {
+    const int split = id / per_split;
+    const TileAt at = tile_at(id % per_split, tiles_n, tiles_h);
+    return Part{static_cast<int64_t>(at.deep) * kSize, static_cast<int64_t>(at.wide) * kSize, split,
+                static_cast<int>(static_cast<int64_t>(all_steps) * split / splits),
+                static_cast<int>(static_cast<int64_t>(all_steps) * (split + 1) / splits)};
+  };
+  const int passes = a.grad_bf16 ? 1 : 2;
+  auto once_of = [&](const Part& p) { return p.to == p.from ? 1 : p.to - p.from; };  // nothing left: a step of nothing
+  Feed<kSize> ws(tiles), gs(tiles);
+  ws.load.across(a.H, wave, lane);
+  ws.load.step /= 2;
+  gs.load.along(a.g_pitch, kSize, wave, lane);
+  auto start_w = [&](Feed<kSize>& f) {
+    const Part p = part_of(f.tiles.at);
+    const int64_t v0 = v_begin + static_cast<int64_t>(p.from) * kTileK;
+    const uint16_t* const w = a.weight + v0 * a.H + p.h0;
+    const int64_t left = p.to == p.from ? 0 : ((a.V - v0) * a.H - p.h0) * 2;
+    f.load.aim(w, left);
+    if (passes == 2) f.load.restart_after(2 * once_of(p), w, left);
+    return 2 * passes * once_of(p);
+  };
+  auto start_g = [&](Feed<kSize>& f) {
+    const Part p = part_of(f.tiles.at);
+    const uint16_t* const gp = a.g + p.n0 * a.g_pitch + static_cast<int64_t>(p.from) * kTileK;
+    const int64_t left = ((a.row_pitch - p.n0) * a.g_pitch - static_cast<int64_t>(p.from) * kTileK) * 2;
+    f.load.aim(gp, left);
+    if (passes == 2) f.load.restart_after(once_of(p), gp + part, left);
+    return passes * once_of(p);
   };
   int parity = 0;
-  start();
-  if (job.steps > 0) job.copy(lds, wave);
-  while (tiles.any()) {
-    const int64_t h0 = static_cast<int64_t>(at.deep) * kSize, n0 = static_cast<int64_t>(at.wide) * kSize;
-    float* const sums = a.h_partials + static_cast<int64_t>(split) * tiles_n * kSize * a.H;
+  if (tiles.any()) start_halves(ws, gs, lds, wave, start_w, start_g);
+  for (; tiles.any(); tiles.next()) {
+    const Part p = part_of(tiles.at);
+    const int64_t h0 = p.h0, n0 = p.n0;
+    float* const sums = a.h_partials + static_cast<int64_t>(p.split) * tiles_n * kSize * a.H;
     Accumulators<kSize> acc = {};
-    contract<true, false>(job, lds, parity, wave, lane, acc, [&] {
-      tiles.next();
-      start();
-    });
+    contract_halves(passes * once_of(p), ws, gs, lds, parity, wave, lane, acc, start_w, start_g);
     // Later pieces add to what the earlier ones left: the next step's row is fetched while
     // this one's is added to.
     const Rsrc out = make_rsrc(sums + n0 * a.H, (count - n0) * a.H * 4);
