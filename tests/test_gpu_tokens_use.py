@@ -12,7 +12,8 @@ import paper_1802_01561_amd as vt
 from oracle import tokens as ot
 from paper_1802_01561_amd._lib import lib
 from test_gpu_log_prob_loss import _batch as _loss_batch
-from test_gpu_log_prob_loss import _dev
+from test_gpu_log_prob_loss import PLAIN, _dev
+from test_gpu_log_prob_loss import _check as _check_losses
 from test_gpu_vocab import _batch, _check_grad, _check_log_probs, _gpu, _grad_inputs
 
 pytestmark = pytest.mark.gpu
@@ -67,6 +68,46 @@ def test_parts_of_d_hidden_follow_the_steps_that_count(none):
         ls, ent = _grad_inputs(x, w, b, tokens)
         out = vt.vtrace_vocab_grad(*_gpu(x, w, b, tokens, ls, ent, d_lp, d_h), workspace=ws)
         _check_grad(x, w, b, tokens, d_lp, d_h, out, torch.float32)
+
+
+@pytest.mark.parametrize("N,H,V", [(8192, 64, 130), (8193, 72, 300), (20011, 64, 257), (200000, 8, 40)])
+def test_many_steps(N, H, V):
+    """On both sides of the number of steps up to which one launch lists and gathers them."""
+    x, w, b, tokens, d_lp, d_h = _batch(N, N, 1, H, V, bias=True, none=0.3)
+    tokens[:300] = vt.NO_TOKEN
+    ws = vt.VocabWorkspace(N, 1, V, H)
+    ws.tensor[256:].fill_(0xFF)
+    _check_log_probs(x, w, b, tokens, vt.vtrace_vocab_log_probs(*_gpu(x, w, b, tokens), workspace=ws))
+    ls, ent = _grad_inputs(x, w, b, tokens)
+    d_lp, d_h = (torch.where(tokens >= 0, t, 0.0) for t in (d_lp, d_h))
+    out = vt.vtrace_vocab_grad(*_gpu(x, w, b, tokens, ls, ent, d_lp, d_h))
+    _check_grad(x, w, b, tokens, d_lp, d_h, out, torch.float32)
+
+
+@pytest.mark.parametrize("T,B", [(200000, 1), (70000, 3)])
+def test_losses_of_the_longest_lanes(T, B):
+    y = _loss_batch(T, T, B, lengths=(lambda r: r.integers(0, T + 1, B)) if B > 1 else None)
+    out = vt.vtrace_log_prob_loss_grad(**_dev(y), **PLAIN, with_vs=True, with_pg_advantages=True)
+    _check_losses(y, out, PLAIN)
+
+
+def test_losses_of_many_lanes():
+    """The recursion of all lanes at once in float64 (the oracle walks them one by one)."""
+    T, B = 3, 300001
+    y = _loss_batch(T, T, B)
+    out = vt.vtrace_log_prob_loss_grad(**_dev(y), **PLAIN, with_vs=True, with_pg_advantages=True)
+    f = {k: v.astype(np.float64) for k, v in y.items() if v is not None}
+    rho = np.minimum(1.0, np.exp(f["target_log_probs"] - f["behaviour_log_probs"]))
+    r, g, v = f["rewards"], f["discounts"], f["values"]
+    vs, adv = np.empty((T, B)), np.empty((T, B))
+    after, v_after = f["bootstrap_value"], f["bootstrap_value"]
+    for t in reversed(range(T)):
+        adv[t] = rho[t] * (r[t] + g[t] * after - v[t])
+        vs[t] = v[t] + rho[t] * (r[t] + g[t] * v_after - v[t]) + g[t] * rho[t] * (after - v_after)
+        after, v_after = vs[t], v[t]
+    for got, ref in ((out.vs, vs), (out.pg_advantages, adv), (out.d_log_probs, -adv), (out.d_values, 0.5 * (v - vs))):
+        # as in _check of the losses' tests
+        assert (np.abs(got.cpu().double().numpy() - ref) <= 2.0 ** -24 * np.abs(ref) + 1e-9 * (1.0 + np.abs(ref).max())).all()
 
 
 def test_native_and_python_marshalling_agree():
