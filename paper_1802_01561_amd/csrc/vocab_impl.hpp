@@ -216,7 +216,7 @@ __device__ __forceinline__ void stage_barrier() {
 
 // c += a b.  As an instruction of our own so that the accumulators stay in the accumulation
 // registers: the compiler's allocation moves them to and fro (three moves an MFMA).  It knows
-// nothing of its latency: contract() waits for the last.
+// nothing of its latency: Contraction::end waits for the last.
 __device__ __forceinline__ void mfma(f32x4& c, bf16x8 a, bf16x8 b) {
   asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
