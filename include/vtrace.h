@@ -155,15 +155,20 @@ int64_t vtrace_max_elements(void);
 
 /*
  * Bytes of device workspace that vtrace_loss_grad needs for a [T,B,A] batch
- * (the cross-workgroup loss partials, a completion counter and the error
+ * (the cross-workgroup loss partials, completion counters and the error
  * flag).  Returns 0 for invalid sizes.
+ *
+ * One buffer of the largest of the sizes that the vtrace_*_workspace_bytes
+ * functions (and VTRACE_CLIP_WORKSPACE_BYTES, vtrace_tokens.h) give for them can
+ * serve calls of every kind in turn, cleared once.  Calls that may run at the
+ * same time need a workspace each.
  */
 size_t vtrace_workspace_bytes(int64_t T, int64_t B, int64_t A);
 
 /*
- * Clears a workspace (counter, error flag, partials) with a fill kernel on
- * `stream`.  Call once after allocating it; vtrace_loss_grad leaves the counter
- * at zero again after every call, so a workspace can be reused without clearing.
+ * Clears a workspace (counters, error flag, partials) with a fill kernel on
+ * `stream`.  Call once after allocating it; every call leaves the counters
+ * at zero again, so a workspace can be reused without clearing.
  */
 vtrace_status vtrace_workspace_init(void* workspace, size_t workspace_bytes,
                                     vtrace_stream_t stream);
@@ -330,7 +335,9 @@ vtrace_status vtrace_gather_logits(
  *                   rounded up to 256, and 4 (H + 1) C per workgroup, C = 16 columns
  *                   or 32 from A = 16 on, at most 512 workgroups), is accepted and
  *                   gives those the slower split of four lanes a workgroup, whose
- *                   sums round in another order
+ *                   sums round in another order.  One smaller than
+ *                   vtrace_head_workspace_bytes serves this call alone, no other
+ *                   kind between
  * The products use bfloat16 inputs with float32 accumulation; G enters them as
  * a bfloat16 pair (high part + low part, 2^-17 relative), so d_hidden keeps
  * float32 accuracy.  d_weight, d_bias and the losses are reduced in a fixed

@@ -17,7 +17,8 @@
  * Conventions (device pointers, status codes, streams, no allocation, no
  * synchronisation) and layouts are those of vtrace.h.  Outputs must not alias
  * inputs or each other, except where stated.  Calls are re-entrant; concurrent
- * calls need distinct workspaces.  Repeated calls on the same inputs give
+ * calls need distinct workspaces, and calls in turn, of whatever kind, may share
+ * one (vtrace_workspace_bytes).  Repeated calls on the same inputs give
  * bit-identical results.  Every call may be captured into a HIP graph.
  */
 #ifndef VTRACE_TOKENS_H_

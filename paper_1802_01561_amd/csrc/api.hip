@@ -60,7 +60,7 @@ Kernel forced_kernel() {
 
 size_t workspace_bytes_for(int64_t B) {
   const int64_t max_wg = (B + vtrace::kMinLanesPerWorkgroup - 1) / vtrace::kMinLanesPerWorkgroup;
-  return vtrace::kWsHeaderBytes + 3 * sizeof(double) * static_cast<size_t>(max_wg);
+  return vtrace::kWsDataOffset + 3 * sizeof(double) * static_cast<size_t>(max_wg);
 }
 
 vtrace_status check_common(int64_t T, int64_t B, int64_t A, vtrace_dtype dt, const void* tl,
@@ -99,11 +99,11 @@ StepArgs make_args(int64_t T, int64_t B, int64_t A, const void* tl, const void* 
   return a;
 }
 
-void attach_workspace(StepArgs* a, void* ws) {
+void attach_workspace(StepArgs* a, void* ws, size_t data = vtrace::kWsDataOffset) {
   char* base = static_cast<char*>(ws);
   a->ticket = reinterpret_cast<unsigned int*>(base + vtrace::kWsTicketOffset);
   a->error_flag = reinterpret_cast<unsigned int*>(base + vtrace::kWsFlagOffset);
-  a->partials = reinterpret_cast<double*>(base + vtrace::kWsHeaderBytes);
+  a->partials = reinterpret_cast<double*>(base + data);
 }
 
 // Copies a caller's variant into the launch arguments.
@@ -185,9 +185,8 @@ vtrace_status loss_grad_args(int64_t T, int64_t B, int64_t A, vtrace_dtype logit
 // The workspace of vtrace_loss_grad_static: a device array of fixed size,
 // allocated with the library's code object (each device that runs the library
 // holds its own copy until the process ends), so that the call itself
-// allocates nothing.  Layout as a caller's workspace: the 256-byte header
-// (completion counter, error flag) and three float64 partials per workgroup,
-// at most one workgroup per lane.
+// allocates nothing.  Layout: the 256-byte header (completion counter, error flag)
+// and three float64 partials per workgroup, at most one workgroup per lane.
 constexpr size_t kStaticWorkspaceBytes =
     vtrace::kWsHeaderBytes + 3 * sizeof(double) * static_cast<size_t>(VTRACE_STATIC_MAX_LANES);
 static_assert(kStaticWorkspaceBytes == VTRACE_STATIC_WORKSPACE_BYTES, "header states the array's size");
@@ -373,7 +372,7 @@ vtrace_status vtrace_loss_grad_static(int64_t T, int64_t B, int64_t A, vtrace_dt
   void* ws = nullptr;
   st = static_workspace(as_hip(stream), &ws);
   if (st != VTRACE_OK) return st;
-  attach_workspace(&a, ws);
+  attach_workspace(&a, ws, vtrace::kWsHeaderBytes);
   a.error_flag = nullptr;  // nothing reads a flag in the shared array
   return launch(a, lt, Mode::LossGrad, as_hip(stream));
 }

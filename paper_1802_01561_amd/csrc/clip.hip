@@ -26,7 +26,6 @@ constexpr int kWaves = kThreads / kWave;
 // Elements of a chunk; short calls take smaller ones to have more workgroups.
 constexpr int kChunkBits = 14, kSmallChunkBits = 12;
 constexpr int64_t kSmallCall = int64_t(1) << 24;
-constexpr size_t kFactorOffset = 8;  // in the workspace's header, behind the counter and the error flag
 
 // Tensors of a launch: as many as 4 KB of arguments hold.
 template <bool kOut>
@@ -229,7 +228,7 @@ int64_t fill(const ClipItem* items, int64_t count, int64_t from, ClipTable<kOut>
 
 }  // namespace
 
-size_t clip_workspace_bytes() { return kWsHeaderBytes + kCounterBytes + kClipMostBlocks * sizeof(double); }
+size_t clip_workspace_bytes() { return kWsDataOffset + kClipMostBlocks * sizeof(double); }
 
 namespace {
 
@@ -242,9 +241,9 @@ hipError_t launch_pass(const ClipItem* items, int64_t count, int bits, unsigned 
   t.max_norm = max_norm;
   t.norm = norm;
   t.ticket = reinterpret_cast<unsigned int*>(base + kWsTicketOffset);
-  t.factor = reinterpret_cast<float*>(base + kFactorOffset);
+  t.factor = reinterpret_cast<float*>(base + kWsFactorOffset);
   t.counters = reinterpret_cast<unsigned int*>(base + kWsHeaderBytes);
-  t.partials = reinterpret_cast<double*>(base + kWsHeaderBytes + kCounterBytes);
+  t.partials = reinterpret_cast<double*>(base + kWsDataOffset);
   int64_t from = 0;
   do {
     const int64_t n = fill(items, count, from, &t);

@@ -83,6 +83,7 @@ size_t head_loss_bytes(int64_t nwg) {
   return (n + 255) / 256 * 256;
 }
 
+// With the data right behind the header.
 size_t head_bytes(int64_t nwg, int64_t A, int64_t H) {
   return kWsHeaderBytes + head_loss_bytes(nwg) +
          sizeof(float) * static_cast<size_t>(nwg) * static_cast<size_t>(H + 1) * static_cast<size_t>(head_columns(A));
@@ -99,18 +100,22 @@ bool prefer_split(int64_t T, int64_t B) { return T > 16 && B <= (T > 32 ? 512 : 
 
 }  // namespace
 
-size_t head_workspace_bytes(int64_t B, int64_t A, int64_t H) { return head_bytes(head_workgroups(B, true), A, H); }
+size_t head_workspace_bytes(int64_t B, int64_t A, int64_t H) {
+  return head_bytes(head_workgroups(B, true), A, H) + kWsCounterBytes;
+}
 size_t head_workspace_least_bytes(int64_t B, int64_t A, int64_t H) {
   return head_bytes(head_workgroups(B, false), A, H);
 }
 
 void head_attach_workspace(HeadArgs* a, void* ws, size_t bytes) {
-  a->split = prefer_split(a->T, a->B) && bytes >= head_workspace_bytes(a->B, a->A, a->H);
+  a->split = prefer_split(a->T, a->B) && bytes >= head_bytes(head_workgroups(a->B, true), a->A, a->H);
+  // A workspace without room for the other kinds' counters has none: it is this kind's alone.
+  const int64_t nwg = head_workgroups(a->B, a->split);
+  const size_t data = bytes >= head_bytes(nwg, a->A, a->H) + kWsCounterBytes ? kWsDataOffset : kWsHeaderBytes;
   char* base = static_cast<char*>(ws);
   a->error_flag = reinterpret_cast<unsigned int*>(base + kWsFlagOffset);
-  a->loss_partials = reinterpret_cast<double*>(base + kWsHeaderBytes);
-  a->grad_partials =
-      reinterpret_cast<float*>(base + kWsHeaderBytes + head_loss_bytes(head_workgroups(a->B, a->split)));
+  a->loss_partials = reinterpret_cast<double*>(base + data);
+  a->grad_partials = reinterpret_cast<float*>(base + data + head_loss_bytes(nwg));
 }
 
 hipError_t launch_head(const HeadArgs& a, hipStream_t st) {

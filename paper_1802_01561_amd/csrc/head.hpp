@@ -59,9 +59,9 @@ constexpr int64_t kHeadMaxActions = 31;
 constexpr int64_t kHeadMaxBatchTimesHidden = 0xFFFFF000LL / 64;
 bool head_hidden_supported(int64_t H);
 constexpr int kHeadLanes = 4;
-// Workspace of the fused kernel: the 256-byte header, then float64 loss
-// partials and float32 gradient partials per workgroup; enough for a workgroup
-// per lane, and the least a call accepts (a workgroup per four lanes).
+// Workspace of the fused kernel: the 256-byte header, the other kinds' counters, then
+// float64 loss partials and float32 gradient partials per workgroup; enough for a workgroup
+// per lane, and the least a call accepts (a workgroup per four lanes, no counters).
 size_t head_workspace_bytes(int64_t B, int64_t A, int64_t H);
 size_t head_workspace_least_bytes(int64_t B, int64_t A, int64_t H);
 // Sets the workspace pieces and, for a workspace of this size, `split`.

@@ -43,11 +43,18 @@ struct StepArgs {
   double* partials;  // [num_workgroups, 3]
 };
 
-// Workspace layout: a 256-byte header (completion counter, error flag) and then
-// three float64 partial sums per workgroup.
+// Workspace layout: a 256-byte header (completion counter, error flag, a call's own words),
+// the completion counters of the calls with many workgroups (tickets.hpp), and then a call's
+// data, three float64 partial sums per workgroup for the loss calls.  The counter of the
+// header and those behind it are zero between calls: no call has data there, so that one
+// buffer can serve calls of every kind in turn.
 constexpr size_t kWsHeaderBytes = 256;
 constexpr size_t kWsTicketOffset = 0;
 constexpr size_t kWsFlagOffset = 4;
+constexpr size_t kWsActiveCountOffset = 8, kWsSplitsOffset = 12;  // vocabulary layer
+constexpr size_t kWsFactorOffset = 16;                            // clipping
+constexpr size_t kWsCounterBytes = 4096;
+constexpr size_t kWsDataOffset = kWsHeaderBytes + kWsCounterBytes;
 // Every loss kernel covers at least this many lanes per workgroup, so the
 // partials array is sized by ceil(B / kMinLanesPerWorkgroup).  (Tiles of 256
 // steps and the row-split kernel hold a single lane per workgroup.)

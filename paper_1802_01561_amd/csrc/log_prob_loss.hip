@@ -319,7 +319,7 @@ size_t log_prob_workspace_bytes(int64_t T, int64_t B) {
   int64_t chunks, chunk_tiles, groups;
   split_time(T, B, &chunks, &chunk_tiles, &groups);
   const size_t composites = chunks > 1 ? static_cast<size_t>(chunks * B) * 2 * sizeof(double) : 0;
-  return kWsHeaderBytes + kCounterBytes + partial_bytes(groups * chunks) + composites;
+  return kWsDataOffset + partial_bytes(groups * chunks) + composites;
 }
 
 void attach_log_prob_workspace(LogProbArgs* a, void* ws) {
@@ -328,7 +328,7 @@ void attach_log_prob_workspace(LogProbArgs* a, void* ws) {
   char* const base = static_cast<char*>(ws);
   a->step.ticket = reinterpret_cast<unsigned int*>(base + kWsTicketOffset);
   a->counters = reinterpret_cast<unsigned int*>(base + kWsHeaderBytes);
-  char* const sums = base + kWsHeaderBytes + kCounterBytes;
+  char* const sums = base + kWsDataOffset;
   a->step.partials = reinterpret_cast<double*>(sums);
   a->composites = reinterpret_cast<double*>(sums + partial_bytes(groups * a->chunks));
 }

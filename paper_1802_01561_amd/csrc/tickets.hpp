@@ -9,7 +9,7 @@ namespace vtrace {
 // 10 us), so each of 32 counters, a 128-byte line apiece, takes a share of them, and the
 // workgroup that is the last of its counter draws the ticket.  All return to zero.
 constexpr int kCounters = 32, kCounterWords = 32;
-constexpr size_t kCounterBytes = kCounters * kCounterWords * sizeof(unsigned);
+static_assert(kCounters * kCounterWords * sizeof(unsigned) == kWsCounterBytes, "their place in a workspace");
 
 // True in every thread of the workgroup that is the last of the grid to get here; what the
 // thread 0 of each workgroup stored before (with device-scope atomic stores) is then there to

@@ -188,7 +188,7 @@ vtrace_status vtrace_clip_grad_norm(int64_t count, const void* const* gradients,
   if (!workspace) return VTRACE_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return VTRACE_ERR_ALIGN;
   if (workspace_bytes < vtrace::clip_workspace_bytes()) return VTRACE_ERR_WORKSPACE;
-  static_assert(VTRACE_CLIP_WORKSPACE_BYTES == 256 + 4096 + 8 * vtrace::kClipMostBlocks, "header states the size");
+  static_assert(VTRACE_CLIP_WORKSPACE_BYTES == vtrace::kWsDataOffset + 8 * vtrace::kClipMostBlocks, "header states the size");
   try {
     // What is read and what is written, to find outputs that overlap anything.
     struct Range {

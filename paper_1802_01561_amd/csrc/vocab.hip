@@ -336,13 +336,10 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a,
 int64_t round_up(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 unsigned blocks_of(int64_t n, int64_t k) { return static_cast<unsigned>((n + k - 1) / k); }
 
-// Behind the counter and the error flag.
-constexpr size_t kHeaderCountOffset = 8, kHeaderSplitsOffset = 12;
-
 // Pieces of a workspace, each on a 256-byte boundary.
 struct Carver {
   uintptr_t base;  // an integer: sizes are asked for without a workspace
-  size_t at = kWsHeaderBytes;
+  size_t at = kWsDataOffset;
   explicit Carver(void* ws) : base(reinterpret_cast<uintptr_t>(ws)) {}
   template <typename T>
   T* take(int64_t n) {
@@ -354,7 +351,7 @@ struct Carver {
 
 void header(VocabArgs* a, void* ws) {
   a->error_flag = reinterpret_cast<unsigned int*>(reinterpret_cast<uintptr_t>(ws) + kWsFlagOffset);
-  a->active_count = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderCountOffset);
+  a->active_count = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kWsActiveCountOffset);
 }
 
 size_t carve_log_probs(VocabArgs* a, const VocabPlan& p, void* ws) {
@@ -389,7 +386,7 @@ size_t carve_grad(VocabArgs* a, const VocabPlan& p, void* ws) {
   a->small_weight = p.small_weight;
   a->small_hidden = p.small_hidden;
   a->pieces = p.pieces;
-  a->splits = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kHeaderSplitsOffset);
+  a->splits = reinterpret_cast<int32_t*>(reinterpret_cast<uintptr_t>(ws) + kWsSplitsOffset);
   a->active = c.take<int32_t>(a->N);
   a->row_scalars = c.take<float4v>(p.row_pitch);
   a->row_tokens = c.take<int32_t>(p.row_pitch);
