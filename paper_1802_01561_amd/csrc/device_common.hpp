@@ -105,6 +105,17 @@ __device__ __forceinline__ StepWeights variant_weights(int correction, double rh
   return w;
 }
 
+// The product of two coefficients of composed steps x -> a x + b of the recursion.  Where it
+// overflows it is held at the largest finite value: the recursion multiplies by one coefficient
+// after the other, and what it multiplies may be 0 all along, where 0 * inf would be NaN.
+// (Anything else that a coefficient of 1e308 multiplies leaves float32's range all the same.)
+// An infinite coefficient itself stays one.
+__device__ __forceinline__ double coefficient_product(double a, double b) {
+  const double p = a * b;
+  if (__builtin_isinf(p) && !__builtin_isinf(a) && !__builtin_isinf(b)) return __builtin_copysign(__DBL_MAX__, p);
+  return p;
+}
+
 // Reward preprocessing of App. D (values of StepArgs::reward_transform).  NaN
 // stays NaN.
 constexpr int kRewardClip = 1, kRewardAsymmetric = 2;

@@ -41,7 +41,7 @@ struct Map {
   double a, b;  // x -> a x + b
 };
 __device__ __forceinline__ Map after(Map first, Map then) {  // first o then
-  return {first.a * then.a, fma(first.a, then.b, first.b)};
+  return {coefficient_product(first.a, then.a), fma(first.a, then.b, first.b)};
 }
 
 // Suffix composites over the threads of a lane (later threads hold later steps): of the
