@@ -82,18 +82,17 @@ __global__ __launch_bounds__(kListThreads) void vocab_list_kernel(VocabArgs a) {
   if (kGrad && threadIdx.x == 0) *a.splits = best_split(a, total, hidden_tile(a)).parts;
 }
 
-// A step's outputs from the joined statistics: sums of 2^d and of 2^d d, d = z log2 e - c.
+// A step's outputs from the joined statistics: sums of 2^d and of 2^d d, d = (z - c) log2 e.
 template <bool kDot>
 __device__ __forceinline__ void store_step(const VocabArgs& a, int64_t step, int64_t row, double c, double sum,
                                            double dot) {
   constexpr double kLn2 = 0.6931471805599453;
   const int32_t token = a.tokens[step];
   const double log_s = log(sum);
-  const double lse = log_s + c / static_cast<double>(kLog2eF);
   const bool valid = token >= 0 && token < a.V;
   if (!valid) raise_error_flag(a.error_flag);
-  a.log_sums[step] = static_cast<float>(lse);
-  a.log_probs[step] = valid ? static_cast<float>(static_cast<double>(a.token_logit[row]) - lse) : NAN;
+  a.log_sums[step] = static_cast<float>(c + log_s);
+  a.log_probs[step] = valid ? static_cast<float>(static_cast<double>(a.token_logit[row]) - c - log_s) : NAN;
   if constexpr (kDot) a.entropy[step] = static_cast<float>(log_s - kLn2 * (dot / sum));
 }
 template <bool kDot>
@@ -108,13 +107,11 @@ __device__ __forceinline__ void store_no_step(const VocabArgs& a, int64_t step) 
 template <bool kDot>
 __device__ __forceinline__ void add_piece(const VocabArgs& a, int64_t o, float c, double& sum, double& dot) {
   const float p = a.part_sum[o];
-  const float d = p == 0.0f ? 0.0f : a.part_max[o] - c;
-  const double e = static_cast<double>(__builtin_amdgcn_exp2f(d)) * static_cast<double>(p);
+  const double d = p == 0.0f ? 0.0 : (static_cast<double>(a.part_max[o]) - static_cast<double>(c)) * static_cast<double>(kLog2eF);
+  const double ratio = static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d)));
+  const double e = ratio * static_cast<double>(p);
   sum += e;
-  if constexpr (kDot) {
-    const double ratio = static_cast<double>(__builtin_amdgcn_exp2f(d));
-    dot += fma(e, static_cast<double>(d), ratio * static_cast<double>(a.part_dot[o]));
-  }
+  if constexpr (kDot) dot += fma(e, d, ratio * static_cast<double>(a.part_dot[o]));
 }
 __device__ __forceinline__ float piece_top(const VocabArgs& a, int64_t o) {
   return a.part_sum[o] == 0.0f ? -INFINITY : a.part_max[o];

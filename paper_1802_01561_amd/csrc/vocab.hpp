@@ -46,7 +46,7 @@ struct VocabArgs {
   int32_t* active;        // [N] the active steps
   // log_probs: statistics of vocabulary pieces, [pieces, row_pitch] each ([N, pieces] from
   // the kernel for few steps)
-  float* part_max;        // log2 units
+  float* part_max;
   float* part_sum;
   float* part_dot;        // or null
   float* token_logit;     // [row_pitch]

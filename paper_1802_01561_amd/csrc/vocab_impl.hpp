@@ -494,7 +494,10 @@ __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
 }
 // A token ruled out adds p log p = 0, not 0 * -inf.
 constexpr float kLeastLog = -1e30f;
-
+// A logit's exponent about another one, in log2 units.  The difference comes first: scaled
+// each for itself, logits near 1e10 (a finite mask's) round to hundreds of units off, and
+// 2^hundreds overflows.
+__device__ __forceinline__ float log2_ratio(float z, float about) { return (z - about) * kLog2eF; }
 
 // Tile number `id` of `wide` x `deep`: consecutive numbers share operands in an XCD's L2
 // (8 tiles along `wide`, then along `deep`).

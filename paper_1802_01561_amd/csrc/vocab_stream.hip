@@ -92,11 +92,11 @@ __global__ __launch_bounds__(kStreamThreads) void vocab_stream_kernel(VocabArgs 
         top = fmaxf(top, z[i]);
       }
       top = group_max(top);
-      const float c = top == -INFINITY ? 0.0f : top * kLog2eF;
+      const float c = top == -INFINITY ? 0.0f : top;
       float sum = 0.0f, dot = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float d = fmaf(z[i], kLog2eF, -c);
+        const float d = log2_ratio(z[i], c);
         const float e = __builtin_amdgcn_exp2f(d);
         sum += e;
         dot = fmaf(e, fmaxf(d, kLeastLog), dot);
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kStreamThreads) void vocab_stream_kernel(VocabArgs 
 #pragma unroll
       for (int r = 0; r < R; ++r) c = fmaxf(c, s_stat[0][r][row]);
       auto add = [&](float part_c, float part, float part_dot) {
-        const float d = part_c == -INFINITY ? 0.0f : part_c - c;
+        const float d = part_c == -INFINITY ? 0.0f : log2_ratio(part_c, c);
         const float e = __builtin_amdgcn_exp2f(d), p = part * e;
         run_sum += p;
         if constexpr (kDot) run_dot += fmaf(p, d, part_dot * e);
@@ -262,19 +262,19 @@ __global__ __launch_bounds__(kWaves* kWave, kPerCu* kWaves / 4) void vocab_narro
             a.token_logit[row] = acc[m][n][i];
         }
       top = group_max(top);
-      const float c = fmaxf(run_c[n], top == -INFINITY ? run_c[n] : top * kLog2eF), zero = c == -INFINITY ? 0.0f : c;
+      const float c = fmaxf(run_c[n], top), zero = c == -INFINITY ? 0.0f : c;
       float sum = 0.0f, dot = 0.0f;
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float d = fmaf(acc[m][n][i], kLog2eF, -zero);
+          const float d = log2_ratio(acc[m][n][i], zero);
           const float e = __builtin_amdgcn_exp2f(d);
           sum += e;
           if constexpr (kDot) dot = fmaf(e, fmaxf(d, kLeastLog), dot);
         }
       // The lane's sums so far, moved to the new maximum.
-      const float d = run_c[n] == -INFINITY ? 0.0f : run_c[n] - c;
+      const float d = run_c[n] == -INFINITY ? 0.0f : log2_ratio(run_c[n], c);
       const float e = __builtin_amdgcn_exp2f(d), p = run_sum[n] * e;
       if constexpr (kDot) run_dot[n] = fmaf(p, d, run_dot[n] * e) + dot;
       run_sum[n] = p + sum;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kWaves* kWave, kPerCu* kWaves / 4) void vocab_narro
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     const float* const p = s_stat + w * kRows + row;
-    const float d = p[0] == -INFINITY ? 0.0f : p[0] - c;
+    const float d = p[0] == -INFINITY ? 0.0f : log2_ratio(p[0], c);
     const float e = __builtin_amdgcn_exp2f(d), part = p[kWaves * kRows] * e;
     sum += part;
     dot += fmaf(part, d, p[2 * kWaves * kRows] * e);

@@ -4,11 +4,12 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 import paper_1802_01561_amd as vt
 from oracle import tokens as ot
 from test_gpu_log_prob_loss import PLAIN, _dev
-from test_gpu_vocab import U
+from test_gpu_vocab import U, _batch, _check_grad, _check_log_probs, _gpu, _grad_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +41,39 @@ def test_products_of_ratios_beyond_float64(T, B, c_bar, log_ratio, ends):
         got, ref = getattr(out, name).cpu().double().numpy(), getattr(o, name)
         # values of the first two steps: two ratios, each within 1e-9 of itself, and one rounding
         assert (np.abs(got - ref) <= (U + 1e-8) * np.abs(ref) + 1e-8 * (name == "losses") * T).all(), (name, got, ref)
+
+
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e15, -1e20, -1e30, -9e36])
+@pytest.mark.parametrize("N,V", [(3, 3000), (20, 40000), (48, 30011), (100, 20000), (200, 3000), (700, 9000)])
+def test_low_finite_biases_over_whole_pieces(N, V, mask):
+    """A bias of -1e30 rules tokens out as well as -inf does, where a whole stretch of the
+    vocabulary has it: beside allowed tokens its exponentials are 0."""
+    H = 72
+    x, w, b, tokens, d_lp, d_h = _batch(N + V, N, 1, H, V, bias=True, none=0.1)
+    b[V // 3:] = mask
+    b[:40] = mask
+    ruled_out = b == b[0]
+    tokens = torch.where(ruled_out[tokens.long().clamp(min=0)] & (tokens >= 0), 40 + tokens % (V // 3 - 40), tokens).int()
+    b64 = torch.where(ruled_out, torch.tensor(-math.inf), b)
+    args = _gpu(x, w, b, tokens)
+    _check_log_probs(x, w, b64, tokens, vt.vtrace_vocab_log_probs(*args))
+    plain = vt.vtrace_vocab_log_probs(*args, with_entropy=False)
+    _check_log_probs(x, w, b64, tokens, plain)
+    ls, ent = _grad_inputs(x, w, b64, tokens)
+    out = vt.vtrace_vocab_grad(*args, *_gpu(ls, ent, d_lp, d_h))
+    _check_grad(x, w, b64, tokens, d_lp, d_h, out, torch.float32)
+    assert not out.d_weight[ruled_out.cuda()].any()
+
+
+@pytest.mark.parametrize("offset", [-1e30, -1e10, 3e8, 1e30])
+@pytest.mark.parametrize("N,V", [(3, 3000), (48, 30011), (100, 20000), (200, 3000)])
+def test_a_large_bias_common_to_all_tokens(N, V, offset):
+    """What is left of the logits beside it is float32's rounding of their sum: equal logits."""
+    H = 72
+    x, w, _, tokens, _, _ = _batch(N + V, N, 1, H, V)
+    x[:] = 0
+    out = vt.vtrace_vocab_log_probs(*_gpu(x, w, torch.full((V,), offset), tokens))
+    # sums of equal terms: 64 roundings of the log-sum's argument, as in the other tests
+    for got in (out.log_probs, -out.entropy):
+        assert ((got.double() + math.log(V)).abs() <= U * (64.0 + 2.0 * math.log(V))).all()
+    assert (out.log_sums.double() - np.float32(offset)).abs().max() <= 2.0 * U * abs(offset)
