@@ -336,18 +336,18 @@ def vtrace_clip_grad_norm(gradients: Sequence[torch.Tensor], max_norm: Optional[
     if max_norm is None and out is not None:
         raise ValueError("out needs max_norm")
     first = gradients[0]
+    outs = gradients if out is None else list(out)  # once: an iterator has nothing left for the second way in
     if stream is None and type(workspace) is ClipWorkspace:
         fast = _fast_call(first)
         if fast:
             device = fast.device()
-            r = fast.call_clip(fast.clip, gradients, gradients if out is None else list(out), max_norm is not None,
-                               max_norm, norm, workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            r = fast.call_clip(fast.clip, gradients, outs, max_norm is not None, max_norm, norm, workspace.tensor,
+                               workspace.nbytes, device, fast.stream(device))
             if r is not None:
                 return _outputs(r)[0]
     if not isinstance(first, torch.Tensor):
         raise TypeError("gradients must be torch.Tensors")
     dev = first.device
-    outs = gradients if out is None else list(out)
     if len(outs) != len(gradients):
         raise ValueError(f"{len(outs)} outputs for {len(gradients)} gradients")
     n = len(gradients)

@@ -77,3 +77,14 @@ def test_a_large_bias_common_to_all_tokens(N, V, offset):
     for got in (out.log_probs, -out.entropy):
         assert ((got.double() + math.log(V)).abs() <= U * (64.0 + 2.0 * math.log(V))).all()
     assert (out.log_sums.double() - np.float32(offset)).abs().max() <= 2.0 * U * abs(offset)
+
+
+def test_clipped_into_an_iterator():
+    """``out`` may be any iterable, by either way of marshalling."""
+    g = [torch.ones(4, device="cuda"), torch.ones(12, device="cuda").bfloat16()]
+    marked = torch.ones(0, device="cuda").as_subclass(type("Marked", (torch.Tensor,), {}))  # which native code declines
+    for extra in ([], [marked]):
+        for kw in (dict(workspace=vt.ClipWorkspace()), dict()):
+            out = [torch.zeros_like(t) for t in g]
+            norm = vt.vtrace_clip_grad_norm(iter([*g, *extra]), 1.0, out=(t for t in [*out, *extra]), **kw)
+            assert float(norm) == 4.0 and all((t == 0.25).all() for t in out)
