@@ -446,8 +446,9 @@ VocabPlan plan_vocab_log_probs(int64_t N, int64_t V, int64_t H) {
       const int64_t tiles = (V + p.tile_tokens - 1) / p.tile_tokens;
       p.pieces = tiles < slots ? tiles : slots;
     } else {
-      // Tokens of a workgroup: as many as leave about a workgroup or two a CU.
-      p.tile_tokens = V >= 64 * 2 * kCus ? 64 : V >= 24 * kCus ? 32 : 16;
+      // Tokens of a workgroup: as many as leave about a workgroup or two a CU (64 of them with
+      // more than 32 steps would not fit the registers).
+      p.tile_tokens = V >= 64 * 2 * kCus && N <= 32 ? 64 : V >= 24 * kCus ? 32 : 16;
       const int64_t tiles = (V + p.tile_tokens - 1) / p.tile_tokens;
       p.pieces = tiles < 4 * kCus ? tiles : 4 * kCus;
     }

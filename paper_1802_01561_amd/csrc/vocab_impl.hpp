@@ -485,9 +485,7 @@ __device__ __forceinline__ float group_sum(float x) {
 // so low that the logit's scaling could overflow, the token is ruled out.  (A buffer without
 // a bias is empty and reads 0.)
 constexpr float kRuledOut = -1e37f;
-template <bool kBias = true>
 __device__ __forceinline__ float start_of_logit(const VocabArgs& a, int64_t v) {
-  if constexpr (!kBias) return v >= a.V ? -INFINITY : 0.0f;
   const Rsrc bias = make_rsrc(a.bias, a.bias ? a.V * 4 : 0);
   const float b = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bias, static_cast<uint32_t>(v) * 4, 0, 0));
   return v >= a.V || b < kRuledOut ? -INFINITY : b;

@@ -316,39 +316,42 @@ __global__ __launch_bounds__(kWaves* kWave, kPerCu* kWaves / 4) void vocab_narro
   if constexpr (kDot) a.part_dot[o] = dot;
 }
 
+// A plan that a kernel does not cover (its steps would be left without statistics) is refused.
 template <int R, int NT, bool kDot>
-void launch_stream(const VocabArgs& a, hipStream_t st) {
+hipError_t launch_stream(const VocabArgs& a, hipStream_t st) {
+  if (a.N > 16 * NT || a.tile_tokens != 16 * R) return hipErrorInvalidValue;
   hipLaunchKernelGGL((vocab_stream_kernel<R, NT, kDot>), dim3(static_cast<unsigned>(a.pieces)), dim3(kStreamThreads), 0,
                      st, a);
+  return hipGetLastError();
 }
 template <int R, bool kDot>
-void launch_stream_rows(const VocabArgs& a, hipStream_t st) {
-  if (a.N <= 16) launch_stream<R, 1, kDot>(a, st);
-  else if (a.N <= 32 || R == 4) launch_stream<R, 2, kDot>(a, st);  // more steps of so many tokens are narrow
-  else if constexpr (R < 4) launch_stream<R, 4, kDot>(a, st);
+hipError_t launch_stream_rows(const VocabArgs& a, hipStream_t st) {
+  if (a.N <= 16) return launch_stream<R, 1, kDot>(a, st);
+  if constexpr (R == 4) return launch_stream<R, 2, kDot>(a, st);
+  else return a.N <= 32 ? launch_stream<R, 2, kDot>(a, st) : launch_stream<R, 4, kDot>(a, st);
 }
 template <int kRows, int kWaves, int kPerCu, bool kDot>
-void launch_narrow(const VocabArgs& a, hipStream_t st) {
+hipError_t launch_narrow(const VocabArgs& a, hipStream_t st) {
+  if (a.N > kRows || a.tile_tokens > 32 * kWaves) return hipErrorInvalidValue;
   hipLaunchKernelGGL((vocab_narrow_kernel<kRows, kWaves, kPerCu, kDot>), dim3(static_cast<unsigned>(a.pieces)),
                      dim3(kWaves * kWave), 0, st, a);
+  return hipGetLastError();
 }
 template <bool kDot>
-void launch(const VocabArgs& a, hipStream_t st) {
-  if (a.narrow && a.N <= 32 && a.narrow_per_cu == 1) launch_narrow<32, 4, 1, kDot>(a, st);
-  else if (a.narrow && a.N <= 32) launch_narrow<32, 4, 2, kDot>(a, st);
-  else if (a.narrow && a.N <= 64) launch_narrow<64, 4, 2, kDot>(a, st);
-  else if (a.narrow) launch_narrow<128, 8, 1, kDot>(a, st);
-  else if (a.tile_tokens == 64) launch_stream_rows<4, kDot>(a, st);
-  else if (a.tile_tokens == 32) launch_stream_rows<2, kDot>(a, st);
-  else launch_stream_rows<1, kDot>(a, st);
+hipError_t launch(const VocabArgs& a, hipStream_t st) {
+  if (a.narrow && a.N <= 32 && a.narrow_per_cu == 1) return launch_narrow<32, 4, 1, kDot>(a, st);
+  if (a.narrow && a.N <= 32) return launch_narrow<32, 4, 2, kDot>(a, st);
+  if (a.narrow && a.N <= 64) return launch_narrow<64, 4, 2, kDot>(a, st);
+  if (a.narrow) return launch_narrow<128, 8, 1, kDot>(a, st);
+  if (a.tile_tokens == 64) return launch_stream_rows<4, kDot>(a, st);
+  if (a.tile_tokens == 32) return launch_stream_rows<2, kDot>(a, st);
+  return launch_stream_rows<1, kDot>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_vocab_few(const VocabArgs& a, hipStream_t st) {
-  if (a.entropy) launch<true>(a, st);
-  else launch<false>(a, st);
-  return hipGetLastError();
+  return a.entropy ? launch<true>(a, st) : launch<false>(a, st);
 }
 
 }  // namespace vtrace
