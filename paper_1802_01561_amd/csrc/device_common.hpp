@@ -105,15 +105,22 @@ __device__ __forceinline__ StepWeights variant_weights(int correction, double rh
   return w;
 }
 
-// The product of two coefficients of composed steps x -> a x + b of the recursion.  Where it
-// overflows it is held at the largest finite value: the recursion multiplies by one coefficient
-// after the other, and what it multiplies may be 0 all along, where 0 * inf would be NaN.
-// (Anything else that a coefficient of 1e308 multiplies leaves float32's range all the same.)
-// An infinite coefficient itself stays one.
+// The product of two coefficients (from 0 on) of composed steps x -> a x + b of the recursion.
+// Where it overflows it is held at the largest finite value: the recursion multiplies by one
+// coefficient after the other, and what it multiplies may be 0 all along, where 0 * inf would be
+// NaN.  (Anything else that a coefficient of 1e308 multiplies leaves float32's range all the
+// same.)  Coefficients that are infinite or NaN themselves multiply as they are.  On the upper
+// words, three instructions without a branch: T = 1000, B = 512, A = 18 39.8 us, with a comparison
+// and a branch in their place 41.4, unchecked 39.1.
 __device__ __forceinline__ double coefficient_product(double a, double b) {
+  constexpr int kLargest = 0x7fefffff;  // the upper word of the largest finite value
+  auto upper = [](double x) { return static_cast<int>(static_cast<unsigned long long>(__double_as_longlong(x)) >> 32); };
   const double p = a * b;
-  if (__builtin_isinf(p) && !__builtin_isinf(a) && !__builtin_isinf(b)) return __builtin_copysign(__DBL_MAX__, p);
-  return p;
+  const int in = upper(a) > upper(b) ? upper(a) : upper(b);
+  const int most = (in > kLargest ? in : kLargest) | 0xfffff;  // with an infinity or a NaN: beyond any
+  const int hi = upper(p) < most ? upper(p) : most;
+  const unsigned long long lo = static_cast<unsigned long long>(__double_as_longlong(p)) & 0xffffffffu;
+  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(hi)) << 32 | lo));
 }
 
 // Reward preprocessing of App. D (values of StepArgs::reward_transform).  NaN

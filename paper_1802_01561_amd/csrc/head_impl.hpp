@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kHeadThreads, 2) void head_kernel(HeadArgs a) {
         const double Dn = dpp_f64<0x100 + off>(D);
         if (s + off < kL) {
           D = fma(Gs, Dn, D);
-          Gs = Gs * Gn;
+          Gs = coefficient_product(Gs, Gn);
         }
       });
       double entering = 0.0;  // kSplit: v - V(x) at the later wave's first step

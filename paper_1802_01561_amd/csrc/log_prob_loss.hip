@@ -40,8 +40,15 @@ constexpr uint32_t kOutOfRange = 0x80000000u;
 struct Map {
   double a, b;  // x -> a x + b
 };
+// coefficient_product with a branch, of either sign: here, where registers are short, the
+// cheaper form (T = 1000, B = 8192 113 us, without a branch 118, unchecked 111).
+__device__ __forceinline__ double product(double a, double b) {
+  const double p = a * b;
+  if (__builtin_isinf(p) && !__builtin_isinf(a) && !__builtin_isinf(b)) return __builtin_copysign(__DBL_MAX__, p);
+  return p;
+}
 __device__ __forceinline__ Map after(Map first, Map then) {  // first o then
-  return {coefficient_product(first.a, then.a), fma(first.a, then.b, first.b)};
+  return {product(first.a, then.a), fma(first.a, then.b, first.b)};
 }
 
 // Suffix composites over the threads of a lane (later threads hold later steps): of the

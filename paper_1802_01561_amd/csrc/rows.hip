@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kRowsThreads, K == 2 ? 3 : 2) void rows_kernel(Step
         const double Dn = dpp_f64<0x100 + off>(D);
         if (s % kDppRow + off < kDppRow) {
           D = fma(Gs, Dn, D);
-          Gs = Gs * Gn;
+          Gs = coefficient_product(Gs, Gn);
         }
       });
       if constexpr (L == 64) {  // the DPP rows, last to first

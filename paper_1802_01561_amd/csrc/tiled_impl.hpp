@@ -514,7 +514,7 @@ __device__ __forceinline__ void chunk_walk(const StepArgs& a, v4u* lds, int64_t 
       const double Dn = dpp_f64<0x100 + off>(D);
       if (sr + off < kSeg) {
         D = fma(G, Dn, D);
-        G = G * Gn;
+        G = coefficient_product(G, Gn);
       }
     });
     double D16 = 0.0;  // L = 32: v - V(x) at step 16 of the lane
@@ -535,9 +535,9 @@ __device__ __forceinline__ void chunk_walk(const StepArgs& a, v4u* lds, int64_t 
       const double Dr = wl < 16 ? D16w : wl < 32 ? D32 : D48;
       if (wl < 48) D = fma(G, Dr, D);
       if constexpr (L > kWave) {
-        const double Gr2 = G32 * G48, Gr1 = G16 * Gr2;
+        const double Gr2 = coefficient_product(G32, G48), Gr1 = coefficient_product(G16, Gr2);
         const double Gr = wl < 16 ? Gr1 : wl < 32 ? Gr2 : G48;
-        if (wl < 48) G *= Gr;
+        if (wl < 48) G = coefficient_product(G, Gr);
         constexpr int W = S::LANE_WAVES;
         const int w_lane = (tid / kWave) % W;  // this wave's place in its lane
         WaveMap* const lane_maps = maps + lane_local * W;
