@@ -79,7 +79,7 @@ typedef enum {
   VTRACE_ERR_DTYPE = 3,     /* unknown logits dtype */
   VTRACE_ERR_PARAM = 4,     /* NaN or out-of-range scalar parameter */
   VTRACE_ERR_ALIGN = 5,     /* a base pointer breaks the alignment rule above */
-  VTRACE_ERR_WORKSPACE = 6, /* workspace NULL or smaller than vtrace_workspace_bytes */
+  VTRACE_ERR_WORKSPACE = 6, /* workspace NULL or smaller than the call's vtrace_*_workspace_bytes */
   VTRACE_ERR_HIP = 7        /* the HIP runtime rejected the launch */
 } vtrace_status;
 

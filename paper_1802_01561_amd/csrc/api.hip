@@ -235,16 +235,18 @@ const char* vtrace_status_string(int32_t status) {
     case VTRACE_ERR_NULL: return "a required pointer is NULL";
     case VTRACE_ERR_SHAPE:
       return "T, B and A must be >= 1 and T*B*A within vtrace_max_elements(); the fused output "
-             "layer also needs A <= 31 and H in {64, 128, 256}";
+             "layer also needs A <= 31 and H in {64, 128, 256}; vtrace_tokens.h has the ranges of the "
+             "token-policy calls";
     case VTRACE_ERR_DTYPE: return "unknown logits dtype";
     case VTRACE_ERR_PARAM:
       return "bad parameter: rho_bar, c_bar must be >= 0 (inf allowed), lambda in [0,1], "
              "costs finite, none NaN; a variant needs a known correction and Q estimate and, "
-             "for epsilon-correction, a finite epsilon > 0";
+             "for epsilon-correction, a finite epsilon > 0; max_norm must be >= 0, and a clipped "
+             "gradient may overlap nothing but its own input";
     case VTRACE_ERR_ALIGN:
       return "misaligned pointer: logits/d_logits/gathered/hidden/d_hidden need 16 bytes, "
              "others their element size";
-    case VTRACE_ERR_WORKSPACE: return "workspace missing or smaller than vtrace_workspace_bytes()";
+    case VTRACE_ERR_WORKSPACE: return "workspace missing or smaller than the call's vtrace_*_workspace_bytes()";
     case VTRACE_ERR_HIP: return "the HIP runtime rejected the kernel launch";
   }
   return "unknown status";

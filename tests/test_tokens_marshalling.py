@@ -5,6 +5,7 @@ import torch
 
 import paper_1802_01561_amd as vt
 from paper_1802_01561_amd import tokens
+from paper_1802_01561_amd._lib import lib
 
 
 def test_outputs_are_taken_from_an_iterator_once(monkeypatch):
@@ -24,3 +25,10 @@ def test_outputs_are_taken_from_an_iterator_once(monkeypatch):
     with pytest.raises(ValueError, match="GPU"):  # past the count of the outputs
         vt.vtrace_clip_grad_norm(iter(g), 1.0, out=(t.clone() for t in g), workspace=workspace)
     assert [len(part) for part in seen[0]] == [2, 2]
+
+
+def test_error_texts_cover_the_token_calls():
+    L = lib()
+    assert b"vtrace_tokens.h" in L.vtrace_status_string(2)
+    assert b"max_norm" in L.vtrace_status_string(4)
+    assert b"vtrace_*_workspace_bytes" in L.vtrace_status_string(6)
