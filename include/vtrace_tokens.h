@@ -57,9 +57,10 @@ extern "C" {
  *   workspace      vtrace_vocab_workspace_bytes(T,B,V,H) bytes, 16-byte aligned,
  *                  cleared once by vtrace_workspace_init
  * Numerics: bfloat16 products accumulated in float32 from the bias, exponentials
- * in float32, their sums in float32 over the tokens that one wave (or, up to 128
- * steps, one workgroup: V / 256 tokens or more) takes and joined in float64.  Any
- * other token makes that step's log_probs NaN and raises the workspace's flag
+ * in float32 of differences to the largest logit of a piece, their sums in float32
+ * over the piece and joined in float64.  A piece is the 64 or 128 tokens of one
+ * wave, or, up to 128 steps, the tokens of one workgroup: V / 1024 to V / 256, at
+ * least 16.  Any other token makes that step's log_probs NaN and raises the workspace's flag
  * (vtrace_error_flag).  A step whose tokens are all ruled out has log_sums
  * -INFINITY and NaN elsewhere; NaN and Inf inputs are propagated, also from the
  * row of a token that is ruled out (0 * NaN): such rows have to hold numbers.
@@ -86,10 +87,13 @@ vtrace_status vtrace_vocab_log_probs(
  *                       (entropy is then not read and may be NULL)
  *   grad_dtype          VTRACE_F32 or VTRACE_BF16; d_hidden, d_weight 16-byte aligned
  *   workspace           vtrace_vocab_grad_workspace_bytes(T,B,V,H,grad_dtype) bytes
- * Everything else as above.  G enters its two products as bfloat16, like a
- * bfloat16 gradient (2^-9 a term), for bfloat16 outputs, and as a bfloat16 pair
- * (high + low part, 2^-18 a term) for float32 ones; sums over steps and tokens are
- * float32 (d_bias: 64 or 128 steps, then float64).  A token that is neither in
+ * Everything else as above.  grad_dtype is also the choice of how G enters its two
+ * products: as one bfloat16 (2^-8 a term) for bfloat16 outputs, and as a bfloat16
+ * pair (high + low part, 2^-17 a term) for float32 ones; sums over steps and tokens
+ * are float32 (d_bias: 64 or 128 steps, then float64).  With few steps nothing
+ * averages G's rounding out, and a bfloat16 output has two.  pi_v is
+ * exp(z - log_sums): the float32 rounding of a log-sum of magnitude M, M 2^-24,
+ * is pi's relative error.  A token that is neither in
  * the vocabulary nor VTRACE_NO_TOKEN makes that step's G NaN, and with it
  * d_weight and d_bias.
  */

@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabArgs 
   }
 }
 
-// d_bias of one piece: the sums of 128 steps each, in order.
+// d_bias of one piece: the sums of 64 or 128 steps each, in order.
 __global__ __launch_bounds__(kFinishThreads) void vocab_bias_kernel(VocabArgs a, int64_t v_begin) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kFinishThreads + threadIdx.x;
   if (i >= a.g_pitch || v_begin + i >= a.V) return;

@@ -2,7 +2,7 @@
 //   d_weight[v, h] = sum_n G[n, v] x[n, h],   d_hidden[n, h] += sum_v G[n, v] weight[v, h].
 // In both, m runs along h, so that a lane holds four consecutive elements of a row of
 // the result.  G's low parts, where there are any, are a second pass over k: G = high + low
-// to 2^-18 of itself, for outputs whose own rounding is 2^-24.
+// to 2^-17 of itself (half a step of bfloat16 twice), for float32 outputs.
 //
 // Measured: 4096 steps, H = 4096, V = 131072, bfloat16, in eight pieces (4.4 TFLOP each)
 // d_weight 3.31 ms, 1.33 PFLOP/s, d_hidden 3.22 ms, 1.37.
