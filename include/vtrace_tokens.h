@@ -93,9 +93,9 @@ vtrace_status vtrace_vocab_log_probs(
  * are float32 (d_bias: 64 or 128 steps, then float64).  With few steps nothing
  * averages G's rounding out, and a bfloat16 output has two.  pi_v is
  * exp(z - log_sums): the float32 rounding of a log-sum of magnitude M, M 2^-24,
- * is pi's relative error.  A token that is neither in
- * the vocabulary nor VTRACE_NO_TOKEN makes that step's G NaN, and with it
- * d_weight and d_bias.
+ * is pi's relative error.  A G below 2^-126 may count as 0.  A token that is
+ * neither in the vocabulary nor VTRACE_NO_TOKEN makes that step's G NaN, and with
+ * it d_weight and d_bias.
  */
 size_t vtrace_vocab_grad_workspace_bytes(int64_t T, int64_t B, int64_t V, int64_t H,
                                          vtrace_dtype grad_dtype);
