@@ -85,187 +85,187 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void vocab_lo
   if (job.steps > 0) job.copy(lds, wave);
   fetch();
   while (tiles.any()) {
-  const int64_t n0 = static_cast<int64_t>(at.wide) * kSize;
-  const int64_t vt = static_cast<int64_t>(at.deep) * kSize;  // in this launch's piece
-  const int64_t v0 = v_begin + vt;                           // in the vocabulary
-  const int tile_deep = at.deep;
-  // What follows from the lane's number is formed in each tile: kept from tile to tile it
-  // would take the registers that the contraction needs.
-  int here = lane;
-  asm volatile("" : "+v"(here));
-  const int s = here % 16, g = here / 16;
-  // Accumulator (m, n) of lane (s, g) holds tokens 8 g + token_at(m, 0..3) of step 16 n + s;
-  // it starts as start_of_logit.
-  const int64_t first = v0 + wm;
-  const int own = static_cast<int>(a.V - first < kSize ? a.V - first : kSize) - 8 * g;
-  // Two of each: a wave may be in its next tile while another ends this one.
-  turn ^= kSize;
-  if (static_cast<int>(threadIdx.x) < kSize) {
-    s_tokens[turn + threadIdx.x] = token;
-    if constexpr (kMode >= kGrad) s_scalars[turn + threadIdx.x] = scalars;
-    if constexpr (kBias) s_starts[turn + threadIdx.x] = start_at;
-  }
-  if constexpr (kBias) {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  }
-  Accumulators<kSize> acc;
-#pragma unroll
-  for (int m = 0; m < kMT; ++m) {
-    f32x4 b;
-    if constexpr (kBias) {
-      b = *reinterpret_cast<const f32x4*>(s_starts + turn + wm + 8 * g + token_at(m, 0));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = token_at(m, i) >= own ? -INFINITY : 0.0f;
+    const int64_t n0 = static_cast<int64_t>(at.wide) * kSize;
+    const int64_t vt = static_cast<int64_t>(at.deep) * kSize;  // in this launch's piece
+    const int64_t v0 = v_begin + vt;                           // in the vocabulary
+    const int tile_deep = at.deep;
+    // What follows from the lane's number is formed in each tile: kept from tile to tile it
+    // would take the registers that the contraction needs.
+    int here = lane;
+    asm volatile("" : "+v"(here));
+    const int s = here % 16, g = here / 16;
+    // Accumulator (m, n) of lane (s, g) holds tokens 8 g + token_at(m, 0..3) of step 16 n + s;
+    // it starts as start_of_logit.
+    const int64_t first = v0 + wm;
+    const int own = static_cast<int>(a.V - first < kSize ? a.V - first : kSize) - 8 * g;
+    // Two of each: a wave may be in its next tile while another ends this one.
+    turn ^= kSize;
+    if (static_cast<int>(threadIdx.x) < kSize) {
+      s_tokens[turn + threadIdx.x] = token;
+      if constexpr (kMode >= kGrad) s_scalars[turn + threadIdx.x] = scalars;
+      if constexpr (kBias) s_starts[turn + threadIdx.x] = start_at;
     }
+    if constexpr (kBias) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    Accumulators<kSize> acc;
 #pragma unroll
-    for (int n = 0; n < kNT; ++n) acc[m][n] = b;
-  }
-  contract<false>(job, lds, parity, wave, lane, acc, [&] {
-    tiles.next();
-    start();
-  });
-  fetch();
-  __builtin_amdgcn_sched_barrier(0);
-
-  // A step's token, counted from this lane's first (what token_at gives, where it has it).
-  auto taken_of = [&](int32_t token) {
-    return token < 0 || token < first || token >= first + kWaveM ? -1 : static_cast<int>(token - first) - 8 * g;
-  };
-  if constexpr (kMode < kGrad) {
-    const int64_t piece = tile_deep * 2 + wave % 2;
+    for (int m = 0; m < kMT; ++m) {
+      f32x4 b;
+      if constexpr (kBias) {
+        b = *reinterpret_cast<const f32x4*>(s_starts + turn + wm + 8 * g + token_at(m, 0));
+      } else {
 #pragma unroll
-    for (int n = 0; n < kNT; ++n) {
-      const int64_t row = n0 + wn + 16 * n + s;
-      const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
-      float z[kMT][4];
-      float top = -INFINITY;
-#pragma unroll
-      for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          z[m][i] = element(acc[m][n], i);
-          top = fmaxf(top, z[m][i]);
-        }
-      top = group_max(top);
-      const float c = top == -INFINITY ? 0.0f : top;
-      float sum = 0.0f, dot = 0.0f;
-#pragma unroll
-      for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float d = log2_ratio(z[m][i], c);
-          const float e = __builtin_amdgcn_exp2f(d);
-          sum += e;
-          if constexpr (kMode == kStatsDot) dot = fmaf(e, fmaxf(d, kLeastLog), dot);
-        }
-      sum = group_sum(sum);
-      if constexpr (kMode == kStatsDot) dot = group_sum(dot);
-      if (g == 0) {
-        const int64_t o = piece * a.row_pitch + row;
-        a.part_max[o] = c;
-        a.part_sum[o] = sum;
-        if constexpr (kMode == kStatsDot) a.part_dot[o] = dot;
+        for (int i = 0; i < 4; ++i) b[i] = token_at(m, i) >= own ? -INFINITY : 0.0f;
       }
-      // The taken token's logit, where this lane holds it.
-      if (__any(taken >= 0)) {
-        float logit = 0.0f;
-        bool mine = false;
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) acc[m][n] = b;
+    }
+    contract<false>(job, lds, parity, wave, lane, acc, [&] {
+      tiles.next();
+      start();
+    });
+    fetch();
+    __builtin_amdgcn_sched_barrier(0);
+
+    // A step's token, counted from this lane's first (what token_at gives, where it has it).
+    auto taken_of = [&](int32_t token) {
+      return token < 0 || token < first || token >= first + kWaveM ? -1 : static_cast<int>(token - first) - 8 * g;
+    };
+    if constexpr (kMode < kGrad) {
+      const int64_t piece = tile_deep * 2 + wave % 2;
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) {
+        const int64_t row = n0 + wn + 16 * n + s;
+        const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
+        float z[kMT][4];
+        float top = -INFINITY;
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            logit = taken == token_at(m, i) ? z[m][i] : logit;
-            mine |= taken == token_at(m, i);
+            z[m][i] = element(acc[m][n], i);
+            top = fmaxf(top, z[m][i]);
           }
-        if (mine) a.token_logit[row] = logit;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  } else {
-    const int64_t P = a.row_pitch;
-    float col[kMT][4];
-    if constexpr (kBias) {
-#pragma unroll
-      for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) col[m][i] = 0.0f;
-    }
-#pragma unroll
-    for (int n = 0; n < kNT; ++n) {
-      const int64_t row = n0 + wn + 16 * n + s;
-      // G = p (c0 + c1 log2 p) + d_lp 1[v = a] with p = 2^(z log2 e - l2): see the gather kernel.
-      const float4v scalars = s_scalars[turn + wn + 16 * n + s];
-      const float l2 = scalars[0], c0 = scalars[1], c1 = scalars[2], d_lp = scalars[3];
-      const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
-      float grad[kMT][4];
-#pragma unroll
-      for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float d = fmaf(element(acc[m][n], i), kLog2eF, -l2);
-          const float p = __builtin_amdgcn_exp2f(d);
-          grad[m][i] = kMode == kGradDot ? p * fmaf(c1, fmaxf(d, kLeastLog), c0) : p * c0;
-        }
-      if (__any(taken >= 0)) {
+        top = group_max(top);
+        const float c = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f, dot = 0.0f;
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) grad[m][i] += taken == token_at(m, i) ? d_lp : 0.0f;
+          for (int i = 0; i < 4; ++i) {
+            const float d = log2_ratio(z[m][i], c);
+            const float e = __builtin_amdgcn_exp2f(d);
+            sum += e;
+            if constexpr (kMode == kStatsDot) dot = fmaf(e, fmaxf(d, kLeastLog), dot);
+          }
+        sum = group_sum(sum);
+        if constexpr (kMode == kStatsDot) dot = group_sum(dot);
+        if (g == 0) {
+          const int64_t o = piece * a.row_pitch + row;
+          a.part_max[o] = c;
+          a.part_sum[o] = sum;
+          if constexpr (kMode == kStatsDot) a.part_dot[o] = dot;
+        }
+        // The taken token's logit, where this lane holds it.
+        if (__any(taken >= 0)) {
+          float logit = 0.0f;
+          bool mine = false;
+#pragma unroll
+          for (int m = 0; m < kMT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              logit = taken == token_at(m, i) ? z[m][i] : logit;
+              mine |= taken == token_at(m, i);
+            }
+          if (mine) a.token_logit[row] = logit;
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    } else {
+      const int64_t P = a.row_pitch;
+      float col[kMT][4];
       if constexpr (kBias) {
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            col[m][i] += grad[m][i];
-            asm volatile("" : "+v"(col[m][i]));  // here, not later: it would have to keep what it adds
-          }
+          for (int i = 0; i < 4; ++i) col[m][i] = 0.0f;
       }
-      uint16_t* out = a.g + row * a.g_pitch + vt + wm + 8 * g;
-      uint16_t* out_low = out + P * a.g_pitch;
 #pragma unroll
-      for (int p = 0; p < kMT / 2; ++p) {
-        const float* const x = grad[2 * p];
-        const float* const y = grad[2 * p + 1];
-        v4u hi;
-        hi.x = pack_bf16x2(x[0], x[1]);
-        hi.y = pack_bf16x2(x[2], x[3]);
-        hi.z = pack_bf16x2(y[0], y[1]);
-        hi.w = pack_bf16x2(y[2], y[3]);
-        *reinterpret_cast<v4u*>(out + 32 * p) = hi;
-        if (!a.grad_bf16) {
-          auto low = [](float f0, float f1, unsigned h) {
-            return pack_bf16x2(f0 - __uint_as_float(h << 16), f1 - __uint_as_float(h & 0xffff0000u));
-          };
-          v4u lo;
-          lo.x = low(x[0], x[1], hi.x);
-          lo.y = low(x[2], x[3], hi.y);
-          lo.z = low(y[0], y[1], hi.z);
-          lo.w = low(y[2], y[3], hi.w);
-          *reinterpret_cast<v4u*>(out_low + 32 * p) = lo;
+      for (int n = 0; n < kNT; ++n) {
+        const int64_t row = n0 + wn + 16 * n + s;
+        // G = p (c0 + c1 log2 p) + d_lp 1[v = a] with p = 2^(z log2 e - l2): see the gather kernel.
+        const float4v scalars = s_scalars[turn + wn + 16 * n + s];
+        const float l2 = scalars[0], c0 = scalars[1], c1 = scalars[2], d_lp = scalars[3];
+        const int taken = taken_of(s_tokens[turn + wn + 16 * n + s]);
+        float grad[kMT][4];
+#pragma unroll
+        for (int m = 0; m < kMT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float d = fmaf(element(acc[m][n], i), kLog2eF, -l2);
+            const float p = __builtin_amdgcn_exp2f(d);
+            grad[m][i] = kMode == kGradDot ? p * fmaf(c1, fmaxf(d, kLeastLog), c0) : p * c0;
+          }
+        if (__any(taken >= 0)) {
+#pragma unroll
+          for (int m = 0; m < kMT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) grad[m][i] += taken == token_at(m, i) ? d_lp : 0.0f;
+        }
+        if constexpr (kBias) {
+#pragma unroll
+          for (int m = 0; m < kMT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              col[m][i] += grad[m][i];
+              asm volatile("" : "+v"(col[m][i]));  // here, not later: it would have to keep what it adds
+            }
+        }
+        uint16_t* out = a.g + row * a.g_pitch + vt + wm + 8 * g;
+        uint16_t* out_low = out + P * a.g_pitch;
+#pragma unroll
+        for (int p = 0; p < kMT / 2; ++p) {
+          const float* const x = grad[2 * p];
+          const float* const y = grad[2 * p + 1];
+          v4u hi;
+          hi.x = pack_bf16x2(x[0], x[1]);
+          hi.y = pack_bf16x2(x[2], x[3]);
+          hi.z = pack_bf16x2(y[0], y[1]);
+          hi.w = pack_bf16x2(y[2], y[3]);
+          *reinterpret_cast<v4u*>(out + 32 * p) = hi;
+          if (!a.grad_bf16) {
+            auto low = [](float f0, float f1, unsigned h) {
+              return pack_bf16x2(f0 - __uint_as_float(h << 16), f1 - __uint_as_float(h & 0xffff0000u));
+            };
+            v4u lo;
+            lo.x = low(x[0], x[1], hi.x);
+            lo.y = low(x[2], x[3], hi.y);
+            lo.z = low(y[0], y[1], hi.z);
+            lo.w = low(y[2], y[3], hi.w);
+            *reinterpret_cast<v4u*>(out_low + 32 * p) = lo;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (kBias) {
+        // d_bias: this wave's 128 steps, summed over the 16 lanes of a group; lane s keeps
+        // the sums of accumulators s and s + 16.
+        float keep[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4 * kMT; ++j) {
+          const float x = row_sum(col[j / 4][j % 4]);
+          keep[j / 16] = s == j % 16 ? x : keep[j / 16];
+        }
+        float* const out = a.bias_partials + (n0 + wn) / kBiasSteps * a.g_pitch + vt + wm + 8 * g + token_at(s / 4, s % 4);
+        out[0] = keep[0];
+        if constexpr (kSize == kTile) {
+          out[64] = keep[1];
+          out[a.g_pitch] = 0.0f;
+          out[a.g_pitch + 64] = 0.0f;
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (kBias) {
-      // d_bias: this wave's 128 steps, summed over the 16 lanes of a group; lane s keeps
-      // the sums of accumulators s and s + 16.
-      float keep[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int j = 0; j < 4 * kMT; ++j) {
-        const float x = row_sum(col[j / 4][j % 4]);
-        keep[j / 16] = s == j % 16 ? x : keep[j / 16];
-      }
-      float* const out = a.bias_partials + (n0 + wn) / kBiasSteps * a.g_pitch + vt + wm + 8 * g + token_at(s / 4, s % 4);
-      out[0] = keep[0];
-      if constexpr (kSize == kTile) {
-        out[64] = keep[1];
-        out[a.g_pitch] = 0.0f;
-        out[a.g_pitch + 64] = 0.0f;
-      }
-    }
-  }
   }
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
