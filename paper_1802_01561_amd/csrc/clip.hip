@@ -12,7 +12,8 @@
 // written once) 430 + 895 us, 5.6 and 5.4 TB/s (torch's copy of 8 GB: 4.8).  The norm's
 // workgroups take several chunks (one partial sum each); the second pass has a workgroup a
 // chunk (2048 workgroups in turn: 1060 us).  Walking it backwards, from what the first pass
-// left in the Infinity Cache, gained nothing.
+// left in the Infinity Cache, gained nothing.  Outputs whose place in 16 bytes is not their
+// gradient's are written element by element: 60 M float32 290 us, at the same place 113.
 #include "clip.hpp"
 #include "device_common.hpp"
 #include "tickets.hpp"

@@ -13,9 +13,10 @@
 // composite of those behind it.  The inputs are then read twice, the second time mostly
 // from the Infinity Cache.
 //
-// Measured, us a call in a graph: T = 100, B = 32 (one launch) 9; T = 16384, B = 128 (1.56 M
-// steps of 36 bytes, 10 us at 5.5 TB/s) 33, bound by the latency of two walks of two tiles
-// each (four waves a SIMD; at three, 41); T = 1000, B = 16384 (590 MB) 186, 3.2 TB/s.
+// Measured, us a call back to back: T = 100, B = 32 (one launch) 8.4; T = 16384, B = 128 (1.56 M
+// steps of 36 bytes, 10 us at 5.5 TB/s) 32, bound by the latency of two walks of two tiles
+// each (four waves a SIMD; at three, 41); T = 1000, B = 16384 (590 MB) 181, 3.3 TB/s, bound by
+// 16 tiles one after the other, each with its loads, scan and stores in turn.
 #include "device_common.hpp"
 #include "log_prob_loss.hpp"
 #include "tickets.hpp"

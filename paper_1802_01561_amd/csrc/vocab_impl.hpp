@@ -22,11 +22,11 @@
 // evenly.
 //
 // A step of 64 k takes 1.56 us on all CUs, 1.375 PFLOP/s (large products of the vendor's
-// library 1.45 to 1.49), with the matrix units busy 60% of it.  What bounds it are the copies,
-// 64 KB a CU and step, 10.7 TB/s from the L2s with 80% hits: without them a timing copy took 25%
-// less, without the reads of LDS too 37%.  A tile costs 7 to 14 us more: filling and
-// draining the pipeline, and its stores, which all CUs make at about the same time (without
-// those of G its kernel takes 836 us instead of 914, without its exponentials 914).  Waiting
+// library 1.45 to 1.49), with the matrix units busy 54 to 64% of it.  What bounds it are the
+// copies, 64 KB a CU and step, 10.5 TB/s from the L2s with 80% hits: without them a timing copy
+// took 22 to 28% less, without the reads of LDS too 35 to 41%.  A tile costs 7 to 14 us more:
+// filling and draining the pipeline, and its stores, which all CUs make at about the same time
+// (a timing copy without those of G took 9% less, one without its exponentials as long).  Waiting
 // at the next tile's start for the copies alone and not for the stores behind them, stores
 // past the caches, whole 256-byte rows by way of LDS, and row pitches off the powers of two
 // changed nothing.

@@ -11,8 +11,8 @@
 //   sum 2^d and, for the entropy, sum 2^d d.
 // The pieces are joined in float64 (vocab.hip).
 //
-// Measured: statistics of 6200 steps, H = 4096, V = 131072 (6.66 TFLOP) in 5.24 ms,
-// 1.27 PFLOP/s; G of 4096 steps in eight pieces (4.4 TFLOP, 1.07 GB of G) in 3.44 ms, 1.28.
+// Measured: statistics of 6200 steps, H = 4096, V = 131072 (6.66 TFLOP) in 5.33 ms,
+// 1.25 PFLOP/s; G of 4096 steps in eight pieces (4.4 TFLOP, 1.07 GB of G) in 3.5 ms, 1.25.
 #include "vocab_impl.hpp"
 
 namespace vtrace {
