@@ -60,9 +60,10 @@ extern "C" {
  * in float32 of differences to the largest logit of a piece, their sums in float32
  * over the piece and joined in float64.  A piece is the 64 or 128 tokens of one
  * wave, or, up to 128 steps, the tokens of one workgroup: V / 1024 to V / 256, at
- * least 16.  Any other token makes that step's log_probs NaN and raises the workspace's flag
- * (vtrace_error_flag).  A step whose tokens are all ruled out has log_sums
- * -INFINITY and NaN elsewhere; NaN and Inf inputs are propagated, also from the
+ * least 16.  Any other token makes that step's log_probs NaN and raises the
+ * workspace's flag (vtrace_error_flag).  A step whose tokens are all ruled out has
+ * log_sums -INFINITY and NaN elsewhere; a finite bias of -1e9 or less has the same
+ * effect beside allowed tokens.  NaN and Inf inputs are propagated, also from the
  * row of a token that is ruled out (0 * NaN): such rows have to hold numbers.
  */
 size_t vtrace_vocab_workspace_bytes(int64_t T, int64_t B, int64_t V, int64_t H);

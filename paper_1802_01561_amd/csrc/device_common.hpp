@@ -106,14 +106,14 @@ __device__ __forceinline__ StepWeights variant_weights(int correction, double rh
 }
 
 // The product of two coefficients (from 0 on) of composed steps x -> a x + b of the recursion.
-// Where it overflows it is held at the largest finite value: the recursion multiplies by one
-// coefficient after the other, and what it multiplies may be 0 all along, where 0 * inf would be
-// NaN.  (Anything else that a coefficient of 1e308 multiplies leaves float32's range all the
-// same.)  Coefficients that are infinite or NaN themselves multiply as they are.  On the upper
-// words, three instructions without a branch: T = 1000, B = 512, A = 18 39.8 us, with a comparison
-// and a branch in their place 41.4, unchecked 39.1.
+// Where it overflows it is held just below infinity, at 2^1024 (1 - 2^-21): the recursion
+// multiplies by one coefficient after the other, and what it multiplies may be 0 all along,
+// where 0 * inf would be NaN.  (Anything else that a coefficient of 1e308 multiplies leaves
+// float32's range all the same.)  Coefficients that are infinite or NaN themselves multiply as
+// they are.  On the upper words, three instructions without a branch: T = 1000, B = 512, A = 18
+// 39.8 us, with a comparison and a branch in their place 41.4, unchecked 39.1.
 __device__ __forceinline__ double coefficient_product(double a, double b) {
-  constexpr int kLargest = 0x7fefffff;  // the upper word of the largest finite value
+  constexpr int kLargest = 0x7fefffff;  // the upper word of the largest finite values
   auto upper = [](double x) { return static_cast<int>(static_cast<unsigned long long>(__double_as_longlong(x)) >> 32); };
   const double p = a * b;
   const int in = upper(a) > upper(b) ? upper(a) : upper(b);
