@@ -285,8 +285,8 @@ def vtrace_log_prob_loss_grad(target_log_probs, behaviour_log_probs, entropy, re
             r = fast.call_log_prob_loss(
                 fast.log_prob_loss, target_log_probs, behaviour_log_probs, entropy, rewards, discounts, values,
                 bootstrap_value, lengths, rho_bar, c_bar, lam, baseline_cost, entropy_cost, known[1],
-                *(out or (None,) * 6), out is None and entropy is not None, out is None and with_vs,
-                out is None and with_pg_advantages, workspace.tensor, workspace.nbytes, device, fast.stream(device))
+                *(out or (None,) * 6), out is None and entropy is not None, out is None and bool(with_vs),
+                out is None and bool(with_pg_advantages), workspace.tensor, workspace.nbytes, device, fast.stream(device))
             if r is not None:
                 return _outputs(r, out, LogProbLossGrad)
     variant = _variant(correction, q_estimate, epsilon, "log_probs", reward_transform)

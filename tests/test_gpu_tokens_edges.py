@@ -88,3 +88,13 @@ def test_clipped_into_an_iterator():
             out = [torch.zeros_like(t) for t in g]
             norm = vt.vtrace_clip_grad_norm(iter([*g, *extra]), 1.0, out=(t for t in [*out, *extra]), **kw)
             assert float(norm) == 4.0 and all((t == 0.25).all() for t in out)
+
+
+def test_wanted_outputs_by_truth():
+    """with_vs = 1 asks for vs, whichever way the call is marshalled."""
+    y = _dev(_growing_lanes(40, 3, 0.1, False))
+    for kw in (dict(workspace=vt.LogProbWorkspace(40, 3)), dict()):
+        out = vt.vtrace_log_prob_loss_grad(**y, with_vs=1, with_pg_advantages=np.bool_(True), **kw)
+        assert out.vs is not None and out.pg_advantages is not None
+        out = vt.vtrace_log_prob_loss_grad(**y, with_vs=0, with_pg_advantages=None, **kw)
+        assert out.vs is None and out.pg_advantages is None
