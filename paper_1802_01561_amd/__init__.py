@@ -2,8 +2,9 @@
 (Espeholt et al., 2018) as hand-written HIP kernels for AMD Instinct MI355X.
 
 The computation lives in ``libvtrace.so`` (C ABI in ``include/vtrace.h`` and, for
-policies over a token vocabulary, ``include/vtrace_tokens.h``); this package only
-loads it and marshals torch tensors into it.
+policies over a token vocabulary, ``include/vtrace_tokens.h`` and
+``include/vtrace_parameters.h``); this package only loads it and marshals torch tensors
+into it.
 """
 
 from ._lib import LIB_PATH, VtraceError  # noqa: F401
@@ -21,6 +22,16 @@ from .binding import (  # noqa: F401
     vtrace_max_elements,
     vtrace_targets,
     vtrace_workspace_bytes,
+)
+from .parameters import (  # noqa: F401
+    QUINTIC,
+    EmbedWorkspace,
+    OrthogonalWorkspace,
+    vtrace_orthogonalize,
+    vtrace_orthogonalize_workspace_bytes,
+    vtrace_vocab_embed,
+    vtrace_vocab_embed_grad,
+    vtrace_vocab_embed_grad_workspace_bytes,
 )
 from .tokens import (  # noqa: F401
     NO_TOKEN,

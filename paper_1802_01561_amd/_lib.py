@@ -1,4 +1,5 @@
-"""ctypes declarations of the libvtrace C ABI (include/vtrace.h and vtrace_tokens.h).
+"""ctypes declarations of the libvtrace C ABI (include/vtrace.h, vtrace_tokens.h and
+vtrace_parameters.h).
 
 Loading fails loudly when the library has not been built: there is no
 fallback implementation anywhere in this package.
@@ -82,6 +83,15 @@ TOKEN_SIGNATURES = {
                                   + [ctypes.c_size_t, _P]),
     "vtrace_clip_grad_norm": (_I, [_I64] + [_P] * 4 + [_F] + [_P] * 2 + [ctypes.c_size_t, _P]),
 }
+# Every symbol include/vtrace_parameters.h declares.
+PARAMETER_SIGNATURES = {
+    "vtrace_vocab_embed": (_I, [_I64] * 4 + [_I] * 2 + [_P] * 2 + [_F] + [_P] * 2 + [ctypes.c_size_t, _P]),
+    "vtrace_vocab_embed_grad_workspace_bytes": (ctypes.c_size_t, [_I64] * 4),
+    "vtrace_vocab_embed_grad": (_I, [_I64] * 4 + [_I] * 2 + [_P] * 2 + [_F, ctypes.c_int32] + [_P] * 2
+                                + [ctypes.c_size_t, _P]),
+    "vtrace_orthogonalize_workspace_bytes": (ctypes.c_size_t, [_I64] + [_P] * 3),
+    "vtrace_orthogonalize": (_I, [_I64] + [_P] * 6 + [ctypes.c_int32, _P, _F, _P, ctypes.c_size_t, _P]),
+}
 CLIP_WORKSPACE_BYTES = 20736  # VTRACE_CLIP_WORKSPACE_BYTES
 
 _lib = None
@@ -102,7 +112,7 @@ def lib():
             raise RuntimeError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_1802_01561_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in {**SIGNATURES, **TOKEN_SIGNATURES}.items():
+        for name, (res, args) in {**SIGNATURES, **TOKEN_SIGNATURES, **PARAMETER_SIGNATURES}.items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

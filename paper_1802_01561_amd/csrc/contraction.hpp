@@ -199,6 +199,36 @@ struct Reader {
   }
 };
 
+// An operand in three parts, one after the other along k: A = (low, high, high) against
+// B = (high, low, high) are the products of two sums high + low, but for low low.
+template <int kRows>
+struct PartsLoader : Loader<kRows> {
+  int each;
+  const char* last;
+
+  // Behind aim() at the first part: `steps` of each part, `bytes` from the start of one to its end.
+  __device__ __forceinline__ void parts(int steps, const void* second, const void* third, int64_t bytes) {
+    this->restart_after(steps, second, bytes);
+    each = steps;
+    last = static_cast<const char*>(third);
+  }
+  __device__ __forceinline__ Rsrc begin(bool more = true) {
+    const bool turn = this->done == this->first;
+    const Rsrc r = Loader<kRows>::begin(more);
+    if (turn) {
+      this->first += each;
+      this->again = last;
+    }
+    return r;
+  }
+  __device__ __forceinline__ void copy(Rsrc r, char* lds, int wave, int i) const { Loader<kRows>::copy(r, lds, wave, i); }
+  __device__ __forceinline__ void copy(char* lds, int wave) {
+    const Rsrc r = begin();
+#pragma unroll
+    for (int i = 0; i < Loader<kRows>::kCopies; ++i) copy(r, lds, wave, i);
+  }
+};
+
 // vmcnt(0) and lgkmcnt(0): the copies into LDS have arrived and this wave's reads are done.
 constexpr int kWaitAll = 0x0070;
 
@@ -336,19 +366,19 @@ struct Job {
   }
 };
 
-// acc += A B over the job's steps, both operands "along" or both "across".  A wave passes the barrier when it
+// acc += A B over the job's steps, both operands "along", both "across", or A alone "across".  A wave passes the barrier when it
 // has read all of a step and its copies of the next have arrived, so behind it the next stage
 // is whole and this one free.
 //
 // The first step's copies are under way when this is called (to stage `parity`).  With the
 // last step's products go the copies of the next tile's first: next() makes `job` that
 // tile's, and what follows the contraction hides their latency.
-template <bool kAcross, bool kHalfFloats = false, int kSize, typename LoaderT, typename Next>
+template <bool kAAcross, bool kBAcross = kAAcross, bool kHalfFloats = false, int kSize, typename LoaderT, typename Next>
 __device__ __forceinline__ void contract(Job<kSize, LoaderT>& job, char* lds, int& parity, int wave, int lane,
                                          Accumulators<kSize>& acc, Next next) {
   constexpr int kStage = 2 * operand_bytes(kSize);
   const int steps = job.steps;
-  Contraction<kAcross, kAcross, kSize, kHalfFloats> c;
+  Contraction<kAAcross, kBAcross, kSize, kHalfFloats> c;
   c.start(wave, lane);
   int it = 0;
   do {

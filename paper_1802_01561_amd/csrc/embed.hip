@@ -1,0 +1,536 @@
+// The vocabulary's rows as a network's inputs, and their gradient:
+//   rows[n, :] = scale table[a_n, :],   d_table[v, :] = scale sum over {n : a_n = v} of d_rows[n, :].
+//
+// Both are bound by memory.  The gradient's steps are put in the order of their tokens (stable:
+// a token's steps stay in theirs, so that sums are the same in every call), cut into chunks of
+// as many steps, and a chunk's runs of one token are summed in registers.  A run inside a chunk
+// is a row of the result; what a run leaves in a chunk that it enters or leaves is a partial
+// sum, added to the others of its run by a second launch.  No atomics: a frequent token's
+// thousands of steps are read by as many chunks as anything else.
+//
+// Sums are float32 within a chunk (at most kMostChunk steps) and float64 over the chunks.
+#include "device_common.hpp"
+#include "embed.hpp"
+#include "wave_ops.hpp"
+
+namespace vtrace {
+namespace {
+
+constexpr int kThreads = 256;
+// A thread's elements of a row: one 16-byte vector of bfloat16, two of float32.
+constexpr int kUnit = 8;
+
+struct Unit {
+  float x[kUnit];
+};
+
+__device__ __forceinline__ Unit load_unit(const uint16_t* p) {
+  const v4u w = *reinterpret_cast<const v4u*>(p);
+  Unit u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u.x[2 * i] = __uint_as_float(w[i] << 16);
+    u.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+  return u;
+}
+__device__ __forceinline__ Unit load_unit(const float* p) {
+  Unit u;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const v4u w = *reinterpret_cast<const v4u*>(p + 4 * h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.x[4 * h + i] = __uint_as_float(w[i]);
+  }
+  return u;
+}
+__device__ __forceinline__ void store_unit(uint16_t* p, const Unit& u) {
+  v4u w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(u.x[2 * i], u.x[2 * i + 1]);
+  *reinterpret_cast<v4u*>(p) = w;
+}
+__device__ __forceinline__ void store_unit(float* p, const Unit& u) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v4u w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(u.x[4 * h + i]);
+    *reinterpret_cast<v4u*>(p + 4 * h) = w;
+  }
+}
+
+// How many threads share a row: a power of two, up to a workgroup.
+int row_lanes_log2(int64_t H, int most_log2) {
+  int bits = 0;
+  while (bits < most_log2 && (int64_t(kUnit) << bits) < H) ++bits;
+  return bits;
+}
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// kRows rows a group of threads, their loads in flight together.
+template <typename In, typename Out, int kRows>
+__global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes_log2) {
+  const int groups = kThreads >> lanes_log2, lanes = 1 << lanes_log2;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kRows * groups + (threadIdx.x >> lanes_log2);
+  const int lane = threadIdx.x & (lanes - 1), units = static_cast<int>(a.H / kUnit);
+  int32_t token[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const int64_t n = first + r * groups;
+    token[r] = n < a.N ? a.tokens[n] : -1;
+    if (lane == 0 && token[r] != -1 && (token[r] < 0 || token[r] >= a.V)) raise_error_flag(a.error_flag);
+  }
+  for (int c = lane; c < units; c += lanes) {
+    Unit u[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (token[r] >= 0 && token[r] < a.V)
+        u[r] = load_unit(static_cast<const In*>(a.table) + static_cast<int64_t>(token[r]) * a.H + c * kUnit);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int64_t n = first + r * groups;
+      if (n >= a.N) continue;
+      const bool valid = token[r] >= 0 && token[r] < a.V;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) u[r].x[i] = valid ? u[r].x[i] * a.scale : token[r] == -1 ? 0.0f : NAN;
+      store_unit(static_cast<Out*>(a.rows) + n * a.H + c * kUnit, u[r]);
+    }
+  }
+}
+
+// ---- The steps in the order of their tokens. ----
+
+// Up to here every step's place is counted directly, N^2 comparisons in one launch.
+constexpr int64_t kMostRanked = 16384;
+constexpr int kRankThreads = 1024;
+
+__device__ __forceinline__ bool invalid(int32_t token, int64_t V) { return token != -1 && (token < 0 || token >= V); }
+
+// A workgroup's 64 steps, one a lane; each wave counts a part of all steps that come before
+// them.  Tokens compare as unsigned numbers, so that what is no token of the vocabulary comes last.
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedArgs a) {
+  constexpr int kWaves = kRankThreads / kWave;
+  __shared__ int s_rank[kWaves][kWave];
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int N = static_cast<int>(a.N);
+  const int n0 = blockIdx.x * kWave, n = n0 + lane;
+  const uint32_t mine = n < N ? static_cast<uint32_t>(a.tokens[n]) : 0xffffffffu;
+  const int per = (N + kWaves - 1) / kWaves;
+  const int from = wave * per < N ? wave * per : N, to = from + per < N ? from + per : N;
+  auto inside = [&](int j) { return j < from ? from : j > to ? to : j; };
+  const int own = inside(n0), behind = inside(n0 + kWave);
+  int rank = 0;
+#pragma unroll 16
+  for (int j = from; j < own; ++j) rank += static_cast<uint32_t>(a.tokens[j]) <= mine;
+  for (int j = own; j < behind; ++j) {
+    const uint32_t t = static_cast<uint32_t>(a.tokens[j]);
+    rank += t < mine || (t == mine && j < n);
+  }
+#pragma unroll 16
+  for (int j = behind; j < to; ++j) rank += static_cast<uint32_t>(a.tokens[j]) < mine;
+  s_rank[wave][lane] = rank;
+  __syncthreads();
+  if (wave != 0 || n >= N) return;
+  int at = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) at += s_rank[w][lane];
+  a.keys[0][at] = mine;
+  a.steps[0][at] = static_cast<uint32_t>(n);
+  if (invalid(static_cast<int32_t>(mine), a.V)) raise_error_flag(a.error_flag);
+}
+
+// More steps: passes over digits of the token, from the lowest up, each of them stable.  A pass
+// counts every block's digits, adds the counts up in the order (digit, block), and moves.
+constexpr int kMostDigitBits = 9, kMostDigits = 1 << kMostDigitBits;
+constexpr int kSortItems = 4096;  // of a block
+constexpr int kSortWaves = kThreads / kWave;
+constexpr int kScanThreads = 1024;
+
+// What is no token of the vocabulary is V.
+__device__ __forceinline__ uint32_t sort_key(const EmbedArgs& a, int from, int64_t i) {
+  if (from >= 0) return a.keys[from][i];
+  const uint32_t t = static_cast<uint32_t>(a.tokens[i]);
+  return t < static_cast<uint32_t>(a.V) ? t : static_cast<uint32_t>(a.V);
+}
+
+__global__ __launch_bounds__(kThreads) void embed_count_kernel(EmbedArgs a, int from, int shift, int bits) {
+  __shared__ uint32_t s_count[kMostDigits];
+  const int digits = 1 << bits;
+  for (int d = threadIdx.x; d < digits; d += kThreads) s_count[d] = 0;
+  __syncthreads();
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortItems;
+  for (int k = threadIdx.x; k < kSortItems; k += kThreads) {
+    if (first + k >= a.N) break;
+    if (from < 0 && invalid(a.tokens[first + k], a.V)) raise_error_flag(a.error_flag);
+    atomicAdd(&s_count[(sort_key(a, from, first + k) >> shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kThreads) a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x] = s_count[d];
+}
+
+// counts[i] = sum of counts[0 .. i), by one workgroup.
+__global__ __launch_bounds__(kScanThreads) void embed_scan_kernel(uint32_t* counts, int64_t n) {
+  constexpr int kWaves = kScanThreads / kWave, kItems = 4;
+  __shared__ uint32_t s_sum[2][kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  uint32_t total = 0;
+  int flip = 0;
+  for (int64_t base = 0; base < n; base += kScanThreads * kItems, flip ^= 1) {
+    const int64_t first = base + static_cast<int64_t>(threadIdx.x) * kItems;
+    uint32_t x[kItems], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      x[i] = first + i < n ? counts[first + i] : 0;
+      mine += x[i];
+    }
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t y = __shfl_up(upto, o, kWave);
+      if (lane >= o) upto += y;
+    }
+    if (lane == kWave - 1) s_sum[flip][wave] = upto;
+    __syncthreads();
+    uint32_t at = total + upto - mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t s = s_sum[flip][w];
+      if (w < wave) at += s;
+      total += s;
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      if (first + i < n) counts[first + i] = at;
+      at += x[i];
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void embed_move_kernel(EmbedArgs a, int from, int to, int shift, int bits) {
+  constexpr int kRounds = kSortItems / kThreads;  // of 64 consecutive items a wave
+  __shared__ uint32_t s_at[kSortWaves][kMostDigits];
+  const int digits = 1 << bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (int d = threadIdx.x; d < kSortWaves * kMostDigits; d += kThreads) s_at[d / kMostDigits][d % kMostDigits] = 0;
+  __syncthreads();
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortItems + wave * (kRounds * kWave) + lane;
+  uint32_t key[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t i = first + r * kWave;
+    key[r] = i < a.N ? sort_key(a, from, i) : 0;
+    if (i < a.N) atomicAdd(&s_at[wave][(key[r] >> shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kThreads) {
+    uint32_t at = a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t n = s_at[w][d];
+      s_at[w][d] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t i = first + r * kWave;
+    const int d = (key[r] >> shift) & (digits - 1);
+    // The lanes with the same digit, by its bits.
+    unsigned long long same = __ballot(i < a.N);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned long long set = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? set : ~set;
+    }
+    if (i >= a.N) continue;  // the last lanes of the last round or rounds
+    const int before = __popcll(same & ((1ull << lane) - 1));
+    const uint32_t at = s_at[wave][d];
+    __builtin_amdgcn_wave_barrier();  // every lane has read before one of them writes
+    if (before == 0) s_at[wave][d] = at + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    a.keys[to][at + before] = key[r];
+    a.steps[to][at + before] = from < 0 ? static_cast<uint32_t>(i) : a.steps[from][i];
+  }
+}
+
+// ---- Sums. ----
+
+constexpr int kLeastChunk = 4, kMostChunk = 128;
+constexpr int kBatch = 4;  // rows in flight of a chunk
+constexpr int kFillRows = 64;  // most rows of a workgroup that fills
+constexpr int64_t kFillBytes = 65536;
+
+template <typename Out>
+__device__ __forceinline__ void write_row(Out* p, const Unit& sum, float scale, bool accumulate) {
+  Unit u = sum;
+  if (accumulate) {
+    const Unit was = load_unit(p);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) u.x[i] = fmaf(sum.x[i], scale, was.x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) u.x[i] *= scale;
+  }
+  store_unit(p, u);
+}
+// Zeros in the rows of tokens that no step has: workgroup `block` of those that do this.
+template <typename Out>
+__device__ void fill_rows(const EmbedArgs& a, int64_t block, int rows, int lanes_log2) {
+  __shared__ int s_present[kFillRows];
+  const int64_t v0 = block * rows;
+  if (static_cast<int>(threadIdx.x) < rows) {
+    const int64_t v = v0 + threadIdx.x;
+    int64_t lo = 0, hi = a.N;  // the first step whose token is not before v
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (a.keys[0][mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+    s_present[threadIdx.x] = v >= a.V || (lo < a.N && a.keys[0][lo] == v);
+  }
+  __syncthreads();
+  const int lanes = 1 << lanes_log2, units = static_cast<int>(a.H / kUnit);
+  for (int r = threadIdx.x >> lanes_log2; r < rows; r += kThreads >> lanes_log2) {
+    if (s_present[r]) continue;
+    for (int c = threadIdx.x & (lanes - 1); c < units; c += lanes)
+      store_unit(static_cast<Out*>(a.d_table) + (v0 + r) * a.H + c * kUnit, Unit{});
+  }
+}
+
+__device__ __forceinline__ float* partial_row(const EmbedArgs& a, int64_t chunk, int which) {
+  return a.partials + (2 * chunk + which) * a.H;
+}
+
+// Chunks of the sorted steps, one a group of threads (and a slab of the row, where it has more
+// than a workgroup's units); then, in further workgroups, the rows that no step has.
+// Slot 0 of a chunk's partial sums is that of the run that comes from the chunk before it,
+// slot 1 of the one that begins here and goes on behind it.
+template <typename In, typename Out>
+__global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int lanes_log2, int slabs, int64_t sum_blocks,
+                                                             int fill) {
+  if (blockIdx.x >= sum_blocks) {
+    fill_rows<Out>(a, blockIdx.x - sum_blocks, fill, lanes_log2);
+    return;
+  }
+  const int lanes = 1 << lanes_log2;
+  const int64_t chunk = static_cast<int64_t>(blockIdx.x / slabs) * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
+  const int64_t begin = chunk * a.chunk;
+  const int unit = static_cast<int>(blockIdx.x % slabs) * kThreads + (threadIdx.x & (lanes - 1));
+  if (begin >= a.N || unit >= static_cast<int>(a.H / kUnit)) return;
+  const int64_t end = begin + a.chunk < a.N ? begin + a.chunk : a.N;
+  const uint32_t* const keys = a.keys[0];
+  const uint32_t V = static_cast<uint32_t>(a.V);
+  const int64_t column = static_cast<int64_t>(unit) * kUnit;
+  const In* const d_rows = static_cast<const In*>(a.d_rows) + column;
+  Out* const d_table = static_cast<Out*>(a.d_table) + column;
+  uint32_t run = keys[begin];
+  if (run >= V) return;
+  const bool entered = begin > 0 && keys[begin - 1] == run;
+  const uint32_t after = end < a.N ? keys[end] : 0xffffffffu;
+  Unit sum = {};
+  bool first = true;
+  auto leave = [&](bool goes_on) {
+    if (first && entered) store_unit(partial_row(a, chunk, 0) + column, sum);
+    else if (goes_on) store_unit(partial_row(a, chunk, 1) + column, sum);
+    else write_row(d_table + static_cast<int64_t>(run) * a.H, sum, a.scale, a.accumulate);
+  };
+  for (int64_t i = begin; i < end; i += kBatch) {
+    uint32_t key[kBatch];
+    Unit u[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      key[b] = i + b < end ? keys[i + b] : 0xffffffffu;
+      if (key[b] < V) u[b] = load_unit(d_rows + static_cast<int64_t>(a.steps[0][i + b]) * a.H);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (key[b] >= V) continue;
+      if (key[b] != run) {
+        leave(false);
+        run = key[b];
+        first = false;
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) sum.x[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < kUnit; ++e) sum.x[e] += u[b].x[e];
+    }
+  }
+  leave(after == run);
+}
+
+// The run that begins in a chunk and goes on behind it: its parts, in order, in float64; the
+// groups of a workgroup take turns with them.
+template <typename Out>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, int lanes_log2, int slabs) {
+  __shared__ double s_sum[kThreads][kUnit];
+  const int64_t chunk = blockIdx.x / slabs;
+  const int64_t begin = chunk * a.chunk, end = begin + a.chunk;
+  const uint32_t* const keys = a.keys[0];
+  if (end >= a.N) return;
+  const uint32_t run = keys[end - 1];
+  if (run >= static_cast<uint32_t>(a.V) || keys[end] != run || (begin > 0 && keys[begin - 1] == run)) return;
+  // The last chunk that begins with it.
+  int64_t lo = chunk + 1, hi = (a.N + a.chunk - 1) / a.chunk - 1;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi + 1) / 2;
+    if (keys[mid * a.chunk] == run) lo = mid;
+    else hi = mid - 1;
+  }
+  const int64_t last = lo;
+  const int lanes = 1 << lanes_log2, groups = kThreads >> lanes_log2, group = threadIdx.x >> lanes_log2;
+  const int unit = static_cast<int>(blockIdx.x % slabs) * lanes + (threadIdx.x & (lanes - 1));
+  const bool in = unit < static_cast<int>(a.H / kUnit);
+  const int64_t column = static_cast<int64_t>(unit) * kUnit;
+  double sum[kUnit] = {};
+  auto add = [&](int64_t c, int which) {
+    const Unit u = load_unit(partial_row(a, c, which) + column);
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) sum[e] += static_cast<double>(u.x[e]);
+  };
+  if (in) {
+    if (group == 0) add(chunk, 1);
+#pragma unroll 4
+    for (int64_t c = chunk + 1 + group; c <= last; c += groups) add(c, 0);
+  }
+#pragma unroll
+  for (int e = 0; e < kUnit; ++e) s_sum[threadIdx.x][e] = sum[e];
+  __syncthreads();
+  if (group != 0 || !in) return;
+  for (int g = 1; g < groups; ++g)
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) sum[e] += s_sum[g * lanes + threadIdx.x][e];
+  Unit u;
+#pragma unroll
+  for (int e = 0; e < kUnit; ++e) u.x[e] = static_cast<float>(sum[e]);
+  write_row(static_cast<Out*>(a.d_table) + static_cast<int64_t>(run) * a.H + column, u, a.scale, a.accumulate);
+}
+
+template <typename In, typename Out>
+hipError_t launch_sums(const EmbedArgs& a, hipStream_t st) {
+  const int lanes = row_lanes_log2(a.H, 8);
+  const int64_t slabs = ceil_div(a.H / kUnit, kThreads), chunks = ceil_div(a.N, a.chunk);
+  const int64_t sums = ceil_div(chunks, kThreads >> lanes) * slabs;
+  int64_t fill = 0, fills = 0;
+  if (!a.accumulate) {
+    fill = kFillBytes / (a.H * static_cast<int64_t>(sizeof(Out)));
+    fill = fill < 1 ? 1 : fill > kFillRows ? kFillRows : fill;
+    fills = ceil_div(a.V, fill);
+  }
+  hipLaunchKernelGGL((embed_sum_kernel<In, Out>), dim3(static_cast<unsigned>(sums + fills)), dim3(kThreads), 0, st, a, lanes,
+                     static_cast<int>(slabs), sums, static_cast<int>(fill));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || chunks < 2) return e;
+  const int join_lanes = row_lanes_log2(a.H, 6);
+  const int64_t join_slabs = ceil_div(a.H / kUnit, int64_t(1) << join_lanes);
+  hipLaunchKernelGGL(embed_join_kernel<Out>, dim3(static_cast<unsigned>(chunks * join_slabs)), dim3(kThreads), 0, st, a,
+                     join_lanes, static_cast<int>(join_slabs));
+  return hipGetLastError();
+}
+
+int passes_of(int64_t V, int* bits) {
+  int all = 1;  // keys are 0 .. V
+  while ((V >> all) != 0) ++all;
+  const int passes = (all + kMostDigitBits - 1) / kMostDigitBits;
+  *bits = (all + passes - 1) / passes;
+  return passes;
+}
+
+// Which of the two buffers the first pass fills, so that the last one fills buffer 0.
+hipError_t launch_order(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) {
+  if (p.ranks) {
+    hipLaunchKernelGGL(embed_rank_kernel, dim3(static_cast<unsigned>(ceil_div(a.N, kWave))), dim3(kRankThreads), 0, st, a);
+    return hipGetLastError();
+  }
+  int bits = 0;
+  const int passes = passes_of(a.V, &bits);
+  const int64_t blocks = ceil_div(a.N, kSortItems);
+  int from = -1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int to = (passes - 1 - pass) % 2;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    hipLaunchKernelGGL(embed_count_kernel, grid, dim3(kThreads), 0, st, a, from, pass * bits, bits);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(kScanThreads), 0, st, a.counts, blocks << bits);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(embed_move_kernel, grid, dim3(kThreads), 0, st, a, from, to, pass * bits, bits);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    from = to;
+  }
+  return hipSuccess;
+}
+
+template <typename In, typename Out>
+hipError_t launch_lookup(const EmbedArgs& a, hipStream_t st) {
+  const int lanes = row_lanes_log2(a.H, 8), groups = kThreads >> lanes;
+  constexpr int kRows = 4;
+  if (a.N >= 4096 * groups) {
+    hipLaunchKernelGGL((embed_kernel<In, Out, kRows>), dim3(static_cast<unsigned>(ceil_div(a.N, kRows * groups))), dim3(kThreads),
+                       0, st, a, lanes);
+  } else {
+    hipLaunchKernelGGL((embed_kernel<In, Out, 1>), dim3(static_cast<unsigned>(ceil_div(a.N, groups))), dim3(kThreads), 0, st, a,
+                       lanes);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+EmbedPlan plan_embed_grad(int64_t N, int64_t V, int64_t H) {
+  EmbedPlan p = {};
+  p.ranks = N <= kMostRanked;
+  // Chunks as long as leave a thousand workgroups: four a CU, with kBatch rows each in flight.
+  const int lanes = row_lanes_log2(H, 8);
+  const int64_t slabs = ceil_div(H / kUnit, kThreads), groups = kThreads >> lanes;
+  p.chunk = kLeastChunk;
+  while (p.chunk < kMostChunk && N * slabs / (groups * p.chunk * 2) >= 1024) p.chunk *= 2;
+  size_t at = kWsDataOffset;
+  auto take = [&](size_t bytes) {
+    const size_t begin = at;
+    at += (bytes + 255) / 256 * 256;
+    return begin;
+  };
+  const int buffers = p.ranks ? 1 : 2;
+  for (int b = 0; b < buffers; ++b) {
+    p.keys_at[b] = take(N * 4);
+    p.steps_at[b] = take(N * 4);
+  }
+  if (!p.ranks) {
+    int bits = 0;
+    passes_of(V, &bits);
+    p.counts_at = take((ceil_div(N, kSortItems) << bits) * 4);
+  }
+  p.partials_at = take(ceil_div(N, p.chunk) * 2 * H * 4);
+  p.bytes = at;
+  return p;
+}
+
+void attach_embed_grad(EmbedArgs* a, const EmbedPlan& p, void* ws) {
+  char* const base = static_cast<char*>(ws);
+  a->error_flag = reinterpret_cast<unsigned int*>(base + kWsFlagOffset);
+  for (int b = 0; b < 2; ++b) {
+    a->keys[b] = reinterpret_cast<uint32_t*>(base + p.keys_at[b]);
+    a->steps[b] = reinterpret_cast<uint32_t*>(base + p.steps_at[b]);
+  }
+  a->counts = reinterpret_cast<uint32_t*>(base + p.counts_at);
+  a->partials = reinterpret_cast<float*>(base + p.partials_at);
+  a->chunk = p.chunk;
+}
+
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
+  if (a.table_bf16) return a.steps_bf16 ? launch_lookup<uint16_t, uint16_t>(a, st) : launch_lookup<uint16_t, float>(a, st);
+  return a.steps_bf16 ? launch_lookup<float, uint16_t>(a, st) : launch_lookup<float, float>(a, st);
+}
+
+hipError_t launch_embed_grad(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) {
+  const hipError_t e = launch_order(a, p, st);
+  if (e != hipSuccess) return e;
+  if (a.steps_bf16) return a.table_bf16 ? launch_sums<uint16_t, uint16_t>(a, st) : launch_sums<uint16_t, float>(a, st);
+  return a.table_bf16 ? launch_sums<float, uint16_t>(a, st) : launch_sums<float, float>(a, st);
+}
+
+}  // namespace vtrace

@@ -1,0 +1,175 @@
+"""The vocabulary's rows as inputs and their gradient against the oracle, in float64.
+
+Tolerances.  A lookup is a float32 product (2^-24) rounded to the output's type.  A sum of n
+steps is n - 1 float32 additions in chunks of at most 128 steps, whose sums are float64
+additions and one rounding to float32: (min(n, 128) + 1) 2^-24 of the sum of sizes; scaling
+and adding are one float32 operation each, then comes the output's rounding."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1802_01561_amd as vt
+from oracle import parameters as op
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+HALF_STEP = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+def _f32(x):
+    return float(np.float32(x))
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _tokens(seed, N, V, kind="uniform", none=0.1):
+    r = np.random.default_rng(seed)
+    if kind == "uniform":
+        t = r.integers(0, V, N)
+    elif kind == "text":
+        t = np.minimum(np.exp(r.random(N) * np.log(V + 1.0)).astype(np.int64) - 1, V - 1)
+    elif kind == "one":
+        t = np.full(N, V // 2)
+    elif kind == "ends":
+        t = np.where(r.random(N) < 0.5, 0, V - 1)
+    t[r.random(N) < none] = vt.NO_TOKEN
+    return t.astype(np.int32)
+
+
+def _normal(seed, shape, dtype):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(dtype)
+
+
+def _check_embed(w, tokens, scale, dtype, got):
+    ref = op.embed(_np(w), tokens.reshape(-1), _f32(scale)).reshape(tuple(got.shape))
+    got = _np(got)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    fine = ~np.isnan(ref)
+    tol = 1.01 * (2.0 ** -24 + HALF_STEP[dtype]) * np.abs(ref)
+    assert (np.abs(got - ref)[fine] <= tol[fine]).all()
+
+
+def check_grad(d, tokens, V, scale, got, before=None):
+    H = d.shape[-1]
+    ref, count, size = op.embed_grad(_np(d).reshape(-1, H), tokens.reshape(-1), V, _f32(scale))
+    dtype = got.dtype
+    tol = (np.minimum(count, 128)[:, None] + 2) * 2.0 ** -24 * size
+    if before is not None:
+        ref = np.where(count[:, None] > 0, ref + _np(before), _np(before))
+    tol = 1.01 * (tol + (HALF_STEP[dtype] + 2.0 ** -24) * np.abs(ref))
+    if before is not None:
+        tol[count == 0] = 0.0
+    err = np.abs(_np(got) - ref)
+    assert (err <= tol).all(), (np.argwhere(~(err <= tol))[:5], err.max())
+
+
+@pytest.mark.parametrize("T,B,H,V", [(1, 1, 8, 1), (1, 48, 2048, 1003), (7, 3, 16, 100), (20, 32, 256, 3000), (5, 5, 1000, 77),
+                                     (83, 13, 72, 501), (3, 2, 2056, 9), (2, 3, 32768, 5), (4097, 4, 2048, 50), (17000, 1, 8, 40)])
+@pytest.mark.parametrize("table,out", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+def test_embed(T, B, H, V, table, out):
+    w = _normal(H + V, (V, H), table)
+    tokens = _tokens(T, T * B, V).reshape(T, B)
+    for scale in (1.0, 45.2548):
+        got = vt.vtrace_vocab_embed(w.cuda(), torch.from_numpy(tokens).cuda(), scale, out_dtype=out)
+        assert got.dtype == out
+        _check_embed(w, tokens, scale, out, got)
+
+
+def test_embed_of_tokens_outside_the_vocabulary():
+    w = _normal(0, (10, 64), BF16)
+    tokens = np.array([[0, -1, 9], [10, -2, 2 ** 31 - 1], [-2 ** 31, 3, -1]], dtype=np.int32)
+    ws = vt.EmbedWorkspace(3, 3, 10, 64)
+    got = vt.vtrace_vocab_embed(w.cuda(), torch.from_numpy(tokens[:1]).cuda(), workspace=ws)
+    _check_embed(w, tokens[:1], 1.0, BF16, got)
+    assert vt.vtrace_error_flag(ws) == 0
+    _check_embed(w, tokens, 1.0, BF16, vt.vtrace_vocab_embed(w.cuda(), torch.from_numpy(tokens).cuda(), workspace=ws))
+    assert vt.vtrace_error_flag(ws) != 0
+
+
+SIZES = [(1, 1, 8, 1), (1, 1, 64, 5), (1, 3, 72, 2), (1, 4, 256, 3), (5, 1, 256, 100), (20, 32, 256, 3000), (83, 13, 1000, 501),
+         (100, 32, 1024, 777), (9, 7, 2056, 40), (3, 3, 32768, 4), (64, 64, 64, 300), (16384, 1, 8, 257), (2000, 8, 16, 70001)]
+LONG = [(16385, 1, 8, 1), (4096, 5, 64, 511), (5000, 7, 24, 512), (4099, 11, 40, 100003), (65536, 2, 8, 300), (300000, 1, 8, 262144)]
+
+
+@pytest.mark.parametrize("T,B,H,V", SIZES + LONG)
+@pytest.mark.parametrize("kind", ["uniform", "text", "one", "ends"])
+def test_embed_grad(T, B, H, V, kind):
+    tokens = _tokens(T + V, T * B, V, kind).reshape(T, B)
+    t = torch.from_numpy(tokens).cuda()
+    for steps, grad, scale in ((F32, F32, 1.0), (BF16, BF16, 8.5), (BF16, F32, 1.0), (F32, BF16, -1.0)):
+        if (T, B, H, V) in LONG and steps is not grad:
+            continue
+        d = _normal(T, (T, B, H), steps)
+        d[torch.from_numpy(tokens) == vt.NO_TOKEN] = float("nan")  # not read
+        clean = torch.nan_to_num(d)
+        ws = vt.EmbedWorkspace(T, B, V, H)
+        ws.tensor[4352:].fill_(0xFF)
+        out = torch.full((V, H), float("nan"), dtype=grad, device="cuda")
+        got = vt.vtrace_vocab_embed_grad(d.cuda(), t, V, scale, out=out, workspace=ws)
+        assert got is out
+        check_grad(clean, tokens, V, scale, got)
+        before = _normal(V, (V, H), grad)
+        into = before.cuda()
+        assert vt.vtrace_vocab_embed_grad(d.cuda(), t, V, scale, accumulate_into=into, workspace=ws) is into
+        check_grad(clean, tokens, V, scale, into, before)
+        assert vt.vtrace_error_flag(ws) == 0
+
+
+@pytest.mark.parametrize("N,H", [(129, 2048), (1000, 256), (16384, 8), (20000, 16), (70000, 8)])
+def test_runs_of_every_length(N, H):
+    """Runs of 1, 2, 3, ... steps: their ends fall at every place of a chunk."""
+    V, lengths = 0, []
+    while sum(lengths) < N:
+        V += 1
+        lengths.append(V)
+    tokens = np.repeat(np.arange(V), lengths)[:N].astype(np.int32)
+    np.random.default_rng(N).shuffle(tokens)
+    d = _normal(N, (N, 1, H), F32)
+    got = vt.vtrace_vocab_embed_grad(d.cuda(), torch.from_numpy(tokens).cuda().view(N, 1), V)
+    check_grad(d, tokens, V, 1.0, got)
+
+
+@pytest.mark.parametrize("N", [70, 20000])
+def test_steps_without_a_token_alone(N):
+    t = torch.full((N, 1), vt.NO_TOKEN, dtype=torch.int32, device="cuda")
+    d = torch.full((N, 1, 16), float("nan"), device="cuda")
+    assert torch.equal(vt.vtrace_vocab_embed_grad(d, t, 33), torch.zeros(33, 16, device="cuda"))
+    before = torch.randn(33, 16, device="cuda")
+    assert torch.equal(vt.vtrace_vocab_embed_grad(d, t, 33, accumulate_into=before.clone()), before)
+
+
+@pytest.mark.parametrize("N", [100, 20000])
+def test_gradient_of_tokens_outside_the_vocabulary(N):
+    V, H = 12, 24
+    tokens = _tokens(N, N, V)
+    ws = vt.EmbedWorkspace(N, 1, V, H)
+    d = _normal(N, (N, 1, H), F32)
+    vt.vtrace_vocab_embed_grad(d.cuda(), torch.from_numpy(tokens).cuda().view(N, 1), V, workspace=ws)
+    assert vt.vtrace_error_flag(ws) == 0
+    tokens[[3, 50, 99]] = [V, -2, 2 ** 31 - 1]
+    got = vt.vtrace_vocab_embed_grad(d.cuda(), torch.from_numpy(tokens).cuda().view(N, 1), V, workspace=ws)
+    assert vt.vtrace_error_flag(ws) != 0
+    check_grad(d, tokens, V, 1.0, got)  # they add nothing
+
+
+@pytest.mark.parametrize("N", [3000, 30000])
+def test_gradient_is_the_same_in_every_call(N):
+    V, H = 500, 40
+    t = torch.from_numpy(_tokens(N, N, V, "text")).cuda().view(N, 1)
+    d = _normal(N, (N, 1, H), F32).cuda()
+    first = vt.vtrace_vocab_embed_grad(d, t, V)
+    for _ in range(5):
+        assert torch.equal(first, vt.vtrace_vocab_embed_grad(d, t, V))
+
+
+def test_nan_and_infinity_stay_in_their_rows():
+    tokens = np.array([1, 2, 1, 3, 2], dtype=np.int32)
+    d = _normal(0, (5, 1, 16), F32)
+    d[2, 0, 3], d[3, 0, 4] = float("nan"), float("inf")
+    got = vt.vtrace_vocab_embed_grad(d.cuda(), torch.from_numpy(tokens).cuda().view(5, 1), 5).cpu()
+    assert torch.isnan(got[1, 3]) and torch.isinf(got[3, 4]) and torch.isfinite(got).sum() == got.numel() - 2
