@@ -1,0 +1,188 @@
+"""The C ABI of the calls on parameters on the host: exported symbols and argument validation.
+Every call carries an invalid argument, so nothing is launched and the fake pointers are never
+dereferenced."""
+
+import ctypes
+import math
+import os
+import re
+
+import pytest
+import torch
+
+import paper_1802_01561_amd as vt
+from paper_1802_01561_amd import _lib, parameters
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "vtrace_parameters.h")
+OK, NULL, SHAPE, DTYPE, PARAM, ALIGN, WS = 0, 1, 2, 3, 4, 5, 6
+P = 0x10000
+
+
+@pytest.fixture(scope="module")
+def L():
+    return _lib.lib()
+
+
+def test_library_exports_every_declared_symbol(L):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(vtrace_[a-z_]+)\s*\(", text))
+    assert names == set(_lib.PARAMETER_SIGNATURES)
+    assert all(hasattr(L, n) for n in names)
+    assert set(parameters.__all__) <= set(dir(vt))
+
+
+BAD_SHAPES = [dict(T=0), dict(B=0), dict(T=-1, B=-1), dict(V=0), dict(V=(1 << 24) + 1), dict(H=0), dict(H=4), dict(H=12),
+              dict(H=32776), dict(T=1 << 20, B=1 << 6), dict(T=1 << 23, B=1, H=32768), dict(V=1 << 23, H=32768),
+              dict(T=1 << 62, B=1 << 62)]
+
+
+def test_embed_workspace_bytes(L):
+    n = L.vtrace_vocab_embed_grad_workspace_bytes
+    assert 4352 < n(1, 1, 10, 8) < n(100, 32, 10, 8) < n(100000, 32, 10, 8)
+    for kw in BAD_SHAPES:
+        s = {**dict(T=5, B=4, V=100, H=64), **kw}
+        assert n(s["T"], s["B"], s["V"], s["H"]) == 0, kw
+
+
+def _embed(L, **kw):
+    a = dict(T=5, B=4, V=100, H=64, wt=0, et=1, w=P, t=P, s=1.0, e=P, ws=None, n=0)
+    a.update(kw)
+    return L.vtrace_vocab_embed(*(a[k] for k in ("T", "B", "V", "H", "wt", "et", "w", "t", "s", "e", "ws", "n")), None)
+
+
+@pytest.mark.parametrize("kw,status", [(kw, SHAPE) for kw in BAD_SHAPES] + [
+    (dict(w=None), NULL), (dict(t=None), NULL), (dict(e=None), NULL), (dict(wt=2), DTYPE), (dict(et=-1), DTYPE),
+    (dict(s=math.nan), PARAM), (dict(s=math.inf), PARAM), (dict(w=P + 8), ALIGN), (dict(e=P + 4), ALIGN), (dict(t=P + 2), ALIGN),
+    (dict(ws=P + 8, n=256), ALIGN), (dict(ws=P, n=255), WS)])
+def test_embed_rejects(L, kw, status):
+    assert _embed(L, **kw) == status
+
+
+def _grad(L, **kw):
+    a = dict(T=5, B=4, V=100, H=64, et=0, gt=1, d=P, t=P, s=1.0, acc=0, dw=P, ws=P, n=1 << 30)
+    a.update(kw)
+    return L.vtrace_vocab_embed_grad(
+        *(a[k] for k in ("T", "B", "V", "H", "et", "gt", "d", "t", "s", "acc", "dw", "ws", "n")), None)
+
+
+@pytest.mark.parametrize("kw,status", [(kw, SHAPE) for kw in BAD_SHAPES] + [
+    (dict(d=None), NULL), (dict(t=None), NULL), (dict(dw=None), NULL), (dict(et=2), DTYPE), (dict(gt=3), DTYPE),
+    (dict(s=math.nan), PARAM), (dict(s=-math.inf), PARAM), (dict(d=P + 8), ALIGN), (dict(dw=P + 2), ALIGN), (dict(t=P + 1), ALIGN),
+    (dict(ws=None), WS), (dict(ws=P + 8), ALIGN), (dict(n=256), WS)])
+def test_embed_grad_rejects(L, kw, status):
+    assert _grad(L, **kw) == status
+
+
+def test_embed_grad_workspace_is_exact(L):
+    for T, B, V, H in [(1, 1, 100, 64), (5, 40, 1000, 8), (50000, 1, 70000, 8)]:
+        n = L.vtrace_vocab_embed_grad_workspace_bytes(T, B, V, H)
+        assert _grad(L, T=T, B=B, V=V, H=H, n=n - 1) == WS
+
+
+def _array(t, x):
+    return None if x is None else (t * max(1, len(x)))(*x)
+
+
+QUINTIC = [3.4445, -4.775, 2.0315] * 5
+
+
+def _ortho_bytes(L, rows, columns, dtypes, count=None):
+    return L.vtrace_orthogonalize_workspace_bytes(len(rows) if count is None else count, _array(ctypes.c_int64, rows),
+                                                  _array(ctypes.c_int64, columns), _array(ctypes.c_int32, dtypes))
+
+
+def test_orthogonalize_workspace_bytes(L):
+    one = _ortho_bytes(L, [100], [300], [1])
+    assert 4352 < one < _ortho_bytes(L, [100], [300], [0])
+    assert one == _ortho_bytes(L, [300], [100], [1]) == _ortho_bytes(L, [0, 300, 7], [7, 100, 0], [1, 1, 0])
+    assert one < _ortho_bytes(L, [100, 100], [300, 300], [1, 1])
+    # types are worked on in turn: the larger of the two decides
+    assert _ortho_bytes(L, [100, 100], [300, 300], [1, 0]) == _ortho_bytes(L, [100], [300], [0])
+    assert _ortho_bytes(L, [], [], []) > 0
+    for bad in (([-1], [3], [0]), ([3], [-1], [0]), ([65537], [1], [0]), ([65536], [65536], [0]), ([3], [3], [2])):
+        assert _ortho_bytes(L, *bad) == 0, bad
+    assert _ortho_bytes(L, [3], [3], [0], count=-1) == 0 and _ortho_bytes(L, [3], [3], [0], count=(1 << 16) + 1) == 0
+    assert L.vtrace_orthogonalize_workspace_bytes(1, None, None, None) == 0
+
+
+A, B, C, W = 0x1000000, 0x2000000, 0x3000000, 0x4000000
+
+
+def _ortho(L, ins, outs, rows=(8,), columns=(8,), dtypes=(0,), scales=None, steps=5, coefficients=QUINTIC, epsilon=1e-7, ws=W,
+           n=1 << 24, count=None):
+    return L.vtrace_orthogonalize(
+        len(rows) if count is None else count, _array(ctypes.c_void_p, ins), _array(ctypes.c_void_p, outs),
+        _array(ctypes.c_int64, rows), _array(ctypes.c_int64, columns), _array(ctypes.c_int32, dtypes),
+        _array(ctypes.c_float, scales), steps, _array(ctypes.c_float, coefficients), epsilon, ws, n, None)
+
+
+def test_orthogonalize_rejects(L):
+    assert _ortho(L, None, [B]) == NULL
+    assert _ortho(L, [A], None) == NULL
+    assert _ortho(L, [A], [B], coefficients=None) == NULL
+    assert _ortho(L, [None], [B]) == NULL
+    assert _ortho(L, [A], [None]) == NULL
+    assert _ortho(L, [A], [B], count=-1) == SHAPE
+    assert _ortho(L, [A], [B], count=(1 << 16) + 1) == SHAPE
+    assert _ortho(L, [A], [B], rows=[-1]) == SHAPE
+    assert _ortho(L, [A], [B], columns=[65537]) == SHAPE
+    assert _ortho(L, [A], [B], rows=[65536], columns=[65536]) == SHAPE
+    assert _ortho(L, [A], [B], dtypes=[2]) == DTYPE
+    assert _ortho(L, [A], [B], scales=[math.nan]) == PARAM
+    for steps in (0, -1, 65):
+        assert _ortho(L, [A], [B], steps=steps, coefficients=QUINTIC * 20) == PARAM
+    for eps in (0.0, -1.0, math.nan, math.inf):
+        assert _ortho(L, [A], [B], epsilon=eps) == PARAM
+    assert _ortho(L, [A + 2], [B]) == ALIGN
+    assert _ortho(L, [A], [B + 1], dtypes=[1]) == ALIGN
+    assert _ortho(L, [A], [B], ws=None) == WS
+    assert _ortho(L, [A], [B], ws=W + 8) == ALIGN
+    assert _ortho(L, [A], [B], n=_ortho_bytes(L, [8], [8], [0]) - 1) == WS
+    # outputs that overlap something: another output, another matrix, their own in part, the workspace
+    two = dict(rows=[8, 8], columns=[8, 8], dtypes=[0, 0])
+    assert _ortho(L, [A, C], [B, B + 252], **two) == PARAM
+    assert _ortho(L, [A, A], [A, A], **two) == PARAM
+    assert _ortho(L, [A, B], [C, A + 8], **two) == PARAM
+    assert _ortho(L, [A], [A + 8]) == PARAM
+    assert _ortho(L, [A], [W + (1 << 20)]) == PARAM
+    assert _ortho(L, [W + 64], [B]) == PARAM
+
+
+@pytest.mark.parametrize("coefficients", [
+    [math.nan, 0, 0], [1, math.inf, 0], [4, 0, 0],  # singular values of 4
+    [1.5, -13, 0],  # eigenvalues of b A over a range of 13
+    [0, 0, 12.5], [3.4445, -4.775, 2.0315] * 4 + [3.0, 5.0, 3.0], [3.4, 0, 0] * 2, [2.0, 1.0, 1.0]])
+def test_orthogonalize_rejects_steps_that_leave_the_operands_range(L, coefficients):
+    assert _ortho(L, [A], [B], steps=len(coefficients) // 3, coefficients=coefficients) == PARAM
+
+
+@pytest.mark.parametrize("coefficients", [[1.5, -0.5, 0], [1.875, -1.25, 0.375], [8.2872, -23.5959, 17.3004], [1, 0, 0], [3.4445, -4.775, 2.0315]])
+def test_orthogonalize_takes_other_steps(L, coefficients):
+    """As many as go on behind them: the refusal here is the missing workspace."""
+    assert _ortho(L, [A], [B], steps=4, coefficients=[1.5, -0.5, 0] * 3 + coefficients, ws=None) == WS
+
+
+def test_python_binding_validates_before_calling():
+    w, t = torch.zeros(10, 64), torch.zeros(2, 3, dtype=torch.int32)
+    d, m = torch.zeros(2, 3, 64), torch.zeros(4, 5)
+    for call in (lambda: vt.vtrace_vocab_embed(w, t), lambda: vt.vtrace_vocab_embed(w[0], t),
+                 lambda: vt.vtrace_vocab_embed(w, t, out_dtype=torch.float16), lambda: vt.vtrace_vocab_embed(w.half(), t),
+                 lambda: vt.vtrace_vocab_embed_grad(d, t, 10), lambda: vt.vtrace_vocab_embed_grad(d[0], t, 10),
+                 lambda: vt.vtrace_vocab_embed_grad(d, t, 10, grad_dtype=torch.float16),
+                 lambda: vt.vtrace_vocab_embed_grad(d, t, 10, accumulate_into=w, out=w),
+                 lambda: vt.vtrace_orthogonalize([]), lambda: vt.vtrace_orthogonalize([m]),
+                 lambda: vt.vtrace_orthogonalize([m[0]]), lambda: vt.vtrace_orthogonalize([m], out=[]),
+                 lambda: vt.vtrace_orthogonalize([m], [1.0, 2.0]), lambda: vt.vtrace_orthogonalize([m], steps=0),
+                 lambda: vt.vtrace_orthogonalize([m], steps=2.0), lambda: vt.vtrace_orthogonalize([m], steps=True),
+                 lambda: vt.vtrace_orthogonalize([m], coefficients=(1.0, 2.0)),
+                 lambda: vt.vtrace_orthogonalize([m], coefficients=[(1.5, -0.5, 0.0)] * 4),
+                 lambda: vt.EmbedWorkspace(0, 1, 10, 64, device="cpu"), lambda: vt.EmbedWorkspace(1, 1, 10, 64, device="cpu"),
+                 lambda: vt.OrthogonalWorkspace([m])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: vt.vtrace_vocab_embed(None, t), lambda: vt.vtrace_vocab_embed_grad(None, t, 10),
+                 lambda: vt.vtrace_vocab_embed_grad(d, t, 10, out=1.0), lambda: vt.vtrace_orthogonalize([1.0]),
+                 lambda: vt.vtrace_orthogonalize([m.half()])):
+        with pytest.raises(TypeError):
+            call()
