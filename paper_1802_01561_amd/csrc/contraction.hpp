@@ -76,6 +76,11 @@ __device__ __forceinline__ void copy_to_lds(Rsrc r, char* lds, uint32_t offset) 
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)lds, 16, offset, 0, 0, 0);
 }
 
+// The same from `ahead` bytes behind the descriptor's base on, which are the same for all lanes.
+__device__ __forceinline__ void copy_to_lds(Rsrc r, char* lds, uint32_t offset, int ahead) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)lds, 16, offset, ahead, 0, 0);
+}
+
 __device__ __forceinline__ int swizzle_of(int r) { return (r & 3) | ((r >> 1) & 4); }
 
 // Copies one operand's tiles of kRows x 64 to LDS (by kWaves waves), step after step along k.

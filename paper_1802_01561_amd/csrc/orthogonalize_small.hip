@@ -1,0 +1,252 @@
+// The products of Newton-Schulz steps for matrices too small or too few to fill the chip with
+// tiles of 128: a workgroup of four waves for each 64 x 64 or 32 x 32 of the result.
+//
+// Everything here is latency, so that what counts are bytes in flight: operands are copied
+// straight to LDS, kStages steps of 64 k ahead.  (Fragments read from memory into registers, a
+// 16-byte piece of 16 rows each, make 64 requests where these make 8: 1024 x 1024 in 16 us a
+// product.)  All three products have both operands' k innermost, which for the last one, B X,
+// takes X^T, kept beside X.
+#include "orthogonalize_impl.hpp"
+
+namespace vtrace {
+namespace {
+
+// Until an accumulator's last product is written (mfma).
+__device__ __forceinline__ void wait_for_product(f32x4& c) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c)); }
+
+constexpr int kSmallWaves = 4, kSmallThreads = kSmallWaves * kWave;
+// Steps of k in LDS, of two operands in `parts` parts.
+__host__ __device__ constexpr int small_stages(int side, int parts) { return side == 64 ? 6 - parts : parts == 1 ? 8 : 5; }
+
+// kKind 0: A from X; 1: B from A; 2: X, or of the last step the result.  Wave (wm, wn) has a
+// quarter of the tile; a lane of the MFMA layout holds columns j + 16 m + 4 g + 0..3 of row
+// i + 16 n + s of that.
+template <int kKind, typename Out, bool kLast, int kSide>
+__global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int turn, OrthoStep step) {
+  constexpr bool kPair = sizeof(Out) == 4;
+  constexpr int kParts = kPair ? 2 : 1, kN = kSide / 32;
+  constexpr int kStages = small_stages(kSide, kParts), kBytes = kSide * kTileK * 2, kStage = 2 * kParts * kBytes;
+  __shared__ __align__(1024) char lds[kStages * kStage];
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int s = lane % 16, g = lane / 16;
+  const Entry& e = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_tile[kKind]; })];
+  const int id = blockIdx.x - e.first_tile[kKind];
+  TileAt at;
+  if constexpr (kKind < 2) {
+    at = triangle_at(id);
+  } else {
+    const int rows = e.pr / kSide;
+    at = {id % rows, id / rows};
+  }
+  const Pieces p = pieces_of<kPair>(e, turn);
+  const TransposedPieces pt = transposed_of<kPair>(e, turn);
+  const int64_t pitch = kKind == 0 ? e.pc : e.pr;
+  const int steps = static_cast<int>(pitch / kTileK);
+
+  // A descriptor for each operand, at its tile's rows, and where in it the steps begin; rows
+  // behind the last one arrive as zeros.
+  typedef Loader<kSide, kSmallWaves> Places;
+  Places places[2];
+  Rsrc operand[kParts][2], nothing[kParts][2];
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    const int64_t first = static_cast<int64_t>(o == 0 ? at.wide : at.deep) * kSide;
+    const int64_t rows = (kKind == 2 && o == 1 ? e.c : e.r) - first;
+    places[o].along(pitch, static_cast<int>(rows < kSide ? rows : kSide), wave, lane);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const uint16_t* const array = kKind == 0 ? p.from[k] : kKind == 1 ? p.a[k] : o == 0 ? p.b[k] : pt.from[k];
+      operand[k][o] = make_rsrc(array + first * pitch, 0x7fffffff);
+      nothing[k][o] = make_rsrc(array, 0);
+    }
+  }
+  auto copy = [&](int stage, int step) {
+    const bool more = step < steps;
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        char* const to = lds + stage * kStage + (2 * k + o) * kBytes + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < Places::kCopies; ++i)
+          copy_to_lds(more ? operand[k][o] : nothing[k][o], to + i * Places::kCopyBytes, places[o].off[i],
+                      more ? step * (kTileK * 2) : 0);
+      }
+  };
+  constexpr int kCopies = 2 * kParts * Places::kCopies;
+  const int wm = (wave % 2) * (kSide / 2), wn = (wave / 2) * (kSide / 2);
+  Reader<false, false, kN, kSide> ri, rj;
+  ri.start(wn, s, g);
+  rj.start(wm, s, g);
+  f32x4 acc[kN][kN] = {};  // [m][n]
+  const int i0 = at.wide * kSide + wn + s, j0 = at.deep * kSide + wm + 4 * g;
+  // What the results take beside the products is under way before them.
+  f32x4 x[kN][kN];
+  v2u o[kParts][kN][kN];
+  float of_row[kN];
+  f32x4 of_column[kN];
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    const int i = i0 + 16 * n, i_in = i < e.r ? i : e.r - 1;  // rows behind the last one: nobody stores them
+    if constexpr (kKind == 1) of_row[n] = p.d[i_in];
+    if constexpr (kKind == 2) of_row[n] = p.e[i_in];
+#pragma unroll
+    for (int m = 0; m < kN; ++m) {
+      const int j = j0 + 16 * m;
+      if constexpr (kKind == 1) {
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) o[k][m][n] = *reinterpret_cast<const v2u*>(p.a[k] + static_cast<int64_t>(i_in) * e.pr + j);
+      }
+      if constexpr (kKind == 2) x[m][n] = *reinterpret_cast<const f32x4*>(p.x + static_cast<int64_t>(i_in) * e.pc + j);
+    }
+  }
+  if constexpr (kKind == 1) {
+#pragma unroll
+    for (int m = 0; m < kN; ++m)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = j0 + 16 * m + q;
+        of_column[m][q] = p.d[j < e.r ? j : e.r - 1];
+      }
+  }
+#pragma unroll
+  for (int k = 0; k + 1 < kStages; ++k) copy(k, k);
+  int stage = 0;
+  for (int k = 0; k < steps; ++k) {
+    stage_barrier<(kStages - 2) * kCopies>();
+    copy(stage == 0 ? kStages - 1 : stage - 1, k + kStages - 1);
+    const char* const from = lds + stage * kStage;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      bf16x8 fi[kParts][kN], fj[kParts][kN];
+#pragma unroll
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          fi[part][n] = ri.read(from + 2 * part * kBytes, n, kk);
+          fj[part][n] = rj.read(from + (2 * part + 1) * kBytes, n, kk);
+        }
+#pragma unroll
+      for (int m = 0; m < kN; ++m)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          if constexpr (kPair) {
+            mfma<true>(acc[m][n], fj[1][m], fi[0][n]);
+            mfma<true>(acc[m][n], fj[0][m], fi[1][n]);
+          }
+          mfma<true>(acc[m][n], fj[0][m], fi[0][n]);
+        }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  }
+
+  // Until the last products are written.
+#pragma unroll
+  for (int m = 0; m < kN; ++m)
+#pragma unroll
+    for (int n = 0; n < kN; ++n) wait_for_product(acc[m][n]);
+  // The tile by way of LDS, so that rows and columns of it are stored in whole pieces.
+  stage_barrier();
+  float(*const s_y)[kSide + 1] = reinterpret_cast<float(*)[kSide + 1]>(lds);
+#pragma unroll
+  for (int n = 0; n < kN; ++n)
+#pragma unroll
+    for (int m = 0; m < kN; ++m)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = i0 + 16 * n, j = j0 + 16 * m + q;
+        const bool in = i < e.r && j < (kKind == 2 ? e.c : e.r);
+        const float sum = element(acc[m][n], q);
+        float y;
+        if constexpr (kKind == 0) {
+          y = sum * (1.0f / (kScaleX * kScaleX));
+          if (in && i == j) p.d[i] = y;
+        } else if constexpr (kKind == 1) {
+          const float oo = sum * (1.0f / (kScaleA * kScaleA)), di = of_row[n];
+          float off = half_value(static_cast<uint16_t>(o[0][m][n][q / 2] >> (16 * (q % 2))));
+          if constexpr (kPair) off += half_value(static_cast<uint16_t>(o[1][m][n][q / 2] >> (16 * (q % 2))));
+          y = fmaf(off * (1.0f / kScaleA), fmaf(step.c, di + of_column[m][q], step.b), step.c * oo);
+          if (in && i == j) p.e[i] = fmaf(step.b, di, step.c * fmaf(di, di, oo));
+        } else {
+          y = fmaf(step.a + of_row[n], x[m][n][q], sum * (1.0f / (kScaleA * kScaleX)));
+        }
+        s_y[wn + s + 16 * n][wm + 4 * g + 16 * m + q] = in && (kKind == 2 || i != j) ? y : 0.0f;
+      }
+  __syncthreads();
+
+  constexpr int kQuads = kSide / 4;
+  const int r0 = at.wide * kSide, c0 = at.deep * kSide;
+  // An operand's four elements from `at` on.
+  auto store_operand = [&](uint16_t* const (&out)[2], int64_t to, float (&y)[4], float scale) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] *= scale;
+    v2u part[2];
+    split4<kPair>(y, &part[0], &part[1]);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) *reinterpret_cast<v2u*>(out[k] + to) = part[k];
+  };
+#pragma unroll
+  for (int w = 0; w < kSide * kQuads / kSmallThreads; ++w) {
+    const int id = w * kSmallThreads + threadIdx.x, y0 = id / kQuads, x0 = id % kQuads * 4;
+    // Along the tile's rows.
+    if (r0 + y0 < e.r && !(kLast && e.transposed)) {
+      const int i = r0 + y0, j = c0 + x0;
+      float y[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] = s_y[y0][x0 + q];
+      if constexpr (kLast) {
+        Out* const out = static_cast<Out*>(e.out);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] *= e.scale;
+        store_result(out + static_cast<int64_t>(i) * e.c + j, y, e.c - j,
+                     e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
+      } else if constexpr (kKind == 2) {
+        const int64_t to = static_cast<int64_t>(i) * e.pc + j;
+        *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
+        store_operand(p.to, to, y, kScaleX);
+      } else {
+        store_operand(kKind == 0 ? p.a : p.b, static_cast<int64_t>(i) * e.pr + j, y, kScaleA);
+      }
+    }
+    // And along its columns: the other half of a symmetric result, or X^T.
+    if ((kKind < 2 && at.wide == at.deep) || c0 + y0 >= (kKind == 2 ? e.c : e.r)) continue;
+    const int j = c0 + y0, i = r0 + x0;
+    float y[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = s_y[x0 + q][y0];
+    if constexpr (kLast) {
+      if (!e.transposed) continue;
+      Out* const out = static_cast<Out*>(e.out);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] *= e.scale;
+      store_result(out + static_cast<int64_t>(j) * e.r + i, y, e.r - i,
+                   e.r % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
+    } else {
+      store_operand(kKind == 0 ? p.a : kKind == 1 ? p.b : pt.to, static_cast<int64_t>(j) * e.pr + i, y, kKind == 2 ? kScaleX : kScaleA);
+    }
+  }
+}
+
+template <int kKind, typename Out, bool kLast>
+hipError_t launch_kind(const Table& t, int turn, const OrthoStep& p, hipStream_t st) {
+  const dim3 grid(t.total_tiles[kKind]), block(kSmallThreads);
+  if (t.size[kKind] == 32) hipLaunchKernelGGL((ortho_small_kernel<kKind, Out, kLast, 32>), grid, block, 0, st, t, turn, p);
+  else hipLaunchKernelGGL((ortho_small_kernel<kKind, Out, kLast, 64>), grid, block, 0, st, t, turn, p);
+  return hipGetLastError();
+}
+
+template <typename Out>
+hipError_t launch_type(const Table& t, int kind, bool last, int turn, const OrthoStep& p, hipStream_t st) {
+  if (kind == 0) return launch_kind<0, Out, false>(t, turn, p, st);
+  if (kind == 1) return launch_kind<1, Out, false>(t, turn, p, st);
+  return last ? launch_kind<2, Out, true>(t, turn, p, st) : launch_kind<2, Out, false>(t, turn, p, st);
+}
+
+}  // namespace
+
+hipError_t launch_ortho_small(const Table& t, int kind, bool pair, bool last, int turn, const OrthoStep& p, hipStream_t st) {
+  return pair ? launch_type<float>(t, kind, last, turn, p, st) : launch_type<uint16_t>(t, kind, last, turn, p, st);
+}
+
+}  // namespace vtrace
