@@ -11,8 +11,11 @@
 namespace vtrace {
 namespace {
 
-// Until an accumulator's last product is written (mfma).
-__device__ __forceinline__ void wait_for_product(f32x4& c) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c)); }
+// Until the last products are written (mfma).
+__device__ __forceinline__ void wait_for_products(f32x4 (&c)[1][1]) { asm volatile("s_nop 15" : "+a"(c[0][0])); }
+__device__ __forceinline__ void wait_for_products(f32x4 (&c)[2][2]) {
+  asm volatile("s_nop 15" : "+a"(c[0][0]), "+a"(c[0][1]), "+a"(c[1][0]), "+a"(c[1][1]));
+}
 
 constexpr int kSmallWaves = 4, kSmallThreads = kSmallWaves * kWave;
 // Steps of k in LDS, of two operands in `parts` parts.
@@ -80,6 +83,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
   ri.start(wn, s, g);
   rj.start(wm, s, g);
   f32x4 acc[kN][kN] = {};  // [m][n]
+  f32x4 total[kN][kN] = {};
   const int i0 = at.wide * kSide + wn + s, j0 = at.deep * kSide + wm + 4 * g;
   // What the results take beside the products is under way before them.
   f32x4 x[kN][kN];
@@ -139,13 +143,22 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
         }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
+    // Float32 results: sums over 256 k apiece, added up.  The rounding errors of one long sum would
+    // be the most of a result's (256 x 2592: 1.6e-6 off, so 1.0e-6).
+    if (kPair && k % 4 == 3 && k + 1 < steps) {
+      wait_for_products(acc);
+#pragma unroll
+      for (int m = 0; m < kN; ++m)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) total[m][n][q] += element(acc[m][n], q);
+          acc[m][n] = f32x4{};
+        }
+    }
   }
 
-  // Until the last products are written.
-#pragma unroll
-  for (int m = 0; m < kN; ++m)
-#pragma unroll
-    for (int n = 0; n < kN; ++n) wait_for_product(acc[m][n]);
+  wait_for_products(acc);
   // The tile by way of LDS, so that rows and columns of it are stored in whole pieces.
   stage_barrier();
   float(*const s_y)[kSide + 1] = reinterpret_cast<float(*)[kSide + 1]>(lds);
@@ -157,7 +170,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
       for (int q = 0; q < 4; ++q) {
         const int i = i0 + 16 * n, j = j0 + 16 * m + q;
         const bool in = i < e.r && j < (kKind == 2 ? e.c : e.r);
-        const float sum = element(acc[m][n], q);
+        const float sum = total[m][n][q] + element(acc[m][n], q);
         float y;
         if constexpr (kKind == 0) {
           y = sum * (1.0f / (kScaleX * kScaleX));
