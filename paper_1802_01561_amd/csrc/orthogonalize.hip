@@ -126,13 +126,12 @@ __global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t) {
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = s_tile[k][j + q];
-    *reinterpret_cast<f32x4*>(p.x + at) = f32x4{v[0], v[1], v[2], v[3]};
+    if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + at) = f32x4{v[0], v[1], v[2], v[3]};
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] *= kScaleX;
-    v2u high, low;
-    split4<kPair>(v, &high, &low);
+    const v2u high = high4(v);
     *reinterpret_cast<v2u*>(p.to[0] + at) = high;
-    if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + at) = low;
+    *reinterpret_cast<v2u*>((kPair ? p.to[1] : p.low) + at) = low4(v, high);
   }
   if (!t.small) return;
   const TransposedPieces pt = transposed_of<kPair>(g, 1);
@@ -142,10 +141,9 @@ __global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t) {
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = s_tile[j + q][k] * kScaleX;
-    v2u high, low;
-    split4<kPair>(v, &high, &low);
+    const v2u high = high4(v);
     *reinterpret_cast<v2u*>(pt.to[0] + at) = high;
-    if constexpr (kPair) *reinterpret_cast<v2u*>(pt.to[1] + at) = low;
+    if constexpr (kPair) *reinterpret_cast<v2u*>(pt.to[1] + at) = low4(v, high);
   }
 }
 
@@ -304,7 +302,7 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
     }
     e = launch_ortho_tiles_symmetric(t, false, kPair, t.size[0], turn, steps[k], st);
     if (e == hipSuccess) e = launch_ortho_tiles_symmetric(t, true, kPair, t.size[1], turn, steps[k], st);
-    if (e == hipSuccess) e = launch_ortho_tiles_update(t, kPair, last, t.size[2], turn, steps[k], st);
+    if (e == hipSuccess) e = launch_ortho_tiles_update(t, kPair, step_count - 1 - k, t.size[2], turn, steps[k], st);
   }
   return e;
 }

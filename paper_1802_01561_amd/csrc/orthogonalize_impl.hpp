@@ -38,8 +38,9 @@ struct Table {
 static_assert(sizeof(Table) <= 4000, "kernel arguments");
 
 struct Pieces {
-  float* x;           // [r, pc] X
-  uint16_t* from[2];  // [r, pc] X as an operand: high and low parts
+  float* x;           // [r, pc] X, of float32 matrices
+  uint16_t* low;      // [r, pc] of bfloat16 ones what the operand leaves of X
+  uint16_t* from[2];  // [r, pc] X as an operand: high and (float32 matrices) low parts
   uint16_t* to[2];    // [r, pc] the same behind this step
   uint16_t* a[2];     // [r, pr] A without its diagonal
   uint16_t* b[2];     // B without its diagonal
@@ -49,7 +50,8 @@ struct Pieces {
 __host__ __device__ inline int64_t round_up(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 template <bool kPair>
 __host__ __device__ inline int64_t piece_bytes(int64_t r, int64_t pr, int64_t pc) {
-  return r * pc * (4 + 2 * 2 * (kPair ? 2 : 1)) + r * pr * 2 * 2 * (kPair ? 2 : 1) + 2 * round_up(r * 4, 256);
+  constexpr int kParts = kPair ? 2 : 1;
+  return r * pc * (2 * kParts + 2 * 2 * kParts) + r * pr * 2 * 2 * kParts + 2 * round_up(r * 4, 256);
 }
 // Behind them, for the small matrices' kernels: X^T as an operand, before and after a step.
 template <bool kPair>
@@ -63,25 +65,18 @@ __device__ __forceinline__ Pieces pieces_of(const Entry& t, int turn) {
   constexpr int kParts = kPair ? 2 : 1;
   Pieces p;
   char* at = t.base;
-  const int64_t x = static_cast<int64_t>(t.r) * t.pc, a = static_cast<int64_t>(t.r) * t.pr;
+  const int64_t x = static_cast<int64_t>(t.r) * t.pc * 2, a = static_cast<int64_t>(t.r) * t.pr * 2;
   p.x = reinterpret_cast<float*>(at);
-  at += x * 4;
+  p.low = reinterpret_cast<uint16_t*>(at);
+  at += x * kParts;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    p.from[k] = reinterpret_cast<uint16_t*>(at + (turn * kParts + (kPair ? k : 0)) * x * 2);
-    p.to[k] = reinterpret_cast<uint16_t*>(at + ((turn ^ 1) * kParts + (kPair ? k : 0)) * x * 2);
+    p.from[k] = reinterpret_cast<uint16_t*>(at + (turn * kParts + (kPair ? k : 0)) * x);
+    p.to[k] = reinterpret_cast<uint16_t*>(at + ((turn ^ 1) * kParts + (kPair ? k : 0)) * x);
+    p.a[k] = reinterpret_cast<uint16_t*>(at + 2 * kParts * x + (kPair ? k : 0) * a);
+    p.b[k] = reinterpret_cast<uint16_t*>(at + 2 * kParts * x + (kParts + (kPair ? k : 0)) * a);
   }
-  at += 2 * kParts * x * 2;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    p.a[k] = reinterpret_cast<uint16_t*>(at);
-    if (k < kParts) at += a * 2;
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    p.b[k] = reinterpret_cast<uint16_t*>(at);
-    if (k < kParts) at += a * 2;
-  }
+  at += 2 * kParts * (x + a);
   p.d = reinterpret_cast<float*>(at);
   p.e = reinterpret_cast<float*>(at + round_up(static_cast<int64_t>(t.r) * 4, 256));
   return p;
@@ -120,21 +115,18 @@ __device__ __forceinline__ int entry_of(const Table& t, int id, First first) {
 __device__ __forceinline__ uint16_t half_bits(float x) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(x)); }
 __device__ __forceinline__ float half_value(uint16_t bits) { return static_cast<float>(__builtin_bit_cast(_Float16, bits)); }
 
-// Four consecutive values as operands: float16, and (kPair) what that leaves of them.
-template <bool kPair>
-__device__ __forceinline__ void split4(const float (&y)[4], v2u* high, v2u* low) {
-  uint16_t h[4], l[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h[i] = half_bits(y[i]);
-    l[i] = kPair ? half_bits(y[i] - half_value(h[i])) : 0;
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    (*high)[i] = h[2 * i] | static_cast<unsigned>(h[2 * i + 1]) << 16;
-    (*low)[i] = l[2 * i] | static_cast<unsigned>(l[2 * i + 1]) << 16;
-  }
+// Two values as operands: float16, and what that leaves of them (twice half a step of
+// float16: 22 bits together).
+__device__ __forceinline__ unsigned high2(float x, float y) {
+  return half_bits(x) | static_cast<unsigned>(half_bits(y)) << 16;
 }
+__device__ __forceinline__ float high_of(unsigned pair, int i) { return half_value(static_cast<uint16_t>(pair >> (16 * i))); }
+__device__ __forceinline__ unsigned low2(float x, float y, unsigned high) {
+  return high2(x - high_of(high, 0), y - high_of(high, 1));
+}
+// Four.
+__device__ __forceinline__ v2u high4(const float (&y)[4]) { return {high2(y[0], y[1]), high2(y[2], y[3])}; }
+__device__ __forceinline__ v2u low4(const float (&y)[4], v2u high) { return {low2(y[0], y[1], high[0]), low2(y[2], y[3], high[1])}; }
 
 // Tile `id` of a lower triangle: rows 0, 1 1, 2 2 2, ...
 __device__ __forceinline__ TileAt triangle_at(int id) {
@@ -172,7 +164,8 @@ __device__ __forceinline__ void store_result(Out* p, const float (&y)[4], int le
 // `pair`: float32 matrices.
 hipError_t launch_ortho_tiles_symmetric(const Table& t, bool square, bool pair, int size, int turn, const OrthoStep& p,
                                         hipStream_t s);
-hipError_t launch_ortho_tiles_update(const Table& t, bool pair, bool last, int size, int turn, const OrthoStep& p, hipStream_t s);
+// `left`: steps that follow.
+hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int left, int size, int turn, const OrthoStep& p, hipStream_t s);
 hipError_t launch_ortho_small(const Table& t, int kind, bool pair, bool last, int turn, const OrthoStep& p, hipStream_t s);
 
 }  // namespace vtrace

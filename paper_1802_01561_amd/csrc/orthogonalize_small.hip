@@ -11,10 +11,11 @@
 namespace vtrace {
 namespace {
 
-// Until the last products are written (mfma).
-__device__ __forceinline__ void wait_for_products(f32x4 (&c)[1][1]) { asm volatile("s_nop 15" : "+a"(c[0][0])); }
-__device__ __forceinline__ void wait_for_products(f32x4 (&c)[2][2]) {
-  asm volatile("s_nop 15" : "+a"(c[0][0]), "+a"(c[0][1]), "+a"(c[1][0]), "+a"(c[1][1]));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// The compiler's own instruction, whose latency it knows: here accumulators move at the loop's end.
+__device__ __forceinline__ void multiply_add(f32x4& c, bf16x8 a, bf16x8 b) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 constexpr int kSmallWaves = 4, kSmallThreads = kSmallWaves * kWave;
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
   const int i0 = at.wide * kSide + wn + s, j0 = at.deep * kSide + wm + 4 * g;
   // What the results take beside the products is under way before them.
   f32x4 x[kN][kN];
-  v2u o[kParts][kN][kN];
+  v2u o[2][kN][kN];  // of A, or of X: high and low parts
   float of_row[kN];
   f32x4 of_column[kN];
 #pragma unroll
@@ -102,7 +103,15 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
 #pragma unroll
         for (int k = 0; k < kParts; ++k) o[k][m][n] = *reinterpret_cast<const v2u*>(p.a[k] + static_cast<int64_t>(i_in) * e.pr + j);
       }
-      if constexpr (kKind == 2) x[m][n] = *reinterpret_cast<const f32x4*>(p.x + static_cast<int64_t>(i_in) * e.pc + j);
+      if constexpr (kKind == 2) {
+        const int64_t from = static_cast<int64_t>(i_in) * e.pc + j;
+        if constexpr (kPair) {
+          x[m][n] = *reinterpret_cast<const f32x4*>(p.x + from);
+        } else {
+          o[0][m][n] = *reinterpret_cast<const v2u*>(p.from[0] + from);
+          o[1][m][n] = *reinterpret_cast<const v2u*>(p.low + from);
+        }
+      }
     }
   }
   if constexpr (kKind == 1) {
@@ -136,29 +145,27 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
           if constexpr (kPair) {
-            mfma<true>(acc[m][n], fj[1][m], fi[0][n]);
-            mfma<true>(acc[m][n], fj[0][m], fi[1][n]);
+            multiply_add(acc[m][n], fj[1][m], fi[0][n]);
+            multiply_add(acc[m][n], fj[0][m], fi[1][n]);
           }
-          mfma<true>(acc[m][n], fj[0][m], fi[0][n]);
+          multiply_add(acc[m][n], fj[0][m], fi[0][n]);
         }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
     // Float32 results: sums over 256 k apiece, added up.  The rounding errors of one long sum would
     // be the most of a result's (256 x 2592: 1.6e-6 off, so 1.0e-6).
     if (kPair && k % 4 == 3 && k + 1 < steps) {
-      wait_for_products(acc);
-#pragma unroll
+    #pragma unroll
       for (int m = 0; m < kN; ++m)
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) total[m][n][q] += element(acc[m][n], q);
+          for (int q = 0; q < 4; ++q) total[m][n][q] += acc[m][n][q];
           acc[m][n] = f32x4{};
         }
     }
   }
 
-  wait_for_products(acc);
   // The tile by way of LDS, so that rows and columns of it are stored in whole pieces.
   stage_barrier();
   float(*const s_y)[kSide + 1] = reinterpret_cast<float(*)[kSide + 1]>(lds);
@@ -170,19 +177,22 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
       for (int q = 0; q < 4; ++q) {
         const int i = i0 + 16 * n, j = j0 + 16 * m + q;
         const bool in = i < e.r && j < (kKind == 2 ? e.c : e.r);
-        const float sum = total[m][n][q] + element(acc[m][n], q);
+        const float sum = total[m][n][q] + acc[m][n][q];
         float y;
         if constexpr (kKind == 0) {
           y = sum * (1.0f / (kScaleX * kScaleX));
           if (in && i == j) p.d[i] = y;
         } else if constexpr (kKind == 1) {
           const float oo = sum * (1.0f / (kScaleA * kScaleA)), di = of_row[n];
-          float off = half_value(static_cast<uint16_t>(o[0][m][n][q / 2] >> (16 * (q % 2))));
-          if constexpr (kPair) off += half_value(static_cast<uint16_t>(o[1][m][n][q / 2] >> (16 * (q % 2))));
+          float off = high_of(o[0][m][n][q / 2], q % 2);
+          if constexpr (kPair) off += high_of(o[1][m][n][q / 2], q % 2);
           y = fmaf(off * (1.0f / kScaleA), fmaf(step.c, di + of_column[m][q], step.b), step.c * oo);
           if (in && i == j) p.e[i] = fmaf(step.b, di, step.c * fmaf(di, di, oo));
         } else {
-          y = fmaf(step.a + of_row[n], x[m][n][q], sum * (1.0f / (kScaleA * kScaleX)));
+          float before;
+          if constexpr (kPair) before = x[m][n][q];
+          else before = (high_of(o[0][m][n][q / 2], q % 2) + high_of(o[1][m][n][q / 2], q % 2)) * (1.0f / kScaleX);
+          y = fmaf(step.a + of_row[n], before, sum * (1.0f / (kScaleA * kScaleX)));
         }
         s_y[wn + s + 16 * n][wm + 4 * g + 16 * m + q] = in && (kKind == 2 || i != j) ? y : 0.0f;
       }
@@ -190,14 +200,13 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
 
   constexpr int kQuads = kSide / 4;
   const int r0 = at.wide * kSide, c0 = at.deep * kSide;
-  // An operand's four elements from `at` on.
-  auto store_operand = [&](uint16_t* const (&out)[2], int64_t to, float (&y)[4], float scale) {
+  // Four elements of an operand, and what it leaves of them where that is wanted.
+  auto store_operand = [&](uint16_t* high_out, uint16_t* low_out, int64_t to, float (&y)[4], float scale) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) y[q] *= scale;
-    v2u part[2];
-    split4<kPair>(y, &part[0], &part[1]);
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) *reinterpret_cast<v2u*>(out[k] + to) = part[k];
+    const v2u high = high4(y);
+    *reinterpret_cast<v2u*>(high_out + to) = high;
+    if (low_out != nullptr) *reinterpret_cast<v2u*>(low_out + to) = low4(y, high);
   };
 #pragma unroll
   for (int w = 0; w < kSide * kQuads / kSmallThreads; ++w) {
@@ -216,10 +225,11 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
                      e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
       } else if constexpr (kKind == 2) {
         const int64_t to = static_cast<int64_t>(i) * e.pc + j;
-        *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
-        store_operand(p.to, to, y, kScaleX);
+        if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
+        store_operand(p.to[0], kPair ? p.to[1] : p.low, to, y, kScaleX);
       } else {
-        store_operand(kKind == 0 ? p.a : p.b, static_cast<int64_t>(i) * e.pr + j, y, kScaleA);
+        uint16_t* const* const out = kKind == 0 ? p.a : p.b;
+        store_operand(out[0], kPair ? out[1] : nullptr, static_cast<int64_t>(i) * e.pr + j, y, kScaleA);
       }
     }
     // And along its columns: the other half of a symmetric result, or X^T.
@@ -236,7 +246,8 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
       store_result(out + static_cast<int64_t>(j) * e.r + i, y, e.r - i,
                    e.r % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
     } else {
-      store_operand(kKind == 0 ? p.a : kKind == 1 ? p.b : pt.to, static_cast<int64_t>(j) * e.pr + i, y, kKind == 2 ? kScaleX : kScaleA);
+      uint16_t* const* const out = kKind == 0 ? p.a : kKind == 1 ? p.b : pt.to;
+      store_operand(out[0], kPair ? out[1] : nullptr, static_cast<int64_t>(j) * e.pr + i, y, kKind == 2 ? kScaleX : kScaleA);
     }
   }
 }

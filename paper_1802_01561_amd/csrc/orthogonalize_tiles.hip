@@ -14,13 +14,25 @@ struct Place {
   int i, j;
 };
 
+// A wave's 32 rows of half a tile's columns, to be read turned: 32-byte pieces exchanged within a row
+// as in the stages, so that both kinds of access fall on all banks.
+template <int kSize>
+__device__ __forceinline__ int turned_swizzle(int row) {
+  return swizzle_of(row) & (kSize / 32 - 1);
+}
+__device__ __forceinline__ s16x4 transposed_read(const char* lds) {
+  typedef __attribute__((address_space(3))) s16x4* LdsVec;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)lds);
+}
+
 // A (kSquare false, from X) or B (true, from A): the tiles (i, j), j <= i, of a symmetric
 // product M M^T, M's rows "along" for both operands.  A lane of the MFMA layout holds columns
 // j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
 template <bool kSquare, bool kPair, int kSize>
 __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_symmetric_kernel(Table t, int turn, float b, float c) {
   constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = kSquare ? 1 : 0;
-  __shared__ __align__(1024) char lds[tile_lds(kSize)];
+  constexpr int kTurnedBytes = 32 * kSize;  // of a wave: 32 rows of kSize / 2 columns, or 16 of both parts
+  __shared__ __align__(1024) char lds[tile_lds(kSize) + 4 * kTurnedBytes];
   Tiles tiles(t.total_tiles[kKind]);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -69,62 +81,100 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
     });
     const Entry& e = t.at[here.entry];
     const Pieces p = pieces_of<kPair>(e, turn);
-    const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 8 * g;
+    const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2);
     const bool mirrored = here.i != here.j;
-    uint16_t* const high = kSquare ? p.b[0] : p.a[0];
-    uint16_t* const low = kSquare ? p.b[1] : p.a[1];
-    float* const diagonal = kSquare ? p.e : p.d;
+    uint16_t* const* const out = kSquare ? p.b : p.a;
+    char* const turned = lds + tile_lds(kSize) + wave * kTurnedBytes;
+    // Eight elements of a row of A, as they lie.
+    auto load_row = [&](v4u (&o)[kPair ? 2 : 1][kMT / 2], int n) {
+      const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
+#pragma unroll
+      for (int m = 0; m < kMT / 2; ++m) {
+        const int j = j0 + 8 * g + 32 * m;
+        const int64_t at = static_cast<int64_t>(i) * e.pr + (j < e.pr ? j : 0);
+        o[0][m] = *reinterpret_cast<const v4u*>(p.a[0] + at);
+        if constexpr (kPair) o[1][m] = *reinterpret_cast<const v4u*>(p.a[1] + at);
+      }
+    };
+    v4u o[2][kPair ? 2 : 1][kMT / 2];
+    float dj[kMT / 2][8];
+    if constexpr (kSquare) {
+      load_row(o[0], 0);
+#pragma unroll
+      for (int m = 0; m < kMT / 2; ++m)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int j = j0 + 8 * g + 32 * m + q;
+          dj[m][q] = p.d[j < e.r ? j : e.r - 1];
+        }
+    }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
       const int i = i0 + 16 * n + s;
       const bool row = i < e.r;
       float di = 0.0f;
-      if constexpr (kSquare) di = row ? p.d[i] : 0.0f;
+      if constexpr (kSquare) {
+        di = p.d[row ? i : e.r - 1];
+        if (n + 1 < kNT) load_row(o[(n + 1) % 2], n + 1);
+      }
 #pragma unroll
-      for (int m = 0; m < kMT; ++m) {
-        const int j = j0 + 32 * (m / 2) + 4 * (m % 2);
-        const int64_t to = static_cast<int64_t>(i) * e.pr + j;
-        float y[4];
-        if constexpr (kSquare) {
-          v2u ah = {}, al = {};
-          if (row && j < e.pr) {
-            ah = *reinterpret_cast<const v2u*>(p.a[0] + to);
-            if constexpr (kPair) al = *reinterpret_cast<const v2u*>(p.a[1] + to);
-          }
+      for (int m = 0; m < kMT / 2; ++m) {
+        const int j = j0 + 8 * g + 32 * m;
+        float y[8];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float oo = element(acc[m][n], q) * (1.0f / (kScaleA * kScaleA));
-            const int shift = 16 * (q % 2);
-            float o = half_value(static_cast<uint16_t>(ah[q / 2] >> shift));
-            if constexpr (kPair) o += half_value(static_cast<uint16_t>(al[q / 2] >> shift));
-            const float dj = j + q < e.r ? p.d[j + q] : 0.0f;
-            y[q] = fmaf(o * (1.0f / kScaleA), fmaf(c, di + dj, b), c * oo);
-            if (i == j + q && row) diagonal[i] = fmaf(b, di, c * fmaf(di, di, oo));
+        for (int q = 0; q < 8; ++q) {
+          const float sum = element(acc[2 * m + q / 4][n], q % 4);
+          const bool in = row && j + q < e.r;
+          if constexpr (kSquare) {
+            const float oo = sum * (1.0f / (kScaleA * kScaleA));
+            float off = high_of(o[n % 2][0][m][q / 2], q % 2);
+            if constexpr (kPair) off += high_of(o[n % 2][1][m][q / 2], q % 2);
+            y[q] = fmaf(off * (1.0f / kScaleA), fmaf(c, di + dj[m][q], b), c * oo);
+            if (in && i == j + q) p.e[i] = fmaf(b, di, c * fmaf(di, di, oo));
+          } else {
+            y[q] = sum * (1.0f / (kScaleX * kScaleX));
+            if (in && i == j + q) p.d[i] = y[q];
           }
-        } else {
+          y[q] = in && i != j + q ? y[q] * kScaleA : 0.0f;
+        }
+        v4u part[2];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            y[q] = element(acc[m][n], q) * (1.0f / (kScaleX * kScaleX));
-            if (i == j + q && row) diagonal[i] = y[q];
-          }
+        for (int q = 0; q < 4; ++q) {
+          part[0][q] = high2(y[2 * q], y[2 * q + 1]);
+          if constexpr (kPair) part[1][q] = low2(y[2 * q], y[2 * q + 1], part[0][q]);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = i == j + q ? 0.0f : y[q] * kScaleA;
-        v2u h, l;
-        split4<kPair>(y, &h, &l);
-        if (row && j < e.pr) {
-          *reinterpret_cast<v2u*>(high + to) = h;
-          if constexpr (kPair) *reinterpret_cast<v2u*>(low + to) = l;
-        }
-        if (mirrored && i < e.pr) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (j + q >= e.r) continue;
-            const int64_t back = static_cast<int64_t>(j + q) * e.pr + i;
-            high[back] = static_cast<uint16_t>(h[q / 2] >> (16 * (q % 2)));
-            if constexpr (kPair) low[back] = static_cast<uint16_t>(l[q / 2] >> (16 * (q % 2)));
+        for (int k = 0; k < (kPair ? 2 : 1); ++k) {
+          if (row && j < e.pr) *reinterpret_cast<v4u*>(out[k] + static_cast<int64_t>(i) * e.pr + j) = part[k];
+          if (mirrored) {
+            const int at = 16 * (kPair ? k : n % 2) + s, piece = 2 * m + g / 2;
+            *reinterpret_cast<v4u*>(turned + at * kSize + ((piece ^ turned_swizzle<kSize>(at)) * 32) + (g % 2) * 16) = part[k];
           }
         }
+      }
+      if (mirrored && (kPair || n % 2 == 1)) {
+        // The wave's last rows, turned: a lane has eight (float32 matrices: four) consecutive elements
+        // of a row above the diagonal.  A wave's accesses to LDS are in order.
+        asm volatile("" ::: "memory");
+        constexpr int kHalves = kPair ? 1 : 2;
+        const int back = i0 + 16 * (n + 1 - kHalves) + 4 * kHalves * g;
+#pragma unroll
+        for (int k = 0; k < (kPair ? 2 : 1); ++k)
+#pragma unroll
+          for (int block = 0; block < kSize / 32; ++block) {
+            s16x4 half[kHalves];
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              const int at = 16 * k + 4 * kHalves * g + 4 * h + s / 4;
+              half[h] = transposed_read(turned + at * kSize + ((block ^ turned_swizzle<kSize>(at)) * 32) + (s % 4) * 8);
+            }
+            const int j = j0 + 16 * block + s;
+            if (j >= e.r || back >= e.pr) continue;
+            uint16_t* const to = out[k] + static_cast<int64_t>(j) * e.pr + back;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) *reinterpret_cast<s16x4*>(to + 4 * h) = half[h];
+          }
+        asm volatile("" ::: "memory");
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -135,7 +185,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
 // X <- a X + B X, or of the last step the result: m runs along X's columns (X "across"), n along
 // its rows (B "along").  A lane holds columns j + 16 m + 4 g + 0..3 of row i + 16 n + s.
 template <typename Out, bool kPair, bool kLast, int kSize>
-__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_update_kernel(Table t, int turn, float a) {
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_update_kernel(Table t, int turn, float a, bool low) {
   constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = 2;
   __shared__ __align__(1024) char lds[tile_lds(kSize)];
   Tiles tiles(t.total_tiles[kKind]);
@@ -191,20 +241,49 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
     const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 4 * g;
     Out* const out = static_cast<Out*>(e.out);
     const bool vectors = e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0;
-#pragma unroll
-    for (int n = 0; n < kNT; ++n) {
-      const int i = i0 + 16 * n + s;
-      const bool row = i < e.r;
-      const float factor = row ? a + p.e[i] : 0.0f;
+    // X of the next 16 rows is fetched while these are stored.
+    f32x4 x[2][kPair ? kMT : 1];
+    v2u part[2][2][kPair ? 1 : kMT];
+    float of_row[2];
+    auto load_rows = [&](int n) {
+      const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
+      of_row[n % 2] = p.e[i];
 #pragma unroll
       for (int m = 0; m < kMT; ++m) {
         const int j = j0 + 16 * m;
-        if (!row || j >= e.pc) continue;
-        const int64_t to = static_cast<int64_t>(i) * e.pc + j;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p.x + to);
+        const int64_t from = static_cast<int64_t>(i) * e.pc + (j < e.pc ? j : 0);
+        if constexpr (kPair) {
+          x[n % 2][m] = *reinterpret_cast<const f32x4*>(p.x + from);
+        } else {
+          part[n % 2][0][m] = *reinterpret_cast<const v2u*>(p.from[0] + from);
+          if constexpr (!kLast) part[n % 2][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
+        }
+      }
+    };
+    load_rows(0);
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      if (n + 1 < kNT) load_rows(n + 1);
+      const int i = i0 + 16 * n + s;
+      const bool row = i < e.r;
+      const float factor = a + of_row[n % 2];
+#pragma unroll
+      for (int m = 0; m < kMT; ++m) {
+        const int j = j0 + 16 * m;
         float y[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = fmaf(factor, x[q], element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
+        for (int q = 0; q < 4; ++q) {
+          float before;
+          if constexpr (kPair) {
+            before = x[n % 2][m][q];
+          } else {
+            before = high_of(part[n % 2][0][m][q / 2], q % 2);
+            if constexpr (!kLast) before += high_of(part[n % 2][1][m][q / 2], q % 2);
+            before *= 1.0f / kScaleX;
+          }
+          y[q] = fmaf(factor, before, element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
+        }
+        if (!row || j >= e.pc) continue;
         if constexpr (kLast) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) y[q] *= e.scale;
@@ -220,13 +299,14 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
             }
           }
         } else {
-          *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
+          const int64_t to = static_cast<int64_t>(i) * e.pc + j;
+          if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
 #pragma unroll
           for (int q = 0; q < 4; ++q) y[q] *= kScaleX;
-          v2u h, l;
-          split4<kPair>(y, &h, &l);
-          *reinterpret_cast<v2u*>(p.to[0] + to) = h;
-          if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + to) = l;
+          const v2u high = high4(y);
+          *reinterpret_cast<v2u*>(p.to[0] + to) = high;
+          if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + to) = low4(y, high);
+          else if (low) *reinterpret_cast<v2u*>(p.low + to) = low4(y, high);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -244,10 +324,10 @@ hipError_t launch_symmetric(const Table& t, int size, int turn, const OrthoStep&
 }
 
 template <typename Out, bool kPair, bool kLast>
-hipError_t launch_update(const Table& t, int size, int turn, const OrthoStep& p, hipStream_t st) {
+hipError_t launch_update(const Table& t, int size, int turn, const OrthoStep& p, bool low, hipStream_t st) {
   const dim3 grid(workgroups_of(t.total_tiles[2], size)), block(kGemmThreads);
-  if (size == kTile) hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kTile>), grid, block, 0, st, t, turn, p.a);
-  else hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kSmallTile>), grid, block, 0, st, t, turn, p.a);
+  if (size == kTile) hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kTile>), grid, block, 0, st, t, turn, p.a, low);
+  else hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kSmallTile>), grid, block, 0, st, t, turn, p.a, low);
   return hipGetLastError();
 }
 
@@ -259,10 +339,14 @@ hipError_t launch_ortho_tiles_symmetric(const Table& t, bool square, bool pair, 
   return pair ? launch_symmetric<false, true>(t, size, turn, p, st) : launch_symmetric<false, false>(t, size, turn, p, st);
 }
 
-hipError_t launch_ortho_tiles_update(const Table& t, bool pair, bool last, int size, int turn, const OrthoStep& p,
+hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int left, int size, int turn, const OrthoStep& p,
                                      hipStream_t st) {
-  if (pair) return last ? launch_update<float, true, true>(t, size, turn, p, st) : launch_update<float, true, false>(t, size, turn, p, st);
-  return last ? launch_update<uint16_t, false, true>(t, size, turn, p, st) : launch_update<uint16_t, false, false>(t, size, turn, p, st);
+  const bool low = left > 1;  // the last step takes the operand alone as X
+  if (pair)
+    return left == 0 ? launch_update<float, true, true>(t, size, turn, p, low, st)
+                     : launch_update<float, true, false>(t, size, turn, p, low, st);
+  return left == 0 ? launch_update<uint16_t, false, true>(t, size, turn, p, low, st)
+                   : launch_update<uint16_t, false, false>(t, size, turn, p, low, st);
 }
 
 }  // namespace vtrace
