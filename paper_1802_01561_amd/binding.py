@@ -124,6 +124,11 @@ class _FastCall:
             ctypes.cast(f, ctypes.c_void_p).value
             for f in (L.vtrace_vocab_log_probs, L.vtrace_vocab_grad, L.vtrace_log_prob_loss_grad,
                       L.vtrace_clip_grad_norm))
+        self.call_vocab_embed, self.call_vocab_embed_grad, self.call_orthogonalize = (
+            _fast_call.vocab_embed, _fast_call.vocab_embed_grad, _fast_call.orthogonalize)
+        self.vocab_embed, self.vocab_embed_grad, self.orthogonalize = (
+            ctypes.cast(f, ctypes.c_void_p).value
+            for f in (L.vtrace_vocab_embed, L.vtrace_vocab_embed_grad, L.vtrace_orthogonalize))
         self.device, self.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 

@@ -23,26 +23,37 @@ constexpr int kUnit = 8;
 struct Unit {
   float x[kUnit];
 };
+// The same as it lies in memory.
+template <typename T>
+struct Raw {
+  v4u w[kUnit * sizeof(T) / 16];
+};
 
-__device__ __forceinline__ Unit load_unit(const uint16_t* p) {
-  const v4u w = *reinterpret_cast<const v4u*>(p);
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* p) {
+  Raw<T> r;
+#pragma unroll
+  for (unsigned h = 0; h < sizeof(r.w) / 16; ++h) r.w[h] = reinterpret_cast<const v4u*>(p)[h];
+  return r;
+}
+__device__ __forceinline__ Unit values(const Raw<uint16_t>& r) {
   Unit u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    u.x[2 * i] = __uint_as_float(w[i] << 16);
-    u.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    u.x[2 * i] = __uint_as_float(r.w[0][i] << 16);
+    u.x[2 * i + 1] = __uint_as_float(r.w[0][i] & 0xffff0000u);
   }
   return u;
 }
-__device__ __forceinline__ Unit load_unit(const float* p) {
+__device__ __forceinline__ Unit values(const Raw<float>& r) {
   Unit u;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const v4u w = *reinterpret_cast<const v4u*>(p + 4 * h);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u.x[4 * h + i] = __uint_as_float(w[i]);
-  }
+  for (int i = 0; i < kUnit; ++i) u.x[i] = __uint_as_float(r.w[i / 4][i % 4]);
   return u;
+}
+template <typename T>
+__device__ __forceinline__ Unit load_unit(const T* p) {
+  return values(load_raw(p));
 }
 __device__ __forceinline__ void store_unit(uint16_t* p, const Unit& u) {
   v4u w;
@@ -56,7 +67,7 @@ __device__ __forceinline__ void store_unit(float* p, const Unit& u) {
     v4u w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(u.x[4 * h + i]);
-    *reinterpret_cast<v4u*>(p + 4 * h) = w;
+    reinterpret_cast<v4u*>(p)[h] = w;
   }
 }
 
@@ -144,8 +155,9 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedArgs a) {
 // More steps: passes over digits of the token, from the lowest up, each of them stable.  A pass
 // counts every block's digits, adds the counts up in the order (digit, block), and moves.
 constexpr int kMostDigitBits = 9, kMostDigits = 1 << kMostDigitBits;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortItems = 4096;  // of a block
-constexpr int kSortWaves = kThreads / kWave;
+constexpr int kSortRounds = kSortItems / kSortThreads;  // of 64 consecutive items a wave
 constexpr int kScanThreads = 1024;
 
 // What is no token of the vocabulary is V.
@@ -155,19 +167,55 @@ __device__ __forceinline__ uint32_t sort_key(const EmbedArgs& a, int from, int64
   return t < static_cast<uint32_t>(a.V) ? t : static_cast<uint32_t>(a.V);
 }
 
-__global__ __launch_bounds__(kThreads) void embed_count_kernel(EmbedArgs a, int from, int shift, int bits) {
-  __shared__ uint32_t s_count[kMostDigits];
-  const int digits = 1 << bits;
-  for (int d = threadIdx.x; d < digits; d += kThreads) s_count[d] = 0;
+// A wave's items of a block, `kSortRounds` times 64 in their order: what each has before it of the
+// same digit among them, and in s_at how many there are of each digit.  Frequent tokens give most
+// lanes the same digit: lanes find each other by its bits and one of them counts.
+struct SortItems {
+  uint32_t key[kSortRounds];
+  int rank[kSortRounds];
+  int64_t first;
+};
+__device__ __forceinline__ void rank_items(const EmbedArgs& a, int from, int shift, int bits, uint32_t* s_at, SortItems* t) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  t->first = static_cast<int64_t>(blockIdx.x) * kSortItems + wave * (kSortRounds * kWave) + lane;
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) t->key[r] = t->first + r * kWave < a.N ? sort_key(a, from, t->first + r * kWave) : 0;
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) {
+    const bool in = t->first + r * kWave < a.N;
+    const int d = (t->key[r] >> shift) & ((1 << bits) - 1);
+    unsigned long long same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned long long set = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? set : ~set;
+    }
+    const int before = __popcll(same & ((1ull << lane) - 1));
+    const uint32_t at = s_at[d];
+    __builtin_amdgcn_wave_barrier();  // every lane has read before one of them writes
+    if (in && before == 0) s_at[d] = at + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    t->rank[r] = at + before;
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(EmbedArgs a, int from, int shift, int bits) {
+  __shared__ uint32_t s_at[kSortWaves][kMostDigits];
+  for (int d = threadIdx.x; d < kSortWaves * kMostDigits; d += kSortThreads) s_at[d / kMostDigits][d % kMostDigits] = 0;
   __syncthreads();
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortItems;
-  for (int k = threadIdx.x; k < kSortItems; k += kThreads) {
-    if (first + k >= a.N) break;
-    if (from < 0 && invalid(a.tokens[first + k], a.V)) raise_error_flag(a.error_flag);
-    atomicAdd(&s_count[(sort_key(a, from, first + k) >> shift) & (digits - 1)], 1u);
+  SortItems t;
+  rank_items(a, from, shift, bits, s_at[threadIdx.x / kWave], &t);
+  if (from < 0) {
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+      if (t.first + r * kWave < a.N && invalid(a.tokens[t.first + r * kWave], a.V)) raise_error_flag(a.error_flag);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kThreads) a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x] = s_count[d];
+  for (int d = threadIdx.x; d < 1 << bits; d += kSortThreads) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) n += s_at[w][d];
+    a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x] = n;
+  }
 }
 
 // counts[i] = sum of counts[0 .. i), by one workgroup.
@@ -208,22 +256,21 @@ __global__ __launch_bounds__(kScanThreads) void embed_scan_kernel(uint32_t* coun
   }
 }
 
-__global__ __launch_bounds__(kThreads) void embed_move_kernel(EmbedArgs a, int from, int to, int shift, int bits) {
-  constexpr int kRounds = kSortItems / kThreads;  // of 64 consecutive items a wave
+__global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, int from, int to, int shift, int bits) {
   __shared__ uint32_t s_at[kSortWaves][kMostDigits];
-  const int digits = 1 << bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (int d = threadIdx.x; d < kSortWaves * kMostDigits; d += kThreads) s_at[d / kMostDigits][d % kMostDigits] = 0;
+  for (int d = threadIdx.x; d < kSortWaves * kMostDigits; d += kSortThreads) s_at[d / kMostDigits][d % kMostDigits] = 0;
   __syncthreads();
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortItems + wave * (kRounds * kWave) + lane;
-  uint32_t key[kRounds];
+  SortItems t;
+  const int wave = threadIdx.x / kWave;
+  rank_items(a, from, shift, bits, s_at[wave], &t);
+  uint32_t step[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = first + r * kWave;
-    key[r] = i < a.N ? sort_key(a, from, i) : 0;
-    if (i < a.N) atomicAdd(&s_at[wave][(key[r] >> shift) & (digits - 1)], 1u);
+  for (int r = 0; r < kSortRounds; ++r) {
+    const int64_t i = t.first + r * kWave;
+    step[r] = from < 0 ? static_cast<uint32_t>(i) : i < a.N ? a.steps[from][i] : 0;
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kThreads) {
+  for (int d = threadIdx.x; d < 1 << bits; d += kSortThreads) {
     uint32_t at = a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x];
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
@@ -234,67 +281,85 @@ __global__ __launch_bounds__(kThreads) void embed_move_kernel(EmbedArgs a, int f
   }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = first + r * kWave;
-    const int d = (key[r] >> shift) & (digits - 1);
-    // The lanes with the same digit, by its bits.
-    unsigned long long same = __ballot(i < a.N);
-    for (int b = 0; b < bits; ++b) {
-      const unsigned long long set = __ballot((d >> b) & 1);
-      same &= (d >> b) & 1 ? set : ~set;
-    }
-    if (i >= a.N) continue;  // the last lanes of the last round or rounds
-    const int before = __popcll(same & ((1ull << lane) - 1));
-    const uint32_t at = s_at[wave][d];
-    __builtin_amdgcn_wave_barrier();  // every lane has read before one of them writes
-    if (before == 0) s_at[wave][d] = at + __popcll(same);
-    __builtin_amdgcn_wave_barrier();
-    a.keys[to][at + before] = key[r];
-    a.steps[to][at + before] = from < 0 ? static_cast<uint32_t>(i) : a.steps[from][i];
+  for (int r = 0; r < kSortRounds; ++r) {
+    if (t.first + r * kWave >= a.N) continue;
+    const uint32_t at = s_at[wave][(t.key[r] >> shift) & ((1 << bits) - 1)] + t.rank[r];
+    a.keys[to][at] = t.key[r];
+    a.steps[to][at] = step[r];
   }
 }
 
 // ---- Sums. ----
 
 constexpr int kLeastChunk = 4, kMostChunk = 128;
-constexpr int kBatch = 4;  // rows in flight of a chunk
-constexpr int kFillRows = 64;  // most rows of a workgroup that fills
+constexpr int kBatch = 4;  // rows of a chunk in flight
+constexpr int kFillRows = 256;  // most rows of a workgroup that fills
 constexpr int64_t kFillBytes = 65536;
 
+// A run's sum, scaled and (with `was`) added to what its row held.
 template <typename Out>
-__device__ __forceinline__ void write_row(Out* p, const Unit& sum, float scale, bool accumulate) {
-  Unit u = sum;
-  if (accumulate) {
-    const Unit was = load_unit(p);
+__device__ __forceinline__ void write_row(Out* p, const Unit& sum, float scale, bool accumulate, const Unit& was) {
+  Unit u;
 #pragma unroll
-    for (int i = 0; i < kUnit; ++i) u.x[i] = fmaf(sum.x[i], scale, was.x[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kUnit; ++i) u.x[i] *= scale;
-  }
+  for (int i = 0; i < kUnit; ++i) u.x[i] = accumulate ? fmaf(sum.x[i], scale, was.x[i]) : sum.x[i] * scale;
   store_unit(p, u);
 }
-// Zeros in the rows of tokens that no step has: workgroup `block` of those that do this.
+
+// The place of the first sorted step whose token is not before v, by a workgroup: 256 places at a
+// time.
+__device__ __forceinline__ int64_t first_step_of(const EmbedArgs& a, int64_t v) {
+  __shared__ int s_before[kThreads / kWave];
+  int64_t lo = 0, hi = a.N;
+  while (lo < hi) {
+    const int64_t stride = (hi - lo + kThreads - 1) / kThreads, at = lo + threadIdx.x * stride;
+    const unsigned long long before = __ballot(at < hi && a.keys[0][at] < v);
+    if (threadIdx.x % kWave == 0) s_before[threadIdx.x / kWave] = __popcll(before);
+    __syncthreads();
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) n += s_before[w];
+    __syncthreads();
+    if (n == 0) return lo;
+    const int64_t end = lo + n * stride;
+    lo += (n - 1) * stride + 1;
+    hi = end < hi ? end : hi;
+  }
+  return lo;
+}
+
+// Zeros in the rows of tokens that no step has: workgroup `block` of those that do this.  Rows are
+// vectors of 16 bytes, 1 << lanes_log2 threads each.
 template <typename Out>
 __device__ void fill_rows(const EmbedArgs& a, int64_t block, int rows, int lanes_log2) {
   __shared__ int s_present[kFillRows];
-  const int64_t v0 = block * rows;
-  if (static_cast<int>(threadIdx.x) < rows) {
+  const int64_t v0 = block * rows, v1 = v0 + rows < a.V ? v0 + rows : a.V;
+  if (static_cast<int>(threadIdx.x) < rows) s_present[threadIdx.x] = 0;
+  const int64_t first = first_step_of(a, v0);  // behind a barrier, unless there is no step
+  __syncthreads();
+  // The steps of these rows: all of them, or after some a search for each row that is not met yet.
+  constexpr int kMostLooks = 4;
+  int64_t i = first + threadIdx.x;
+  for (int look = 0; look < kMostLooks; ++look, i += kThreads) {
+    const uint32_t key = i < a.N ? a.keys[0][i] : 0xffffffffu;
+    if (key < v1) s_present[key - v0] = 1;
+    if (!__syncthreads_or(i == first + (look + 1) * kThreads - 1 && key < v1)) break;
+    if (look + 1 < kMostLooks || static_cast<int>(threadIdx.x) >= v1 - v0) continue;
     const int64_t v = v0 + threadIdx.x;
-    int64_t lo = 0, hi = a.N;  // the first step whose token is not before v
+    int64_t lo = first, hi = a.N;
     while (lo < hi) {
       const int64_t mid = (lo + hi) / 2;
       if (a.keys[0][mid] < v) lo = mid + 1;
       else hi = mid;
     }
-    s_present[threadIdx.x] = v >= a.V || (lo < a.N && a.keys[0][lo] == v);
+    if (lo < a.N && a.keys[0][lo] == v) s_present[threadIdx.x] = 1;
   }
   __syncthreads();
-  const int lanes = 1 << lanes_log2, units = static_cast<int>(a.H / kUnit);
-  for (int r = threadIdx.x >> lanes_log2; r < rows; r += kThreads >> lanes_log2) {
+  const int lanes = 1 << lanes_log2, vectors = static_cast<int>(a.H * sizeof(Out) / 16);
+  const v4u zero = {0u, 0u, 0u, 0u};
+  for (int r = threadIdx.x >> lanes_log2; r < v1 - v0; r += kThreads >> lanes_log2) {
     if (s_present[r]) continue;
-    for (int c = threadIdx.x & (lanes - 1); c < units; c += lanes)
-      store_unit(static_cast<Out*>(a.d_table) + (v0 + r) * a.H + c * kUnit, Unit{});
+    v4u* const row = reinterpret_cast<v4u*>(static_cast<Out*>(a.d_table) + (v0 + r) * a.H);
+    for (int c = threadIdx.x & (lanes - 1); c < vectors; c += lanes) row[c] = zero;
   }
 }
 
@@ -306,12 +371,14 @@ __device__ __forceinline__ float* partial_row(const EmbedArgs& a, int64_t chunk,
 // than a workgroup's units); then, in further workgroups, the rows that no step has.
 // Slot 0 of a chunk's partial sums is that of the run that comes from the chunk before it,
 // slot 1 of the one that begins here and goes on behind it.
-template <typename In, typename Out>
+template <typename In, typename Out, bool kAccumulate>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int lanes_log2, int slabs, int64_t sum_blocks,
-                                                             int fill) {
-  if (blockIdx.x >= sum_blocks) {
-    fill_rows<Out>(a, blockIdx.x - sum_blocks, fill, lanes_log2);
-    return;
+                                                             int fill, int fill_lanes_log2) {
+  if constexpr (!kAccumulate) {
+    if (blockIdx.x >= sum_blocks) {
+      fill_rows<Out>(a, blockIdx.x - sum_blocks, fill, fill_lanes_log2);
+      return;
+    }
   }
   const int lanes = 1 << lanes_log2;
   const int64_t chunk = static_cast<int64_t>(blockIdx.x / slabs) * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
@@ -324,40 +391,40 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int la
   const int64_t column = static_cast<int64_t>(unit) * kUnit;
   const In* const d_rows = static_cast<const In*>(a.d_rows) + column;
   Out* const d_table = static_cast<Out*>(a.d_table) + column;
-  uint32_t run = keys[begin];
-  if (run >= V) return;
-  const bool entered = begin > 0 && keys[begin - 1] == run;
-  const uint32_t after = end < a.N ? keys[end] : 0xffffffffu;
+  const uint32_t previous = begin > 0 ? keys[begin - 1] : 0xffffffffu;
+  bool first = true;  // the chunk's first run, which may come from the chunk before
   Unit sum = {};
-  bool first = true;
-  auto leave = [&](bool goes_on) {
-    if (first && entered) store_unit(partial_row(a, chunk, 0) + column, sum);
-    else if (goes_on) store_unit(partial_row(a, chunk, 1) + column, sum);
-    else write_row(d_table + static_cast<int64_t>(run) * a.H, sum, a.scale, a.accumulate);
-  };
   for (int64_t i = begin; i < end; i += kBatch) {
-    uint32_t key[kBatch];
-    Unit u[kBatch];
+    // Tokens one step further than the batch: a run ends where the next one differs.
+    uint32_t key[kBatch + 1];
+#pragma unroll
+    for (int b = 0; b <= kBatch; ++b) key[b] = i + b < a.N ? keys[i + b] : 0xffffffffu;
+    Raw<In> row[kBatch];
+    Raw<Out> was[kAccumulate ? kBatch : 1];
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      key[b] = i + b < end ? keys[i + b] : 0xffffffffu;
-      if (key[b] < V) u[b] = load_unit(d_rows + static_cast<int64_t>(a.steps[0][i + b]) * a.H);
+      if (i + b >= end || key[b] >= V) continue;
+      row[b] = load_raw(d_rows + static_cast<int64_t>(a.steps[0][i + b]) * a.H);
+      if constexpr (kAccumulate) {
+        if (key[b] != key[b + 1]) was[b] = load_raw(static_cast<const Out*>(d_table) + static_cast<int64_t>(key[b]) * a.H);
+      }
     }
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      if (key[b] >= V) continue;
-      if (key[b] != run) {
-        leave(false);
-        run = key[b];
-        first = false;
+      if (i + b >= end || key[b] >= V) continue;
+      const Unit u = values(row[b]);
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) sum.x[e] = 0.0f;
-      }
+      for (int e = 0; e < kUnit; ++e) sum.x[e] += u.x[e];
+      const bool ends = key[b] != key[b + 1];
+      if (!ends && i + b + 1 < end) continue;
+      if (first && previous == key[b]) store_unit(partial_row(a, chunk, 0) + column, sum);
+      else if (!ends) store_unit(partial_row(a, chunk, 1) + column, sum);
+      else write_row(d_table + static_cast<int64_t>(key[b]) * a.H, sum, a.scale, kAccumulate, kAccumulate ? values(was[kAccumulate ? b : 0]) : Unit{});
+      first = false;
 #pragma unroll
-      for (int e = 0; e < kUnit; ++e) sum.x[e] += u[b].x[e];
+      for (int e = 0; e < kUnit; ++e) sum.x[e] = 0.0f;
     }
   }
-  leave(after == run);
 }
 
 // The run that begins in a chunk and goes on behind it: its parts, in order, in float64; the
@@ -369,16 +436,16 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, int l
   const int64_t begin = chunk * a.chunk, end = begin + a.chunk;
   const uint32_t* const keys = a.keys[0];
   if (end >= a.N) return;
-  const uint32_t run = keys[end - 1];
-  if (run >= static_cast<uint32_t>(a.V) || keys[end] != run || (begin > 0 && keys[begin - 1] == run)) return;
-  // The last chunk that begins with it.
-  int64_t lo = chunk + 1, hi = (a.N + a.chunk - 1) / a.chunk - 1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (keys[mid * a.chunk] == run) lo = mid;
-    else hi = mid - 1;
+  const uint32_t run = keys[end - 1], after = keys[end], before = begin > 0 ? keys[begin - 1] : 0xffffffffu;
+  if (run >= static_cast<uint32_t>(a.V) || after != run || before == run) return;
+  // The last chunk that begins with it: 256 chunks at a time, the next ones first.
+  int64_t last = chunk + 1;
+  for (bool more = true; more;) {
+    const int64_t at = (last + 1 + threadIdx.x) * a.chunk;
+    const int n = __syncthreads_count(at < a.N && keys[at] == run);
+    last += n;
+    more = n == kThreads;
   }
-  const int64_t last = lo;
   const int lanes = 1 << lanes_log2, groups = kThreads >> lanes_log2, group = threadIdx.x >> lanes_log2;
   const int unit = static_cast<int>(blockIdx.x % slabs) * lanes + (threadIdx.x & (lanes - 1));
   const bool in = unit < static_cast<int>(a.H / kUnit);
@@ -404,7 +471,8 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, int l
   Unit u;
 #pragma unroll
   for (int e = 0; e < kUnit; ++e) u.x[e] = static_cast<float>(sum[e]);
-  write_row(static_cast<Out*>(a.d_table) + static_cast<int64_t>(run) * a.H + column, u, a.scale, a.accumulate);
+  Out* const to = static_cast<Out*>(a.d_table) + static_cast<int64_t>(run) * a.H + column;
+  write_row(to, u, a.scale, a.accumulate, a.accumulate ? load_unit(static_cast<const Out*>(to)) : Unit{});
 }
 
 template <typename In, typename Out>
@@ -418,8 +486,13 @@ hipError_t launch_sums(const EmbedArgs& a, hipStream_t st) {
     fill = fill < 1 ? 1 : fill > kFillRows ? kFillRows : fill;
     fills = ceil_div(a.V, fill);
   }
-  hipLaunchKernelGGL((embed_sum_kernel<In, Out>), dim3(static_cast<unsigned>(sums + fills)), dim3(kThreads), 0, st, a, lanes,
-                     static_cast<int>(slabs), sums, static_cast<int>(fill));
+  const int fill_lanes = row_lanes_log2(a.H * static_cast<int64_t>(sizeof(Out)) / 2, 8);  // 16 bytes each
+  const dim3 grid(static_cast<unsigned>(sums + fills));
+  if (a.accumulate)
+    hipLaunchKernelGGL((embed_sum_kernel<In, Out, true>), grid, dim3(kThreads), 0, st, a, lanes, static_cast<int>(slabs), sums, 0, 0);
+  else
+    hipLaunchKernelGGL((embed_sum_kernel<In, Out, false>), grid, dim3(kThreads), 0, st, a, lanes, static_cast<int>(slabs), sums,
+                       static_cast<int>(fill), fill_lanes);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || chunks < 2) return e;
   const int join_lanes = row_lanes_log2(a.H, 6);
@@ -450,13 +523,13 @@ hipError_t launch_order(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) 
   for (int pass = 0; pass < passes; ++pass) {
     const int to = (passes - 1 - pass) % 2;
     const dim3 grid(static_cast<unsigned>(blocks));
-    hipLaunchKernelGGL(embed_count_kernel, grid, dim3(kThreads), 0, st, a, from, pass * bits, bits);
+    hipLaunchKernelGGL(embed_count_kernel, grid, dim3(kSortThreads), 0, st, a, from, pass * bits, bits);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(kScanThreads), 0, st, a.counts, blocks << bits);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embed_move_kernel, grid, dim3(kThreads), 0, st, a, from, to, pass * bits, bits);
+    hipLaunchKernelGGL(embed_move_kernel, grid, dim3(kSortThreads), 0, st, a, from, to, pass * bits, bits);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     from = to;

@@ -1,7 +1,8 @@
 // Argument marshalling of the ordinary call, without Python objects per argument:
 // plain contiguous device tensors of the expected types and shapes, preallocated
 // outputs, a workspace and the current stream.  Each function checks exactly that
-// and calls the C entry point it is given (include/vtrace.h, vtrace_tokens.h); on
+// and calls the C entry point it is given (include/vtrace.h, vtrace_tokens.h,
+// vtrace_parameters.h); on
 // anything else it returns None, having done nothing, and the Python path (binding.py,
 // tokens.py), which allocates and reports errors, takes the call.
 //
@@ -19,6 +20,7 @@
 #include <vector>
 
 #include "vtrace.h"
+#include "vtrace_parameters.h"
 #include "vtrace_tokens.h"
 
 namespace {
@@ -446,6 +448,107 @@ PyObject* clip(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return out.result(st);
 }
 
+// vocab_embed(fn, weight, tokens, scale, bf16_out, out, workspace, bytes, device, stream)
+PyObject* vocab_embed(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 10 || watched()) Py_RETURN_NONE;
+  Args a;
+  const at::Tensor* w = a.first(v[1], 2);
+  const at::Tensor* t = a.ok ? plain_tensor(v[2]) : nullptr;
+  vtrace_dtype dt;
+  if (w == nullptr || t == nullptr || t->dim() != 2 || !logits_type(*w, &dt) || !on_device(&a, v[8])) Py_RETURN_NONE;
+  const int64_t V = w->size(0), H = w->size(1), T = t->size(0), B = t->size(1);
+  const auto fn = a.address<decltype(&vtrace_vocab_embed)>(v[0]);
+  void* const tokens = a.tensor(v[2], {T, B}, I32);
+  const float scale = a.number(v[3]);
+  const bool bf16 = v[4] == Py_True;
+  void* const ws = v[6] == Py_None ? nullptr : workspace_here(&a, v[6]);
+  const size_t bytes = a.integer(v[7]);
+  const auto stream = a.address<vtrace_stream_t>(v[9]);
+  Outputs out(1);
+  void* const rows = out.add(&a, v[5], true, {T, B, H}, bf16 ? BF16 : F32);
+  if (!a.ok) Py_RETURN_NONE;
+  vtrace_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fn(T, B, V, H, dt, bf16 ? VTRACE_BF16 : VTRACE_F32, w->data_ptr(), static_cast<const int32_t*>(tokens), scale, rows, ws,
+          bytes, stream);
+  Py_END_ALLOW_THREADS;
+  return out.result(st);
+}
+
+// vocab_embed_grad(fn, d_embedded, tokens, V, scale, bf16_grad, accumulates, d_weight, workspace, bytes, device,
+//                  stream)
+PyObject* vocab_embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 12 || watched()) Py_RETURN_NONE;
+  Args a;
+  const at::Tensor* d = a.first(v[1], 3);
+  vtrace_dtype dt;
+  if (d == nullptr || !logits_type(*d, &dt) || !on_device(&a, v[10])) Py_RETURN_NONE;
+  const int64_t T = d->size(0), B = d->size(1), H = d->size(2), V = static_cast<int64_t>(a.integer(v[3]));
+  const auto fn = a.address<decltype(&vtrace_vocab_embed_grad)>(v[0]);
+  void* const tokens = a.tensor(v[2], {T, B}, I32);
+  const float scale = a.number(v[4]);
+  const bool bf16 = v[5] == Py_True, accumulates = v[6] == Py_True;
+  void* const ws = workspace_here(&a, v[8]);
+  const size_t bytes = a.integer(v[9]);
+  const auto stream = a.address<vtrace_stream_t>(v[11]);
+  if (V < 1 || V > (int64_t(1) << 24) || (accumulates && v[7] == Py_None)) Py_RETURN_NONE;
+  Outputs out(1);
+  void* const d_weight = out.add(&a, v[7], true, {V, H}, bf16 ? BF16 : F32);
+  if (!a.ok) Py_RETURN_NONE;
+  vtrace_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fn(T, B, V, H, dt, bf16 ? VTRACE_BF16 : VTRACE_F32, d->data_ptr(), static_cast<const int32_t*>(tokens), scale,
+          accumulates ? 1 : 0, d_weight, ws, bytes, stream);
+  Py_END_ALLOW_THREADS;
+  return out.result(st);
+}
+
+// orthogonalize(fn, matrices, outputs, scale, steps, coefficients, epsilon, workspace, bytes, device, stream):
+// matrices a list, outputs a list or None, coefficients an address.
+PyObject* orthogonalize(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 11 || watched() || !PyList_CheckExact(v[1]) || (v[2] != Py_None && !PyList_CheckExact(v[2]))) Py_RETURN_NONE;
+  const Py_ssize_t count = PyList_GET_SIZE(v[1]);
+  if (count == 0 || (v[2] != Py_None && PyList_GET_SIZE(v[2]) != count)) Py_RETURN_NONE;
+  std::vector<const void*> in(count);
+  std::vector<void*> to(count);
+  std::vector<int64_t> rows(count), columns(count);
+  std::vector<int32_t> types(count);
+  Args a;
+  Outputs out(count);
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    PyObject* const mi = PyList_GET_ITEM(v[1], i);
+    const at::Tensor* m = plain_tensor(mi);
+    vtrace_dtype dt;
+    if (m == nullptr || m->dim() != 2 || !logits_type(*m, &dt)) Py_RETURN_NONE;
+    if (i == 0) {
+      a.device = m->device();
+      if (!on_device(&a, v[9])) Py_RETURN_NONE;
+    }
+    if (m->device() != a.device) Py_RETURN_NONE;
+    in[i] = m->data_ptr();
+    rows[i] = m->size(0);
+    columns[i] = m->size(1);
+    types[i] = dt;
+    to[i] = out.add(&a, v[2] == Py_None ? Py_None : PyList_GET_ITEM(v[2], i), true, {rows[i], columns[i]}, m->scalar_type());
+    if (!a.ok) Py_RETURN_NONE;
+  }
+  const auto fn = a.address<decltype(&vtrace_orthogonalize)>(v[0]);
+  const std::vector<float> scales(count, a.number(v[3]));
+  const size_t steps = a.integer(v[4]);
+  const auto coefficients = a.address<const float*>(v[5]);
+  const float epsilon = a.number(v[6]);
+  void* const ws = workspace_here(&a, v[7]);
+  const size_t bytes = a.integer(v[8]);
+  const auto stream = a.address<vtrace_stream_t>(v[10]);
+  if (!a.ok || steps > 64) Py_RETURN_NONE;
+  vtrace_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fn(count, in.data(), to.data(), rows.data(), columns.data(), types.data(), scales.data(), static_cast<int32_t>(steps),
+          coefficients, epsilon, ws, bytes, stream);
+  Py_END_ALLOW_THREADS;
+  return out.result(st);
+}
+
 // A C++ exception (none is expected: every access is checked first) leaves the
 // call to the Python path.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
@@ -460,7 +563,8 @@ PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 #define METHOD(name) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(targets),    METHOD(loss),          METHOD(head), METHOD(vocab_log_probs),
-                         METHOD(vocab_grad), METHOD(log_prob_loss), METHOD(clip), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(vocab_grad), METHOD(log_prob_loss), METHOD(clip), METHOD(vocab_embed), METHOD(vocab_embed_grad),
+                         METHOD(orthogonalize), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -15,8 +15,8 @@ from typing import Optional, Sequence, Union
 import torch
 
 from ._lib import check, lib
-from .binding import _p, _require
-from .tokens import _DTYPES, _CallWorkspace, _grad_dtype_code, _On, _workspace
+from .binding import _fast_call, _p, _require
+from .tokens import _DTYPES, _CallWorkspace, _grad_dtype_code, _On, _outputs, _workspace
 
 __all__ = [
     "QUINTIC",
@@ -102,6 +102,18 @@ def vtrace_vocab_embed(vocab_weight, tokens, scale: float = 1.0, *, out_dtype=No
     not in the vocabulary.
 
     ``workspace`` (any of this library's) is there for its error flag alone."""
+    # As in tokens.py, native code takes the ordinary call, or declines.
+    if stream is None and type(scale) is float and (workspace is None or isinstance(workspace, _CallWorkspace)):
+        fast = _fast_call(vocab_weight)
+        if fast:
+            wanted = out.dtype if type(out) is torch.Tensor else out_dtype or vocab_weight.dtype
+            if wanted in _DTYPES:
+                device = fast.device()
+                r = fast.call_vocab_embed(fast.vocab_embed, vocab_weight, tokens, scale, wanted is torch.bfloat16, out,
+                                          None if workspace is None else workspace.tensor,
+                                          0 if workspace is None else workspace.nbytes, device, fast.stream(device))
+                if r is not None:
+                    return _outputs(r)[0]
     if not isinstance(vocab_weight, torch.Tensor):
         raise TypeError("vocab_weight must be a torch.Tensor")
     if vocab_weight.dim() != 2:
@@ -137,13 +149,23 @@ def vtrace_vocab_embed_grad(d_embedded, tokens, vocab_size: int, scale: float = 
     of ``grad_dtype`` is written, rows that no step has with zeros."""
     if accumulate_into is not None and out is not None:
         raise ValueError("out and accumulate_into are one or the other")
+    given = accumulate_into if out is None else out
+    if stream is None and type(scale) is float and type(workspace) is EmbedWorkspace:
+        fast = _fast_call(d_embedded)
+        wanted = given.dtype if type(given) is torch.Tensor else grad_dtype
+        if fast and wanted in _DTYPES:
+            device = fast.device()
+            r = fast.call_vocab_embed_grad(fast.vocab_embed_grad, d_embedded, tokens, vocab_size, scale,
+                                           wanted is torch.bfloat16, accumulate_into is not None, given,
+                                           workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return _outputs(r)[0]
     if not isinstance(d_embedded, torch.Tensor):
         raise TypeError("d_embedded must be a torch.Tensor")
     if d_embedded.dim() != 3:
         raise ValueError("d_embedded must be [T, B, H]")
     T, B, H = d_embedded.shape
     dev = d_embedded.device
-    given = accumulate_into if out is None else out
     if given is not None:
         if not isinstance(given, torch.Tensor):
             raise TypeError("out and accumulate_into must be torch.Tensors")
@@ -164,14 +186,22 @@ def vtrace_vocab_embed_grad(d_embedded, tokens, vocab_size: int, scale: float = 
     return given
 
 
+_quintic = {}  # steps -> the table of QUINTIC for so many
+
+
 def _coefficients(coefficients, steps: int):
     """3 floats for each step, from one triple for all or a triple for each."""
+    if coefficients is QUINTIC and steps in _quintic:
+        return _quintic[steps]
     rows = list(coefficients)
     if len(rows) == 3 and not any(hasattr(r, "__len__") for r in rows):
         rows = [rows] * steps
     if len(rows) != steps or any(len(r) != 3 for r in rows):
         raise ValueError(f"coefficients must be a triple, or {steps} of them")
-    return (ctypes.c_float * (3 * steps))(*(float(x) for r in rows for x in r))
+    table = (ctypes.c_float * (3 * steps))(*(float(x) for r in rows for x in r))
+    if coefficients is QUINTIC:
+        _quintic[steps] = table
+    return table
 
 
 def vtrace_orthogonalize(matrices: Sequence[torch.Tensor], scale: Union[float, Sequence[float]] = 1.0, *, steps: int = 5,
@@ -194,6 +224,14 @@ def vtrace_orthogonalize(matrices: Sequence[torch.Tensor], scale: Union[float, S
     if isinstance(steps, bool) or not isinstance(steps, int) or not 1 <= steps <= 64:
         raise ValueError(f"steps must be 1 to 64, got {steps}")
     table = _coefficients(coefficients, steps)
+    if stream is None and type(scale) is float and type(epsilon) is float and type(workspace) is OrthogonalWorkspace:
+        fast = _fast_call(matrices[0])
+        if fast:
+            device = fast.device()
+            r = fast.call_orthogonalize(fast.orthogonalize, matrices, outs, scale, steps, ctypes.addressof(table), epsilon,
+                                        workspace.tensor, workspace.nbytes, device, fast.stream(device))
+            if r is not None:
+                return list(_outputs(r))
     if hasattr(scale, "__len__"):
         if len(scale) != n:
             raise ValueError(f"{len(scale)} scales for {n} matrices")
