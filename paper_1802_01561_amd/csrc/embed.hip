@@ -55,19 +55,27 @@ template <typename T>
 __device__ __forceinline__ Unit load_unit(const T* p) {
   return values(load_raw(p));
 }
+template <bool kPast>
+__device__ __forceinline__ void store_vector(v4u* p, const v4u& w) {
+  if constexpr (kPast) __builtin_nontemporal_store(w, p);
+  else *p = w;
+}
+// kPast: past the caches.
+template <bool kPast = false>
 __device__ __forceinline__ void store_unit(uint16_t* p, const Unit& u) {
   v4u w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(u.x[2 * i], u.x[2 * i + 1]);
-  *reinterpret_cast<v4u*>(p) = w;
+  store_vector<kPast>(reinterpret_cast<v4u*>(p), w);
 }
+template <bool kPast = false>
 __device__ __forceinline__ void store_unit(float* p, const Unit& u) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     v4u w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(u.x[4 * h + i]);
-    reinterpret_cast<v4u*>(p)[h] = w;
+    store_vector<kPast>(reinterpret_cast<v4u*>(p) + h, w);
   }
 }
 
@@ -79,8 +87,11 @@ int row_lanes_log2(int64_t H, int most_log2) {
 }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// kRows rows a group of threads, their loads in flight together.
-template <typename In, typename Out, int kRows>
+constexpr int64_t kCachedBytes = int64_t(1) << 27;  // half of the Infinity Cache
+
+// kRows rows a group of threads, their loads in flight together.  Outputs larger than what the
+// caches hold go past them: 65536 rows of 2048 bfloat16 87 -> 60 us (2 or 8 rows a group: 88, 108).
+template <typename In, typename Out, int kRows, bool kPast>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes_log2) {
   const int groups = kThreads >> lanes_log2, lanes = 1 << lanes_log2;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * kRows * groups + (threadIdx.x >> lanes_log2);
@@ -105,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes_
       const bool valid = token[r] >= 0 && token[r] < a.V;
 #pragma unroll
       for (int i = 0; i < kUnit; ++i) u[r].x[i] = valid ? u[r].x[i] * a.scale : token[r] == -1 ? 0.0f : NAN;
-      store_unit(static_cast<Out*>(a.rows) + n * a.H + c * kUnit, u[r]);
+      store_unit<kPast>(static_cast<Out*>(a.rows) + n * a.H + c * kUnit, u[r]);
     }
   }
 }
@@ -118,35 +129,51 @@ constexpr int kRankThreads = 1024;
 
 __device__ __forceinline__ bool invalid(int32_t token, int64_t V) { return token != -1 && (token < 0 || token >= V); }
 
-// A workgroup's 64 steps, one a lane; each wave counts a part of all steps that come before
-// them.  Tokens compare as unsigned numbers, so that what is no token of the vocabulary comes last.
+// A workgroup's 16 steps: each 16 threads count one 64th of all steps that come before them, from
+// LDS, where all tokens are.  Tokens compare as unsigned numbers, so that what is no token of the
+// vocabulary comes last.  Bound by the comparisons where N is some thousands (with 64 steps a
+// workgroup, which leaves most CUs without one, 3200 steps 9.7 us, so 5.5).
+constexpr int kRankSteps = 16;
 __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedArgs a) {
-  constexpr int kWaves = kRankThreads / kWave;
-  __shared__ int s_rank[kWaves][kWave];
-  const int lane = threadIdx.x % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  constexpr int kSlices = kRankThreads / kRankSteps;
+  __shared__ __align__(16) uint32_t s_token[kMostRanked];
+  __shared__ int s_rank[kSlices][kRankSteps];
+  const int step = threadIdx.x % kRankSteps, slice = threadIdx.x / kRankSteps;
   const int N = static_cast<int>(a.N);
-  const int n0 = blockIdx.x * kWave, n = n0 + lane;
-  const uint32_t mine = n < N ? static_cast<uint32_t>(a.tokens[n]) : 0xffffffffu;
-  const int per = (N + kWaves - 1) / kWaves;
-  const int from = wave * per < N ? wave * per : N, to = from + per < N ? from + per : N;
-  auto inside = [&](int j) { return j < from ? from : j > to ? to : j; };
-  const int own = inside(n0), behind = inside(n0 + kWave);
-  int rank = 0;
-#pragma unroll 16
-  for (int j = from; j < own; ++j) rank += static_cast<uint32_t>(a.tokens[j]) <= mine;
-  for (int j = own; j < behind; ++j) {
-    const uint32_t t = static_cast<uint32_t>(a.tokens[j]);
-    rank += t < mine || (t == mine && j < n);
-  }
-#pragma unroll 16
-  for (int j = behind; j < to; ++j) rank += static_cast<uint32_t>(a.tokens[j]) < mine;
-  s_rank[wave][lane] = rank;
+  const int n0 = blockIdx.x * kRankSteps, n = n0 + step;
+  // In fours, whose last one is filled up with what comes behind everything.
+  const int fours = (N + 3) / 4;
+  for (int j = threadIdx.x; j < 4 * fours; j += kRankThreads) s_token[j] = j < N ? static_cast<uint32_t>(a.tokens[j]) : 0xffffffffu;
   __syncthreads();
-  if (wave != 0 || n >= N) return;
+  const uint32_t mine = n < N ? s_token[n] : 0xffffffffu;
+  const int per = (fours + kSlices - 1) / kSlices;
+  const int from = slice * per < fours ? slice * per : fours, to = from + per < fours ? from + per : fours;
+  auto inside = [&](int j) { return j < from ? from : j > to ? to : j; };
+  const int own = inside(n0 / 4), behind = inside((n0 + kRankSteps) / 4);
+  int rank = 0;
+#pragma unroll 4
+  for (int j = from; j < own; ++j) {
+    const v4u t = *reinterpret_cast<const v4u*>(s_token + 4 * j);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) rank += t[q] <= mine;
+  }
+  for (int j = 4 * own; j < 4 * behind; ++j) rank += s_token[j] < mine || (s_token[j] == mine && j < n);
+#pragma unroll 4
+  for (int j = behind; j < to; ++j) {
+    const v4u t = *reinterpret_cast<const v4u*>(s_token + 4 * j);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) rank += t[q] < mine;
+  }
+  s_rank[slice][step] = rank;
+  __syncthreads();
+  // Sums over the slices: four threads of a wave a step, then their sums.
+  if (threadIdx.x >= kWave) return;
   int at = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) at += s_rank[w][lane];
+  for (int w = 0; w < kSlices / 4; ++w) at += s_rank[4 * w + slice][step];
+  at += __shfl_xor(at, 16, kWave);
+  at += __shfl_xor(at, 32, kWave);
+  if (slice != 0 || n >= N) return;
   a.keys[0][at] = mine;
   a.steps[0][at] = static_cast<uint32_t>(n);
   if (invalid(static_cast<int32_t>(mine), a.V)) raise_error_flag(a.error_flag);
@@ -256,8 +283,24 @@ __global__ __launch_bounds__(kScanThreads) void embed_scan_kernel(uint32_t* coun
   }
 }
 
+// kScans: up to kMostSelfScanned blocks add up the counts themselves.
+constexpr int kMostSelfScanned = 64;
+template <bool kScans>
 __global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, int from, int to, int shift, int bits) {
   __shared__ uint32_t s_at[kSortWaves][kMostDigits];
+  __shared__ uint32_t s_digits[kMostDigits / kWave];
+  uint32_t own = 0, all = 0;  // a thread's digit: in the blocks before this one, and in all
+  if constexpr (kScans) {
+    if (static_cast<int>(threadIdx.x) < 1 << bits) {
+      const uint32_t* const counts = a.counts + static_cast<int64_t>(threadIdx.x) * gridDim.x;
+#pragma unroll 16
+      for (unsigned b = 0; b < gridDim.x; ++b) {
+        const uint32_t n = counts[b];
+        all += n;
+        if (b < blockIdx.x) own += n;
+      }
+    }
+  }
   for (int d = threadIdx.x; d < kSortWaves * kMostDigits; d += kSortThreads) s_at[d / kMostDigits][d % kMostDigits] = 0;
   __syncthreads();
   SortItems t;
@@ -269,9 +312,23 @@ __global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, i
     const int64_t i = t.first + r * kWave;
     step[r] = from < 0 ? static_cast<uint32_t>(i) : i < a.N ? a.steps[from][i] : 0;
   }
+  if constexpr (kScans) {
+    // And those of all smaller digits.
+    uint32_t upto = all;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t y = __shfl_up(upto, o, kWave);
+      if (static_cast<int>(threadIdx.x) % kWave >= o) upto += y;
+    }
+    if (threadIdx.x % kWave == kWave - 1 && threadIdx.x < kMostDigits) s_digits[threadIdx.x / kWave] = upto;
+    own += upto - all;
+  }
   __syncthreads();
+  if constexpr (kScans) {
+    for (int w = 0; w < wave && w < kMostDigits / kWave; ++w) own += s_digits[w];
+  }
   for (int d = threadIdx.x; d < 1 << bits; d += kSortThreads) {
-    uint32_t at = a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x];
+    uint32_t at = kScans ? own : a.counts[static_cast<int64_t>(d) * gridDim.x + blockIdx.x];
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
       const uint32_t n = s_at[w][d];
@@ -292,7 +349,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, i
 // ---- Sums. ----
 
 constexpr int kLeastChunk = 4, kMostChunk = 128;
-constexpr int kBatch = 4;  // rows of a chunk in flight
+constexpr int kBatch = 8;  // rows of a chunk in flight
 constexpr int kFillRows = 256;  // most rows of a workgroup that fills
 constexpr int64_t kFillBytes = 65536;
 
@@ -429,37 +486,47 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int la
 
 // The run that begins in a chunk and goes on behind it: its parts, in order, in float64; the
 // groups of a workgroup take turns with them.
+constexpr int kJoinThreads = 256;
 template <typename Out>
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, int lanes_log2, int slabs) {
-  __shared__ double s_sum[kThreads][kUnit];
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, int lanes_log2, int slabs) {
+  __shared__ double s_sum[kJoinThreads][kUnit];
   const int64_t chunk = blockIdx.x / slabs;
   const int64_t begin = chunk * a.chunk, end = begin + a.chunk;
   const uint32_t* const keys = a.keys[0];
   if (end >= a.N) return;
   const uint32_t run = keys[end - 1], after = keys[end], before = begin > 0 ? keys[begin - 1] : 0xffffffffu;
   if (run >= static_cast<uint32_t>(a.V) || after != run || before == run) return;
-  // The last chunk that begins with it: 256 chunks at a time, the next ones first.
+  // The last chunk that begins with it: as many as there are threads at a time.
   int64_t last = chunk + 1;
   for (bool more = true; more;) {
     const int64_t at = (last + 1 + threadIdx.x) * a.chunk;
     const int n = __syncthreads_count(at < a.N && keys[at] == run);
     last += n;
-    more = n == kThreads;
+    more = n == kJoinThreads;
   }
-  const int lanes = 1 << lanes_log2, groups = kThreads >> lanes_log2, group = threadIdx.x >> lanes_log2;
+  const int lanes = 1 << lanes_log2, groups = kJoinThreads >> lanes_log2, group = threadIdx.x >> lanes_log2;
   const int unit = static_cast<int>(blockIdx.x % slabs) * lanes + (threadIdx.x & (lanes - 1));
   const bool in = unit < static_cast<int>(a.H / kUnit);
   const int64_t column = static_cast<int64_t>(unit) * kUnit;
   double sum[kUnit] = {};
-  auto add = [&](int64_t c, int which) {
-    const Unit u = load_unit(partial_row(a, c, which) + column);
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) sum[e] += static_cast<double>(u.x[e]);
-  };
   if (in) {
-    if (group == 0) add(chunk, 1);
-#pragma unroll 4
-    for (int64_t c = chunk + 1 + group; c <= last; c += groups) add(c, 0);
+    // Parts: this chunk's own, and of each that follows the first.  Eight in flight.
+    constexpr int kParts = 8;
+    for (int64_t c = chunk + group; c <= last; c += groups * kParts) {
+      Raw<float> part[kParts];
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        const int64_t at = c + k * groups;
+        if (at <= last) part[k] = load_raw(static_cast<const float*>(partial_row(a, at, at == chunk ? 1 : 0) + column));
+      }
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        if (c + k * groups > last) continue;
+        const Unit u = values(part[k]);
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) sum[e] += static_cast<double>(u.x[e]);
+      }
+    }
   }
 #pragma unroll
   for (int e = 0; e < kUnit; ++e) s_sum[threadIdx.x][e] = sum[e];
@@ -497,7 +564,7 @@ hipError_t launch_sums(const EmbedArgs& a, hipStream_t st) {
   if (e != hipSuccess || chunks < 2) return e;
   const int join_lanes = row_lanes_log2(a.H, 6);
   const int64_t join_slabs = ceil_div(a.H / kUnit, int64_t(1) << join_lanes);
-  hipLaunchKernelGGL(embed_join_kernel<Out>, dim3(static_cast<unsigned>(chunks * join_slabs)), dim3(kThreads), 0, st, a,
+  hipLaunchKernelGGL(embed_join_kernel<Out>, dim3(static_cast<unsigned>(chunks * join_slabs)), dim3(kJoinThreads), 0, st, a,
                      join_lanes, static_cast<int>(join_slabs));
   return hipGetLastError();
 }
@@ -513,7 +580,7 @@ int passes_of(int64_t V, int* bits) {
 // Which of the two buffers the first pass fills, so that the last one fills buffer 0.
 hipError_t launch_order(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) {
   if (p.ranks) {
-    hipLaunchKernelGGL(embed_rank_kernel, dim3(static_cast<unsigned>(ceil_div(a.N, kWave))), dim3(kRankThreads), 0, st, a);
+    hipLaunchKernelGGL(embed_rank_kernel, dim3(static_cast<unsigned>(ceil_div(a.N, kRankSteps))), dim3(kRankThreads), 0, st, a);
     return hipGetLastError();
   }
   int bits = 0;
@@ -526,10 +593,14 @@ hipError_t launch_order(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) 
     hipLaunchKernelGGL(embed_count_kernel, grid, dim3(kSortThreads), 0, st, a, from, pass * bits, bits);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(kScanThreads), 0, st, a.counts, blocks << bits);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embed_move_kernel, grid, dim3(kSortThreads), 0, st, a, from, to, pass * bits, bits);
+    if (blocks <= kMostSelfScanned) {
+      hipLaunchKernelGGL(embed_move_kernel<true>, grid, dim3(kSortThreads), 0, st, a, from, to, pass * bits, bits);
+    } else {
+      hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(kScanThreads), 0, st, a.counts, blocks << bits);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(embed_move_kernel<false>, grid, dim3(kSortThreads), 0, st, a, from, to, pass * bits, bits);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     from = to;
@@ -540,14 +611,12 @@ hipError_t launch_order(const EmbedArgs& a, const EmbedPlan& p, hipStream_t st) 
 template <typename In, typename Out>
 hipError_t launch_lookup(const EmbedArgs& a, hipStream_t st) {
   const int lanes = row_lanes_log2(a.H, 8), groups = kThreads >> lanes;
-  constexpr int kRows = 4;
-  if (a.N >= 4096 * groups) {
-    hipLaunchKernelGGL((embed_kernel<In, Out, kRows>), dim3(static_cast<unsigned>(ceil_div(a.N, kRows * groups))), dim3(kThreads),
-                       0, st, a, lanes);
-  } else {
-    hipLaunchKernelGGL((embed_kernel<In, Out, 1>), dim3(static_cast<unsigned>(ceil_div(a.N, groups))), dim3(kThreads), 0, st, a,
-                       lanes);
-  }
+  auto launch = [&](auto kernel, int rows) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(ceil_div(a.N, rows * groups))), dim3(kThreads), 0, st, a, lanes);
+  };
+  if (a.N < 4096 * groups) launch(embed_kernel<In, Out, 1, false>, 1);
+  else if (a.N * a.H * static_cast<int64_t>(sizeof(Out)) < kCachedBytes) launch(embed_kernel<In, Out, 4, false>, 4);
+  else launch(embed_kernel<In, Out, 4, true>, 4);
   return hipGetLastError();
 }
 
