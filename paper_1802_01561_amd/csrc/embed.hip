@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedArgs a) {
 // counts every block's digits, adds the counts up in the order (digit, block), and moves.
 constexpr int kMostDigitBits = 9, kMostDigits = 1 << kMostDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kSortItems = 4096;  // of a block
+constexpr int kSortItems = 2048;  // of a block
 constexpr int kSortRounds = kSortItems / kSortThreads;  // of 64 consecutive items a wave
 constexpr int kScanThreads = 1024;
 
