@@ -100,23 +100,26 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes_
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     const int64_t n = first + r * groups;
-    token[r] = n < a.N ? a.tokens[n] : -1;
-    if (lane == 0 && token[r] != -1 && (token[r] < 0 || token[r] >= a.V)) raise_error_flag(a.error_flag);
+    token[r] = a.tokens[n < a.N ? n : a.N - 1];
+    if (n < a.N && lane == 0 && token[r] != -1 && (token[r] < 0 || token[r] >= a.V)) raise_error_flag(a.error_flag);
   }
   for (int c = lane; c < units; c += lanes) {
-    Unit u[kRows];
+    // (Loads under a condition would be waited for one by one: tokens that are none read row 0.)
+    Raw<In> row[kRows];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      if (token[r] >= 0 && token[r] < a.V)
-        u[r] = load_unit(static_cast<const In*>(a.table) + static_cast<int64_t>(token[r]) * a.H + c * kUnit);
+    for (int r = 0; r < kRows; ++r) {
+      const int64_t t = token[r] >= 0 && token[r] < a.V ? token[r] : 0;
+      row[r] = load_raw(static_cast<const In*>(a.table) + t * a.H + c * kUnit);
+    }
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const int64_t n = first + r * groups;
       if (n >= a.N) continue;
       const bool valid = token[r] >= 0 && token[r] < a.V;
+      Unit u = values(row[r]);
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i) u[r].x[i] = valid ? u[r].x[i] * a.scale : token[r] == -1 ? 0.0f : NAN;
-      store_unit<kPast>(static_cast<Out*>(a.rows) + n * a.H + c * kUnit, u[r]);
+      for (int i = 0; i < kUnit; ++i) u.x[i] = valid ? u.x[i] * a.scale : token[r] == -1 ? 0.0f : NAN;
+      store_unit<kPast>(static_cast<Out*>(a.rows) + n * a.H + c * kUnit, u);
     }
   }
 }
@@ -206,7 +209,7 @@ __device__ __forceinline__ void rank_items(const EmbedArgs& a, int from, int shi
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   t->first = static_cast<int64_t>(blockIdx.x) * kSortItems + wave * (kSortRounds * kWave) + lane;
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) t->key[r] = t->first + r * kWave < a.N ? sort_key(a, from, t->first + r * kWave) : 0;
+  for (int r = 0; r < kSortRounds; ++r) t->key[r] = sort_key(a, from, t->first + r * kWave < a.N ? t->first + r * kWave : a.N - 1);
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const bool in = t->first + r * kWave < a.N;
@@ -310,7 +313,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, i
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const int64_t i = t.first + r * kWave;
-    step[r] = from < 0 ? static_cast<uint32_t>(i) : i < a.N ? a.steps[from][i] : 0;
+    step[r] = from < 0 ? static_cast<uint32_t>(i) : a.steps[from][i < a.N ? i : a.N - 1];
   }
   if constexpr (kScans) {
     // And those of all smaller digits.
@@ -452,18 +455,28 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int la
   bool first = true;  // the chunk's first run, which may come from the chunk before
   Unit sum = {};
   for (int64_t i = begin; i < end; i += kBatch) {
-    // Tokens one step further than the batch: a run ends where the next one differs.
-    uint32_t key[kBatch + 1];
+    // Tokens one step further than the batch: a run ends where the next one differs.  (Loads under
+    // a condition would be waited for one by one: what is behind the end is read at the last
+    // step, and where no run ends a step's own row in place of the table's.)
+    uint32_t key[kBatch + 1], step[kBatch];
 #pragma unroll
-    for (int b = 0; b <= kBatch; ++b) key[b] = i + b < a.N ? keys[i + b] : 0xffffffffu;
+    for (int b = 0; b <= kBatch; ++b) key[b] = keys[i + b < a.N ? i + b : a.N - 1];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) step[b] = a.steps[0][i + b < end ? i + b : end - 1];
+#pragma unroll
+    for (int b = 0; b <= kBatch; ++b)
+      if (i + b >= a.N) key[b] = 0xffffffffu;
+    if (key[0] >= V) break;
     Raw<In> row[kBatch];
     Raw<Out> was[kAccumulate ? kBatch : 1];
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      if (i + b >= end || key[b] >= V) continue;
-      row[b] = load_raw(d_rows + static_cast<int64_t>(a.steps[0][i + b]) * a.H);
+      const In* const from = d_rows + static_cast<int64_t>(step[b]) * a.H;
+      row[b] = load_raw(from);
       if constexpr (kAccumulate) {
-        if (key[b] != key[b + 1]) was[b] = load_raw(static_cast<const Out*>(d_table) + static_cast<int64_t>(key[b]) * a.H);
+        const void* const other = sizeof(Out) > sizeof(In) ? static_cast<const void*>(d_table) : from;
+        const void* const held = d_table + static_cast<int64_t>(key[b]) * a.H;
+        was[b] = load_raw(static_cast<const Out*>(key[b] < V && key[b] != key[b + 1] ? held : other));
       }
     }
 #pragma unroll
@@ -516,8 +529,8 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, i
       Raw<float> part[kParts];
 #pragma unroll
       for (int k = 0; k < kParts; ++k) {
-        const int64_t at = c + k * groups;
-        if (at <= last) part[k] = load_raw(static_cast<const float*>(partial_row(a, at, at == chunk ? 1 : 0) + column));
+        const int64_t at = c + k * groups <= last ? c + k * groups : last;
+        part[k] = load_raw(static_cast<const float*>(partial_row(a, at, at == chunk ? 1 : 0) + column));
       }
 #pragma unroll
       for (int k = 0; k < kParts; ++k) {

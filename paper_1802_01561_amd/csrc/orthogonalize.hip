@@ -102,18 +102,20 @@ __global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t) {
   const int y0 = g.transposed ? j0 : i0, x0 = g.transposed ? i0 : j0;
   const int rows = g.transposed ? g.c : g.r, columns = g.transposed ? g.r : g.c;
   const int row = threadIdx.x / kScaleTile, column = threadIdx.x % kScaleTile;
-  float given[kPasses];
+  // (Loads under a condition would be waited for one by one: places behind the ends are moved to them.)
+  In given[kPasses];
 #pragma unroll
   for (int k = 0; k < kPasses; ++k) {
-    const int y = y0 + row + k * kPerPass;
-    given[k] = y < rows && x0 + column < columns ? logit_to_float(in[static_cast<int64_t>(y) * columns + x0 + column]) : 0.0f;
+    const int y = y0 + row + k * kPerPass, x = x0 + column;
+    given[k] = in[static_cast<int64_t>(y < rows ? y : rows - 1) * columns + (x < columns ? x : columns - 1)];
   }
   const double squares = block_sum(static_cast<int>(threadIdx.x) < g.partials ? t.partials[g.first_partial + threadIdx.x] : 0.0);
   const double norm = sqrt(squares), least = t.epsilon;
   const double factor = 1.0 / (norm < least ? least : norm);  // a NaN norm stays
 #pragma unroll
   for (int k = 0; k < kPasses; ++k) {
-    const float v = static_cast<float>(static_cast<double>(given[k]) * factor);
+    const bool inside = y0 + row + k * kPerPass < rows && x0 + column < columns;
+    const float v = inside ? static_cast<float>(static_cast<double>(logit_to_float(given[k])) * factor) : 0.0f;
     if (g.transposed) s_tile[column][row + k * kPerPass] = v;
     else s_tile[row + k * kPerPass][column] = v;
   }
