@@ -214,20 +214,23 @@ int tile_for(const Table& t, int kind, int passes) {
   return tiles_cost(t, kind, kTile, passes) <= tiles_cost(t, kind, kSmallTile, passes) ? kTile : kSmallTile;
 }
 
-// In the small matrices' kernels, tiles of 64 or 32: a launch, and the longer of what all CUs
-// take for the steps of 64 k of all tiles and what one tile takes for its own.
-// 1024 x 1024, us with tiles of 32, 64 and those above: one bfloat16 matrix 186, 149, 322, four 501,
-// 342, 349, sixteen 1806, 992, 836; float32 253, 224, 666, four 704, 673, 702.
+// In the small matrices' kernels, tiles of 64 or 32: a launch, and the longest of what the rounds of
+// tiles take (2.5 us and their steps of 64 k each), what the longest tile does, and the steps
+// of all of them where several share a CU.
+// 1024 x 1024, us with tiles of 32, 64 and those above: one bfloat16 matrix 189, 156, 322, four 504,
+// 349, 349, sixteen 1806, 992, 770; float32 268, 249, 666, four 750, 754, 702.
 double small_cost(const Table& t, int kind, int size, bool pair) {
-  double work = 0.0, longest = 0.0;
+  double work = 0.0, longest = 0.0, tiles = 0.0;
   for (int i = 0; i < t.count; ++i) {
-    const double steps = (kind == 0 ? t.at[i].pc : t.at[i].pr) / kTileK;
-    work += static_cast<double>(tiles_in(t.at[i], kind, size)) * steps;
+    const double steps = (kind == 0 ? t.at[i].pc : t.at[i].pr) / kTileK, n = static_cast<double>(tiles_in(t.at[i], kind, size));
+    tiles += n;
+    work += n * steps;
     longest = std::max(longest, steps);
   }
-  const double all = size == 64 ? (pair ? 0.9 : 0.345) : pair ? 0.237 : 0.164;
-  const double one = size == 64 ? (pair ? 0.6 : 0.28) : pair ? 0.2 : 0.15;
-  return 4.0 + std::max(work * all / kCus, longest * one);
+  const double one = size == 64 ? (pair ? 0.5 : 0.26) : pair ? 0.25 : 0.13;
+  const double shared = size == 64 ? (pair ? 0.5 : 0.345) : pair ? 0.237 : 0.164;
+  const double rounds = std::ceil(tiles / (kCus * (size == 64 && pair ? 1 : 2)));
+  return 4.5 + std::max({rounds * (2.5 + one * work / tiles) - 2.5, longest * one, work * shared / kCus});
 }
 
 // VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256) forces the tiles, to cross-check them.

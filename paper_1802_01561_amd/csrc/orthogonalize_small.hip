@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
   ri.start(wn, s, g);
   rj.start(wm, s, g);
   f32x4 acc[kN][kN] = {};  // [m][n]
-  f32x4 total[kN][kN] = {};
+  f32x4 cross[kN][kN] = {}, total[kN][kN] = {};  // of the low parts; of all
   const int i0 = at.wide * kSide + wn + s, j0 = at.deep * kSide + wm + 4 * g;
   // What the results take beside the products is under way before them.
   f32x4 x[kN][kN];
@@ -125,46 +125,74 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
   }
 #pragma unroll
   for (int k = 0; k + 1 < kStages; ++k) copy(k, k);
-  int stage = 0;
-  for (int k = 0; k < steps; ++k) {
+  // A step's fragments are read while the one before it is multiplied: from barrier to barrier there
+  // is the longer of the two, not both (one after the other 0.3 us a step).
+  struct Fragments {
+    bf16x8 i[2][kParts][kN], j[2][kParts][kN];
+  };
+  int stage = 0, k = 0;
+  auto read = [&](Fragments& f) {
     stage_barrier<(kStages - 2) * kCopies>();
     copy(stage == 0 ? kStages - 1 : stage - 1, k + kStages - 1);
     const char* const from = lds + stage * kStage;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8 fi[kParts][kN], fj[kParts][kN];
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int part = 0; part < kParts; ++part)
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
-          fi[part][n] = ri.read(from + 2 * part * kBytes, n, kk);
-          fj[part][n] = rj.read(from + (2 * part + 1) * kBytes, n, kk);
+          f.i[kk][part][n] = ri.read(from + 2 * part * kBytes, n, kk);
+          f.j[kk][part][n] = rj.read(from + (2 * part + 1) * kBytes, n, kk);
         }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    ++k;
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](const Fragments& f) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int m = 0; m < kN; ++m)
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
           if constexpr (kPair) {
-            multiply_add(acc[m][n], fj[1][m], fi[0][n]);
-            multiply_add(acc[m][n], fj[0][m], fi[1][n]);
+            multiply_add(cross[m][n], f.j[kk][1][m], f.i[kk][0][n]);
+            multiply_add(cross[m][n], f.j[kk][0][m], f.i[kk][1][n]);
           }
-          multiply_add(acc[m][n], fj[0][m], fi[0][n]);
+          multiply_add(acc[m][n], f.j[kk][0][m], f.i[kk][0][n]);
         }
-    }
-    stage = stage + 1 == kStages ? 0 : stage + 1;
-    // Float32 results: sums over 256 k apiece, added up.  The rounding errors of one long sum would
-    // be the most of a result's (256 x 2592: 1.6e-6 off, so 1.0e-6).
-    if (kPair && k % 4 == 3 && k + 1 < steps) {
-    #pragma unroll
-      for (int m = 0; m < kN; ++m)
+  };
+  // Float32 results: sums over 256 k apiece, added up.  The rounding errors of one long sum would
+  // be the most of a result's (256 x 2592: 1.6e-6 off, so 9e-7).
+  auto add_up = [&](int left) {
+    if (!kPair || (steps - left) % 4 != 0) return;
 #pragma unroll
-        for (int n = 0; n < kN; ++n) {
+    for (int m = 0; m < kN; ++m)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) total[m][n][q] += acc[m][n][q];
-          acc[m][n] = f32x4{};
-        }
-    }
+      for (int n = 0; n < kN; ++n) {
+        total[m][n] += acc[m][n];
+        acc[m][n] = f32x4{};
+      }
+  };
+  Fragments even, odd;
+  read(even);
+  for (int left = steps;;) {
+    if (left > 1) read(odd);
+    multiply(even);
+    if (--left == 0) break;
+    add_up(left);
+    if (left > 1) read(even);
+    multiply(odd);
+    if (--left == 0) break;
+    add_up(left);
   }
+#pragma unroll
+  for (int m = 0; m < kN; ++m)
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      if constexpr (kPair) total[m][n] += cross[m][n];
+      total[m][n] += acc[m][n];
+    }
 
   // The tile by way of LDS, so that rows and columns of it are stored in whole pieces.
   stage_barrier();
@@ -177,7 +205,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
       for (int q = 0; q < 4; ++q) {
         const int i = i0 + 16 * n, j = j0 + 16 * m + q;
         const bool in = i < e.r && j < (kKind == 2 ? e.c : e.r);
-        const float sum = total[m][n][q] + acc[m][n][q];
+        const float sum = total[m][n][q];
         float y;
         if constexpr (kKind == 0) {
           y = sum * (1.0f / (kScaleX * kScaleX));
