@@ -200,25 +200,36 @@ int64_t tiles_in(const Entry& e, int kind, int size) {
   return kind == 2 ? rows * tiles_of(e.pc, size) : rows * (rows + 1) / 2;
 }
 
-// What a launch of one kind takes (us): in tiles of 256 or 128 by their rounds (round_cost).
+// What a launch of one kind takes (us) in tiles of 256 or 128: the longer of all rounds of them and
+// the longest tile.  A step of 64 k as for the vocabulary layer (round_cost), or of 128 where a CU
+// has one tile; what a tile costs beside its steps is its stores, and X's are the most: 240 tiles
+// of 16 to 64 steps of A, 16 of B, 768 of 16 of X 117, 54, 191 us in tiles of 256, 103, 52, 228 in
+// tiles of 128.
 double tiles_cost(const Table& t, int kind, int size, int passes) {
-  double work = 0.0, tiles = 0.0;
+  double work = 0.0, tiles = 0.0, steps = 0.0, longest = 0.0;
   for (int i = 0; i < t.count; ++i) {
     const double n = static_cast<double>(tiles_in(t.at[i], kind, size));
+    const double k = (kind == 0 ? t.at[i].pc : t.at[i].pr) / kTileK * passes;
     tiles += n;
-    work += n * round_cost(size, (kind == 0 ? t.at[i].pc : t.at[i].pr) / kTileK * passes);
+    work += n * k;
+    longest = std::max(longest, k);
   }
-  return std::ceil(tiles / resident_tiles(size)) * work / tiles;
+  steps = work / tiles;
+  const bool alone = size == kSmallTile && tiles <= kCus;
+  auto cost = [&](double k) {
+    const double stores = size == kTile ? (kind == 2 ? 20.0 : 10.0) : kind == 2 ? 10.0 : 3.0;
+    return alone ? 0.8 * k + 3.0 + 0.6 * stores : round_cost(size, 0) + (round_cost(size, 1) - round_cost(size, 0)) * k + stores;
+  };
+  return std::max(cost(longest), std::ceil(tiles / resident_tiles(size)) * cost(steps));
 }
 int tile_for(const Table& t, int kind, int passes) {
   return tiles_cost(t, kind, kTile, passes) <= tiles_cost(t, kind, kSmallTile, passes) ? kTile : kSmallTile;
 }
 
-// In the small matrices' kernels, tiles of 64 or 32: a launch, and the longest of what the rounds of
-// tiles take (2.5 us and their steps of 64 k each), what the longest tile does, and the steps
-// of all of them where several share a CU.
-// 1024 x 1024, us with tiles of 32, 64 and those above: one bfloat16 matrix 189, 156, 322, four 504,
-// 349, 349, sixteen 1806, 992, 770; float32 268, 249, 666, four 750, 754, 702.
+// The same in the small matrices' kernels' tiles of 64 or 32: a launch, and the tile that has a CU for
+// itself, or all rounds of them.
+// 1024 x 1024, us with tiles of 32, 64, 128: one bfloat16 matrix 189, 153, 322, four 503, 353, 304,
+// eight 927, 573, 393; float32 268, 246, 635, two 421, 458, 642, four 735, 756, 655.
 double small_cost(const Table& t, int kind, int size, bool pair) {
   double work = 0.0, longest = 0.0, tiles = 0.0;
   for (int i = 0; i < t.count; ++i) {
@@ -227,10 +238,11 @@ double small_cost(const Table& t, int kind, int size, bool pair) {
     work += n * steps;
     longest = std::max(longest, steps);
   }
-  const double one = size == 64 ? (pair ? 0.5 : 0.26) : pair ? 0.25 : 0.13;
-  const double shared = size == 64 ? (pair ? 0.5 : 0.345) : pair ? 0.237 : 0.164;
+  const double step = size == 64 ? (pair ? 0.5 : 0.26) : pair ? 0.25 : 0.13;
+  const double alone = 2.5 + step * longest;
+  if (tiles <= kCus) return 2.0 + alone;
   const double rounds = std::ceil(tiles / (kCus * (size == 64 && pair ? 1 : 2)));
-  return 4.5 + std::max({rounds * (2.5 + one * work / tiles) - 2.5, longest * one, work * shared / kCus});
+  return 2.0 + std::max(alone, rounds * ((size == 64 ? 6.0 : pair ? 3.5 : 3.0) + step * work / tiles));
 }
 
 // VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256) forces the tiles, to cross-check them.
@@ -246,9 +258,11 @@ Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
   Table t = {};
   t.count = count;
   const bool pair = !items[0].bf16;
+  for (int i = 0; i < count; ++i) t.at[i] = entry_for(items[i]);
+  // The longest tiles first.
+  std::stable_sort(t.at, t.at + count, [](const Entry& x, const Entry& y) { return x.pc > y.pc; });
   for (int i = 0; i < count; ++i) {
     Entry& e = t.at[i];
-    e = entry_for(items[i]);
     const int64_t elements = static_cast<int64_t>(e.r) * e.c;
     e.first_partial = t.total_partials;
     e.partials = static_cast<int32_t>((elements + norm_chunk(elements) - 1) / norm_chunk(elements));
