@@ -232,41 +232,43 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
   while (tiles.any()) {
     const Place here = at;
     Accumulators<kSize> acc = {};
-    contract<true, false, true>(job, lds, parity, wave, lane, acc, [&] {
-      tiles.next();
-      start();
-    });
     const Entry& e = t.at[here.entry];
     const Pieces p = pieces_of<kPair>(e, turn);
     const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 4 * g;
     Out* const out = static_cast<Out*>(e.out);
     const bool vectors = e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0;
-    // X of the next 16 rows is fetched while these are stored.
-    f32x4 x[2][kPair ? kMT : 1];
-    v2u part[2][2][kPair ? 1 : kMT];
-    float of_row[2];
+    // X's rows are fetched kAhead times 16 ahead, the first of them during the last step of k.
+    constexpr int kAhead = 1, kBuffers = kAhead + 1;
+    f32x4 x[kBuffers][kPair ? kMT : 1];
+    v2u part[kBuffers][2][kPair ? 1 : kMT];
+    float of_row[kBuffers];
     auto load_rows = [&](int n) {
       const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
-      of_row[n % 2] = p.e[i];
+      of_row[n % kBuffers] = p.e[i];
 #pragma unroll
       for (int m = 0; m < kMT; ++m) {
         const int j = j0 + 16 * m;
         const int64_t from = static_cast<int64_t>(i) * e.pc + (j < e.pc ? j : 0);
         if constexpr (kPair) {
-          x[n % 2][m] = *reinterpret_cast<const f32x4*>(p.x + from);
+          x[n % kBuffers][m] = *reinterpret_cast<const f32x4*>(p.x + from);
         } else {
-          part[n % 2][0][m] = *reinterpret_cast<const v2u*>(p.from[0] + from);
-          if constexpr (!kLast) part[n % 2][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
+          part[n % kBuffers][0][m] = *reinterpret_cast<const v2u*>(p.from[0] + from);
+          if constexpr (!kLast) part[n % kBuffers][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
         }
       }
     };
-    load_rows(0);
+    contract<true, false, true>(job, lds, parity, wave, lane, acc, [&] {
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) load_rows(n);
+      tiles.next();
+      start();
+    });
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-      if (n + 1 < kNT) load_rows(n + 1);
+      if (n + kAhead < kNT) load_rows(n + kAhead);
       const int i = i0 + 16 * n + s;
       const bool row = i < e.r;
-      const float factor = a + of_row[n % 2];
+      const float factor = a + of_row[n % kBuffers];
 #pragma unroll
       for (int m = 0; m < kMT; ++m) {
         const int j = j0 + 16 * m;
@@ -275,10 +277,10 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
         for (int q = 0; q < 4; ++q) {
           float before;
           if constexpr (kPair) {
-            before = x[n % 2][m][q];
+            before = x[n % kBuffers][m][q];
           } else {
-            before = high_of(part[n % 2][0][m][q / 2], q % 2);
-            if constexpr (!kLast) before += high_of(part[n % 2][1][m][q / 2], q % 2);
+            before = high_of(part[n % kBuffers][0][m][q / 2], q % 2);
+            if constexpr (!kLast) before += high_of(part[n % kBuffers][1][m][q / 2], q % 2);
             before *= 1.0f / kScaleX;
           }
           y[q] = fmaf(factor, before, element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
