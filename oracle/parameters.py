@@ -72,21 +72,47 @@ def _product(a, b):
     return total
 
 
-def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.0, parts=1):
+class _Symmetric:
+    """A symmetric matrix as it is kept: its diagonal in float32, the rest as an operand."""
+
+    def __init__(self, off, diagonal, parts):
+        self.diagonal = diagonal.astype(np.float32).astype(np.float64)
+        off = off.astype(np.float32).astype(np.float64)
+        self.operand = _operand(off - np.diag(np.diagonal(off)), 8192.0, parts)
+        self.off = sum(self.operand)
+
+
+def _combine(m, n, of_m, of_n, of_mn, parts):
+    """of_m M + of_n N + of_mn M N."""
+    oo = _product(m.operand, n.operand)
+    dm, dn = m.diagonal[:, None], n.diagonal[None, :]
+    off = of_m * m.off + of_n * n.off + of_mn * (dm * n.off + m.off * dn + oo)
+    return _Symmetric(off, of_m * m.diagonal + of_n * n.diagonal + of_mn * (m.diagonal * n.diagonal + np.diagonal(oo)), parts)
+
+
+def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.0, parts=1, together=1):
     """orthogonalize() with the roundings of the operands, of the sums of products and of what is
-    kept between the products: X float32, operands float16 in one part or two, diagonals apart."""
-    single = lambda y: _f64(y.astype(np.float32))  # noqa: E731
+    kept between the products: X float32, operands float16 in one part or two, diagonals apart.
+    together 2: steps two at once, the second's matrices from the first's."""
+    single = lambda y: _f64(np.asarray(y).astype(np.float32))  # noqa: E731
     x = single(_start(g, epsilon))
     tall = x.shape[0] > x.shape[1]
     x = x.T if tall else x
-    for a, b, c in coefficients:
+    k = 0
+    while k < len(coefficients):
+        a, b, c = coefficients[k]
         xs = _operand(x, 4096.0, parts)
         gram = _product(xs, [y.T for y in xs])
-        d = np.diagonal(gram).copy()
-        os = _operand(gram - np.diag(d), 8192.0, parts)
-        oo = _product(os, os)
-        poly = single(sum(os) * (b + c * (d[:, None] + d[None, :])) + c * oo)
-        e = single(b * d + c * (d * d + np.diagonal(oo)))
-        ps = _operand(poly - np.diag(np.diagonal(poly)), 8192.0, parts)
-        x = single(single(a + e)[:, None] * x + _product(ps, xs))
+        m = _Symmetric(gram, np.diagonal(gram).copy(), parts)
+        p = _combine(m, m, b, 0.0, c, parts)
+        k += 1
+        if together == 2 and k < len(coefficients):
+            a2, b2, c2 = coefficients[k]
+            t = _combine(m, p, a, 0.0, 1.0, parts)
+            m = _combine(t, p, a, 0.0, 1.0, parts)
+            q = _combine(m, m, b2, 0.0, c2, parts)
+            p = _combine(q, p, a, a2, 1.0, parts)
+            a = float(np.float32(a * a2))
+            k += 1
+        x = single(single(a + p.diagonal)[:, None] * x + _product(p.operand, xs))
     return scale * (x.T if tall else x)

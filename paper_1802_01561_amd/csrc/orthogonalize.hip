@@ -245,12 +245,19 @@ double small_cost(const Table& t, int kind, int size, bool pair) {
   return 2.0 + std::max(alone, rounds * ((size == 64 ? 6.0 : pair ? 3.5 : 3.0) + step * work / tiles));
 }
 
-// VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256) forces the tiles, to cross-check them.
-int forced_tile() {
+// VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256, with x1 or x2 behind) forces the tiles
+// and whether steps are taken two at once, to cross-check them.
+struct Forced {
+  int size = 0, together = 0;
+};
+Forced forced_kernel() {
+  Forced f;
   const char* const k = std::getenv("VTRACE_KERNEL");
+  if (k == nullptr) return f;
   for (const int size : {32, 64, kSmallTile, kTile})
-    if (k && std::string(k) == "ortho_" + std::to_string(size)) return size;
-  return 0;
+    for (int together = 0; together <= 2; ++together)
+      if (k == "ortho_" + std::to_string(size) + (together ? "x" + std::to_string(together) : "")) f = {size, together};
+  return f;
 }
 
 // The entries of a group of matrices, all of one type, and the workspace's bytes for them.
@@ -271,20 +278,26 @@ Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
     t.total_blocks += static_cast<int32_t>(tiles_of(e.r, kScaleTile) * (e.pc / kScaleTile));
   }
   const int passes = pair ? 3 : 1;
-  double tiles = 0.0, small = 0.0;
+  double tiles[3], small[3];
   int small_size[3];
   for (int kind = 0; kind < 3; ++kind) {
     t.size[kind] = tile_for(t, kind, passes);
-    tiles += tiles_cost(t, kind, t.size[kind], passes);
+    tiles[kind] = tiles_cost(t, kind, t.size[kind], passes);
     small_size[kind] = small_cost(t, kind, 32, pair) <= small_cost(t, kind, 64, pair) ? 32 : 64;
-    small += small_cost(t, kind, small_size[kind], pair);
+    small[kind] = small_cost(t, kind, small_size[kind], pair);
   }
-  t.small = small < tiles;
+  // Two steps: A and X twice, or once and three products more of B's size.
+  auto one_by_one = [](const double (&us)[3]) { return 2.0 * (us[0] + us[1] + us[2]); };
+  auto together = [](const double (&us)[3]) { return us[0] + 5.0 * us[1] + us[2]; };
+  t.small = std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
   if (t.small) std::copy_n(small_size, 3, t.size);
-  if (const int forced = forced_tile()) {
-    t.small = forced < kSmallTile;
-    std::fill_n(t.size, 3, forced);
+  t.twos = t.small ? together(small) < one_by_one(small) : together(tiles) < one_by_one(tiles);
+  const Forced forced = forced_kernel();
+  if (forced.size) {
+    t.small = forced.size < kSmallTile;
+    std::fill_n(t.size, 3, forced.size);
   }
+  if (forced.together) t.twos = forced.together == 2;
   int64_t at = round_up(kWsDataOffset, 256) + static_cast<int64_t>(kPartialBytes);
   t.partials = reinterpret_cast<double*>(reinterpret_cast<uintptr_t>(ws) + kWsDataOffset);
   for (int i = 0; i < count; ++i) {
@@ -301,35 +314,10 @@ Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
   return t;
 }
 
-template <typename T, bool kPair>
-hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
-                        hipStream_t st) {
-  size_t bytes;
-  Table t = table_of(items, count, ws, &bytes);
-  t.epsilon = epsilon;
-  hipLaunchKernelGGL(ortho_norm_kernel<T>, dim3(t.total_partials), dim3(kNormThreads), 0, st, t);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((ortho_scale_kernel<T, kPair>), dim3(t.total_blocks), dim3(kNormThreads), 0, st, t);
-  e = hipGetLastError();
-  for (int k = 0; k < step_count && e == hipSuccess; ++k) {
-    const int turn = k % 2;
-    const bool last = k + 1 == step_count;
-    if (t.small) {
-      for (int kind = 0; kind < 3 && e == hipSuccess; ++kind) e = launch_ortho_small(t, kind, kPair, last, turn, steps[k], st);
-      continue;
-    }
-    e = launch_ortho_tiles_symmetric(t, false, kPair, t.size[0], turn, steps[k], st);
-    if (e == hipSuccess) e = launch_ortho_tiles_symmetric(t, true, kPair, t.size[1], turn, steps[k], st);
-    if (e == hipSuccess) e = launch_ortho_tiles_update(t, kPair, step_count - 1 - k, t.size[2], turn, steps[k], st);
-  }
-  return e;
-}
-
-}  // namespace
-
-bool ortho_steps_ok(const OrthoStep* steps, int count) {
-  double most = 1.0;  // the largest singular value that there may be
+// The largest singular value that there may be before each of the steps, starting from 1; false
+// where they leave the operands' range.
+bool singular_bounds(const OrthoStep* steps, int count, double (&before)[kOrthoMostSteps]) {
+  double most = 1.0;
   for (int k = 0; k < count; ++k) {
     const double a = steps[k].a, b = steps[k].b, c = steps[k].c;
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
@@ -357,9 +345,92 @@ bool ortho_steps_ok(const OrthoStep* steps, int count) {
       at(-a / (3.0 * b));
     }
     if (!(next <= kMostSingular)) return false;
+    before[k] = most;
     most = next;
   }
   return true;
+}
+
+
+// Whether two steps at once (launch_group) stay in the operands' range, singular values being at
+// most `most` before them: the eigenvalues of what is formed are polynomials of t = s^2 of degree up
+// to 12, whose range over [0, most^2] is at most 1 / cos(12 pi / 128) times (5% over) that over 64
+// Chebyshev points.
+bool two_steps_ok(const OrthoStep& p, const OrthoStep& q, double most) {
+  constexpr int kPoints = 64;
+  double low[3] = {0.0, 0.0, 0.0}, high[3] = {0.0, 0.0, 0.0};
+  for (int i = 0; i < kPoints; ++i) {
+    const double t = most * most * 0.5 * (1.0 + std::cos((2 * i + 1) * M_PI / (2 * kPoints)));
+    const double first = p.a + t * (p.b + t * p.c), then = t * first * first;
+    const double value[3] = {t * first, then, first * (q.a + then * (q.b + then * q.c)) - static_cast<double>(p.a) * q.a};
+    for (int v = 0; v < 3; ++v) {
+      low[v] = std::min(low[v], value[v]);
+      high[v] = std::max(high[v], value[v]);
+    }
+  }
+  for (int v = 0; v < 3; ++v)
+    if (!(high[v] - low[v] <= kMostRange)) return false;
+  return true;
+}
+
+// Two steps at once.  With P = a I + B of the first, X' = P X has X' X'^T = P A P, so that both steps
+// take one product with X each way, and the second's matrices come from the first's:
+//   T = A P,   A' = T P,   B' = b' A' + c' A' A',   X'' = (a' I + B') (a I + B) X = (a a' I + Q) X,
+//   Q = a' B + a B' + B' B.
+// All are polynomials of A, and so commute and are symmetric: half their tiles are computed.
+// Where X has more columns than rows, or its loads and stores take as long as products, that is
+// less: 3 r^2 c operations and X twice against three products of r^3.
+template <typename T, bool kPair>
+hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
+                        hipStream_t st) {
+  size_t bytes;
+  Table t = table_of(items, count, ws, &bytes);
+  t.epsilon = epsilon;
+  double most[kOrthoMostSteps];
+  if (!singular_bounds(steps, step_count, most)) return hipErrorInvalidValue;
+  auto steps_from = [&](int k) {
+    return k < step_count && k + 1 < step_count && t.twos && two_steps_ok(steps[k], steps[k + 1], most[k]) ? 2 : 1;
+  };
+  hipLaunchKernelGGL(ortho_norm_kernel<T>, dim3(t.total_partials), dim3(kNormThreads), 0, st, t);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((ortho_scale_kernel<T, kPair>), dim3(t.total_blocks), dim3(kNormThreads), 0, st, t);
+  e = hipGetLastError();
+  int turn = 0;
+  auto symmetric = [&](int of, const Product& p) {
+    if (e != hipSuccess) return;
+    e = t.small ? launch_ortho_small_symmetric(t, of, kPair, turn, p, st) : launch_ortho_tiles_symmetric(t, of, kPair, turn, p, st);
+  };
+  bool low = true;
+  for (int k = 0; k < step_count && e == hipSuccess;) {
+    const int together = steps_from(k), next = k + together;
+    const OrthoStep& p = steps[k];
+    symmetric(kOfX, {0, 0, 0, 0.0f, 0.0f, 0.0f});
+    symmetric(kOfOne, {1, 0, 0, p.b, 0.0f, p.c});
+    Update u = {1, p.a, next == step_count, low, false};
+    if (together == 2) {
+      const OrthoStep& q = steps[k + 1];
+      symmetric(kOfTwo, {2, 0, 1, p.a, 0.0f, 1.0f});
+      symmetric(kOfTwo, {0, 2, 1, p.a, 0.0f, 1.0f});
+      symmetric(kOfOne, {2, 0, 0, q.b, 0.0f, q.c});
+      symmetric(kOfTwo, {0, 2, 1, p.a, q.a, 1.0f});
+      u.by = 0;
+      u.of_x = p.a * q.a;
+    }
+    // A last step for itself takes the operand alone as X: 2^-12 of it, which no step makes larger.
+    u.low_out = low = !(next + 1 == step_count);
+    if (e == hipSuccess) e = t.small ? launch_ortho_small_update(t, kPair, turn, u, st) : launch_ortho_tiles_update(t, kPair, turn, u, st);
+    turn ^= 1;
+    k = next;
+  }
+  return e;
+}
+
+}  // namespace
+
+bool ortho_steps_ok(const OrthoStep* steps, int count) {
+  double before[kOrthoMostSteps];
+  return singular_bounds(steps, count, before);
 }
 
 size_t ortho_workspace_bytes(const OrthoItem* items, int64_t count) {

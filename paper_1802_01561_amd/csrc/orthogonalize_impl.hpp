@@ -33,25 +33,36 @@ struct Table {
   int total_partials, total_blocks, total_tiles[3];
   int size[3];  // of the tiles of A, B and X
   float epsilon;
+  bool twos;   // two steps at once
   bool small;  // the small matrices' kernels, which keep X^T as well
 };
 static_assert(sizeof(Table) <= 4000, "kernel arguments");
+
+// A symmetric matrix C = of_m M + of_n N + of_mn M N from those numbered m and n, which commute; or
+// (A) from X.
+struct Product {
+  int out, m, n;
+  float of_m, of_n, of_mn;
+};
+// What a product is of: X and X^T, one matrix, or two.
+enum { kOfX = 0, kOfOne = 1, kOfTwo = 2 };
+
+constexpr int kSymmetric = 3;
 
 struct Pieces {
   float* x;           // [r, pc] X, of float32 matrices
   uint16_t* low;      // [r, pc] of bfloat16 ones what the operand leaves of X
   uint16_t* from[2];  // [r, pc] X as an operand: high and (float32 matrices) low parts
   uint16_t* to[2];    // [r, pc] the same behind this step
-  uint16_t* a[2];     // [r, pr] A without its diagonal
-  uint16_t* b[2];     // B without its diagonal
-  float* d;           // [r] A's diagonal
-  float* e;           // [r] B's
+  // Symmetric matrices (A, B and what is made of them): [r, pr] without the diagonal, and that, [r].
+  uint16_t* sym[kSymmetric][2];
+  float* diagonal[kSymmetric];
 };
 __host__ __device__ inline int64_t round_up(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 template <bool kPair>
 __host__ __device__ inline int64_t piece_bytes(int64_t r, int64_t pr, int64_t pc) {
   constexpr int kParts = kPair ? 2 : 1;
-  return r * pc * (2 * kParts + 2 * 2 * kParts) + r * pr * 2 * 2 * kParts + 2 * round_up(r * 4, 256);
+  return r * pc * (2 * kParts + 2 * 2 * kParts) + kSymmetric * (r * pr * 2 * kParts + round_up(r * 4, 256));
 }
 // Behind them, for the small matrices' kernels: X^T as an operand, before and after a step.
 template <bool kPair>
@@ -73,13 +84,23 @@ __device__ __forceinline__ Pieces pieces_of(const Entry& t, int turn) {
   for (int k = 0; k < 2; ++k) {
     p.from[k] = reinterpret_cast<uint16_t*>(at + (turn * kParts + (kPair ? k : 0)) * x);
     p.to[k] = reinterpret_cast<uint16_t*>(at + ((turn ^ 1) * kParts + (kPair ? k : 0)) * x);
-    p.a[k] = reinterpret_cast<uint16_t*>(at + 2 * kParts * x + (kPair ? k : 0) * a);
-    p.b[k] = reinterpret_cast<uint16_t*>(at + 2 * kParts * x + (kParts + (kPair ? k : 0)) * a);
   }
-  at += 2 * kParts * (x + a);
-  p.d = reinterpret_cast<float*>(at);
-  p.e = reinterpret_cast<float*>(at + round_up(static_cast<int64_t>(t.r) * 4, 256));
+  at += 2 * kParts * x;
+#pragma unroll
+  for (int m = 0; m < kSymmetric; ++m) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) p.sym[m][k] = reinterpret_cast<uint16_t*>(at + (m * kParts + (kPair ? k : 0)) * a);
+    p.diagonal[m] = reinterpret_cast<float*>(at + kSymmetric * kParts * a + m * round_up(static_cast<int64_t>(t.r) * 4, 256));
+  }
   return p;
+}
+// One of them, whichever it is (an index into an array in registers would put it into memory).
+template <bool kPair>
+__device__ __forceinline__ uint16_t* symmetric_of(const Entry& t, const Pieces& p, int m, int k) {
+  return p.sym[0][k] + static_cast<int64_t>(m) * t.r * t.pr * (kPair ? 2 : 1);
+}
+__device__ __forceinline__ float* diagonal_of(const Entry& t, const Pieces& p, int m) {
+  return p.diagonal[0] + m * (round_up(static_cast<int64_t>(t.r) * 4, 256) / 4);
 }
 
 struct TransposedPieces {
@@ -128,6 +149,19 @@ __device__ __forceinline__ unsigned low2(float x, float y, unsigned high) {
 __device__ __forceinline__ v2u high4(const float (&y)[4]) { return {high2(y[0], y[1]), high2(y[2], y[3])}; }
 __device__ __forceinline__ v2u low4(const float (&y)[4], v2u high) { return {low2(y[0], y[1], high[0]), low2(y[2], y[3], high[1])}; }
 
+// An element of a product beside the diagonal, and on it, from its factors' elements there (on the
+// diagonal: dm, dn) and the sum of O O'.
+template <int kOf>
+__device__ __forceinline__ float product_off(const Product& f, float m, float n, float dm_i, float dn_j, float oo) {
+  if constexpr (kOf == kOfOne) return fmaf(m, fmaf(f.of_mn, dm_i + dn_j, f.of_m), f.of_mn * oo);
+  else return fmaf(m, fmaf(f.of_mn, dn_j, f.of_m), fmaf(n, fmaf(f.of_mn, dm_i, f.of_n), f.of_mn * oo));
+}
+template <int kOf>
+__device__ __forceinline__ float product_diagonal(const Product& f, float dm, float dn, float oo) {
+  const float linear = kOf == kOfOne ? f.of_m * dm : fmaf(f.of_m, dm, f.of_n * dn);
+  return linear + f.of_mn * fmaf(dm, dn, oo);
+}
+
 // Tile `id` of a lower triangle: rows 0, 1 1, 2 2 2, ...
 __device__ __forceinline__ TileAt triangle_at(int id) {
   int row = static_cast<int>((sqrtf(8.0f * static_cast<float>(id) + 1.0f) - 1.0f) * 0.5f);
@@ -160,12 +194,17 @@ __device__ __forceinline__ void store_result(Out* p, const float (&y)[4], int le
 
 }  // namespace
 
-// The launches of one translation unit each, of one step: A (square false) or B (true), and X.
-// `pair`: float32 matrices.
-hipError_t launch_ortho_tiles_symmetric(const Table& t, bool square, bool pair, int size, int turn, const OrthoStep& p,
-                                        hipStream_t s);
-// `left`: steps that follow.
-hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int left, int size, int turn, const OrthoStep& p, hipStream_t s);
-hipError_t launch_ortho_small(const Table& t, int kind, bool pair, bool last, int turn, const OrthoStep& p, hipStream_t s);
+// The launches of one translation unit each: a symmetric matrix, or X <- of_x X + C X with the
+// symmetric matrix numbered `by`.  `pair`: float32 matrices.
+// Of bfloat16 ones, low_in and low_out: whether X's remainder beside the operand is read, and written.
+struct Update {
+  int by;
+  float of_x;
+  bool last, low_in, low_out;
+};
+hipError_t launch_ortho_tiles_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t s);
+hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t s);
+hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t s);
+hipError_t launch_ortho_small_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t s);
 
 }  // namespace vtrace

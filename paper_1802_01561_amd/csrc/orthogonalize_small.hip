@@ -22,12 +22,14 @@ constexpr int kSmallWaves = 4, kSmallThreads = kSmallWaves * kWave;
 // Steps of k in LDS, of two operands in `parts` parts.
 __host__ __device__ constexpr int small_stages(int side, int parts) { return side == 64 ? 6 - parts : parts == 1 ? 8 : 5; }
 
-// kKind 0: A from X; 1: B from A; 2: X, or of the last step the result.  Wave (wm, wn) has a
+// kOf: a symmetric matrix of X, one or two; kUpdate: X, or of the last step the result.  Wave (wm, wn) has a
 // quarter of the tile; a lane of the MFMA layout holds columns j + 16 m + 4 g + 0..3 of row
 // i + 16 n + s of that.
-template <int kKind, typename Out, bool kLast, int kSide>
-__global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int turn, OrthoStep step) {
+constexpr int kUpdate = 3;
+template <int kOf, typename Out, bool kLast, int kSide>
+__global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int turn, std::conditional_t<kOf == kUpdate, Update, Product> f) {
   constexpr bool kPair = sizeof(Out) == 4;
+  constexpr int kKind = kOf == kOfX ? 0 : kOf == kUpdate ? 2 : 1;
   constexpr int kParts = kPair ? 2 : 1, kN = kSide / 32;
   constexpr int kStages = small_stages(kSide, kParts), kBytes = kSide * kTileK * 2, kStage = 2 * kParts * kBytes;
   __shared__ __align__(1024) char lds[kStages * kStage];
@@ -60,7 +62,10 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
     places[o].along(pitch, static_cast<int>(rows < kSide ? rows : kSide), wave, lane);
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-      const uint16_t* const array = kKind == 0 ? p.from[k] : kKind == 1 ? p.a[k] : o == 0 ? p.b[k] : pt.from[k];
+      const uint16_t* array;
+      if constexpr (kOf == kOfX) array = p.from[k];
+      else if constexpr (kOf == kUpdate) array = o == 0 ? symmetric_of<kPair>(e, p, f.by, k) : pt.from[k];
+      else array = symmetric_of<kPair>(e, p, o == 0 ? f.m : f.n, k);
       operand[k][o] = make_rsrc(array + first * pitch, 0x7fffffff);
       nothing[k][o] = make_rsrc(array, 0);
     }
@@ -87,40 +92,44 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
   f32x4 cross[kN][kN] = {}, total[kN][kN] = {};  // of the low parts; of all
   const int i0 = at.wide * kSide + wn + s, j0 = at.deep * kSide + wm + 4 * g;
   // What the results take beside the products is under way before them.
+  constexpr int kMatrices = kOf == kOfTwo ? 2 : 1;
   f32x4 x[kN][kN];
-  v2u o[2][kN][kN];  // of A, or of X: high and low parts
+  v2u o[kMatrices][2][kN][kN];  // of M and N, or of X: high and low parts
   float of_row[kN];
   f32x4 of_column[kN];
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
     const int i = i0 + 16 * n, i_in = i < e.r ? i : e.r - 1;  // rows behind the last one: nobody stores them
-    if constexpr (kKind == 1) of_row[n] = p.d[i_in];
-    if constexpr (kKind == 2) of_row[n] = p.e[i_in];
+    if constexpr (kOf == kOfOne || kOf == kOfTwo) of_row[n] = diagonal_of(e, p, f.m)[i_in];
+    if constexpr (kOf == kUpdate) of_row[n] = diagonal_of(e, p, f.by)[i_in];
 #pragma unroll
     for (int m = 0; m < kN; ++m) {
       const int j = j0 + 16 * m;
-      if constexpr (kKind == 1) {
+      if constexpr (kOf == kOfOne || kOf == kOfTwo) {
 #pragma unroll
-        for (int k = 0; k < kParts; ++k) o[k][m][n] = *reinterpret_cast<const v2u*>(p.a[k] + static_cast<int64_t>(i_in) * e.pr + j);
+        for (int w = 0; w < kMatrices; ++w)
+#pragma unroll
+          for (int k = 0; k < kParts; ++k)
+            o[w][k][m][n] = *reinterpret_cast<const v2u*>(symmetric_of<kPair>(e, p, w == 0 ? f.m : f.n, k) + static_cast<int64_t>(i_in) * e.pr + j);
       }
-      if constexpr (kKind == 2) {
+      if constexpr (kOf == kUpdate) {
         const int64_t from = static_cast<int64_t>(i_in) * e.pc + j;
         if constexpr (kPair) {
           x[m][n] = *reinterpret_cast<const f32x4*>(p.x + from);
         } else {
-          o[0][m][n] = *reinterpret_cast<const v2u*>(p.from[0] + from);
-          o[1][m][n] = *reinterpret_cast<const v2u*>(p.low + from);
+          o[0][0][m][n] = *reinterpret_cast<const v2u*>(p.from[0] + from);
+          o[0][1][m][n] = *reinterpret_cast<const v2u*>(p.low + from);
         }
       }
     }
   }
-  if constexpr (kKind == 1) {
+  if constexpr (kOf == kOfOne || kOf == kOfTwo) {
 #pragma unroll
     for (int m = 0; m < kN; ++m)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int j = j0 + 16 * m + q;
-        of_column[m][q] = p.d[j < e.r ? j : e.r - 1];
+        of_column[m][q] = diagonal_of(e, p, f.n)[j < e.r ? j : e.r - 1];
       }
   }
 #pragma unroll
@@ -207,20 +216,25 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
         const bool in = i < e.r && j < (kKind == 2 ? e.c : e.r);
         const float sum = total[m][n][q];
         float y;
-        if constexpr (kKind == 0) {
+        if constexpr (kOf == kOfX) {
           y = sum * (1.0f / (kScaleX * kScaleX));
-          if (in && i == j) p.d[i] = y;
-        } else if constexpr (kKind == 1) {
-          const float oo = sum * (1.0f / (kScaleA * kScaleA)), di = of_row[n];
-          float off = high_of(o[0][m][n][q / 2], q % 2);
-          if constexpr (kPair) off += high_of(o[1][m][n][q / 2], q % 2);
-          y = fmaf(off * (1.0f / kScaleA), fmaf(step.c, di + of_column[m][q], step.b), step.c * oo);
-          if (in && i == j) p.e[i] = fmaf(step.b, di, step.c * fmaf(di, di, oo));
-        } else {
+          if (in && i == j) diagonal_of(e, p, f.out)[i] = y;
+        } else if constexpr (kOf == kUpdate) {
           float before;
           if constexpr (kPair) before = x[m][n][q];
-          else before = (high_of(o[0][m][n][q / 2], q % 2) + high_of(o[1][m][n][q / 2], q % 2)) * (1.0f / kScaleX);
-          y = fmaf(step.a + of_row[n], before, sum * (1.0f / (kScaleA * kScaleX)));
+          else before = (high_of(o[0][0][m][n][q / 2], q % 2) + high_of(o[0][1][m][n][q / 2], q % 2)) * (1.0f / kScaleX);
+          y = fmaf(f.of_x + of_row[n], before, sum * (1.0f / (kScaleA * kScaleX)));
+        } else {
+          const float oo = sum * (1.0f / (kScaleA * kScaleA)), di = of_row[n];
+          float off[kMatrices];
+#pragma unroll
+          for (int w = 0; w < kMatrices; ++w) {
+            off[w] = high_of(o[w][0][m][n][q / 2], q % 2);
+            if constexpr (kPair) off[w] += high_of(o[w][1][m][n][q / 2], q % 2);
+            off[w] *= 1.0f / kScaleA;
+          }
+          y = product_off<kOf>(f, off[0], off[kMatrices - 1], di, of_column[m][q], oo);
+          if (in && i == j) diagonal_of(e, p, f.out)[i] = product_diagonal<kOf>(f, di, of_column[m][q], oo);
         }
         s_y[wn + s + 16 * n][wm + 4 * g + 16 * m + q] = in && (kKind == 2 || i != j) ? y : 0.0f;
       }
@@ -251,13 +265,13 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
         for (int q = 0; q < 4; ++q) y[q] *= e.scale;
         store_result(out + static_cast<int64_t>(i) * e.c + j, y, e.c - j,
                      e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
-      } else if constexpr (kKind == 2) {
+      } else if constexpr (kOf == kUpdate) {
         const int64_t to = static_cast<int64_t>(i) * e.pc + j;
         if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
         store_operand(p.to[0], kPair ? p.to[1] : p.low, to, y, kScaleX);
       } else {
-        uint16_t* const* const out = kKind == 0 ? p.a : p.b;
-        store_operand(out[0], kPair ? out[1] : nullptr, static_cast<int64_t>(i) * e.pr + j, y, kScaleA);
+        store_operand(symmetric_of<kPair>(e, p, f.out, 0), kPair ? symmetric_of<kPair>(e, p, f.out, 1) : nullptr,
+                      static_cast<int64_t>(i) * e.pr + j, y, kScaleA);
       }
     }
     // And along its columns: the other half of a symmetric result, or X^T.
@@ -273,32 +287,39 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
       for (int q = 0; q < 4; ++q) y[q] *= e.scale;
       store_result(out + static_cast<int64_t>(j) * e.r + i, y, e.r - i,
                    e.r % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0);
+    } else if constexpr (kOf == kUpdate) {
+      store_operand(pt.to[0], kPair ? pt.to[1] : nullptr, static_cast<int64_t>(j) * e.pr + i, y, kScaleX);
     } else {
-      uint16_t* const* const out = kKind == 0 ? p.a : kKind == 1 ? p.b : pt.to;
-      store_operand(out[0], kPair ? out[1] : nullptr, static_cast<int64_t>(j) * e.pr + i, y, kKind == 2 ? kScaleX : kScaleA);
+      store_operand(symmetric_of<kPair>(e, p, f.out, 0), kPair ? symmetric_of<kPair>(e, p, f.out, 1) : nullptr,
+                    static_cast<int64_t>(j) * e.pr + i, y, kScaleA);
     }
   }
 }
 
-template <int kKind, typename Out, bool kLast>
-hipError_t launch_kind(const Table& t, int turn, const OrthoStep& p, hipStream_t st) {
+template <int kOf, typename Out, bool kLast, typename F>
+hipError_t launch_kind(const Table& t, int turn, const F& f, hipStream_t st) {
+  constexpr int kKind = kOf == kOfX ? 0 : kOf == kUpdate ? 2 : 1;
   const dim3 grid(t.total_tiles[kKind]), block(kSmallThreads);
-  if (t.size[kKind] == 32) hipLaunchKernelGGL((ortho_small_kernel<kKind, Out, kLast, 32>), grid, block, 0, st, t, turn, p);
-  else hipLaunchKernelGGL((ortho_small_kernel<kKind, Out, kLast, 64>), grid, block, 0, st, t, turn, p);
+  if (t.size[kKind] == 32) hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 32>), grid, block, 0, st, t, turn, f);
+  else hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 64>), grid, block, 0, st, t, turn, f);
   return hipGetLastError();
 }
 
 template <typename Out>
-hipError_t launch_type(const Table& t, int kind, bool last, int turn, const OrthoStep& p, hipStream_t st) {
-  if (kind == 0) return launch_kind<0, Out, false>(t, turn, p, st);
-  if (kind == 1) return launch_kind<1, Out, false>(t, turn, p, st);
-  return last ? launch_kind<2, Out, true>(t, turn, p, st) : launch_kind<2, Out, false>(t, turn, p, st);
+hipError_t launch_symmetric(const Table& t, int of, int turn, const Product& p, hipStream_t st) {
+  if (of == kOfX) return launch_kind<kOfX, Out, false>(t, turn, p, st);
+  return of == kOfOne ? launch_kind<kOfOne, Out, false>(t, turn, p, st) : launch_kind<kOfTwo, Out, false>(t, turn, p, st);
 }
 
 }  // namespace
 
-hipError_t launch_ortho_small(const Table& t, int kind, bool pair, bool last, int turn, const OrthoStep& p, hipStream_t st) {
-  return pair ? launch_type<float>(t, kind, last, turn, p, st) : launch_type<uint16_t>(t, kind, last, turn, p, st);
+hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t st) {
+  return pair ? launch_symmetric<float>(t, of, turn, p, st) : launch_symmetric<uint16_t>(t, of, turn, p, st);
+}
+
+hipError_t launch_ortho_small_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t st) {
+  if (pair) return u.last ? launch_kind<kUpdate, float, true>(t, turn, u, st) : launch_kind<kUpdate, float, false>(t, turn, u, st);
+  return u.last ? launch_kind<kUpdate, uint16_t, true>(t, turn, u, st) : launch_kind<kUpdate, uint16_t, false>(t, turn, u, st);
 }
 
 }  // namespace vtrace

@@ -25,12 +25,11 @@ __device__ __forceinline__ s16x4 transposed_read(const char* lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)lds);
 }
 
-// A (kSquare false, from X) or B (true, from A): the tiles (i, j), j <= i, of a symmetric
-// product M M^T, M's rows "along" for both operands.  A lane of the MFMA layout holds columns
-// j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
-template <bool kSquare, bool kPair, int kSize>
-__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_symmetric_kernel(Table t, int turn, float b, float c) {
-  constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = kSquare ? 1 : 0;
+// A symmetric matrix: the tiles (i, j), j <= i, of M N, rows of both "along".  A lane of the MFMA
+// layout holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
+template <int kOf, bool kPair, int kSize>
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_symmetric_kernel(Table t, int turn, Product f) {
+  constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = kOf == kOfX ? 0 : 1, kParts = kPair ? 2 : 1;
   constexpr int kTurnedBytes = 32 * kSize;  // of a wave: 32 rows of kSize / 2 columns, or 16 of both parts
   __shared__ __align__(1024) char lds[tile_lds(kSize) + 4 * kTurnedBytes];
   Tiles tiles(t.total_tiles[kKind]);
@@ -49,23 +48,24 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
     at.i = tile.wide;
     at.j = tile.deep;
     const Pieces p = pieces_of<kPair>(e, turn);
-    const int64_t pitch = kSquare ? e.pr : e.pc;
-    const uint16_t* const high = kSquare ? p.a[0] : p.from[0];
-    const uint16_t* const low = kSquare ? p.a[1] : p.from[1];
+    const int64_t pitch = kOf == kOfX ? e.pc : e.pr;
+    auto operand = [&](int matrix, int k) { return kOf == kOfX ? p.from[k] : symmetric_of<kPair>(e, p, matrix, k); };
     const int64_t ia = static_cast<int64_t>(at.j) * kSize, ib = static_cast<int64_t>(at.i) * kSize;
     const int64_t left_a = (e.r - ia) * pitch * 2, left_b = (e.r - ib) * pitch * 2;
+    const uint16_t* const a = operand(f.n, 0) + ia * pitch;
+    const uint16_t* const b = operand(f.m, 0) + ib * pitch;
     const int once = static_cast<int>(pitch / kTileK);
     job.a.along(pitch, kSize, wave, lane);
     job.b.along(pitch, kSize, wave, lane);
     if constexpr (kPair) {
-      job.a.aim(low + ia * pitch, left_a);
-      job.a.parts(once, high + ia * pitch, high + ia * pitch, left_a);
-      job.b.aim(high + ib * pitch, left_b);
-      job.b.parts(once, low + ib * pitch, high + ib * pitch, left_b);
+      job.a.aim(operand(f.n, 1) + ia * pitch, left_a);
+      job.a.parts(once, a, a, left_a);
+      job.b.aim(b, left_b);
+      job.b.parts(once, operand(f.m, 1) + ib * pitch, b, left_b);
       job.steps = 3 * once;
     } else {
-      job.a.aim(high + ia * pitch, left_a);
-      job.b.aim(high + ib * pitch, left_b);
+      job.a.aim(a, left_a);
+      job.b.aim(b, left_b);
       job.steps = once;
     }
   };
@@ -83,29 +83,40 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
     const Pieces p = pieces_of<kPair>(e, turn);
     const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2);
     const bool mirrored = here.i != here.j;
-    uint16_t* const* const out = kSquare ? p.b : p.a;
+    uint16_t* const out[kParts] = {symmetric_of<kPair>(e, p, f.out, 0)};
+    if constexpr (kPair) const_cast<uint16_t*&>(out[kParts - 1]) = symmetric_of<kPair>(e, p, f.out, 1);
     char* const turned = lds + tile_lds(kSize) + wave * kTurnedBytes;
-    // Eight elements of a row of A, as they lie.
-    auto load_row = [&](v4u (&o)[kPair ? 2 : 1][kMT / 2], int n) {
-      const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
-#pragma unroll
-      for (int m = 0; m < kMT / 2; ++m) {
-        const int j = j0 + 8 * g + 32 * m;
-        const int64_t at = static_cast<int64_t>(i) * e.pr + (j < e.pr ? j : 0);
-        o[0][m] = *reinterpret_cast<const v4u*>(p.a[0] + at);
-        if constexpr (kPair) o[1][m] = *reinterpret_cast<const v4u*>(p.a[1] + at);
-      }
-    };
-    v4u o[2][kPair ? 2 : 1][kMT / 2];
+    const float* const dm = diagonal_of(e, p, f.m);
+    const float* const dn = diagonal_of(e, p, f.n);
+    float* const d_out = diagonal_of(e, p, f.out);
+    // Eight elements of a row of M (and N), as they lie: of the next 16 rows, while these are stored,
+    // or (two matrices in two parts, which the registers do not hold beside a tile of 256) where they
+    // are used.
+    constexpr bool kLate = kOf == kOfTwo && kPair && kSize == kTile;
+    constexpr int kMatrices = kOf == kOfTwo ? 2 : 1, kBuffers = kLate ? 1 : 2, kPieces = kLate ? 1 : kMT / 2;
+    v4u o[kBuffers][kMatrices][kParts][kPieces];
     float dj[kMT / 2][8];
-    if constexpr (kSquare) {
-      load_row(o[0], 0);
+    auto load_piece = [&](int n, int m) {
+      const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1, j = j0 + 8 * g + 32 * m;
+      const int64_t from = static_cast<int64_t>(i) * e.pr + (j < e.pr ? j : 0);
+#pragma unroll
+      for (int w = 0; w < kMatrices; ++w)
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+          o[n % kBuffers][w][k][m % kPieces] = *reinterpret_cast<const v4u*>(symmetric_of<kPair>(e, p, w == 0 ? f.m : f.n, k) + from);
+    };
+    auto load_row = [&](int n) {
+#pragma unroll
+      for (int m = 0; m < kMT / 2; ++m) load_piece(n, m);
+    };
+    if constexpr (kOf != kOfX) {
+      if (!kLate) load_row(0);
 #pragma unroll
       for (int m = 0; m < kMT / 2; ++m)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           const int j = j0 + 8 * g + 32 * m + q;
-          dj[m][q] = p.d[j < e.r ? j : e.r - 1];
+          dj[m][q] = dn[j < e.r ? j : e.r - 1];
         }
     }
 #pragma unroll
@@ -113,27 +124,34 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
       const int i = i0 + 16 * n + s;
       const bool row = i < e.r;
       float di = 0.0f;
-      if constexpr (kSquare) {
-        di = p.d[row ? i : e.r - 1];
-        if (n + 1 < kNT) load_row(o[(n + 1) % 2], n + 1);
+      if constexpr (kOf != kOfX) {
+        di = dm[row ? i : e.r - 1];
+        if (!kLate && n + 1 < kNT) load_row(n + 1);
       }
 #pragma unroll
       for (int m = 0; m < kMT / 2; ++m) {
         const int j = j0 + 8 * g + 32 * m;
+        if constexpr (kLate) load_piece(n, m);
         float y[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           const float sum = element(acc[2 * m + q / 4][n], q % 4);
           const bool in = row && j + q < e.r;
-          if constexpr (kSquare) {
-            const float oo = sum * (1.0f / (kScaleA * kScaleA));
-            float off = high_of(o[n % 2][0][m][q / 2], q % 2);
-            if constexpr (kPair) off += high_of(o[n % 2][1][m][q / 2], q % 2);
-            y[q] = fmaf(off * (1.0f / kScaleA), fmaf(c, di + dj[m][q], b), c * oo);
-            if (in && i == j + q) p.e[i] = fmaf(b, di, c * fmaf(di, di, oo));
-          } else {
+          if constexpr (kOf == kOfX) {
             y[q] = sum * (1.0f / (kScaleX * kScaleX));
-            if (in && i == j + q) p.d[i] = y[q];
+            if (in && i == j + q) d_out[i] = y[q];
+          } else {
+            // With M = D + O and N = D' + O': M N without its diagonal is D O' + O D' + O O'.
+            const float oo = sum * (1.0f / (kScaleA * kScaleA));
+            float off[kMatrices];
+#pragma unroll
+            for (int w = 0; w < kMatrices; ++w) {
+              off[w] = high_of(o[n % kBuffers][w][0][m % kPieces][q / 2], q % 2);
+              if constexpr (kPair) off[w] += high_of(o[n % kBuffers][w][kParts - 1][m % kPieces][q / 2], q % 2);
+              off[w] *= 1.0f / kScaleA;
+            }
+            y[q] = product_off<kOf>(f, off[0], off[kMatrices - 1], di, dj[m][q], oo);
+            if (in && i == j + q) d_out[i] = product_diagonal<kOf>(f, di, dn[i], oo);
           }
           y[q] = in && i != j + q ? y[q] * kScaleA : 0.0f;
         }
@@ -144,7 +162,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
           if constexpr (kPair) part[1][q] = low2(y[2 * q], y[2 * q + 1], part[0][q]);
         }
 #pragma unroll
-        for (int k = 0; k < (kPair ? 2 : 1); ++k) {
+        for (int k = 0; k < kParts; ++k) {
           if (row && j < e.pr) *reinterpret_cast<v4u*>(out[k] + static_cast<int64_t>(i) * e.pr + j) = part[k];
           if (mirrored) {
             const int at = 16 * (kPair ? k : n % 2) + s, piece = 2 * m + g / 2;
@@ -185,7 +203,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
 // X <- a X + B X, or of the last step the result: m runs along X's columns (X "across"), n along
 // its rows (B "along").  A lane holds columns j + 16 m + 4 g + 0..3 of row i + 16 n + s.
 template <typename Out, bool kPair, bool kLast, int kSize>
-__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_update_kernel(Table t, int turn, float a, bool low) {
+__global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_update_kernel(Table t, int turn, Update f) {
   constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = 2;
   __shared__ __align__(1024) char lds[tile_lds(kSize)];
   Tiles tiles(t.total_tiles[kKind]);
@@ -208,13 +226,13 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
     const int64_t i0 = static_cast<int64_t>(at.i) * kSize, j0 = static_cast<int64_t>(at.j) * kSize;
     const int64_t left_x = (static_cast<int64_t>(e.r) * e.pc - j0) * 2, left_b = (e.r - i0) * e.pr * 2;
     const uint16_t* const xh = p.from[0] + j0;
-    const uint16_t* const bh = p.b[0] + i0 * e.pr;
+    const uint16_t* const bh = symmetric_of<kPair>(e, p, f.by, 0) + i0 * e.pr;
     const int once = e.pr / kTileK;
     job.a.across(e.pc, wave, lane);
     job.b.along(e.pr, kSize, wave, lane);
     if constexpr (kPair) {
       const uint16_t* const xl = p.from[1] + j0;
-      const uint16_t* const bl = p.b[1] + i0 * e.pr;
+      const uint16_t* const bl = symmetric_of<kPair>(e, p, f.by, 1) + i0 * e.pr;
       job.a.aim(xl, left_x);
       job.a.parts(once, xh, xh, left_x);
       job.b.aim(bh, left_b);
@@ -235,6 +253,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
     const Entry& e = t.at[here.entry];
     const Pieces p = pieces_of<kPair>(e, turn);
     const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 4 * g;
+    const float* const diagonal = diagonal_of(e, p, f.by);
     Out* const out = static_cast<Out*>(e.out);
     const bool vectors = e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0;
     // X's rows are fetched kAhead times 16 ahead, the first of them during the last step of k.
@@ -244,7 +263,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
     float of_row[kBuffers];
     auto load_rows = [&](int n) {
       const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
-      of_row[n % kBuffers] = p.e[i];
+      of_row[n % kBuffers] = diagonal[i];
 #pragma unroll
       for (int m = 0; m < kMT; ++m) {
         const int j = j0 + 16 * m;
@@ -253,7 +272,8 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           x[n % kBuffers][m] = *reinterpret_cast<const f32x4*>(p.x + from);
         } else {
           part[n % kBuffers][0][m] = *reinterpret_cast<const v2u*>(p.from[0] + from);
-          if constexpr (!kLast) part[n % kBuffers][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
+          part[n % kBuffers][1][m] = v2u{};
+          if (f.low_in) part[n % kBuffers][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
         }
       }
     };
@@ -268,7 +288,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
       if (n + kAhead < kNT) load_rows(n + kAhead);
       const int i = i0 + 16 * n + s;
       const bool row = i < e.r;
-      const float factor = a + of_row[n % kBuffers];
+      const float factor = f.of_x + of_row[n % kBuffers];
 #pragma unroll
       for (int m = 0; m < kMT; ++m) {
         const int j = j0 + 16 * m;
@@ -279,9 +299,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           if constexpr (kPair) {
             before = x[n % kBuffers][m][q];
           } else {
-            before = high_of(part[n % kBuffers][0][m][q / 2], q % 2);
-            if constexpr (!kLast) before += high_of(part[n % kBuffers][1][m][q / 2], q % 2);
-            before *= 1.0f / kScaleX;
+            before = (high_of(part[n % kBuffers][0][m][q / 2], q % 2) + high_of(part[n % kBuffers][1][m][q / 2], q % 2)) * (1.0f / kScaleX);
           }
           y[q] = fmaf(factor, before, element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
         }
@@ -308,7 +326,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           const v2u high = high4(y);
           *reinterpret_cast<v2u*>(p.to[0] + to) = high;
           if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + to) = low4(y, high);
-          else if (low) *reinterpret_cast<v2u*>(p.low + to) = low4(y, high);
+          else if (f.low_out) *reinterpret_cast<v2u*>(p.low + to) = low4(y, high);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -317,38 +335,35 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-template <bool kSquare, bool kPair>
-hipError_t launch_symmetric(const Table& t, int size, int turn, const OrthoStep& p, hipStream_t st) {
-  const dim3 grid(workgroups_of(t.total_tiles[kSquare ? 1 : 0], size)), block(kGemmThreads);
-  if (size == kTile) hipLaunchKernelGGL((ortho_symmetric_kernel<kSquare, kPair, kTile>), grid, block, 0, st, t, turn, p.b, p.c);
-  else hipLaunchKernelGGL((ortho_symmetric_kernel<kSquare, kPair, kSmallTile>), grid, block, 0, st, t, turn, p.b, p.c);
+template <int kOf, bool kPair>
+hipError_t launch_symmetric(const Table& t, int turn, const Product& p, hipStream_t st) {
+  const int kind = kOf == kOfX ? 0 : 1;
+  const dim3 grid(workgroups_of(t.total_tiles[kind], t.size[kind])), block(kGemmThreads);
+  if (t.size[kind] == kTile) hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kTile>), grid, block, 0, st, t, turn, p);
+  else hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kSmallTile>), grid, block, 0, st, t, turn, p);
   return hipGetLastError();
 }
 
-template <typename Out, bool kPair, bool kLast>
-hipError_t launch_update(const Table& t, int size, int turn, const OrthoStep& p, bool low, hipStream_t st) {
-  const dim3 grid(workgroups_of(t.total_tiles[2], size)), block(kGemmThreads);
-  if (size == kTile) hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kTile>), grid, block, 0, st, t, turn, p.a, low);
-  else hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kSmallTile>), grid, block, 0, st, t, turn, p.a, low);
+template <typename Out, bool kLast>
+hipError_t launch_update(const Table& t, int turn, const Update& u, hipStream_t st) {
+  constexpr bool kPair = sizeof(Out) == 4;
+  const dim3 grid(workgroups_of(t.total_tiles[2], t.size[2])), block(kGemmThreads);
+  if (t.size[2] == kTile) hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kTile>), grid, block, 0, st, t, turn, u);
+  else hipLaunchKernelGGL((ortho_update_kernel<Out, kPair, kLast, kSmallTile>), grid, block, 0, st, t, turn, u);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_ortho_tiles_symmetric(const Table& t, bool square, bool pair, int size, int turn, const OrthoStep& p,
-                                        hipStream_t st) {
-  if (square) return pair ? launch_symmetric<true, true>(t, size, turn, p, st) : launch_symmetric<true, false>(t, size, turn, p, st);
-  return pair ? launch_symmetric<false, true>(t, size, turn, p, st) : launch_symmetric<false, false>(t, size, turn, p, st);
+hipError_t launch_ortho_tiles_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t st) {
+  if (of == kOfX) return pair ? launch_symmetric<kOfX, true>(t, turn, p, st) : launch_symmetric<kOfX, false>(t, turn, p, st);
+  if (of == kOfOne) return pair ? launch_symmetric<kOfOne, true>(t, turn, p, st) : launch_symmetric<kOfOne, false>(t, turn, p, st);
+  return pair ? launch_symmetric<kOfTwo, true>(t, turn, p, st) : launch_symmetric<kOfTwo, false>(t, turn, p, st);
 }
 
-hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int left, int size, int turn, const OrthoStep& p,
-                                     hipStream_t st) {
-  const bool low = left > 1;  // the last step takes the operand alone as X
-  if (pair)
-    return left == 0 ? launch_update<float, true, true>(t, size, turn, p, low, st)
-                     : launch_update<float, true, false>(t, size, turn, p, low, st);
-  return left == 0 ? launch_update<uint16_t, false, true>(t, size, turn, p, low, st)
-                   : launch_update<uint16_t, false, false>(t, size, turn, p, low, st);
+hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t st) {
+  if (pair) return u.last ? launch_update<float, true>(t, turn, u, st) : launch_update<float, false>(t, turn, u, st);
+  return u.last ? launch_update<uint16_t, true>(t, turn, u, st) : launch_update<uint16_t, false>(t, turn, u, st);
 }
 
 }  // namespace vtrace

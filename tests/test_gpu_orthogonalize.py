@@ -1,7 +1,7 @@
 """Newton-Schulz products against the oracle, in float64.
 
-Tolerance: the result's rounding, and twice what the oracle's model of the operands' roundings
-and of the float32 sums' roundings is off: the kernel's are as many and of the same sizes, but
+Tolerance: the result's rounding, and twice what the oracle's models (steps one by one, and two
+at once) of the operands' roundings and of the float32 sums' roundings is off: the kernel's are as many and of the same sizes, but
 not the same ones, since a sum in another order may round an operand the other way, and
 the matrix cores' sums are within one step of float32 where the model's are within half.  Where
 one singular value has it all (a single row), the model's error is one sample and may be near
@@ -13,6 +13,8 @@ values grow most (3.44 a step), so that an error can be nearly x y^T with x and 
 distributed: of m of those the largest is above sqrt(2 ln(2 m / p)) root mean squares with a
 probability below p (2 exp(-t^2 / 2) each), and never above sqrt(m); the element's share
 is the product of both.  p is 1e-6."""
+
+import functools
 
 import numpy as np
 import pytest
@@ -41,15 +43,22 @@ def largest(m):
     return min(np.sqrt(m), np.sqrt(2.0 * np.log(2e6 * m)))
 
 
-def check(g, got, steps=STEPS, scale=1.0, epsilon=1e-7):
-    x = g.cpu().double().numpy()
-    steps = [tuple(float(np.float32(v)) for v in s) for s in steps]
-    scale, epsilon = float(np.float32(scale)), float(np.float32(epsilon))
+@functools.lru_cache(maxsize=None)
+def _reference(data, shape, f32, steps, scale, epsilon):
+    """The oracle's result, and how far its models of the roundings are off."""
+    x = np.frombuffer(data).reshape(shape)
     ref = op.orthogonalize(x, steps, epsilon, scale)
-    model = op.orthogonalize_rounded(x, steps, epsilon, scale, parts=2 if g.dtype == F32 else 1)
+    off = max(np.linalg.norm(op.orthogonalize_rounded(x, steps, epsilon, scale, parts=2 if f32 else 1, together=k) - ref) for k in (1, 2))
+    return ref, off
+
+
+def check(g, got, steps=STEPS, scale=1.0, epsilon=1e-7):
+    steps = tuple(tuple(float(np.float32(v)) for v in s) for s in steps)
+    ref, off = _reference(g.cpu().double().numpy().tobytes(), tuple(g.shape), g.dtype == F32, steps, float(np.float32(scale)),
+                          float(np.float32(epsilon)))
     assert got.dtype == g.dtype and got.shape == g.shape
     err = np.abs(got.cpu().double().numpy() - ref)
-    off = np.linalg.norm(model - ref) + 15.0 * np.sqrt(len(steps)) * 2.0 ** -24 * np.linalg.norm(ref)
+    off = off + 15.0 * np.sqrt(len(steps)) * 2.0 ** -24 * np.linalg.norm(ref)
     u = HALF_STEP[g.dtype]
     assert np.linalg.norm(err) <= 2.0 * off + u * np.linalg.norm(ref), (np.linalg.norm(err), off, np.linalg.norm(ref))
     tol = 2.0 * off / np.sqrt(err.size) * largest(err.shape[0]) * largest(err.shape[1]) + u * np.abs(ref)
@@ -60,9 +69,9 @@ SIZES = [(1, 1), (1, 2), (2, 1), (1, 300), (300, 1), (2, 2), (3, 5), (16, 16), (
          (128, 129), (129, 127), (200, 72), (256, 256), (257, 255), (83, 1001), (1000, 83), (513, 300), (640, 640)]
 
 
-@pytest.fixture(params=[None, 32, 64, 128, 256])
+@pytest.fixture(params=[None] + [f"{size}x{together}" for size in (32, 64, 128, 256) for together in (1, 2)])
 def tile(request, monkeypatch):
-    """The kernels that the sizes choose, and each of them for all sizes."""
+    """The kernels that the sizes choose, and each of them for all sizes, steps one by one and two at once."""
     if request.param is None:
         monkeypatch.delenv("VTRACE_KERNEL", raising=False)
     else:

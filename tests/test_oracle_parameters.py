@@ -42,10 +42,13 @@ def test_orthogonalize_goes_by_singular_values(m, n):
 
 
 @pytest.mark.parametrize("m,n", [(40, 40), (24, 100), (100, 24)])
-def test_rounded_products_are_near(m, n):
+@pytest.mark.parametrize("together", [1, 2])
+@pytest.mark.parametrize("steps", [1, 2, 5])
+def test_rounded_products_are_near(m, n, together, steps):
     g = np.random.default_rng(3).normal(size=(m, n))
-    ref = op.orthogonalize(g)
-    off = [np.linalg.norm(op.orthogonalize_rounded(g, parts=p) - ref) / np.linalg.norm(ref) for p in (1, 2)]
+    ref = op.orthogonalize(g, (op.QUINTIC,) * steps)
+    off = [np.linalg.norm(op.orthogonalize_rounded(g, (op.QUINTIC,) * steps, parts=p, together=together) - ref) / np.linalg.norm(ref)
+           for p in (1, 2)]
     assert 1e-5 < off[0] < 2e-3 and off[1] < 3e-6
 
 
