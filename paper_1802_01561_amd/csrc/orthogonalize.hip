@@ -54,9 +54,200 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
+// ---- Matrices of few rows. ----
+//
+// All steps are taken in the small matrices alone, in float64: from A = X X^T, with P = a I + b A + c A A,
+// A' = P A P and X' = P X, so that the result is Q X with Q the product of all P.  Two launches, those
+// of |G| and of X for the other matrices, and each reads G once.  With float16 operands 2 x 2 and
+// 4 x 4 bfloat16 matrices were up to 5.1e-3 off (few rows do not average rounding errors out),
+// and took as many launches as large ones.
+
+constexpr int kFewRows = 32;
+constexpr int kFewTile = 64;                             // columns at a time
+constexpr int64_t kFewChunk = 256, kFewMostChunks = 32;  // of A's partial sums
+constexpr int kFewBlock = 256;                           // columns of a workgroup that forms the result
+
+struct FewSteps {
+  OrthoStep at[kOrthoMostSteps];
+  int count;
+};
+
+__host__ __device__ inline int64_t few_chunk(int64_t c) {
+  const int64_t least = round_up((c + kFewMostChunks - 1) / kFewMostChunks, kFewTile);
+  return least < kFewChunk ? kFewChunk : least;
+}
+__host__ __device__ inline int64_t few_chunks(int64_t c) { return (c + few_chunk(c) - 1) / few_chunk(c); }
+
+typedef float FewTile[kFewRows][kFewTile + 1];
+
+// Columns j0 .. j0 + 63 of G, as many as there are, zeros around them: a thread's places in the
+// order in which they lie in memory.
+template <typename In, typename F>
+__device__ __forceinline__ void few_places(const Entry& g, int j0, F f) {
+  const int columns = g.c - j0 < kFewTile ? g.c - j0 : kFewTile;
+  if (g.transposed) {
+    for (int k = threadIdx.x; k < columns * g.r; k += kNormThreads) f(k % g.r, k / g.r, (static_cast<int64_t>(j0) * g.r + k));
+  } else {
+    const int column = threadIdx.x % kFewTile;
+    if (column >= columns) return;
+    for (int i = threadIdx.x / kFewTile; i < g.r; i += kNormThreads / kFewTile) f(i, column, static_cast<int64_t>(i) * g.c + j0 + column);
+  }
+}
 template <typename In>
+__device__ __forceinline__ void few_load(const Entry& g, int j0, FewTile& tile) {
+  for (int k = threadIdx.x; k < kFewRows * kFewTile; k += kNormThreads) tile[k / kFewTile][k % kFewTile] = 0.0f;
+  __syncthreads();
+  const In* const in = static_cast<const In*>(g.in);
+  few_places<In>(g, j0, [&](int i, int j, int64_t at) { tile[i][j] = logit_to_float(in[at]); });
+  __syncthreads();
+}
+
+// A thread's four elements of a 32 x 32 matrix: two rows, two columns.
+struct Four {
+  double x[2][2];
+};
+__device__ __forceinline__ int four_row() { return 2 * (threadIdx.x / 16); }
+__device__ __forceinline__ int four_column() { return 2 * (threadIdx.x % 16); }
+
+template <typename In>
+__device__ void few_gram(const Table& t, int id) {
+  __shared__ FewTile s_tile;
+  const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_partial; }, t.count, t.few)];
+  const int64_t chunk = id - g.first_partial, from = chunk * few_chunk(g.c);
+  const int64_t to = from + few_chunk(g.c) < g.c ? from + few_chunk(g.c) : g.c;
+  Four sum = {};
+  for (int64_t j0 = from; j0 < to; j0 += kFewTile) {
+    few_load<In>(g, static_cast<int>(j0), s_tile);
+    if (four_row() < g.r && four_column() < g.r) {
+      for (int k = 0; k < kFewTile; ++k) {
+        const double x[2] = {s_tile[four_row()][k], s_tile[four_row() + 1][k]};
+        const double y[2] = {s_tile[four_column()][k], s_tile[four_column() + 1][k]};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) sum.x[i][j] = fma(x[i], y[j], sum.x[i][j]);
+      }
+    }
+    __syncthreads();
+  }
+  double* const out = reinterpret_cast<double*>(g.base) + chunk * kFewRows * kFewRows;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) out[(four_row() + i) * kFewRows + four_column() + j] = sum.x[i][j];
+}
+
+typedef double FewMatrix[kFewRows][kFewRows];
+
+__device__ __forceinline__ Four four_of(const FewMatrix& m) {
+  return {{{m[four_row()][four_column()], m[four_row()][four_column() + 1]},
+           {m[four_row() + 1][four_column()], m[four_row() + 1][four_column() + 1]}}};
+}
+__device__ __forceinline__ void store_four(FewMatrix& m, const Four& f) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) m[four_row() + i][four_column() + j] = f.x[i][j];
+}
+__device__ __forceinline__ Four few_product(const FewMatrix& x, const FewMatrix& y, int r) {
+  Four f = {};
+  if (four_row() < r && four_column() < r) {
+#pragma unroll 4
+    for (int k = 0; k < r; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f.x[i][j] = fma(x[four_row() + i][k], y[k][four_column() + j], f.x[i][j]);
+  }
+  return f;
+}
+
+// The result's columns from 256 * block on; every workgroup of a matrix forms its Q.
+template <typename In>
+__device__ void few_apply(const Table& t, const FewSteps& steps, int id) {
+  __shared__ FewMatrix s_a, s_p, s_q;
+  __shared__ FewTile s_tile;
+  const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_block; }, t.count, t.few)];
+  const int r = g.r;
+  const double* const partials = reinterpret_cast<const double*>(g.base);
+  Four a = {};
+  for (int chunk = 0; chunk < g.partials; ++chunk)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) a.x[i][j] += partials[chunk * kFewRows * kFewRows + (four_row() + i) * kFewRows + four_column() + j];
+  store_four(s_a, a);
+  __syncthreads();
+  double squares = 0.0;
+  for (int i = 0; i < r; ++i) squares += s_a[i][i];
+  const double norm = sqrt(squares), least = t.epsilon;
+  const double factor = 1.0 / (norm < least ? least : norm);  // a NaN norm stays
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) a.x[i][j] = a.x[i][j] * factor * factor;
+  store_four(s_a, a);
+  __syncthreads();
+  for (int k = 0; k < steps.count; ++k) {
+    const double pa = steps.at[k].a, pb = steps.at[k].b, pc = steps.at[k].c;
+    a = four_of(s_a);
+    const Four aa = few_product(s_a, s_a, r);
+    Four p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        p.x[i][j] = (four_row() + i == four_column() + j ? pa : 0.0) + pb * a.x[i][j] + pc * aa.x[i][j];
+    store_four(s_p, p);
+    __syncthreads();
+    const Four q = k == 0 ? p : few_product(s_p, s_q, r);
+    const Four pap = few_product(s_p, s_a, r);
+    __syncthreads();
+    store_four(s_q, q);
+    store_four(s_a, pap);
+    __syncthreads();
+    a = few_product(s_a, s_p, r);
+    __syncthreads();
+    store_four(s_a, a);
+    __syncthreads();
+  }
+  const double scale = factor * g.scale;
+  const int64_t from = static_cast<int64_t>(id - g.first_block) * kFewBlock;
+  for (int64_t j0 = from; j0 < g.c && j0 < from + kFewBlock; j0 += kFewTile) {
+    few_load<In>(g, static_cast<int>(j0), s_tile);
+    // A thread's column, every fourth row.
+    constexpr int kSets = kNormThreads / kFewTile, kMost = kFewRows / kSets;
+    const int column = threadIdx.x % kFewTile, set = threadIdx.x / kFewTile;
+    double y[kMost] = {};
+    for (int k = 0; k < r; ++k) {
+      const double x = s_tile[k][column];
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) y[i] = fma(s_q[set + kSets * i][k], x, y[i]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) s_tile[set + kSets * i][column] = static_cast<float>(y[i] * scale);
+    __syncthreads();
+    In* const out = static_cast<In*>(g.out);
+    few_places<In>(g, static_cast<int>(j0), [&](int i, int j, int64_t at) {
+      if constexpr (sizeof(In) == 4) out[at] = s_tile[i][j];
+      else out[at] = to_bf16(s_tile[i][j]);
+    });
+    __syncthreads();
+  }
+}
+
+// kFew: and A of the matrices of few rows, in further workgroups.
+template <typename In, bool kFew>
 __global__ __launch_bounds__(kNormThreads) void ortho_norm_kernel(Table t) {
   constexpr int kPer = 16 / sizeof(In);
+  if constexpr (kFew) {
+    if (static_cast<int>(blockIdx.x) >= t.total_partials) {
+      few_gram<In>(t, blockIdx.x - t.total_partials);
+      return;
+    }
+  }
   const Entry& g = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_partial; })];
   const int64_t elements = static_cast<int64_t>(g.r) * g.c, chunk = norm_chunk(elements);
   const int64_t from = (blockIdx.x - g.first_partial) * chunk, to = from + chunk < elements ? from + chunk : elements;
@@ -90,9 +281,16 @@ __global__ __launch_bounds__(kNormThreads) void ortho_norm_kernel(Table t) {
 }
 
 constexpr int kScaleTile = 64;
-template <typename In, bool kPair>
-__global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t) {
+// kFew: and the results of the matrices of few rows.
+template <typename In, bool kPair, bool kFew>
+__global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t, FewSteps steps) {
   __shared__ float s_tile[kScaleTile][kScaleTile + 1];
+  if constexpr (kFew) {
+    if (static_cast<int>(blockIdx.x) >= t.total_blocks) {
+      few_apply<In>(t, steps, blockIdx.x - t.total_blocks);
+      return;
+    }
+  }
   const Entry& g = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_block; })];
   const int wide = g.pc / kScaleTile, block = blockIdx.x - g.first_block;
   const int i0 = block / wide * kScaleTile, j0 = block % wide * kScaleTile;
@@ -261,13 +459,18 @@ Forced forced_kernel() {
 }
 
 // The entries of a group of matrices, all of one type, and the workspace's bytes for them.
-Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
+Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_t* bytes) {
   Table t = {};
-  t.count = count;
   const bool pair = !items[0].bf16;
+  const Forced forced = forced_kernel();
+  auto few = [&](const Entry& e) { return few_rows && e.r <= kFewRows && forced.size == 0; };
   for (int i = 0; i < count; ++i) t.at[i] = entry_for(items[i]);
-  // The longest tiles first.
-  std::stable_sort(t.at, t.at + count, [](const Entry& x, const Entry& y) { return x.pc > y.pc; });
+  // Those of few rows last, and of the others the longest tiles first.
+  std::stable_sort(t.at, t.at + count,
+                   [&](const Entry& x, const Entry& y) { return few(x) != few(y) ? few(y) : x.pc > y.pc; });
+  t.few = static_cast<int>(std::count_if(t.at, t.at + count, few));
+  count -= t.few;
+  t.count = count;
   for (int i = 0; i < count; ++i) {
     Entry& e = t.at[i];
     const int64_t elements = static_cast<int64_t>(e.r) * e.c;
@@ -277,22 +480,23 @@ Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
     e.first_block = t.total_blocks;
     t.total_blocks += static_cast<int32_t>(tiles_of(e.r, kScaleTile) * (e.pc / kScaleTile));
   }
-  const int passes = pair ? 3 : 1;
-  double tiles[3], small[3];
-  int small_size[3];
-  for (int kind = 0; kind < 3; ++kind) {
-    t.size[kind] = tile_for(t, kind, passes);
-    tiles[kind] = tiles_cost(t, kind, t.size[kind], passes);
-    small_size[kind] = small_cost(t, kind, 32, pair) <= small_cost(t, kind, 64, pair) ? 32 : 64;
-    small[kind] = small_cost(t, kind, small_size[kind], pair);
+  if (count > 0) {
+    const int passes = pair ? 3 : 1;
+    double tiles[3], small[3];
+    int small_size[3];
+    for (int kind = 0; kind < 3; ++kind) {
+      t.size[kind] = tile_for(t, kind, passes);
+      tiles[kind] = tiles_cost(t, kind, t.size[kind], passes);
+      small_size[kind] = small_cost(t, kind, 32, pair) <= small_cost(t, kind, 64, pair) ? 32 : 64;
+      small[kind] = small_cost(t, kind, small_size[kind], pair);
+    }
+    // Two steps: A and X twice, or once and three products more of B's size.
+    auto one_by_one = [](const double (&us)[3]) { return 2.0 * (us[0] + us[1] + us[2]); };
+    auto together = [](const double (&us)[3]) { return us[0] + 5.0 * us[1] + us[2]; };
+    t.small = std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
+    if (t.small) std::copy_n(small_size, 3, t.size);
+    t.twos = t.small ? together(small) < one_by_one(small) : together(tiles) < one_by_one(tiles);
   }
-  // Two steps: A and X twice, or once and three products more of B's size.
-  auto one_by_one = [](const double (&us)[3]) { return 2.0 * (us[0] + us[1] + us[2]); };
-  auto together = [](const double (&us)[3]) { return us[0] + 5.0 * us[1] + us[2]; };
-  t.small = std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
-  if (t.small) std::copy_n(small_size, 3, t.size);
-  t.twos = t.small ? together(small) < one_by_one(small) : together(tiles) < one_by_one(tiles);
-  const Forced forced = forced_kernel();
   if (forced.size) {
     t.small = forced.size < kSmallTile;
     std::fill_n(t.size, 3, forced.size);
@@ -309,6 +513,16 @@ Table table_of(const OrthoItem* items, int count, char* ws, size_t* bytes) {
       e.first_tile[kind] = t.total_tiles[kind];
       t.total_tiles[kind] += static_cast<int32_t>(tiles_in(e, kind, t.size[kind]));
     }
+  }
+  for (int i = count; i < count + t.few; ++i) {
+    Entry& e = t.at[i];
+    e.base = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
+    e.partials = static_cast<int32_t>(few_chunks(e.c));
+    at += e.partials * static_cast<int64_t>(kFewRows * kFewRows * sizeof(double));
+    e.first_partial = t.few_chunks;
+    t.few_chunks += e.partials;
+    e.first_block = t.few_blocks;
+    t.few_blocks += static_cast<int32_t>(tiles_of(e.c, kFewBlock));
   }
   *bytes = static_cast<size_t>(at);
   return t;
@@ -373,6 +587,15 @@ bool two_steps_ok(const OrthoStep& p, const OrthoStep& q, double most) {
   return true;
 }
 
+// Whether A's own rounding errors stay small where it is stepped by itself: those beside small
+// eigenvalues grow by a^2 a step, from 2^-50 to 2^-24 at most.  (Left to grow they turn an eigenvalue of
+// zero into one that a polynomial with a maximum at zero takes out of its range.)
+bool few_rows_ok(const OrthoStep* steps, int count) {
+  double growth = 1.0;
+  for (int k = 0; k < count; ++k) growth *= std::max(1.0, std::fabs(static_cast<double>(steps[k].a)));
+  return growth <= 8192.0;
+}
+
 // Two steps at once.  With P = a I + B of the first, X' = P X has X' X'^T = P A P, so that both steps
 // take one product with X each way, and the second's matrices come from the first's:
 //   T = A P,   A' = T P,   B' = b' A' + c' A' A',   X'' = (a' I + B') (a I + B) X = (a a' I + Q) X,
@@ -384,7 +607,7 @@ template <typename T, bool kPair>
 hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
                         hipStream_t st) {
   size_t bytes;
-  Table t = table_of(items, count, ws, &bytes);
+  Table t = table_of(items, count, few_rows_ok(steps, step_count), ws, &bytes);
   t.epsilon = epsilon;
   double most[kOrthoMostSteps];
   if (!singular_bounds(steps, step_count, most)) return hipErrorInvalidValue;
@@ -396,11 +619,18 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
     const bool here = k + 1 < step_count && (k == 0 || (k == step_count - 2 && step_count >= 5));
     return t.twos && here && two_steps_ok(steps[k], steps[k + 1], most[k]) ? 2 : 1;
   };
-  hipLaunchKernelGGL(ortho_norm_kernel<T>, dim3(t.total_partials), dim3(kNormThreads), 0, st, t);
+  FewSteps few = {};
+  std::copy_n(steps, step_count, few.at);
+  few.count = step_count;
+  const dim3 norms(t.total_partials + t.few_chunks), blocks(t.total_blocks + t.few_blocks), threads(kNormThreads);
+  if (t.few > 0) hipLaunchKernelGGL((ortho_norm_kernel<T, true>), norms, threads, 0, st, t);
+  else hipLaunchKernelGGL((ortho_norm_kernel<T, false>), norms, threads, 0, st, t);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((ortho_scale_kernel<T, kPair>), dim3(t.total_blocks), dim3(kNormThreads), 0, st, t);
+  if (t.few > 0) hipLaunchKernelGGL((ortho_scale_kernel<T, kPair, true>), blocks, threads, 0, st, t, few);
+  else hipLaunchKernelGGL((ortho_scale_kernel<T, kPair, false>), blocks, threads, 0, st, t, few);
   e = hipGetLastError();
+  if (t.count == 0) return e;
   int turn = 0;
   auto symmetric = [&](int of, const Product& p) {
     if (e != hipSuccess) return;
@@ -443,9 +673,11 @@ size_t ortho_workspace_bytes(const OrthoItem* items, int64_t count) {
   for (const bool bf16 : {true, false}) {
     const std::vector<OrthoItem> of = of_type(items, count, bf16);
     for_groups(of, [&](size_t first, size_t last) {
-      size_t bytes;
-      table_of(of.data() + first, static_cast<int>(last - first), nullptr, &bytes);
-      most = std::max(most, bytes);
+      for (const bool few_rows : {true, false}) {
+        size_t bytes;
+        table_of(of.data() + first, static_cast<int>(last - first), few_rows, nullptr, &bytes);
+        most = std::max(most, bytes);
+      }
     });
   }
   return most;

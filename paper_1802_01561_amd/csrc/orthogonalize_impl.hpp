@@ -26,17 +26,19 @@ struct Entry {
 
 // As many as 4 KB of arguments hold.
 struct Table {
-  static constexpr int kMost = 44;
+  static constexpr int kMost = 40;
   Entry at[kMost];
   double* partials;
-  int count;
+  int count;           // matrices of the tiles' kernels
+  int few;             // behind them, those of few rows
+  int few_chunks, few_blocks;
   int total_partials, total_blocks, total_tiles[3];
   int size[3];  // of the tiles of A, B and X
   float epsilon;
   bool twos;   // two steps at once
   bool small;  // the small matrices' kernels, which keep X^T as well
 };
-static_assert(sizeof(Table) <= 4000, "kernel arguments");
+static_assert(sizeof(Table) <= 4096 - 64 * sizeof(OrthoStep) - 16, "kernel arguments");
 
 // A symmetric matrix C = of_m M + of_n N + of_mn M N from those numbered m and n, which commute; or
 // (A) from X.
@@ -121,16 +123,20 @@ __device__ __forceinline__ TransposedPieces transposed_of(const Entry& t, int tu
   return p;
 }
 
-// The last entry whose first number is not above `id`.
+// The last entry (of those from `from` on, `count` of them) whose first number is not above `id`.
 template <typename First>
-__device__ __forceinline__ int entry_of(const Table& t, int id, First first) {
-  int lo = 0, hi = t.count - 1;
+__device__ __forceinline__ int entry_of(const Table& t, int id, First first, int from, int count) {
+  int lo = from, hi = from + count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (first(t.at[mid]) <= id) lo = mid;
     else hi = mid - 1;
   }
   return lo;
+}
+template <typename First>
+__device__ __forceinline__ int entry_of(const Table& t, int id, First first) {
+  return entry_of(t, id, first, 0, t.count);
 }
 
 __device__ __forceinline__ uint16_t half_bits(float x) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(x)); }
