@@ -64,8 +64,8 @@ __device__ __forceinline__ double block_sum(double x) {
 
 constexpr int kFewRows = 32;
 constexpr int kFewTile = 64;                             // columns at a time
-constexpr int64_t kFewChunk = 256, kFewMostChunks = 32;  // of A's partial sums
-constexpr int kFewBlock = 256;                           // columns of a workgroup that forms the result
+constexpr int64_t kFewMostChunks = 32;                   // of A's partial sums
+constexpr int64_t kFewMostBlocks = 512;                  // workgroups that form results, where more columns each avoid it
 
 struct FewSteps {
   OrthoStep at[kOrthoMostSteps];
@@ -73,41 +73,70 @@ struct FewSteps {
 };
 
 __host__ __device__ inline int64_t few_chunk(int64_t c) {
-  const int64_t least = round_up((c + kFewMostChunks - 1) / kFewMostChunks, kFewTile);
-  return least < kFewChunk ? kFewChunk : least;
+  return round_up((c + kFewMostChunks - 1) / kFewMostChunks, kFewTile);
 }
 __host__ __device__ inline int64_t few_chunks(int64_t c) { return (c + few_chunk(c) - 1) / few_chunk(c); }
 
 typedef float FewTile[kFewRows][kFewTile + 1];
 
-// Columns j0 .. j0 + 63 of G, as many as there are, zeros around them: a thread's places in the
-// order in which they lie in memory.
-template <typename In, typename F>
-__device__ __forceinline__ void few_places(const Entry& g, int j0, F f) {
-  const int columns = g.c - j0 < kFewTile ? g.c - j0 : kFewTile;
-  if (g.transposed) {
-    for (int k = threadIdx.x; k < columns * g.r; k += kNormThreads) f(k % g.r, k / g.r, (static_cast<int64_t>(j0) * g.r + k));
-  } else {
-    const int column = threadIdx.x % kFewTile;
-    if (column >= columns) return;
-    for (int i = threadIdx.x / kFewTile; i < g.r; i += kNormThreads / kFewTile) f(i, column, static_cast<int64_t>(i) * g.c + j0 + column);
-  }
-}
-template <typename In>
-__device__ __forceinline__ void few_load(const Entry& g, int j0, FewTile& tile) {
-  for (int k = threadIdx.x; k < kFewRows * kFewTile; k += kNormThreads) tile[k / kFewTile][k % kFewTile] = 0.0f;
-  __syncthreads();
-  const In* const in = static_cast<const In*>(g.in);
-  few_places<In>(g, j0, [&](int i, int j, int64_t at) { tile[i][j] = logit_to_float(in[at]); });
-  __syncthreads();
-}
-
-// A thread's four elements of a 32 x 32 matrix: two rows, two columns.
-struct Four {
-  double x[2][2];
+// Columns j0 .. j0 + 63 of G, as many as there are: a thread's elements in the order in which they lie
+// in memory.  k / r is (k (2^16 / r + 1)) >> 16: k < 2^11 and r <= 2^5 leave less than 1 / r over.
+struct FewPlace {
+  int row, column;
+  int64_t at;  // in the matrix; -1 where there is none
 };
-__device__ __forceinline__ int four_row() { return 2 * (threadIdx.x / 16); }
-__device__ __forceinline__ int four_column() { return 2 * (threadIdx.x % 16); }
+__device__ __forceinline__ FewPlace few_place(const Entry& g, int j0, int n) {
+  const int columns = g.c - j0 < kFewTile ? g.c - j0 : kFewTile;
+  const int k = threadIdx.x + n * kNormThreads;
+  if (g.transposed) {
+    const int column = (k * (65536 / g.r + 1)) >> 16;
+    return {k - column * g.r, column, k < columns * g.r ? static_cast<int64_t>(j0) * g.r + k : -1};
+  }
+  const int row = k / kFewTile, column = k % kFewTile;
+  return {row, column, row < g.r && column < columns ? static_cast<int64_t>(row) * g.c + j0 + column : -1};
+}
+constexpr int kFewEach = kFewRows * kFewTile / kNormThreads;
+template <typename In>
+struct FewFetch {
+  In x[kFewEach];
+  // Element 0 for those that are not there.
+  __device__ __forceinline__ void fetch(const Entry& g, int64_t j0) {
+#pragma unroll
+    for (int n = 0; n < kFewEach; ++n) {
+      const FewPlace p = few_place(g, static_cast<int>(j0), n);
+      x[n] = static_cast<const In*>(g.in)[p.at < 0 ? 0 : p.at];
+    }
+  }
+  // Zeros around what is there.
+  __device__ __forceinline__ void put(const Entry& g, int64_t j0, FewTile& tile) const {
+#pragma unroll
+    for (int n = 0; n < kFewEach; ++n) {
+      const int k = threadIdx.x + n * kNormThreads;
+      tile[k / kFewTile][k % kFewTile] = 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kFewEach; ++n) {
+      const FewPlace p = few_place(g, static_cast<int>(j0), n);
+      if (p.at >= 0) tile[p.row][p.column] = logit_to_float(x[n]);
+    }
+    __syncthreads();
+  }
+};
+
+// float64 products on the matrix cores: 16 x 16 of them a wave, a lane's four elements are rows
+// lane / 16 + 4 i of column lane % 16.  (Two rows by two columns a thread from local memory,
+// without them: a call for one 32 x 32 matrix 29 us, so 17.)
+typedef double Four __attribute__((ext_vector_type(4)));
+typedef double FewMatrix[kFewRows][kFewRows + 2];
+
+__device__ __forceinline__ Four few_mfma(double x, double y, Four sum) {
+  return __builtin_amdgcn_mfma_f64_16x16x4f64(x, y, sum, 0, 0, 0);
+}
+// The four of a wave's quarter of a matrix.
+__device__ __forceinline__ int four_row(int i) { return threadIdx.x / (2 * kWave) * 16 + threadIdx.x % kWave / 16 + 4 * i; }
+__device__ __forceinline__ int four_column() { return threadIdx.x / kWave % 2 * 16 + threadIdx.x % 16; }
+__device__ __forceinline__ int mfma_k() { return threadIdx.x % kWave / 16; }
 
 template <typename In>
 __device__ void few_gram(const Table& t, int id) {
@@ -115,125 +144,109 @@ __device__ void few_gram(const Table& t, int id) {
   const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_partial; }, t.count, t.few)];
   const int64_t chunk = id - g.first_partial, from = chunk * few_chunk(g.c);
   const int64_t to = from + few_chunk(g.c) < g.c ? from + few_chunk(g.c) : g.c;
+  const int row = threadIdx.x / (2 * kWave) * 16 + threadIdx.x % 16, column = four_column();
   Four sum = {};
+  FewFetch<In> tile;
+  tile.fetch(g, from);
   for (int64_t j0 = from; j0 < to; j0 += kFewTile) {
-    few_load<In>(g, static_cast<int>(j0), s_tile);
-    if (four_row() < g.r && four_column() < g.r) {
-      for (int k = 0; k < kFewTile; ++k) {
-        const double x[2] = {s_tile[four_row()][k], s_tile[four_row() + 1][k]};
-        const double y[2] = {s_tile[four_column()][k], s_tile[four_column() + 1][k]};
+    tile.put(g, j0, s_tile);
+    if (j0 + kFewTile < to) tile.fetch(g, j0 + kFewTile);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) sum.x[i][j] = fma(x[i], y[j], sum.x[i][j]);
-      }
-    }
+    for (int k = 0; k < kFewTile; k += 4) sum = few_mfma(s_tile[row][k + mfma_k()], s_tile[column][k + mfma_k()], sum);
     __syncthreads();
   }
   double* const out = reinterpret_cast<double*>(g.base) + chunk * kFewRows * kFewRows;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) out[(four_row() + i) * kFewRows + four_column() + j] = sum.x[i][j];
+  for (int i = 0; i < 4; ++i) out[four_row(i) * kFewRows + four_column()] = sum[i];
 }
 
-typedef double FewMatrix[kFewRows][kFewRows];
-
-__device__ __forceinline__ Four four_of(const FewMatrix& m) {
-  return {{{m[four_row()][four_column()], m[four_row()][four_column() + 1]},
-           {m[four_row() + 1][four_column()], m[four_row() + 1][four_column() + 1]}}};
-}
 __device__ __forceinline__ void store_four(FewMatrix& m, const Four& f) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) m[four_row() + i][four_column() + j] = f.x[i][j];
+  for (int i = 0; i < 4; ++i) m[four_row(i)][four_column()] = f[i];
 }
-__device__ __forceinline__ Four few_product(const FewMatrix& x, const FewMatrix& y, int r) {
+__device__ __forceinline__ Four few_product(const FewMatrix& x, const FewMatrix& y) {
+  const int row = threadIdx.x / (2 * kWave) * 16 + threadIdx.x % 16, column = four_column();
   Four f = {};
-  if (four_row() < r && four_column() < r) {
-#pragma unroll 4
-    for (int k = 0; k < r; ++k)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) f.x[i][j] = fma(x[four_row() + i][k], y[k][four_column() + j], f.x[i][j]);
-  }
+  for (int k = 0; k < kFewRows; k += 4) f = few_mfma(x[row][k + mfma_k()], y[k + mfma_k()][column], f);
   return f;
 }
 
-// The result's columns from 256 * block on; every workgroup of a matrix forms its Q.
+// The result's columns from few_block * block on; every workgroup of a matrix forms its Q.
 template <typename In>
 __device__ void few_apply(const Table& t, const FewSteps& steps, int id) {
   __shared__ FewMatrix s_a, s_p, s_q;
   __shared__ FewTile s_tile;
   const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_block; }, t.count, t.few)];
-  const int r = g.r;
   const double* const partials = reinterpret_cast<const double*>(g.base);
+  const int64_t from = static_cast<int64_t>(id - g.first_block) * t.few_block;
+  const int64_t to = from + t.few_block < g.c ? from + t.few_block : g.c;
+  FewFetch<In> tile;
+  tile.fetch(g, from);
   Four a = {};
+#pragma unroll 8
   for (int chunk = 0; chunk < g.partials; ++chunk)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) a.x[i][j] += partials[chunk * kFewRows * kFewRows + (four_row() + i) * kFewRows + four_column() + j];
+    for (int i = 0; i < 4; ++i) a[i] += partials[(chunk * kFewRows + four_row(i)) * kFewRows + four_column()];
   store_four(s_a, a);
   __syncthreads();
   double squares = 0.0;
-  for (int i = 0; i < r; ++i) squares += s_a[i][i];
+#pragma unroll
+  for (int i = 0; i < kFewRows; ++i) squares += s_a[i][i];
   const double norm = sqrt(squares), least = t.epsilon;
   const double factor = 1.0 / (norm < least ? least : norm);  // a NaN norm stays
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) a.x[i][j] = a.x[i][j] * factor * factor;
+  a = a * factor * factor;
   store_four(s_a, a);
   __syncthreads();
   for (int k = 0; k < steps.count; ++k) {
     const double pa = steps.at[k].a, pb = steps.at[k].b, pc = steps.at[k].c;
-    a = four_of(s_a);
-    const Four aa = few_product(s_a, s_a, r);
+    const Four aa = few_product(s_a, s_a);
     Four p;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        p.x[i][j] = (four_row() + i == four_column() + j ? pa : 0.0) + pb * a.x[i][j] + pc * aa.x[i][j];
+    for (int i = 0; i < 4; ++i) p[i] = (four_row(i) == four_column() ? pa : 0.0) + pb * a[i] + pc * aa[i];
     store_four(s_p, p);
     __syncthreads();
-    const Four q = k == 0 ? p : few_product(s_p, s_q, r);
-    const Four pap = few_product(s_p, s_a, r);
+    const bool last = k + 1 == steps.count;
+    const Four q = k == 0 ? p : few_product(s_p, s_q);
+    if (!last) a = few_product(s_p, s_a);
     __syncthreads();
     store_four(s_q, q);
-    store_four(s_a, pap);
+    store_four(s_a, a);
     __syncthreads();
-    a = few_product(s_a, s_p, r);
+    if (last) break;
+    a = few_product(s_a, s_p);
     __syncthreads();
     store_four(s_a, a);
     __syncthreads();
   }
   const double scale = factor * g.scale;
-  const int64_t from = static_cast<int64_t>(id - g.first_block) * kFewBlock;
-  for (int64_t j0 = from; j0 < g.c && j0 < from + kFewBlock; j0 += kFewTile) {
-    few_load<In>(g, static_cast<int>(j0), s_tile);
-    // A thread's column, every fourth row.
-    constexpr int kSets = kNormThreads / kFewTile, kMost = kFewRows / kSets;
-    const int column = threadIdx.x % kFewTile, set = threadIdx.x / kFewTile;
-    double y[kMost] = {};
-    for (int k = 0; k < r; ++k) {
-      const double x = s_tile[k][column];
+  for (int64_t j0 = from; j0 < to; j0 += kFewTile) {
+    tile.put(g, j0, s_tile);
+    if (j0 + kFewTile < to) tile.fetch(g, j0 + kFewTile);
+    // A wave's 16 columns, of all rows.
+    const int column = threadIdx.x / kWave * 16 + threadIdx.x % 16;
+    Four y[2] = {};
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) y[i] = fma(s_q[set + kSets * i][k], x, y[i]);
+    for (int k = 0; k < kFewRows; k += 4) {
+      const double x = s_tile[k + mfma_k()][column];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) y[half] = few_mfma(s_q[16 * half + threadIdx.x % 16][k + mfma_k()], x, y[half]);
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) s_tile[set + kSets * i][column] = static_cast<float>(y[i] * scale);
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_tile[16 * half + mfma_k() + 4 * i][column] = static_cast<float>(y[half][i] * scale);
     __syncthreads();
     In* const out = static_cast<In*>(g.out);
-    few_places<In>(g, static_cast<int>(j0), [&](int i, int j, int64_t at) {
-      if constexpr (sizeof(In) == 4) out[at] = s_tile[i][j];
-      else out[at] = to_bf16(s_tile[i][j]);
-    });
+#pragma unroll
+    for (int n = 0; n < kFewEach; ++n) {
+      const FewPlace p = few_place(g, static_cast<int>(j0), n);
+      if (p.at < 0) continue;
+      if constexpr (sizeof(In) == 4) out[p.at] = s_tile[p.row][p.column];
+      else out[p.at] = to_bf16(s_tile[p.row][p.column]);
+    }
     __syncthreads();
   }
 }
@@ -514,6 +527,15 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
       t.total_tiles[kind] += static_cast<int32_t>(tiles_in(e, kind, t.size[kind]));
     }
   }
+  // Every workgroup forms its Q, about 5 us: one tile each, then more (256 columns each, always: one float32
+  // 32 x 4096 matrix 32 us, so 25; eight of 2 x 300 29 and 21).
+  auto few_blocks = [&](int64_t block) {
+    int64_t blocks = 0;
+    for (int i = count; i < count + t.few; ++i) blocks += (t.at[i].c + block - 1) / block;
+    return blocks;
+  };
+  t.few_block = kFewTile;
+  while (t.few_block < 8 * kFewTile && few_blocks(t.few_block) > kFewMostBlocks) t.few_block *= 2;
   for (int i = count; i < count + t.few; ++i) {
     Entry& e = t.at[i];
     e.base = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
@@ -522,7 +544,7 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     e.first_partial = t.few_chunks;
     t.few_chunks += e.partials;
     e.first_block = t.few_blocks;
-    t.few_blocks += static_cast<int32_t>(tiles_of(e.c, kFewBlock));
+    t.few_blocks += (e.c + t.few_block - 1) / t.few_block;
   }
   *bytes = static_cast<size_t>(at);
   return t;

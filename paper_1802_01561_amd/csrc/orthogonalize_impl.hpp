@@ -31,7 +31,7 @@ struct Table {
   double* partials;
   int count;           // matrices of the tiles' kernels
   int few;             // behind them, those of few rows
-  int few_chunks, few_blocks;
+  int few_chunks, few_block, few_blocks;
   int total_partials, total_blocks, total_tiles[3];
   int size[3];  // of the tiles of A, B and X
   float epsilon;
