@@ -344,7 +344,7 @@ __global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t, FewS
     for (int q = 0; q < 4; ++q) v[q] *= kScaleX;
     const v2u high = high4(v);
     *reinterpret_cast<v2u*>(p.to[0] + at) = high;
-    *reinterpret_cast<v2u*>((kPair ? p.to[1] : p.low) + at) = low4(v, high);
+    *reinterpret_cast<v2u*>((kPair ? p.to[1] : p.low) + at) = kPair ? low4(v, high) : left4(v, high);
   }
   if (!t.small) return;
   const TransposedPieces pt = transposed_of<kPair>(g, 1);
@@ -674,7 +674,7 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
       u.by = 0;
       u.of_x = p.a * q.a;
     }
-    // A last step for itself takes the operand alone as X: 2^-12 of it, which no step makes larger.
+    // A last step for itself takes the operand alone as X: 2^-11 of it at most, which no step makes larger.
     u.low_out = low = !(next + 1 == step_count) || steps_from(next) == 2;
     if (e == hipSuccess) e = t.small ? launch_ortho_small_update(t, kPair, turn, u, st) : launch_ortho_tiles_update(t, kPair, turn, u, st);
     turn ^= 1;

@@ -155,6 +155,20 @@ __device__ __forceinline__ unsigned low2(float x, float y, unsigned high) {
 __device__ __forceinline__ v2u high4(const float (&y)[4]) { return {high2(y[0], y[1]), high2(y[2], y[3])}; }
 __device__ __forceinline__ v2u low4(const float (&y)[4], v2u high) { return {low2(y[0], y[1], high[0]), low2(y[2], y[3], high[1])}; }
 
+// bfloat16 matrices: X as what its operand leaves of it beside the operand, times 2^11, at most half a
+// step of the operand: float16 without leaving its range up to 2^15, nor its digits where the
+// operand itself is below float16's (norms below epsilon).
+constexpr float kScaleLeft = 2048.0f;
+__device__ __forceinline__ v2u left4(const float (&y)[4], v2u high) {
+  float left[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) left[q] = (y[q] - high_of(high[q / 2], q % 2)) * kScaleLeft;
+  return high4(left);
+}
+__device__ __forceinline__ float whole_of(v2u high, v2u left, int q) {
+  return fmaf(high_of(left[q / 2], q % 2), 1.0f / kScaleLeft, high_of(high[q / 2], q % 2));
+}
+
 // An element of a product beside the diagonal, and on it, from its factors' elements there (on the
 // diagonal: dm, dn) and the sum of O O'.
 template <int kOf>

@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
         } else if constexpr (kOf == kUpdate) {
           float before;
           if constexpr (kPair) before = x[m][n][q];
-          else before = (high_of(o[0][0][m][n][q / 2], q % 2) + high_of(o[0][1][m][n][q / 2], q % 2)) * (1.0f / kScaleX);
+          else before = whole_of(o[0][0][m][n], o[0][1][m][n], q) * (1.0f / kScaleX);
           y = fmaf(f.of_x + of_row[n], before, sum * (1.0f / (kScaleA * kScaleX)));
         } else {
           const float oo = sum * (1.0f / (kScaleA * kScaleA)), di = of_row[n];
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int
     for (int q = 0; q < 4; ++q) y[q] *= scale;
     const v2u high = high4(y);
     *reinterpret_cast<v2u*>(high_out + to) = high;
-    if (low_out != nullptr) *reinterpret_cast<v2u*>(low_out + to) = low4(y, high);
+    if (low_out != nullptr) *reinterpret_cast<v2u*>(low_out + to) = kPair ? low4(y, high) : left4(y, high);
   };
 #pragma unroll
   for (int w = 0; w < kSide * kQuads / kSmallThreads; ++w) {

@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           if constexpr (kPair) {
             before = x[n % kBuffers][m][q];
           } else {
-            before = (high_of(part[n % kBuffers][0][m][q / 2], q % 2) + high_of(part[n % kBuffers][1][m][q / 2], q % 2)) * (1.0f / kScaleX);
+            before = whole_of(part[n % kBuffers][0][m], part[n % kBuffers][1][m], q) * (1.0f / kScaleX);
           }
           y[q] = fmaf(factor, before, element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
         }
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           const v2u high = high4(y);
           *reinterpret_cast<v2u*>(p.to[0] + to) = high;
           if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + to) = low4(y, high);
-          else if (f.low_out) *reinterpret_cast<v2u*>(p.low + to) = low4(y, high);
+          else if (f.low_out) *reinterpret_cast<v2u*>(p.low + to) = left4(y, high);
         }
       }
       __builtin_amdgcn_sched_barrier(0);

@@ -1,0 +1,352 @@
+"""The calls on a token policy's parameters as a program uses them: one learner step of all of
+them, both ways into the library, calls at the same time, graphs that share a workspace, tensors
+at any element, entries that are not finite, tensors of more than 2^31 elements."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1802_01561_amd as vt
+from oracle import parameters as op
+from paper_1802_01561_amd import binding
+from test_gpu_embed import _check_embed, _normal, _tokens, check_grad
+from test_gpu_log_prob_loss import _batch as _loss_batch
+from test_gpu_log_prob_loss import _dev
+from test_gpu_orthogonalize import check, matrix
+from test_gpu_vocab import _check_grad, _check_log_probs
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+CUBIC = (1.5, -0.5, 0.0)
+
+
+def _same(a, b):
+    assert len(a) == len(b)
+    for p, q in zip(a, b):
+        assert p.dtype == q.dtype and torch.equal(p, q)
+
+
+class Policy:
+    """A tied table and one layer: hidden = tanh(embedded layer^T)."""
+
+    def __init__(self, seed, T=24, B=5, H=72, V=901):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.B, self.H, self.V = T, B, H, V
+        self.table = (torch.randn(V, H, generator=g) / H ** 0.5).bfloat16().cuda()
+        self.layer = (torch.randn(H, H, generator=g) / H ** 0.5).cuda()
+        t = _tokens(seed, T * B, V, "text", 0.1).reshape(T, B)
+        self.inputs = torch.from_numpy(t).cuda()
+        self.actions = torch.from_numpy(np.roll(t, -1, axis=0).copy()).cuda()
+        self.rest = _dev(_loss_batch(seed, T, B))
+        self.vocab, self.vocab_grad = vt.VocabWorkspace(T, B, V, H), vt.VocabWorkspace(T, B, V, H, grad_dtype=F32)
+        self.embed, self.loss, self.clip = vt.EmbedWorkspace(T, B, V, H), vt.LogProbWorkspace(T, B), vt.ClipWorkspace()
+        self.ortho = vt.OrthogonalWorkspace([self.layer])
+
+    def step(self):
+        scale = math.sqrt(self.H)
+        x = vt.vtrace_vocab_embed(self.table, self.inputs, scale, out_dtype=F32, workspace=self.embed)
+        flat = x.view(-1, self.H)
+        hidden = torch.tanh(flat @ self.layer.t())
+        states = hidden.bfloat16().view(self.T, self.B, self.H)
+        o = vt.vtrace_vocab_log_probs(states, self.table, None, self.actions, workspace=self.vocab)
+        y = dict(self.rest, target_log_probs=o.log_probs, entropy=o.entropy)
+        loss = vt.vtrace_log_prob_loss_grad(**y, workspace=self.loss)
+        g = vt.vtrace_vocab_grad(states, self.table, None, self.actions, o.log_sums, o.entropy, loss.d_log_probs, loss.d_entropy,
+                                 grad_dtype=F32, workspace=self.vocab_grad)
+        outer = g.d_weight.clone()
+        d_pre = g.d_hidden.view(-1, self.H) * (1.0 - hidden * hidden)
+        d_layer = d_pre.t().contiguous() @ flat
+        d_x = (d_pre @ self.layer).view(self.T, self.B, self.H)
+        d_table = vt.vtrace_vocab_embed_grad(d_x, self.inputs, self.V, scale, accumulate_into=g.d_weight, workspace=self.embed)
+        assert d_table is g.d_weight
+        both, d_layer_was = d_table.clone(), d_layer.clone()
+        norm = vt.vtrace_clip_grad_norm([d_table, d_layer], 0.5, workspace=self.clip)
+        clipped = d_layer.clone()
+        update, = vt.vtrace_orthogonalize([d_layer], 0.2, out=[d_layer], workspace=self.ortho)
+        assert update is d_layer
+        return [x, states, *o, loss.losses, loss.d_log_probs, loss.d_entropy, g.d_hidden, outer, d_x, both, d_layer_was, d_table,
+                norm, clipped, update]
+
+
+def test_learner_step_of_all_calls():
+    """Each against its oracle, with the inputs that it had."""
+    p = Policy(3)
+    x, states, lp, ls, ent, losses, d_lp, d_ent, d_hidden, outer, d_x, both, d_layer, d_table, norm, clipped, update = p.step()
+    scale = math.sqrt(p.H)
+    tokens, actions = p.inputs.cpu().numpy(), p.actions.cpu()
+    _check_embed(p.table, tokens, scale, F32, x)
+    c = lambda t: t.cpu()  # noqa: E731
+    _check_log_probs(c(states), c(p.table), None, actions, vt.VocabLogProbs(lp, ls, ent))
+    check_grad(d_x, tokens, p.V, scale, both, before=outer)
+    _check_grad(c(states), c(p.table), None, actions, c(d_lp), c(d_ent), vt.VocabGrad(d_hidden, outer, None), F32)
+    total = math.sqrt(sum((t.double() ** 2).sum().item() for t in (both, d_layer)))
+    assert abs(norm.item() - total) <= 2.0 ** -23 * total and total > 0.5  # clipped
+    for was, now in ((both, d_table), (d_layer, clipped)):
+        # the norm, the factor and the product are rounded once each
+        assert torch.allclose(now.double(), was.double() * (0.5 / total), rtol=2.0 ** -22, atol=2.0 ** -149)
+    check(clipped, update, scale=0.2)
+    for ws in (p.vocab, p.vocab_grad, p.embed, p.loss, p.clip, p.ortho):
+        assert vt.vtrace_error_flag(ws) == 0
+
+
+def test_learner_steps_in_graphs_that_share_workspaces():
+    """Two captured apart, replayed in either order, with eager steps between."""
+    ps = [Policy(7), Policy(8)]
+    for name in ("vocab", "vocab_grad", "embed", "loss", "clip", "ortho"):
+        setattr(ps[1], name, getattr(ps[0], name))
+    expect = [[t.clone() for t in p.step()] for p in ps]
+    torch.cuda.synchronize()
+    graphs, held = [], []
+    for p in ps:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(p.step())
+        graphs.append(graph)
+    for order in ((0, 1), (1, 0), (0, 0, 1), (1, 1, 0)):
+        for k in order:
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            _same(held[k], expect[k])
+        _same(ps[1].step(), expect[1])
+        torch.cuda.synchronize()
+
+
+MIXED = [(1, 1), (40, 70), (70, 40), (130, 257), (300, 300), (32, 500), (33, 20)]
+
+
+def _mixed(seed, dtypes=(F32, BF16)):
+    return [matrix(seed + i, m, n, dtypes[i % len(dtypes)], "strong").cuda() for i, (m, n) in enumerate(MIXED)]
+
+
+def test_updates_in_graphs_replayed():
+    """Matrices of all the kernels in one call, on data that changes between replays."""
+    gs, other = _mixed(50), _mixed(90)
+    ws = vt.OrthogonalWorkspace(gs)
+    expect = [vt.vtrace_orthogonalize(x, workspace=ws) for x in (gs, other)]
+    into, out = [g.clone() for g in gs], [torch.empty_like(g) for g in gs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vt.vtrace_orthogonalize(into, out=out, workspace=ws)
+    for k in (1, 0, 0, 1, 1):
+        for a, b in zip(into, (gs, other)[k]):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        _same(out, expect[k])
+        _same(vt.vtrace_orthogonalize(gs, workspace=ws), expect[0])
+
+
+def test_calls_at_the_same_time():
+    """Two streams, a workspace each, several rounds: what each gets alone."""
+    T, B, H, V = 900, 40, 72, 5000  # past what one pass ranks
+    sets = []
+    for seed in (1, 2):
+        gs = _mixed(100 * seed)
+        sets.append((_normal(seed, (V, H), BF16).cuda(), torch.from_numpy(_tokens(seed, T * B, V, "text")).cuda().view(T, B),
+                     _normal(seed + 9, (T, B, H), BF16).cuda(), gs, vt.EmbedWorkspace(T, B, V, H), vt.OrthogonalWorkspace(gs)))
+
+    def calls(w, t, d, gs, ew, ow):
+        return [vt.vtrace_vocab_embed(w, t, workspace=ew), vt.vtrace_vocab_embed_grad(d, t, V, workspace=ew),
+                *vt.vtrace_orthogonalize(gs, workspace=ow), vt.vtrace_vocab_embed_grad(d[:20], t[:20], V, workspace=ew)]
+
+    alone = [calls(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(4):
+        got = []
+        for s, stream in zip(sets, streams):
+            with torch.cuda.stream(stream):
+                got.append(calls(*s))
+        torch.cuda.synchronize()
+        for a, b in zip(alone, got):
+            _same(a, b)
+
+
+def test_native_and_python_marshalling_agree(monkeypatch):
+    """A workspace and no stream goes through native code, a stream through Python."""
+    fast = binding._fast_call(torch.empty(1, device="cuda"))
+    ran = []
+    for name in ("call_vocab_embed", "call_vocab_embed_grad", "call_orthogonalize"):
+        def counted(*args, _f=getattr(fast, name)):
+            r = _f(*args)
+            ran.append(r is not None)
+            return r
+        monkeypatch.setattr(fast, name, counted)
+    here = torch.cuda.current_stream()
+    T, B, H, V = 31, 3, 24, 200
+    t = torch.from_numpy(_tokens(1, T * B, V)).cuda().view(T, B)
+    ew = vt.EmbedWorkspace(T, B, V, H)
+    for table, wanted in ((F32, BF16), (BF16, F32), (BF16, None)):
+        w, d = _normal(2, (V, H), table).cuda(), _normal(3, (T, B, H), table).cuda()
+        a = vt.vtrace_vocab_embed(w, t, 2.5, out_dtype=wanted, workspace=ew)
+        b = vt.vtrace_vocab_embed(w, t, 2.5, out_dtype=wanted, workspace=ew, stream=here)
+        c = vt.vtrace_vocab_embed(w, t, 2.5, out=torch.empty_like(a))
+        _same([a, a], [b, c])
+        assert a.dtype == (wanted or table)
+        wanted = wanted or F32
+        a = vt.vtrace_vocab_embed_grad(d, t, V, 2.5, grad_dtype=wanted, workspace=ew)
+        b = vt.vtrace_vocab_embed_grad(d, t, V, 2.5, grad_dtype=wanted, workspace=ew, stream=here)
+        into = torch.zeros_like(a)
+        c = vt.vtrace_vocab_embed_grad(d, t, V, 2.5, accumulate_into=into, workspace=ew)
+        e = vt.vtrace_vocab_embed_grad(d, t, V, 2.5, out=torch.empty_like(a))
+        _same([a, a, a], [b, c, e])
+        assert c is into
+    gs = _mixed(7)
+    ow = vt.OrthogonalWorkspace(gs)
+    a = vt.vtrace_orthogonalize(gs, 0.5, workspace=ow)
+    b = vt.vtrace_orthogonalize(gs, 0.5, workspace=ow, stream=here)
+    c = vt.vtrace_orthogonalize(iter(gs), [0.5] * len(gs), out=(torch.empty_like(g) for g in gs), workspace=ow)
+    e = vt.vtrace_orthogonalize(iter(gs), 0.5, out=(torch.empty_like(g) for g in gs), workspace=ow)
+    for other in (b, c, e):
+        _same(a, other)
+    # embed native: two of three calls each; gradients with a workspace and without a stream; two of the four updates
+    assert sum(ran) == 6 + 6 + 2, ran
+
+
+def test_scales_one_for_each_and_single_bits():
+    gs = _mixed(20)
+    scales = [0.25 * 2.0 ** i for i in range(len(gs))]
+    a, b = vt.vtrace_orthogonalize(gs, scales), vt.vtrace_orthogonalize(gs)
+    for x, y, s in zip(a, b, scales):
+        assert torch.equal(x, y * s)  # powers of two
+    for x in vt.vtrace_orthogonalize(gs, 0.0):
+        assert (x == 0).all()
+
+
+@pytest.mark.parametrize("first", [1, 2, 3])
+def test_tensors_at_any_element(first):
+    """Inputs and outputs that start, and rows that lie, at no multiple of 16 bytes; what is around them stays."""
+    def moved(t):
+        around = torch.full((t.numel() + 2 * first + 8,), 7.0, dtype=t.dtype, device="cuda")
+        inside = around[first:first + t.numel()].view(t.shape)
+        inside.copy_(t)
+        return around, inside
+
+    def untouched(around, n):
+        assert (around[:first] == 7).all() and (around[first + n:] == 7).all()
+
+    gs = _mixed(30)
+    expect = vt.vtrace_orthogonalize(gs)
+    for in_place in (False, True):
+        ins = [moved(g) for g in gs]
+        outs = ins if in_place else [moved(torch.zeros_like(g)) for g in gs]
+        got = vt.vtrace_orthogonalize([i for _, i in ins], out=[o for _, o in outs])
+        _same(got, expect)
+        for (around, o) in outs:
+            untouched(around, o.numel())
+        if not in_place:
+            _same([i for _, i in ins], gs)
+
+
+@pytest.mark.parametrize("H", [8, 40, 72])
+def test_embed_outputs_leave_what_is_around_them(H):
+    """Rows and the gradient's table between others of the same tensor, at 16 bytes."""
+    T, B, V = 50, 3, 90
+    t = torch.from_numpy(_tokens(H, T * B, V)).cuda().view(T, B)
+    w, d = _normal(1, (V, H), BF16).cuda(), _normal(2, (T, B, H), BF16).cuda()
+    rows = torch.full((T + 2, B, H), 7.0, dtype=BF16, device="cuda")
+    vt.vtrace_vocab_embed(w, t, out=rows[1:-1])
+    assert torch.equal(rows[1:-1], vt.vtrace_vocab_embed(w, t)) and (rows[0] == 7).all() and (rows[-1] == 7).all()
+    for dtype in (F32, BF16):
+        table = torch.full((V + 2, H), 7.0, dtype=dtype, device="cuda")
+        vt.vtrace_vocab_embed_grad(d, t, V, out=table[1:-1])
+        assert torch.equal(table[1:-1], vt.vtrace_vocab_embed_grad(d, t, V, grad_dtype=dtype))
+        assert (table[0] == 7).all() and (table[-1] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_what_is_not_finite_stays_in_its_matrix(dtype, value):
+    gs = _mixed(40, (dtype,))
+    expect = vt.vtrace_orthogonalize(gs)
+    for which in range(len(gs)):
+        bad = [g.clone() for g in gs]
+        bad[which].view(-1)[-1] = value
+        got = vt.vtrace_orthogonalize(bad)
+        assert torch.isnan(got[which]).all()
+        _same([o for i, o in enumerate(got) if i != which], [o for i, o in enumerate(expect) if i != which])
+
+
+@pytest.mark.parametrize("m,n", [(1, 9), (20, 30), (64, 40), (200, 300)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_zeros_and_norms_below_epsilon(m, n, dtype):
+    g = matrix(m, m, n, dtype).cuda()
+    zero, small, large = torch.zeros_like(g), (g.double() * 2.0 ** -40).to(dtype), (g.double() * 2.0 ** 100).to(dtype)
+    got = vt.vtrace_orthogonalize([zero, small, large])
+    assert (got[0] == 0).all()
+    check(small, got[1])
+    check(large, got[2])
+    got, = vt.vtrace_orthogonalize([g], epsilon=1.0)
+    check(g, got, epsilon=1.0)
+
+
+@pytest.mark.parametrize("m,n", [(2, 2), (20, 33), (32, 500), (90, 100), (300, 140)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("coefficients", [(op.QUINTIC,), (op.QUINTIC,) * 2, (op.QUINTIC,) * 3, (op.QUINTIC,) * 4, (op.QUINTIC,) * 6,
+                                          (CUBIC,) * 3, (CUBIC,) * 12, (op.QUINTIC, (2.5, -2.0, 0.5), CUBIC)])
+def test_other_steps(m, n, dtype, coefficients):
+    g = matrix(m + n, m, n, dtype)
+    got, = vt.vtrace_orthogonalize([g.cuda()], steps=len(coefficients), coefficients=coefficients)
+    check(g, got, steps=coefficients)
+
+
+@pytest.mark.parametrize("m,n", [(1, 3), (9, 20), (32, 32)])
+@pytest.mark.parametrize("steps", [7, 8, 64])
+def test_many_steps_of_few_rows(m, n, steps):
+    """On both sides of what the small matrices' own steps take, of full rank and of less."""
+    for rank in (m, max(1, m // 3)):
+        g = torch.Generator().manual_seed(steps + rank)
+        x = (torch.randn(m, rank, generator=g) @ torch.randn(rank, n, generator=g)).cuda()
+        got, = vt.vtrace_orthogonalize([x], steps=steps)
+        s = np.linalg.svd(got.double().cpu().numpy(), compute_uv=False)
+        # of full rank in its float32 elements they have all come near 1; no direction ever leaves the range
+        assert s[:rank].min() > 0.6 and s.max() < 1.3
+
+
+def test_a_workspace_for_more_serves_less_and_other_calls():
+    gs = _mixed(60)
+    T, B, H, V = 40, 5, 24, 300
+    t = torch.from_numpy(_tokens(4, T * B, V)).cuda().view(T, B)
+    d = _normal(5, (T, B, H), F32).cuda()
+    ws, big = vt.OrthogonalWorkspace(gs), vt.EmbedWorkspace(T, B, V, H)
+    ws.tensor[4352:].fill_(0xFF)
+    expect = [vt.vtrace_orthogonalize(gs[k:k + 2]) for k in range(5)]
+    for k in range(5):
+        _same(vt.vtrace_orthogonalize(gs[k:k + 2], workspace=ws), expect[k])
+        vt.vtrace_orthogonalize(gs, workspace=ws)
+    whole = vt.vtrace_vocab_embed_grad(d, t, V)
+    part = vt.vtrace_vocab_embed_grad(d[:7], t[:7], V)
+    for _ in range(3):
+        _same([vt.vtrace_vocab_embed_grad(d, t, V, workspace=big), vt.vtrace_vocab_embed_grad(d[:7], t[:7], V, workspace=big)], [whole, part])
+
+
+@pytest.mark.parametrize("N", [300, 20000])
+def test_gradient_against_differences(N):
+    """The lookup is linear: with small integers, (embed(w + e) - embed(w)) . d = gradient . e, exactly."""
+    H, V, scale = 16, 70, 2.0
+    r = np.random.default_rng(N)
+    whole = lambda *shape: torch.from_numpy(r.integers(-3, 4, shape).astype(np.float32)).cuda()  # noqa: E731
+    w, e, d = whole(V, H), whole(V, H), whole(N, 1, H)
+    t = torch.from_numpy(_tokens(N, N, V, "text")).cuda().view(N, 1)
+    change = (vt.vtrace_vocab_embed(w + e, t, scale) - vt.vtrace_vocab_embed(w, t, scale)).double()
+    grad = vt.vtrace_vocab_embed_grad(d, t, V, scale).double()
+    assert (change * d.double()).sum().item() == (grad * e.double()).sum().item()
+
+
+def test_more_than_2_31_elements():
+    """A table, outputs and a gradient past 32 bits: every token once, in another order."""
+    H, V = 8192, 270001
+    w = torch.empty((V, H), dtype=BF16, device="cuda").random_(-100, 100)
+    order = torch.randperm(V, generator=torch.Generator().manual_seed(1)).int()
+    t = order.cuda().view(V, 1)
+    rows = vt.vtrace_vocab_embed(w, t)
+    ws = vt.EmbedWorkspace(V, 1, V, H)
+    grad = vt.vtrace_vocab_embed_grad(rows, t, V, grad_dtype=BF16, workspace=ws)
+    assert torch.equal(grad, w)
+    for at in (0, 1000, 262143, 262144, 262145, V - 1):
+        assert torch.equal(rows[at, 0], w[order[at].item()])
+    assert vt.vtrace_error_flag(ws) == 0
