@@ -164,11 +164,12 @@ __device__ __forceinline__ void store_four(FewMatrix& m, const Four& f) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[four_row(i)][four_column()] = f[i];
 }
-__device__ __forceinline__ Four few_product(const FewMatrix& x, const FewMatrix& y) {
+__device__ __forceinline__ Four few_product(const FewMatrix& x, const FewMatrix& y, int r) {
   const int row = threadIdx.x / (2 * kWave) * 16 + threadIdx.x % 16, column = four_column();
   Four f = {};
 #pragma unroll
-  for (int k = 0; k < kFewRows; k += 4) f = few_mfma(x[row][k + mfma_k()], y[k + mfma_k()][column], f);
+  for (int k = 0; k < kFewRows; k += 4)
+    if (k < r) f = few_mfma(x[row][k + mfma_k()], y[k + mfma_k()][column], f);
   return f;
 }
 
@@ -201,21 +202,21 @@ __device__ void few_apply(const Table& t, const FewSteps& steps, int id) {
   __syncthreads();
   for (int k = 0; k < steps.count; ++k) {
     const double pa = steps.at[k].a, pb = steps.at[k].b, pc = steps.at[k].c;
-    const Four aa = few_product(s_a, s_a);
+    const Four aa = few_product(s_a, s_a, g.r);
     Four p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = (four_row(i) == four_column() ? pa : 0.0) + pb * a[i] + pc * aa[i];
     store_four(s_p, p);
     __syncthreads();
     const bool last = k + 1 == steps.count;
-    const Four q = k == 0 ? p : few_product(s_p, s_q);
-    if (!last) a = few_product(s_p, s_a);
+    const Four q = k == 0 ? p : few_product(s_p, s_q, g.r);
+    if (!last) a = few_product(s_p, s_a, g.r);
     __syncthreads();
     store_four(s_q, q);
     store_four(s_a, a);
     __syncthreads();
     if (last) break;
-    a = few_product(s_a, s_p);
+    a = few_product(s_a, s_p, g.r);
     __syncthreads();
     store_four(s_a, a);
     __syncthreads();
