@@ -51,7 +51,7 @@ vtrace_status vtrace_vocab_embed(
  *                 (+ d_weight[v,:] as it was, with accumulate).
  *
  *   d_embedded   [T,B,H] of embedded_dtype, 16-byte aligned; rows of steps without a
- *                token are not read
+ *                token are not used
  *   d_weight     [V,H] of grad_dtype, 16-byte aligned.  accumulate 0: all of it is
  *                written, rows of tokens that no step has with zeros; otherwise
  *                rows of tokens that steps have are added to, and no other is touched
@@ -94,12 +94,16 @@ vtrace_status vtrace_vocab_embed_grad(
  *   epsilon       finite, > 0; a matrix of zeros gives zeros
  *   workspace     vtrace_orthogonalize_workspace_bytes(count, rows, columns, dtypes) bytes, 16-byte
  *                 aligned, cleared once by vtrace_workspace_init; 0 for an invalid list
- * Numerics: norms are float64, X is float32 from step to step, sums of products are
- * float32.  Products take float16 operands of a fixed scale, for float32 matrices in two
- * parts (22 bits) each; the diagonals of the symmetric matrices are float32.  Against
- * products in 64 bits results of bfloat16 matrices are off by little more than their
- * own rounding, and those of float32 matrices by 1e-6 to 5e-6, in relation to their norm.  NaN or
- * Inf in a matrix makes all of its result NaN, and that of no other matrix.
+ * Numerics: norms are float64.  Matrices of at most 32 rows or columns are float64 up to the
+ * result's rounding (as long as the coefficients a multiply to at most 8192 over the steps).
+ * Otherwise X has 22 bits (bfloat16 matrices) or is float32 from step to step, sums of
+ * products are float32, products take float16 operands of a fixed scale, for float32 matrices
+ * in two parts (22 bits) each, and the diagonals of the symmetric matrices are float32.  Against
+ * products in 64 bits results of bfloat16 matrices are off by little more than their own
+ * rounding (1.7e-3 to 2.3e-3 for 5 steps of the quintic), and those of float32 matrices by up
+ * to 1.3e-6, in relation to their norm, down to norms of epsilon: far below it, where singular
+ * values stay small, results of bfloat16 matrices are off by up to 2^-36 each.  NaN or Inf in
+ * a matrix makes all of its result NaN, and that of no other matrix.
  */
 size_t vtrace_orthogonalize_workspace_bytes(int64_t count, const int64_t* rows, const int64_t* columns,
                                             const int32_t* dtypes);

@@ -90,7 +90,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kCachedBytes = int64_t(1) << 27;  // half of the Infinity Cache
 
 // kRows rows a group of threads, their loads in flight together.  Outputs larger than what the
-// caches hold go past them: 65536 rows of 2048 bfloat16 87 -> 60 us (2 or 8 rows a group: 88, 108).
+// caches hold go past them: 65536 rows of 2048 bfloat16 87 -> 60 us (2 or 8 rows a group: 88, 108),
+// 4.5 TB/s of stores and 1.4 of distinct rows; 48 rows 2.9 us, a launch.
 template <typename In, typename Out, int kRows, bool kPast>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes_log2) {
   const int groups = kThreads >> lanes_log2, lanes = 1 << lanes_log2;
@@ -182,7 +183,8 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedArgs a) {
   if (invalid(static_cast<int32_t>(mine), a.V)) raise_error_flag(a.error_flag);
 }
 
-// More steps: passes over digits of the token, from the lowest up, each of them stable.  A pass
+// More steps: passes over digits of the token, from the lowest up, each of them stable: of 65536 steps
+// two passes, 5 us to count and 9 to move.  A pass
 // counts every block's digits, adds the counts up in the order (digit, block), and moves.
 constexpr int kMostDigitBits = 9, kMostDigits = 1 << kMostDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
@@ -429,6 +431,8 @@ __device__ __forceinline__ float* partial_row(const EmbedArgs& a, int64_t chunk,
 
 // Chunks of the sorted steps, one a group of threads (and a slab of the row, where it has more
 // than a workgroup's units); then, in further workgroups, the rows that no step has.
+// Bound by memory where steps or rows are many: 65536 steps of 2048 bfloat16 added to 20088 rows 97 us,
+// 4.5 TB/s; 3200 steps of 1024 and 32768 rows 14 us, 5.2 TB/s, most of it the rows of no step.
 // Slot 0 of a chunk's partial sums is that of the run that comes from the chunk before it,
 // slot 1 of the one that begins here and goes on behind it.
 template <typename In, typename Out, bool kAccumulate>
@@ -498,7 +502,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, int la
 }
 
 // The run that begins in a chunk and goes on behind it: its parts, in order, in float64; the
-// groups of a workgroup take turns with them.
+// groups of a workgroup take turns with them.  5 us, a launch; 11 of 65536 steps of 2048 where one
+// token has 3900 of them, eight parts in flight.
 constexpr int kJoinThreads = 256;
 template <typename Out>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, int lanes_log2, int slabs) {

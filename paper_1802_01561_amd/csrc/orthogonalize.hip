@@ -5,7 +5,8 @@
 // vectors.  X is kept with at most as many rows (r) as columns (c): a taller matrix is
 // transposed when it is read, and back when the result is written.
 //
-// Numerics.  X is kept in float32, and the products' operands are float16, of fixed powers of
+// Numerics.  X is kept in 22 bits or more (of bfloat16 matrices its float16 operand and what
+// that leaves, else float32), and the products' operands are float16, of fixed powers of
 // two: singular values stay within a small range (the entry point checks the coefficients), so
 // that bfloat16's exponents are not needed and float16's three more bits are had for
 // nothing (bfloat16 operands: results 1.3e-2 to 3e-2 off, in relation to their norm).  The
@@ -13,9 +14,10 @@
 // are kept out of the operands, in float32:
 //   with A = D + O:  B = b (D + O) + c (D D + D O + O D + O O),   B X = diag(B) X + offdiag(B) X,
 // where only O O and offdiag(B) X are products on the matrix cores (with the diagonals in the
-// operands 1.7e-3 to 2.8e-3 off, without 2e-4 to 7e-4, and one rounding to bfloat16 is 1.7e-3).
-// Float32 matrices have operands in two parts, high + low, and three products for each: 5e-7
-// to 3e-6 off, from the float32 sums (a library's float32 products 2e-6 to 7e-5: small singular
+// operands 1.7e-3 to 2.8e-3 off, without 2e-4 to 7e-4, and one rounding to bfloat16 is 1.7e-3:
+// results of 33 rows and more are 1.7e-3 to 2.3e-3 off).
+// Float32 matrices have operands in two parts, high + low, and three products for each: 4e-7
+// to 1.3e-6 off, from the float32 sums (a library's float32 products 2e-6 to 7e-5: small singular
 // values grow by 3.44 a step, and rounding errors beside the largest with them).
 //
 // A and B are symmetric: their tiles on and below the diagonal are computed, and stored twice.
