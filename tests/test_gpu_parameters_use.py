@@ -350,3 +350,77 @@ def test_more_than_2_31_elements():
     for at in (0, 1000, 262143, 262144, 262145, V - 1):
         assert torch.equal(rows[at, 0], w[order[at].item()])
     assert vt.vtrace_error_flag(ws) == 0
+
+
+def test_most_steps_and_most_tokens():
+    """2^25 steps of the shortest rows, 2^24 tokens: sums of small integers, exactly."""
+    T, B, H, V = 4096, 8192, 8, 1 << 24
+    g = torch.Generator(device="cuda").manual_seed(2)
+    t = torch.randint(-1, V, (T, B), generator=g, device="cuda", dtype=torch.int32)
+    t[::7] %= 1000  # frequent ones
+    t[5] = vt.NO_TOKEN
+    d = torch.randint(-3, 4, (T, B, H), generator=g, device="cuda").to(BF16)
+    ws = vt.EmbedWorkspace(T, B, V, H)
+    flat, rows = t.view(-1).long(), d.view(-1, H).float()
+    expect = torch.zeros((V + 1, H), device="cuda").index_add_(0, torch.where(flat < 0, V, flat), rows)[:V]
+    got = vt.vtrace_vocab_embed_grad(d, t, V, workspace=ws)
+    assert torch.equal(got, expect)
+    before = torch.randint(-3, 4, (V, H), generator=g, device="cuda").float()
+    assert torch.equal(vt.vtrace_vocab_embed_grad(d, t, V, 2.0, accumulate_into=before.clone(), workspace=ws), before + 2.0 * expect)
+    out = vt.vtrace_vocab_embed(expect, t, 0.5, out_dtype=F32, workspace=ws)
+    assert torch.equal(out.view(-1, H), torch.where((flat < 0)[:, None], 0.0, 0.5 * expect[flat.clamp(min=0)]))
+    assert vt.vtrace_error_flag(ws) == 0
+
+
+def test_tokens_at_any_element():
+    T, B, H, V = 30, 7, 16, 50
+    w, d = _normal(1, (V, H), F32).cuda(), _normal(2, (T, B, H), F32).cuda()
+    t = torch.from_numpy(_tokens(3, T * B, V)).cuda()
+    around = torch.full((T * B + 9,), 2 ** 30, dtype=torch.int32, device="cuda")
+    for first in (1, 2, 3):
+        inside = around[first:first + T * B]
+        inside.copy_(t)
+        ws = vt.EmbedWorkspace(T, B, V, H)
+        _same([vt.vtrace_vocab_embed(w, inside.view(T, B), workspace=ws), vt.vtrace_vocab_embed_grad(d, inside.view(T, B), V, workspace=ws)],
+              [vt.vtrace_vocab_embed(w, t.view(T, B)), vt.vtrace_vocab_embed_grad(d, t.view(T, B), V)])
+        assert vt.vtrace_error_flag(ws) == 0
+        around.fill_(2 ** 30)
+
+
+@pytest.mark.parametrize("dtype,m,n", [(BF16, 65536, 32768), (BF16, 32768, 65536), (F32, 65536, 32768), (BF16, 65536, 40),
+                                       (F32, 24, 65536), (F32, 65536, 5000)])
+def test_largest_matrices(dtype, m, n):
+    """Three singular values with vectors of signs, whose products are small integers; anything out of
+    place is off by its whole size.  bfloat16: an operand's rounding (2^-11) counts up to 5 times in B X in each of
+    five steps, on singular values that steps take at most apart by 3.4 once and then by about 1: 2^-6.
+    Float32: terms of few values, of whose sums the roundings do not cancel.  k terms are k / 32
+    additions, each off by up to 2^-24 of what is reached, half of the sum on average: for k = 65536
+    2^10 2^-24 = 2^-14 of A, as much of B and of B X; times B's sizes (4.8 + 2 * 2.0), in five steps, one of
+    which takes them apart by 3.4: 2^-14 * 8.8 * 5 * 3.4 = 2^-6.8."""
+    def signs(count, mask):
+        i = torch.arange(count, device="cuda")
+        p = i & mask
+        for s in (8, 4, 2, 1):
+            p = p ^ (p >> s)
+        return 1.0 - 2.0 * (p & 1).float()
+
+    u = torch.stack([signs(m, k) for k in (0x2D31, 0x0000, 0x7B06)])
+    # orthogonal columns for the sizes that are no power of two as well: halves, quarters, eighths
+    i = torch.arange(n, device="cuda")
+    e = n // 8
+    v = torch.stack([1.0 - 2.0 * ((i // (e * k)) % 2).float() for k in (4, 2, 1)])
+    sizes = torch.tensor([4.0, 2.0, 1.0], device="cuda")
+    g = ((u * sizes[:, None]).t().contiguous() @ v).to(dtype)
+    ws = vt.OrthogonalWorkspace([g])
+    got, = vt.vtrace_orthogonalize([g], workspace=ws)
+    f = sizes.double().cpu().numpy() / math.sqrt(21.0)
+    for _ in range(5):
+        f = f * (3.4445 - 4.7750 * f ** 2 + 2.0315 * f ** 4)
+    f = torch.tensor(f, device="cuda").float()[:, None]
+    worst = size = 0.0
+    for at in range(0, m, 4096):
+        expect = (u[:, at:at + 4096] * f).t().contiguous() @ v / math.sqrt(m * n)
+        worst = max(worst, (got[at:at + 4096].float() - expect).abs().max().item())
+        size = max(size, expect.abs().max().item())
+    print(f"[case] {dtype} {m} x {n}: {worst / size:.2e}", flush=True)
+    assert worst <= 2.0 ** -6 * size
