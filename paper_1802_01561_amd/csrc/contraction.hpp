@@ -171,9 +171,9 @@ struct Loader {
 };
 
 // Where a lane reads its fragments of an operand: byte offsets in the operand's half
-// of a stage.  kTransposed: "across".  kPaired ("along"): tiles 2p and 2p + 1 together
-// give lane group g the rows 32p + 8g .. 32p + 8g + 7 in its accumulators, four of each
-// (so that eight consecutive results are one 16-byte store).
+// of a stage.  kTransposed: "across".  kPaired: tiles 2p and 2p + 1 together
+// give lane group g the rows ("across": the columns) 32p + 8g .. 32p + 8g + 7 in its accumulators,
+// four of each (so that eight consecutive results are one 16-byte store).
 template <bool kTransposed, bool kPaired, int kTiles, int kRows = kTile>
 struct Reader {
   int at[kTransposed ? kTiles : 2];
@@ -183,7 +183,8 @@ struct Reader {
       const int k = 8 * g + s / 4;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
-        at[t] = k * (kRows * 2) + (((first_row / 16 + t) ^ swizzle_of(k)) * 32) + (s % 4) * 8;
+        at[t] = k * (kRows * 2) + (kPaired ? (((first_row / 16 + (t & ~1) + (s % 4) / 2) ^ swizzle_of(k)) * 32) + (s % 2) * 16 + (t & 1) * 8
+                                           : (((first_row / 16 + t) ^ swizzle_of(k)) * 32) + (s % 4) * 8);
     } else {
       const int r = first_row + (kPaired ? 8 * (s / 4) + s % 4 : s);
 #pragma unroll
@@ -272,10 +273,11 @@ __device__ __forceinline__ float element(const f32x4& c, int i) {
 // (all of a step's within the first quarter, the first half: 11.2, 10.3 ms of the largest
 // gradient).  What is read and what is copied to do not overlap, and __restrict says so: the
 // compiler otherwise waits for every copy in flight before a read.
-template <bool kAAcross, bool kBAcross, int kSize, bool kHalfFloats = false>
+// kPaired: of an "across" A too, as of an "along" one.
+template <bool kAAcross, bool kBAcross, int kSize, bool kHalfFloats = false, bool kPaired = !kAAcross>
 struct Contraction {
   static constexpr int kMT = kSize / 32, kNT = kSize / 32, kOperandBytes = operand_bytes(kSize);
-  Reader<kAAcross, !kAAcross, kMT, kSize> ra;
+  Reader<kAAcross, kPaired, kMT, kSize> ra;
   Reader<kBAcross, false, kNT, kSize> rb;
   bf16x8 a0[kMT], b0[kNT], a1[kMT], b1[kNT];
 
@@ -378,12 +380,13 @@ struct Job {
 // The first step's copies are under way when this is called (to stage `parity`).  With the
 // last step's products go the copies of the next tile's first: next() makes `job` that
 // tile's, and what follows the contraction hides their latency.
-template <bool kAAcross, bool kBAcross = kAAcross, bool kHalfFloats = false, int kSize, typename LoaderT, typename Next>
+template <bool kAAcross, bool kBAcross = kAAcross, bool kHalfFloats = false, bool kPaired = !kAAcross, int kSize, typename LoaderT,
+          typename Next>
 __device__ __forceinline__ void contract(Job<kSize, LoaderT>& job, char* lds, int& parity, int wave, int lane,
                                          Accumulators<kSize>& acc, Next next) {
   constexpr int kStage = 2 * operand_bytes(kSize);
   const int steps = job.steps;
-  Contraction<kAAcross, kBAcross, kSize, kHalfFloats> c;
+  Contraction<kAAcross, kBAcross, kSize, kHalfFloats, kPaired> c;
   c.start(wave, lane);
   int it = 0;
   do {

@@ -211,6 +211,19 @@ __device__ __forceinline__ void store_result(Out* p, const float (&y)[4], int le
     else p[q] = to_bf16(y[q]);
   }
 }
+// Eight: `vectors` where they are whole ones of 16 bytes.
+template <typename Out>
+__device__ __forceinline__ void store_results(Out* p, const float (&y)[2][4], int left, bool vectors) {
+  if constexpr (sizeof(Out) == 2) {
+    if (vectors && left >= 8) {
+      *reinterpret_cast<v4u*>(p) = v4u{pack_bf16x2(y[0][0], y[0][1]), pack_bf16x2(y[0][2], y[0][3]), pack_bf16x2(y[1][0], y[1][1]),
+                                       pack_bf16x2(y[1][2], y[1][3])};
+      return;
+    }
+  }
+  store_result(p, y[0], left, vectors);
+  store_result(p + 4, y[1], left - 4, vectors);
+}
 
 }  // namespace
 

@@ -208,7 +208,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
 // 4 of 4096 x 4096 and 2 of 4096 x 16384 1617 us (1.02 PFLOP/s), 24 matrices of hidden size 1024 198
 // (0.52: X's 8 bytes an element beside 16 steps of products; further rows fetched ahead gain nothing).
 // X <- a X + B X, or of the last step the result: m runs along X's columns (X "across"), n along
-// its rows (B "along").  A lane holds columns j + 16 m + 4 g + 0..3 of row i + 16 n + s.
+// its rows (B "along").  A lane holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
 template <typename Out, bool kPair, bool kLast, int kSize>
 __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_update_kernel(Table t, int turn, Update f) {
   constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = 2;
@@ -259,32 +259,33 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
     Accumulators<kSize> acc = {};
     const Entry& e = t.at[here.entry];
     const Pieces p = pieces_of<kPair>(e, turn);
-    const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 4 * g;
+    const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2) + 8 * g;
     const float* const diagonal = diagonal_of(e, p, f.by);
     Out* const out = static_cast<Out*>(e.out);
-    const bool vectors = e.c % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(Out)) == 0;
+    const bool vectors = e.c % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
     // X's rows are fetched kAhead times 16 ahead, the first of them during the last step of k.
     constexpr int kAhead = 1, kBuffers = kAhead + 1;
     f32x4 x[kBuffers][kPair ? kMT : 1];
-    v2u part[kBuffers][2][kPair ? 1 : kMT];
+    v4u part[kBuffers][2][kPair ? 1 : kMT / 2];
     float of_row[kBuffers];
     auto load_rows = [&](int n) {
       const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1;
       of_row[n % kBuffers] = diagonal[i];
 #pragma unroll
-      for (int m = 0; m < kMT; ++m) {
+      for (int m = 0; m < kMT; m += 2) {
         const int j = j0 + 16 * m;
         const int64_t from = static_cast<int64_t>(i) * e.pc + (j < e.pc ? j : 0);
         if constexpr (kPair) {
           x[n % kBuffers][m] = *reinterpret_cast<const f32x4*>(p.x + from);
+          x[n % kBuffers][m + 1] = *reinterpret_cast<const f32x4*>(p.x + from + 4);
         } else {
-          part[n % kBuffers][0][m] = *reinterpret_cast<const v2u*>(p.from[0] + from);
-          part[n % kBuffers][1][m] = v2u{};
-          if (f.low_in) part[n % kBuffers][1][m] = *reinterpret_cast<const v2u*>(p.low + from);
+          part[n % kBuffers][0][m / 2] = *reinterpret_cast<const v4u*>(p.from[0] + from);
+          part[n % kBuffers][1][m / 2] = v4u{};
+          if (f.low_in) part[n % kBuffers][1][m / 2] = *reinterpret_cast<const v4u*>(p.low + from);
         }
       }
     };
-    contract<true, false, true>(job, lds, parity, wave, lane, acc, [&] {
+    contract<true, false, true, true>(job, lds, parity, wave, lane, acc, [&] {
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) load_rows(n);
       tiles.next();
@@ -297,43 +298,54 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
       const bool row = i < e.r;
       const float factor = f.of_x + of_row[n % kBuffers];
 #pragma unroll
-      for (int m = 0; m < kMT; ++m) {
+      for (int m = 0; m < kMT; m += 2) {
         const int j = j0 + 16 * m;
-        float y[4];
+        float y[2][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float before;
-          if constexpr (kPair) {
-            before = x[n % kBuffers][m][q];
-          } else {
-            before = whole_of(part[n % kBuffers][0][m], part[n % kBuffers][1][m], q) * (1.0f / kScaleX);
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float before;
+            if constexpr (kPair) {
+              before = x[n % kBuffers][m + h][q];
+            } else {
+              const v4u high = part[n % kBuffers][0][m / 2], left = part[n % kBuffers][1][m / 2];
+              before = whole_of(v2u{high[2 * h], high[2 * h + 1]}, v2u{left[2 * h], left[2 * h + 1]}, q) * (1.0f / kScaleX);
+            }
+            y[h][q] = fmaf(factor, before, element(acc[m + h][n], q) * (1.0f / (kScaleA * kScaleX)));
           }
-          y[q] = fmaf(factor, before, element(acc[m][n], q) * (1.0f / (kScaleA * kScaleX)));
         }
         if (!row || j >= e.pc) continue;
         if constexpr (kLast) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] *= e.scale;
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[h][q] *= e.scale;
           if (!e.transposed) {
-            store_result(out + static_cast<int64_t>(i) * e.c + j, y, e.c - j, vectors);
+            store_results(out + static_cast<int64_t>(i) * e.c + j, y, e.c - j, vectors);
           } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (j + q >= e.c) continue;
-              const int64_t back = static_cast<int64_t>(j + q) * e.r + i;
-              if constexpr (sizeof(Out) == 4) out[back] = y[q];
-              else out[back] = to_bf16(y[q]);
+            for (int k = 0; k < 8; ++k) {
+              if (j + k >= e.c) continue;
+              const int64_t back = static_cast<int64_t>(j + k) * e.r + i;
+              if constexpr (sizeof(Out) == 4) out[back] = y[k / 4][k % 4];
+              else out[back] = to_bf16(y[k / 4][k % 4]);
             }
           }
         } else {
           const int64_t to = static_cast<int64_t>(i) * e.pc + j;
-          if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + to) = f32x4{y[0], y[1], y[2], y[3]};
+          v2u high[2];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] *= kScaleX;
-          const v2u high = high4(y);
-          *reinterpret_cast<v2u*>(p.to[0] + to) = high;
-          if constexpr (kPair) *reinterpret_cast<v2u*>(p.to[1] + to) = low4(y, high);
-          else if (f.low_out) *reinterpret_cast<v2u*>(p.low + to) = left4(y, high);
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (kPair) *reinterpret_cast<f32x4*>(p.x + to + 4 * h) = f32x4{y[h][0], y[h][1], y[h][2], y[h][3]};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[h][q] *= kScaleX;
+            high[h] = high4(y[h]);
+          }
+          auto both = [](v2u u, v2u v) { return v4u{u[0], u[1], v[0], v[1]}; };
+          *reinterpret_cast<v4u*>(p.to[0] + to) = both(high[0], high[1]);
+          if constexpr (kPair) *reinterpret_cast<v4u*>(p.to[1] + to) = both(low4(y[0], high[0]), low4(y[1], high[1]));
+          else if (f.low_out) *reinterpret_cast<v4u*>(p.low + to) = both(left4(y[0], high[0]), left4(y[1], high[1]));
         }
       }
       __builtin_amdgcn_sched_barrier(0);
