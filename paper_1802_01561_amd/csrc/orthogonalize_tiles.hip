@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
     constexpr bool kLate = kOf == kOfTwo && kPair && kSize == kTile;
     constexpr int kMatrices = kOf == kOfTwo ? 2 : 1, kBuffers = kLate ? 1 : 2, kPieces = kLate ? 1 : kMT / 2;
     v4u o[kBuffers][kMatrices][kParts][kPieces];
-    float dj[kMT / 2][8];
+    float di[kNT] = {}, dj[kMT / 2][8];
     auto load_piece = [&](int n, int m) {
       const int i = i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1, j = j0 + 8 * g + 32 * m;
       const int64_t from = static_cast<int64_t>(i) * e.pr + (j < e.pr ? j : 0);
@@ -123,14 +123,14 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
           const int j = j0 + 8 * g + 32 * m + q;
           dj[m][q] = dn[j < e.r ? j : e.r - 1];
         }
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) di[n] = dm[i0 + 16 * n + s < e.r ? i0 + 16 * n + s : e.r - 1];
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
       const int i = i0 + 16 * n + s;
       const bool row = i < e.r;
-      float di = 0.0f;
       if constexpr (kOf != kOfX) {
-        di = dm[row ? i : e.r - 1];
         if (!kLate && n + 1 < kNT) load_row(n + 1);
       }
 #pragma unroll
@@ -155,8 +155,8 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
               if constexpr (kPair) off[w] += high_of(o[n % kBuffers][w][kParts - 1][m % kPieces][q / 2], q % 2);
               off[w] *= 1.0f / kScaleA;
             }
-            y[q] = product_off<kOf>(f, off[0], off[kMatrices - 1], di, dj[m][q], oo);
-            if (in && i == j + q) d_out[i] = product_diagonal<kOf>(f, di, dn[i], oo);
+            y[q] = product_off<kOf>(f, off[0], off[kMatrices - 1], di[n], dj[m][q], oo);
+            if (in && i == j + q) d_out[i] = product_diagonal<kOf>(f, di[n], dj[m][q], oo);
           }
           y[q] = in && i != j + q ? y[q] * kScaleA : 0.0f;
         }
