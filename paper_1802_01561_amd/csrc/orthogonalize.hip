@@ -422,25 +422,64 @@ int64_t tiles_in(const Entry& e, int kind, int size) {
 // has one tile; what a tile costs beside its steps is its stores, and X's are the most: 240 tiles
 // of 16 to 64 steps of A, 16 of B, 768 of 16 of X 117, 54, 191 us in tiles of 256, 103, 52, 228 in
 // tiles of 128.
-double tiles_cost(const Table& t, int kind, int size, int passes) {
-  double work = 0.0, tiles = 0.0, steps = 0.0, longest = 0.0;
-  for (int i = 0; i < t.count; ++i) {
-    const double n = static_cast<double>(tiles_in(t.at[i], kind, size));
-    const double k = (kind == 0 ? t.at[i].pc : t.at[i].pr) / kTileK * passes;
-    tiles += n;
-    work += n * k;
-    longest = std::max(longest, k);
+//
+// Tiles of equal steps that would leave a round behind theirs mostly empty are split along k, into up to
+// as many pieces as fill it, if that is a fifth less with what their sums cost (us, of tiles of 256: five
+// pieces of 13 steps take as long as one of 64, 20 to store and 12 a piece to join; six of 43 150 less
+// than one of 256).  A of 4 matrices of 4096 x 4096 and 2 of 4096 x 16384, which has 16 of 272 long tiles too
+// many: 1030 -> 780 us.  `split`: into so many wherever there are as many steps.
+double tiles_cost(const Table& t, int kind, int size, int passes, int split, Units* units) {
+  double all = 0.0;
+  for (int i = 0; i < t.count; ++i) all += static_cast<double>(tiles_in(t.at[i], kind, size));
+  const bool alone = size == kSmallTile && all <= kCus;
+  const int64_t slots = alone ? kCus : resident_tiles(size);
+  const double step = alone ? 0.8 : round_cost(size, 1) - round_cost(size, 0);
+  const double stores = size == kTile ? (kind == 2 ? 20.0 : 10.0) : kind == 2 ? 10.0 : 3.0;
+  const double beside = alone ? 3.0 + 0.6 * stores : round_cost(size, 0) + stores;
+  const double to_store = size == kTile ? 20.0 : 10.0, to_join = size == kTile ? 12.0 : 6.0;
+  *units = {};
+  int splits = 0;
+  int64_t at = 0, open = 0;  // tiles so far, and those of a round that is not full
+  double us = 0.0, open_us = 0.0;
+  for (int i = 0; i < t.count;) {
+    auto steps_of = [&](int k) { return (kind == 0 ? t.at[k].pc : t.at[k].pr) / kTileK; };
+    const int steps = steps_of(i);
+    int64_t n = 0;
+    for (; i < t.count && steps_of(i) == steps; ++i) n += tiles_in(t.at[i], kind, size);
+    at += n;
+    const double work = step * steps * passes;
+    const int64_t full = (open + n) / slots, left = (open + n) % slots, own = std::min(left, n);
+    if (full > 0) us += std::max(open_us, work + beside) + static_cast<double>(full - 1) * (work + beside);
+    const double before = full > 0 ? 0.0 : open_us;
+    open = left;
+    open_us = left > 0 ? std::max(before, work + beside) : 0.0;
+    if (own == 0 || splits == Units::kSplits || kind == 2 || (passes == 3 && size == kTile && kind == 1)) continue;  // kWhole
+    int64_t pieces = std::min<int64_t>((slots - left + own) / own, split ? std::min(split, steps) : steps / 4);
+    if (!split) pieces = std::min(pieces, std::max<int64_t>(1, std::lround(std::sqrt(work / to_join))));
+    const double then = work / static_cast<double>(pieces) + to_store + to_join * static_cast<double>(pieces);
+    if (pieces < 2 || (!split && then > 0.8 * work)) continue;
+    units->begin[splits] = static_cast<int>(at - own);
+    units->end[splits] = static_cast<int>(at);
+    units->pieces[splits++] = static_cast<int>(pieces);
+    open = left + own * (pieces - 1);
+    open_us = std::max(before, then + beside);
+    if (open == slots) {
+      us += open_us;
+      open = 0;
+      open_us = 0.0;
+    }
   }
-  steps = work / tiles;
-  const bool alone = size == kSmallTile && tiles <= kCus;
-  auto cost = [&](double k) {
-    const double stores = size == kTile ? (kind == 2 ? 20.0 : 10.0) : kind == 2 ? 10.0 : 3.0;
-    return alone ? 0.8 * k + 3.0 + 0.6 * stores : round_cost(size, 0) + (round_cost(size, 1) - round_cost(size, 0)) * k + stores;
-  };
-  return std::max(cost(longest), std::ceil(tiles / resident_tiles(size)) * cost(steps));
+  units->total = static_cast<int>(at);
+  for (int k = 0; k < Units::kSplits; ++k) {
+    if (k >= splits) units->begin[k] = units->end[k] = 0x7fffffff;
+    else units->total += (units->end[k] - units->begin[k]) * (units->pieces[k] - 1);
+  }
+  return us + open_us;
 }
-int tile_for(const Table& t, int kind, int passes) {
-  return tiles_cost(t, kind, kTile, passes) <= tiles_cost(t, kind, kSmallTile, passes) ? kTile : kSmallTile;
+int64_t sums_bytes(const Units& u, int size) {
+  int64_t slots = 0;
+  for (int k = 0; k < Units::kSplits; ++k) slots += static_cast<int64_t>(u.end[k] - u.begin[k]) * u.pieces[k];
+  return slots * size * size * static_cast<int64_t>(sizeof(float));
 }
 
 // The same in the small matrices' kernels' tiles of 64 or 32: a launch, and the tile that has a CU for
@@ -462,10 +501,11 @@ double small_cost(const Table& t, int kind, int size, bool pair) {
   return 2.0 + std::max(alone, rounds * ((size == 64 ? 6.0 : pair ? 3.5 : 3.0) + step * work / tiles));
 }
 
-// VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256, with x1 or x2 behind) forces the tiles
-// and whether steps are taken two at once, to cross-check them.
+// VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256, with x1 or x2 behind, and of the larger two k2 or k3
+// behind that) forces the tiles, whether steps are taken two at once, and the pieces of tiles that do not
+// fill a round, to cross-check them.
 struct Forced {
-  int size = 0, together = 0;
+  int size = 0, together = 0, split = 0;
 };
 Forced forced_kernel() {
   Forced f;
@@ -473,7 +513,10 @@ Forced forced_kernel() {
   if (k == nullptr) return f;
   for (const int size : {32, 64, kSmallTile, kTile})
     for (int together = 0; together <= 2; ++together)
-      if (k == "ortho_" + std::to_string(size) + (together ? "x" + std::to_string(together) : "")) f = {size, together};
+      for (int split = 0; split <= 3; ++split)
+        if (k == "ortho_" + std::to_string(size) + (together ? "x" + std::to_string(together) : "") +
+                     (split ? "k" + std::to_string(split) : ""))
+          f = {size, together, split};
   return f;
 }
 
@@ -504,8 +547,15 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     double tiles[3], small[3];
     int small_size[3];
     for (int kind = 0; kind < 3; ++kind) {
-      t.size[kind] = tile_for(t, kind, passes);
-      tiles[kind] = tiles_cost(t, kind, t.size[kind], passes);
+      Units units;
+      t.size[kind] = kTile;
+      tiles[kind] = tiles_cost(t, kind, kTile, passes, 0, &t.units[kind]);
+      const double of_small = tiles_cost(t, kind, kSmallTile, passes, 0, &units);
+      if (of_small < tiles[kind]) {
+        t.size[kind] = kSmallTile;
+        tiles[kind] = of_small;
+        t.units[kind] = units;
+      }
       small_size[kind] = small_cost(t, kind, 32, pair) <= small_cost(t, kind, 64, pair) ? 32 : 64;
       small[kind] = small_cost(t, kind, small_size[kind], pair);
     }
@@ -519,6 +569,9 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
   if (forced.size) {
     t.small = forced.size < kSmallTile;
     std::fill_n(t.size, 3, forced.size);
+    for (int kind = 0; kind < 3 && !t.small; ++kind) {
+      tiles_cost(t, kind, forced.size, pair ? 3 : 1, forced.split, &t.units[kind]);
+    }
   }
   if (forced.together) t.twos = forced.together == 2;
   int64_t at = round_up(kWsDataOffset, 256) + static_cast<int64_t>(kPartialBytes);
@@ -533,6 +586,11 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
       t.total_tiles[kind] += static_cast<int32_t>(tiles_in(e, kind, t.size[kind]));
     }
   }
+  t.counters = reinterpret_cast<unsigned*>(reinterpret_cast<uintptr_t>(ws) + kWsHeaderBytes);
+  t.sums = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
+  int64_t sums = 0;
+  for (int kind = 0; kind < 3 && count > 0 && !t.small; ++kind) sums = std::max(sums, sums_bytes(t.units[kind], t.size[kind]));
+  at += sums;
   // Every workgroup forms its Q, about 5 us: one tile each, then more (256 columns each, always: one float32
   // 32 x 4096 matrix 32 us, so 25; eight of 2 x 300 29 and 21).
   auto few_blocks = [&](int64_t block) {

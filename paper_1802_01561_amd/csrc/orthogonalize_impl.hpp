@@ -24,11 +24,47 @@ struct Entry {
   int32_t first_tile[3];
 };
 
+// What the tiles kernels' workgroups take one after the other: tiles, of which those from begin[s] to
+// end[s] are split along k into pieces[s] (X's are not: their kernel took 1.4 to 2.8 times as long, with
+// no tile split).
+struct Units {
+  static constexpr int kSplits = 2;
+  int total;
+  int begin[kSplits], end[kSplits], pieces[kSplits];
+};
+// Of float32 matrices' A and B in tiles of 256 none is: a tile of two matrices in two parts has no
+// registers left for the sums of other pieces.
+template <bool kPair, int kSize, int kKind>
+constexpr bool kWhole = kPair && kSize == kTile && kKind == 1;
+struct Unit {
+  int tile, piece, pieces;
+  int slot;     // of the piece's sums
+  int counter;  // of the tile's pieces that are there
+};
+__host__ __device__ inline Unit unit_at(const Units& u, int id) {
+  int tile = id, slot = 0, counter = 0;
+  for (int s = 0; s < Units::kSplits; ++s) {
+    if (tile < u.begin[s]) break;
+    const int n = u.end[s] - u.begin[s], inside = tile - u.begin[s];
+    if (inside < n * u.pieces[s]) {
+      const int of = inside / u.pieces[s];
+      return {u.begin[s] + of, inside - of * u.pieces[s], u.pieces[s], slot + inside, counter + of};
+    }
+    tile -= n * (u.pieces[s] - 1);
+    slot += n * u.pieces[s];
+    counter += n;
+  }
+  return {tile, 0, 1, 0, 0};
+}
+
 // As many as 4 KB of arguments hold.
 struct Table {
-  static constexpr int kMost = 40;
+  static constexpr int kMost = 38;
   Entry at[kMost];
   double* partials;
+  char* sums;          // of the tiles' pieces
+  unsigned* counters;  // zero between launches
+  Units units[3];      // of X: its tiles
   int count;           // matrices of the tiles' kernels
   int few;             // behind them, those of few rows
   int few_chunks, few_block, few_blocks;

@@ -12,7 +12,64 @@ using OrthoLoader = std::conditional_t<kPair, PartsLoader<kSize>, Loader<kSize>>
 struct Place {
   int entry;
   int i, j;
+  Unit unit;
 };
+
+// A tile whose k is split: the workgroup that is the last of its pieces has the sum of all, in their
+// order, and true; the others leave their sums and have nothing more to do.  Sums go past the L2s by
+// device-scope stores, which have completed before the tile's counter moves.
+constexpr int kJoined = 16;  // sums of four in flight: registers hold no more
+template <int kSize>
+__device__ __forceinline__ bool join_pieces(const Table& t, const Unit& u, int* flag, Accumulators<kSize>& acc) {
+  constexpr int kMT = kSize / 32, kNT = kSize / 32, kAll = kMT * kNT, kBatch = kAll < kJoined ? kAll : kJoined;
+  constexpr int64_t kSums = static_cast<int64_t>(kSize) * kSize * 4;
+  auto place = [&](int slot, int k) {
+    return reinterpret_cast<unsigned long long*>(t.sums + slot * kSums + (static_cast<int64_t>(k) * kGemmThreads + threadIdx.x) * 16);
+  };
+#pragma unroll
+  for (int k = 0; k < kAll; ++k) {
+    unsigned long long* const to = place(u.slot, k);
+    const f32x4& c = acc[k / kNT][k % kNT];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t lo = __float_as_uint(element(c, 2 * h)), hi = __float_as_uint(element(c, 2 * h + 1));
+      __hip_atomic_store(to + h, lo | hi << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);  // keep the compiler from moving the stores past the wait
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // the stores have completed
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned* const counter = t.counters + u.counter;
+    const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(u.pieces) - 1;
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  const bool last = __builtin_amdgcn_readfirstlane(*flag) != 0;
+  __syncthreads();
+  if (!last) return false;
+  const int first = u.slot - u.piece;
+#pragma unroll
+  for (int k0 = 0; k0 < kAll; k0 += kBatch) {
+#pragma unroll
+    for (int k = k0; k < k0 + kBatch; ++k) acc[k / kNT][k % kNT] = f32x4{};
+    for (int p = 0; p < u.pieces; ++p) {
+      unsigned long long x[kBatch][2];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[k][h] = __hip_atomic_load(place(first + p, k0 + k) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[(k0 + k) / kNT][(k0 + k) % kNT][q] += __uint_as_float(static_cast<uint32_t>(x[k][q / 2] >> (32 * (q % 2))));
+    }
+  }
+  return true;
+}
 
 // A wave's 32 rows of half a tile's columns, to be read turned: 32-byte pieces exchanged within a row
 // as in the stages, so that both kinds of access fall on all banks.
@@ -32,12 +89,13 @@ __device__ __forceinline__ s16x4 transposed_read(const char* lds) {
 //
 // A symmetric matrix: the tiles (i, j), j <= i, of M N, rows of both "along".  A lane of the MFMA
 // layout holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
-template <int kOf, bool kPair, int kSize>
+// kSplit: some tiles are split along k (which costs the others 4%).
+template <int kOf, bool kPair, int kSize, bool kSplit>
 __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_symmetric_kernel(Table t, int turn, Product f) {
   constexpr int kMT = kSize / 32, kNT = kSize / 32, kKind = kOf == kOfX ? 0 : 1, kParts = kPair ? 2 : 1;
   constexpr int kTurnedBytes = 32 * kSize;  // of a wave: 32 rows of kSize / 2 columns, or 16 of both parts
   __shared__ __align__(1024) char lds[tile_lds(kSize) + 4 * kTurnedBytes];
-  Tiles tiles(t.total_tiles[kKind]);
+  Tiles tiles(t.units[kKind].total);
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, g = lane / 16;
@@ -47,19 +105,21 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
   auto start = [&] {
     job.steps = 0;
     if (!tiles.any()) return;
-    at.entry = entry_of(t, tiles.at, [](const Entry& e) { return e.first_tile[kKind]; });
+    at.unit = kSplit ? unit_at(t.units[kKind], tiles.at) : Unit{tiles.at, 0, 1, 0, 0};
+    at.entry = entry_of(t, at.unit.tile, [](const Entry& e) { return e.first_tile[kKind]; });
     const Entry& e = t.at[at.entry];
-    const TileAt tile = triangle_at(tiles.at - e.first_tile[kKind]);
+    const TileAt tile = triangle_at(at.unit.tile - e.first_tile[kKind]);
     at.i = tile.wide;
     at.j = tile.deep;
     const Pieces p = pieces_of<kPair>(e, turn);
     const int64_t pitch = kOf == kOfX ? e.pc : e.pr;
-    auto operand = [&](int matrix, int k) { return kOf == kOfX ? p.from[k] : symmetric_of<kPair>(e, p, matrix, k); };
+    const int all = static_cast<int>(pitch / kTileK);
+    const int begin = all * at.unit.piece / at.unit.pieces, once = all * (at.unit.piece + 1) / at.unit.pieces - begin;
+    auto operand = [&](int matrix, int k) { return (kOf == kOfX ? p.from[k] : symmetric_of<kPair>(e, p, matrix, k)) + begin * kTileK; };
     const int64_t ia = static_cast<int64_t>(at.j) * kSize, ib = static_cast<int64_t>(at.i) * kSize;
-    const int64_t left_a = (e.r - ia) * pitch * 2, left_b = (e.r - ib) * pitch * 2;
+    const int64_t left_a = ((e.r - ia) * pitch - begin * kTileK) * 2, left_b = ((e.r - ib) * pitch - begin * kTileK) * 2;
     const uint16_t* const a = operand(f.n, 0) + ia * pitch;
     const uint16_t* const b = operand(f.m, 0) + ib * pitch;
-    const int once = static_cast<int>(pitch / kTileK);
     job.a.along(pitch, kSize, wave, lane);
     job.b.along(pitch, kSize, wave, lane);
     if constexpr (kPair) {
@@ -84,6 +144,9 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
       tiles.next();
       start();
     });
+    if constexpr (kSplit) {
+      if (here.unit.pieces > 1 && !join_pieces<kSize>(t, here.unit, reinterpret_cast<int*>(lds + tile_lds(kSize)), acc)) continue;
+    }
     const Entry& e = t.at[here.entry];
     const Pieces p = pieces_of<kPair>(e, turn);
     const int i0 = here.i * kSize + (wave / 2) * (kSize / 2), j0 = here.j * kSize + (wave % 2) * (kSize / 2);
@@ -357,9 +420,18 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
 template <int kOf, bool kPair>
 hipError_t launch_symmetric(const Table& t, int turn, const Product& p, hipStream_t st) {
   const int kind = kOf == kOfX ? 0 : 1;
-  const dim3 grid(workgroups_of(t.total_tiles[kind], t.size[kind])), block(kGemmThreads);
-  if (t.size[kind] == kTile) hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kTile>), grid, block, 0, st, t, turn, p);
-  else hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kSmallTile>), grid, block, 0, st, t, turn, p);
+  const Units& u = t.units[kind];
+  const dim3 grid(workgroups_of(u.total, t.size[kind])), block(kGemmThreads);
+  const bool split = u.total != t.total_tiles[kind];
+  if constexpr (!kWhole<kPair, kTile, kOf == kOfX ? 0 : 1>) {
+    if (t.size[kind] == kTile && split) {
+      hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kTile, true>), grid, block, 0, st, t, turn, p);
+      return hipGetLastError();
+    }
+  }
+  if (t.size[kind] == kTile) hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kTile, false>), grid, block, 0, st, t, turn, p);
+  else if (split) hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kSmallTile, true>), grid, block, 0, st, t, turn, p);
+  else hipLaunchKernelGGL((ortho_symmetric_kernel<kOf, kPair, kSmallTile, false>), grid, block, 0, st, t, turn, p);
   return hipGetLastError();
 }
 

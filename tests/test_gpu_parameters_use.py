@@ -424,3 +424,30 @@ def test_largest_matrices(dtype, m, n):
         size = max(size, expect.abs().max().item())
     print(f"[case] {dtype} {m} x {n}: {worst / size:.2e}", flush=True)
     assert worst <= 2.0 ** -6 * size
+
+
+@pytest.mark.parametrize("kernel", [f"ortho_{size}x{together}k{pieces}" for size in (128, 256) for together in (1, 2) for pieces in (2, 3)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_tiles_split_along_k(kernel, dtype, monkeypatch):
+    """Pieces of even and uneven lengths, several matrices' tiles, twice in one workspace, in a graph."""
+    monkeypatch.setenv("VTRACE_KERNEL", kernel)
+    shapes = [(130, 700), (640, 640), (257, 255), (70, 64), (300, 1000), (1000, 300)]
+    gs = [matrix(i, m, n, dtype, "strong") for i, (m, n) in enumerate(shapes)]
+    on = [g.cuda() for g in gs]
+    ws = vt.OrthogonalWorkspace(on)
+    ws.tensor[4352:].fill_(0xFF)
+    got = vt.vtrace_orthogonalize(on, workspace=ws)
+    for g, o in zip(gs, got):
+        check(g, o)
+    out = [torch.empty_like(g) for g in on]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vt.vtrace_orthogonalize(on, out=out, workspace=ws)
+    for _ in range(3):
+        for o in out:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        _same(out, got)
+        _same(vt.vtrace_orthogonalize(on, workspace=ws), got)
+    assert int(ws.tensor[:4352].count_nonzero()) == 0  # flag and counters
