@@ -417,11 +417,13 @@ int64_t tiles_in(const Entry& e, int kind, int size) {
   return kind == 2 ? rows * tiles_of(e.pc, size) : rows * (rows + 1) / 2;
 }
 
-// What a launch of one kind takes (us) in tiles of 256 or 128: the longer of all rounds of them and
-// the longest tile.  A step of 64 k as for the vocabulary layer (round_cost), or of 128 where a CU
-// has one tile; what a tile costs beside its steps is its stores, and X's are the most: 240 tiles
-// of 16 to 64 steps of A, 16 of B, 768 of 16 of X 117, 54, 191 us in tiles of 256, 103, 52, 228 in
-// tiles of 128.
+// What a launch of one kind takes (us) in tiles of 256 or 128: rounds of as many as there is room for.
+// Fewer than that take less a step: 72 tiles of 256 1.0 (float32 1.15), 256 of them 1.56; of 128 one a
+// CU 0.8, two 1.0.  What a tile costs beside its steps is its fill and its stores.  bfloat16, x1 / x2
+// (steps one by one, two at once) in tiles of 64, 128, 256, us: 16 of 1024 x 1024 999 / -, 666 / 794,
+// 647 / 749; 2 of 2048 x 2048 774 / -, 542 / 617, 848 / 995; 2 of 3000 x 3000 2675 / -, 1613 / 1780, 1499 /
+// 1540; 8 of 1024 x 4096 1751 / -, 887 / 756, 1123 / 1041; float32 2 of 2048 x 2048 2058 / -, 1453 / 1659,
+// 2059 / 2530.
 //
 // Tiles of equal steps that would leave a round behind theirs mostly empty are split along k, into up to
 // as many pieces as fill it, if that is a fifth less with what their sums cost (us, of tiles of 256: five
@@ -433,9 +435,15 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
   for (int i = 0; i < t.count; ++i) all += static_cast<double>(tiles_in(t.at[i], kind, size));
   const bool alone = size == kSmallTile && all <= kCus;
   const int64_t slots = alone ? kCus : resident_tiles(size);
-  const double step = alone ? 0.8 : round_cost(size, 1) - round_cost(size, 0);
-  const double stores = size == kTile ? (kind == 2 ? 20.0 : 10.0) : kind == 2 ? 10.0 : 3.0;
-  const double beside = alone ? 3.0 + 0.6 * stores : round_cost(size, 0) + stores;
+  // Of a round with so many tiles.
+  auto step = [&](int64_t there) {
+    if (size == kTile) return there > 160 ? 1.56 : passes == 1 ? 1.0 : 1.15;
+    return there > kCus ? 1.0 : 0.8;
+  };
+  auto beside = [&](int64_t there) {
+    if (size == kTile) return kind == 2 ? 28.0 : 21.0;
+    return there > kCus ? (kind == 2 ? 14.0 : 8.0) : kind == 2 ? 9.0 : 5.0;
+  };
   const double to_store = size == kTile ? 20.0 : 10.0, to_join = size == kTile ? 12.0 : 6.0;
   *units = {};
   int splits = 0;
@@ -447,22 +455,26 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
     int64_t n = 0;
     for (; i < t.count && steps_of(i) == steps; ++i) n += tiles_in(t.at[i], kind, size);
     at += n;
-    const double work = step * steps * passes;
+    const double k = static_cast<double>(steps) * passes;
+    auto cost = [&](int64_t there) { return step(there) * k + beside(there); };
     const int64_t full = (open + n) / slots, left = (open + n) % slots, own = std::min(left, n);
-    if (full > 0) us += std::max(open_us, work + beside) + static_cast<double>(full - 1) * (work + beside);
+    if (full > 0) us += std::max(open_us, cost(slots)) + static_cast<double>(full - 1) * cost(slots);
     const double before = full > 0 ? 0.0 : open_us;
     open = left;
-    open_us = left > 0 ? std::max(before, work + beside) : 0.0;
+    open_us = left > 0 ? std::max(before, cost(left)) : 0.0;
     if (own == 0 || splits == Units::kSplits || kind == 2 || (passes == 3 && size == kTile && kind == 1)) continue;  // kWhole
+    const double work = step(left) * k;
     int64_t pieces = std::min<int64_t>((slots - left + own) / own, split ? std::min(split, steps) : steps / 4);
     if (!split) pieces = std::min(pieces, std::max<int64_t>(1, std::lround(std::sqrt(work / to_join))));
-    const double then = work / static_cast<double>(pieces) + to_store + to_join * static_cast<double>(pieces);
-    if (pieces < 2 || (!split && then > 0.8 * work)) continue;
+    if (pieces < 2) continue;
+    const int64_t there = left + own * (pieces - 1);
+    const double then = step(there) * k / static_cast<double>(pieces) + to_store + to_join * static_cast<double>(pieces);
+    if (!split && then > 0.8 * work) continue;
     units->begin[splits] = static_cast<int>(at - own);
     units->end[splits] = static_cast<int>(at);
     units->pieces[splits++] = static_cast<int>(pieces);
-    open = left + own * (pieces - 1);
-    open_us = std::max(before, then + beside);
+    open = there;
+    open_us = std::max(before, then + beside(there));
     if (open == slots) {
       us += open_us;
       open = 0;
@@ -494,11 +506,12 @@ double small_cost(const Table& t, int kind, int size, bool pair) {
     work += n * steps;
     longest = std::max(longest, steps);
   }
+  // Two workgroups of a CU share its path into LDS.
   const double step = size == 64 ? (pair ? 0.5 : 0.26) : pair ? 0.25 : 0.13;
+  const double beside = size == 64 ? (pair ? 6.0 : 2.5) : pair ? 0.5 : 0.8;
   const double alone = 2.5 + step * longest;
   if (tiles <= kCus) return 2.0 + alone;
-  const double rounds = std::ceil(tiles / (kCus * (size == 64 && pair ? 1 : 2)));
-  return 2.0 + std::max(alone, rounds * ((size == 64 ? 6.0 : pair ? 3.5 : 3.0) + step * work / tiles));
+  return 2.0 + std::max(alone, std::ceil(tiles / kCus) * (beside + step * work / tiles));
 }
 
 // VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256, with x1 or x2 behind, and of the larger two k2 or k3
