@@ -435,19 +435,21 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
   for (int i = 0; i < t.count; ++i) all += static_cast<double>(tiles_in(t.at[i], kind, size));
   const bool alone = size == kSmallTile && all <= kCus;
   const int64_t slots = alone ? kCus : resident_tiles(size);
-  // Of a round with so many tiles.
+  int64_t at = 0, open = 0;  // tiles so far, and those of a round that is not full
+  // Of a round with so many tiles, and those that come behind.
   auto step = [&](int64_t there) {
+    there += static_cast<int64_t>(all) - at;
     if (size == kTile) return there > 160 ? 1.56 : passes == 1 ? 1.0 : 1.15;
     return there > kCus ? 1.0 : 0.8;
   };
   auto beside = [&](int64_t there) {
+    there += static_cast<int64_t>(all) - at;
     if (size == kTile) return kind == 2 ? 28.0 : 21.0;
     return there > kCus ? (kind == 2 ? 14.0 : 8.0) : kind == 2 ? 9.0 : 5.0;
   };
   const double to_store = size == kTile ? 20.0 : 10.0, to_join = size == kTile ? 12.0 : 6.0;
   *units = {};
   int splits = 0;
-  int64_t at = 0, open = 0;  // tiles so far, and those of a round that is not full
   double us = 0.0, open_us = 0.0;
   for (int i = 0; i < t.count;) {
     auto steps_of = [&](int k) { return (kind == 0 ? t.at[k].pc : t.at[k].pr) / kTileK; };
