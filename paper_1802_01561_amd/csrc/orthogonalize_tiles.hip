@@ -83,9 +83,9 @@ __device__ __forceinline__ s16x4 transposed_read(const char* lds) {
 }
 
 // Float16 products on the matrix cores bound these kernels where k is long: A of 4 matrices of 4096 x 4096
-// and 2 of 4096 x 16384 takes 1030 us (0.80 PFLOP/s of the halves that are asked for, whose diagonal
-// tiles are computed whole), A A 470 (0.87), A of 24 matrices of hidden size 1024 106 (0.49: one round,
-// each tile with 16 to 64 steps and 10 us of stores).
+// and 2 of 4096 x 16384 takes 780 us (1.06 PFLOP/s of the halves that are asked for, whose diagonal
+// tiles are computed whole), A A 470 (0.88), A A of 24 matrices of hidden size 1024 47 (0.55: one round
+// of 16 steps, 25 us, beside a tile's fill and stores, 21).
 //
 // A symmetric matrix: the tiles (i, j), j <= i, of M N, rows of both "along".  A lane of the MFMA
 // layout holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
@@ -268,8 +268,9 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-// 4 of 4096 x 4096 and 2 of 4096 x 16384 1617 us (1.02 PFLOP/s), 24 matrices of hidden size 1024 198
-// (0.52: X's 8 bytes an element beside 16 steps of products; further rows fetched ahead gain nothing).
+// 4 of 4096 x 4096 and 2 of 4096 x 16384 1485 us (1.11 PFLOP/s), 24 matrices of hidden size 1024 160
+// (0.64: X's 8 bytes an element beside 16 steps of products; four columns a lane, 8-byte loads and stores, took
+// 1630 and 193; rows fetched further ahead, and workgroups that start at different times, gain nothing).
 // X <- a X + B X, or of the last step the result: m runs along X's columns (X "across"), n along
 // its rows (B "along").  A lane holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
 template <typename Out, bool kPair, bool kLast, int kSize>
