@@ -451,3 +451,33 @@ def test_tiles_split_along_k(kernel, dtype, monkeypatch):
         _same(out, got)
         _same(vt.vtrace_orthogonalize(on, workspace=ws), got)
     assert int(ws.tensor[:4352].count_nonzero()) == 0  # flag and counters
+
+
+def test_empty_matrices_and_very_many():
+    """Nothing to do, nothing among something, and more than one launch's table many times over."""
+    empty = [torch.empty((0, 5), device="cuda"), torch.empty((7, 0), dtype=BF16, device="cuda")]
+    for got, g in zip(vt.vtrace_orthogonalize(empty), empty):
+        assert got.shape == g.shape and got.dtype == g.dtype
+    gs = [matrix(i, 1 + i % 9, 1 + i % 7, F32 if i % 3 else BF16) for i in range(2000)]
+    gs[500], gs[777] = matrix(1, 100, 130, F32), matrix(2, 100, 130, BF16)
+    on = [g.cuda() for g in gs]
+    on.insert(3, empty[0])
+    gs.insert(3, empty[0].cpu())
+    got = vt.vtrace_orthogonalize(on)
+    assert got[3].numel() == 0
+    for i in (0, 1, 2, 4, 8, 38, 39, 501, 778, 1999, 2000):
+        check(gs[i], got[i])
+    again = vt.vtrace_orthogonalize(on, out=on)
+    _same(again, got)
+
+
+def test_same_matrix_twice_and_refused_overlaps():
+    g = matrix(9, 40, 60, F32).cuda()
+    a, b = vt.vtrace_orthogonalize([g, g])
+    assert torch.equal(a, b) and torch.equal(a, vt.vtrace_orthogonalize([g])[0])
+    both = torch.empty(2 * g.numel(), device="cuda")
+    overlapping = [both[:g.numel()].view(g.shape), both[g.numel() - 1:-1].view(g.shape)]
+    for outs in ([g, torch.empty_like(g)], [a, a], overlapping):
+        with pytest.raises(vt.VtraceError, match="PARAM"):
+            vt.vtrace_orthogonalize([g, g], out=outs)
+    assert torch.equal(g, matrix(9, 40, 60, F32).cuda())
