@@ -257,19 +257,20 @@ __device__ void few_apply(const Table& t, const FewSteps& steps, int id) {
   }
 }
 
-// kFew: and A of the matrices of few rows, in further workgroups.
+// kFew: and A of the matrices of few rows, by the first workgroups.
 template <typename In, bool kFew>
 __global__ __launch_bounds__(kNormThreads) void ortho_norm_kernel(Table t) {
   constexpr int kPer = 16 / sizeof(In);
+  const int id = kFew ? static_cast<int>(blockIdx.x) - t.few_chunks : blockIdx.x;
   if constexpr (kFew) {
-    if (static_cast<int>(blockIdx.x) >= t.total_partials) {
-      few_gram<In>(t, blockIdx.x - t.total_partials);
+    if (id < 0) {
+      few_gram<In>(t, blockIdx.x);
       return;
     }
   }
-  const Entry& g = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_partial; })];
+  const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_partial; })];
   const int64_t elements = static_cast<int64_t>(g.r) * g.c, chunk = norm_chunk(elements);
-  const int64_t from = (blockIdx.x - g.first_partial) * chunk, to = from + chunk < elements ? from + chunk : elements;
+  const int64_t from = (id - g.first_partial) * chunk, to = from + chunk < elements ? from + chunk : elements;
   const In* const in = static_cast<const In*>(g.in);
   double sum[2] = {0.0, 0.0};
   auto add = [&](int k, float x) {
@@ -296,22 +297,23 @@ __global__ __launch_bounds__(kNormThreads) void ortho_norm_kernel(Table t) {
   }
   for (int64_t i = from + vectors * kPer + threadIdx.x; i < to; i += kNormThreads) add(0, logit_to_float(in[i]));
   const double all = block_sum(sum[0] + sum[1]);
-  if (threadIdx.x == 0) t.partials[blockIdx.x] = all;
+  if (threadIdx.x == 0) t.partials[id] = all;
 }
 
 constexpr int kScaleTile = 64;
-// kFew: and the results of the matrices of few rows.
+// kFew: and the results of the matrices of few rows, by the first workgroups: theirs is the longest way.
 template <typename In, bool kPair, bool kFew>
 __global__ __launch_bounds__(kNormThreads) void ortho_scale_kernel(Table t, FewSteps steps) {
   __shared__ float s_tile[kScaleTile][kScaleTile + 1];
+  const int id = kFew ? static_cast<int>(blockIdx.x) - t.few_blocks : blockIdx.x;
   if constexpr (kFew) {
-    if (static_cast<int>(blockIdx.x) >= t.total_blocks) {
-      few_apply<In>(t, steps, blockIdx.x - t.total_blocks);
+    if (id < 0) {
+      few_apply<In>(t, steps, blockIdx.x);
       return;
     }
   }
-  const Entry& g = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_block; })];
-  const int wide = g.pc / kScaleTile, block = blockIdx.x - g.first_block;
+  const Entry& g = t.at[entry_of(t, id, [](const Entry& e) { return e.first_block; })];
+  const int wide = g.pc / kScaleTile, block = id - g.first_block;
   const int i0 = block / wide * kScaleTile, j0 = block % wide * kScaleTile;
   const In* const in = static_cast<const In*>(g.in);
   constexpr int kPerPass = kNormThreads / kScaleTile, kPasses = kScaleTile / kPerPass;
