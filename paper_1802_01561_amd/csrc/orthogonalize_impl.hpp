@@ -67,6 +67,7 @@ struct Table {
   Units units[3];      // of X: its tiles
   int count;           // matrices of the tiles' kernels
   int few;             // behind them, those of few rows
+  bool few_later;      // their results with the others' first A
   int few_chunks, few_block, few_blocks;
   int total_partials, total_blocks, total_tiles[3];
   int size[3];  // of the tiles of A, B and X
@@ -74,7 +75,6 @@ struct Table {
   bool twos;   // two steps at once
   bool small;  // the small matrices' kernels, which keep X^T as well
 };
-static_assert(sizeof(Table) <= 4096 - 64 * sizeof(OrthoStep) - 16, "kernel arguments");
 
 // A symmetric matrix C = of_m M + of_n N + of_mn M N from those numbered m and n, which commute; or
 // (A) from X.
@@ -82,6 +82,12 @@ struct Product {
   int out, m, n;
   float of_m, of_n, of_mn;
 };
+// The steps of the matrices of few rows.
+struct FewSteps {
+  OrthoStep at[kOrthoMostSteps];
+  int count;
+};
+static_assert(sizeof(Table) + sizeof(Product) + sizeof(FewSteps) + 16 <= 4096, "kernel arguments");
 // What a product is of: X and X^T, one matrix, or two.
 enum { kOfX = 0, kOfOne = 1, kOfTwo = 2 };
 
@@ -273,7 +279,8 @@ struct Update {
 };
 hipError_t launch_ortho_tiles_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t s);
 hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t s);
-hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t s);
+// `few`: of A from X, with the results of the matrices of few rows.
+hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, const FewSteps* few, hipStream_t s);
 hipError_t launch_ortho_small_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t s);
 
 }  // namespace vtrace

@@ -8,6 +8,7 @@
 // takes X^T, kept beside X.  A launch takes 5 to 8 us for a 256 x 1024 float32 matrix (32 x 32, 4 to 16
 // steps of k in three products each), 10 to 13 for 1000 x 1000 bfloat16 (64 x 64, 16 steps), 2 to
 // 3 of them before the first step: what bounds a step is the path into one CU's LDS, 65 KB a us.
+#include "orthogonalize_few.hpp"
 #include "orthogonalize_impl.hpp"
 
 namespace vtrace {
@@ -28,18 +29,28 @@ __host__ __device__ constexpr int small_stages(int side, int parts) { return sid
 // quarter of the tile; a lane of the MFMA layout holds columns j + 16 m + 4 g + 0..3 of row
 // i + 16 n + s of that.
 constexpr int kUpdate = 3;
-template <int kOf, typename Out, bool kLast, int kSide>
-__global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int turn, std::conditional_t<kOf == kUpdate, Update, Product> f) {
+// kFew: and the results of the matrices of few rows, by the first workgroups.
+template <int kOf, typename Out, bool kLast, int kSide, bool kFew>
+__global__ __launch_bounds__(kSmallThreads) void ortho_small_kernel(Table t, int turn, std::conditional_t<kOf == kUpdate, Update, Product> f,
+                                                                    std::conditional_t<kFew, FewSteps, int> few) {
   constexpr bool kPair = sizeof(Out) == 4;
   constexpr int kKind = kOf == kOfX ? 0 : kOf == kUpdate ? 2 : 1;
   constexpr int kParts = kPair ? 2 : 1, kN = kSide / 32;
   constexpr int kStages = small_stages(kSide, kParts), kBytes = kSide * kTileK * 2, kStage = 2 * kParts * kBytes;
   __shared__ __align__(1024) char lds[kStages * kStage];
+  const int workgroup = kFew ? static_cast<int>(blockIdx.x) - t.few_blocks : blockIdx.x;
+  if constexpr (kFew) {
+    static_assert(kFewLds <= kStages * kStage && kFewThreads == kSmallThreads);
+    if (workgroup < 0) {
+      few_apply<Out>(t, few, blockIdx.x, lds);
+      return;
+    }
+  }
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, g = lane / 16;
-  const Entry& e = t.at[entry_of(t, blockIdx.x, [](const Entry& e) { return e.first_tile[kKind]; })];
-  const int id = blockIdx.x - e.first_tile[kKind];
+  const Entry& e = t.at[entry_of(t, workgroup, [](const Entry& e) { return e.first_tile[kKind]; })];
+  const int id = workgroup - e.first_tile[kKind];
   TileAt at;
   if constexpr (kKind < 2) {
     at = triangle_at(id);
@@ -302,21 +313,27 @@ template <int kOf, typename Out, bool kLast, typename F>
 hipError_t launch_kind(const Table& t, int turn, const F& f, hipStream_t st) {
   constexpr int kKind = kOf == kOfX ? 0 : kOf == kUpdate ? 2 : 1;
   const dim3 grid(t.total_tiles[kKind]), block(kSmallThreads);
-  if (t.size[kKind] == 32) hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 32>), grid, block, 0, st, t, turn, f);
-  else hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 64>), grid, block, 0, st, t, turn, f);
+  if (t.size[kKind] == 32) hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 32, false>), grid, block, 0, st, t, turn, f, 0);
+  else hipLaunchKernelGGL((ortho_small_kernel<kOf, Out, kLast, 64, false>), grid, block, 0, st, t, turn, f, 0);
   return hipGetLastError();
 }
 
 template <typename Out>
-hipError_t launch_symmetric(const Table& t, int of, int turn, const Product& p, hipStream_t st) {
+hipError_t launch_symmetric(const Table& t, int of, int turn, const Product& p, const FewSteps* few, hipStream_t st) {
+  if (of == kOfX && few != nullptr) {
+    const dim3 grid(t.total_tiles[0] + t.few_blocks), block(kSmallThreads);
+    if (t.size[0] == 32) hipLaunchKernelGGL((ortho_small_kernel<kOfX, Out, false, 32, true>), grid, block, 0, st, t, turn, p, *few);
+    else hipLaunchKernelGGL((ortho_small_kernel<kOfX, Out, false, 64, true>), grid, block, 0, st, t, turn, p, *few);
+    return hipGetLastError();
+  }
   if (of == kOfX) return launch_kind<kOfX, Out, false>(t, turn, p, st);
   return of == kOfOne ? launch_kind<kOfOne, Out, false>(t, turn, p, st) : launch_kind<kOfTwo, Out, false>(t, turn, p, st);
 }
 
 }  // namespace
 
-hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t st) {
-  return pair ? launch_symmetric<float>(t, of, turn, p, st) : launch_symmetric<uint16_t>(t, of, turn, p, st);
+hipError_t launch_ortho_small_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, const FewSteps* few, hipStream_t st) {
+  return pair ? launch_symmetric<float>(t, of, turn, p, few, st) : launch_symmetric<uint16_t>(t, of, turn, p, few, st);
 }
 
 hipError_t launch_ortho_small_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t st) {

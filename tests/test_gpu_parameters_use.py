@@ -481,3 +481,20 @@ def test_same_matrix_twice_and_refused_overlaps():
         with pytest.raises(vt.VtraceError, match="PARAM"):
             vt.vtrace_orthogonalize([g, g], out=outs)
     assert torch.equal(g, matrix(9, 40, 60, F32).cuda())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("long", [False, True])
+def test_few_rows_beside_others(dtype, long):
+    """With the others' X, or their first A: whichever launch has them, what they get alone, in place too."""
+    few = [matrix(i, m, n, dtype, "strong") for i, (m, n) in enumerate([(1, 3), (32, 500), (700, 20), (32, 32), (9, 65)])]
+    gs = [few[0], matrix(7, 90, 2500 if long else 100, dtype), *few[1:3], matrix(8, 70, 66, dtype), *few[3:]]
+    on = [g.cuda() for g in gs]
+    ws = vt.OrthogonalWorkspace(on)
+    ws.tensor[4352:].fill_(0xFF)
+    got = vt.vtrace_orthogonalize(on, 0.5, workspace=ws)
+    for g, o in zip(gs, got):
+        check(g, o, scale=0.5)
+    alone = vt.vtrace_orthogonalize([g.cuda() for g in few], 0.5)
+    _same([o for i, o in enumerate(got) if i not in (1, 4)], alone)
+    _same(vt.vtrace_orthogonalize(on, 0.5, out=on, workspace=ws), got)
