@@ -94,8 +94,7 @@ def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.
     """orthogonalize() with the roundings of the operands, of the sums of products and of what is
     kept between the products: X float32 (in a last step for itself, of one part: the operand),
     operands float16 in one part or two, diagonals apart.
-    together 2: the first two steps at once, and of five and more the last two, the second's
-    matrices from the first's."""
+    together 2: the first two steps at once, the second's matrices from the first's."""
     single = lambda y: _f64(np.asarray(y).astype(np.float32))  # noqa: E731
     x = single(_start(g, epsilon))
     tall = x.shape[0] > x.shape[1]
@@ -108,7 +107,7 @@ def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.
         m = _Symmetric(gram, np.diagonal(gram).copy(), parts)
         p = _combine(m, m, b, 0.0, c, parts)
         k += 1
-        if together == 2 and (k == 1 or (k == len(coefficients) - 1 and k >= 4)) and k < len(coefficients):
+        if together == 2 and k == 1 and k < len(coefficients):
             a2, b2, c2 = coefficients[k]
             t = _combine(m, p, a, 0.0, 1.0, parts)
             m = _combine(t, p, a, 0.0, 1.0, parts)

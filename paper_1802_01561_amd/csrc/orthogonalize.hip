@@ -327,7 +327,7 @@ double small_cost(const Table& t, int kind, int size, bool pair) {
 }
 
 // VTRACE_KERNEL (ortho_32, ortho_64, ortho_128 or ortho_256, with x1 or x2 behind, and of the larger two k2 or k3
-// behind that) forces the tiles, whether steps are taken two at once, and the pieces of tiles that do not
+// behind that) forces the tiles, whether the first two steps are taken at once, and the pieces of tiles that do not
 // fill a round, to cross-check them.
 struct Forced {
   int size = 0, together = 0, split = 0;
@@ -384,7 +384,7 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
       small_size[kind] = small_cost(t, kind, 32, pair) <= small_cost(t, kind, 64, pair) ? 32 : 64;
       small[kind] = small_cost(t, kind, small_size[kind], pair);
     }
-    // Two steps: A and X twice, or once and three products more of B's size.
+    // The first two steps: A and X twice, or once and three products more of B's size.
     auto one_by_one = [](const double (&us)[3]) { return 2.0 * (us[0] + us[1] + us[2]); };
     auto together = [](const double (&us)[3]) { return us[0] + 5.0 * us[1] + us[2]; };
     t.small = std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
@@ -443,9 +443,8 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
   return t;
 }
 
-// The largest singular value that there may be before each of the steps, starting from 1; false
-// where they leave the operands' range.
-bool singular_bounds(const OrthoStep* steps, int count, double (&before)[kOrthoMostSteps]) {
+// Whether singular values from [0, 1] stay within the operands' range.
+bool singular_values_stay(const OrthoStep* steps, int count) {
   double most = 1.0;
   for (int k = 0; k < count; ++k) {
     const double a = steps[k].a, b = steps[k].b, c = steps[k].c;
@@ -474,22 +473,20 @@ bool singular_bounds(const OrthoStep* steps, int count, double (&before)[kOrthoM
       at(-a / (3.0 * b));
     }
     if (!(next <= kMostSingular)) return false;
-    before[k] = most;
     most = next;
   }
   return true;
 }
 
-
-// Whether two steps at once (launch_group) stay in the operands' range, singular values being at
-// most `most` before them: the eigenvalues of what is formed are polynomials of t = s^2 of degree up
-// to 12, whose range over [0, most^2] is at most 1 / cos(12 pi / 128) times (5% over) that over 64
+// Whether the first two steps at once (launch_group) stay in the operands' range, singular values
+// being at most 1 before them: the eigenvalues of what is formed are polynomials of t = s^2 of degree
+// up to 12, whose range over [0, 1] is at most 1 / cos(12 pi / 128) times (5% over) that over 64
 // Chebyshev points.
-bool two_steps_ok(const OrthoStep& p, const OrthoStep& q, double most) {
+bool two_steps_ok(const OrthoStep& p, const OrthoStep& q) {
   constexpr int kPoints = 64;
   double low[3] = {0.0, 0.0, 0.0}, high[3] = {0.0, 0.0, 0.0};
   for (int i = 0; i < kPoints; ++i) {
-    const double t = most * most * 0.5 * (1.0 + std::cos((2 * i + 1) * M_PI / (2 * kPoints)));
+    const double t = 0.5 * (1.0 + std::cos((2 * i + 1) * M_PI / (2 * kPoints)));
     const double first = p.a + t * (p.b + t * p.c), then = t * first * first;
     const double value[3] = {t * first, then, first * (q.a + then * (q.b + then * q.c)) - static_cast<double>(p.a) * q.a};
     for (int v = 0; v < 3; ++v) {
@@ -518,22 +515,18 @@ bool few_rows_ok(const OrthoStep* steps, int count) {
 // All are polynomials of A, and so commute and are symmetric: half their tiles are computed.
 // Where X has more columns than rows, or its loads and stores take as long as products, that is
 // less: 3 r^2 c operations and X twice against three products of r^3.
+//
+// The first two steps alone.  Their X is of norm 1, so that most singular values are small and Q with
+// them, and the rounding errors are those of steps one by one (2048 x 2048 bfloat16 1.70e-3 off, of which
+// one rounding is 1.66e-3).  Later most are near 1, Q is near -a a', and a result has its errors in full:
+// with the last two of five at once as well 1.97e-3, of 4096 x 4096 2.28e-3 where this has 1.69e-3.
 template <typename T, bool kPair>
 hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
                         hipStream_t st) {
   size_t bytes;
   Table t = table_of(items, count, few_rows_ok(steps, step_count), ws, &bytes);
   t.epsilon = epsilon;
-  double most[kOrthoMostSteps];
-  if (!singular_bounds(steps, step_count, most)) return hipErrorInvalidValue;
-  // The first two and (of five and more) the last two: in between, small singular values grow beside
-  // large ones that are near 1 already, and with them the rounding errors of Q, which is then
-  // large (bfloat16, two and two and one of five: up to 3.8e-3 off beside one rounding's 1.7e-3; two,
-  // one and two 1.2e-3; one by one 8e-4).
-  auto steps_from = [&](int k) {
-    const bool here = k + 1 < step_count && (k == 0 || (k == step_count - 2 && step_count >= 5));
-    return t.twos && here && two_steps_ok(steps[k], steps[k + 1], most[k]) ? 2 : 1;
-  };
+  const bool two_first = t.twos && step_count > 1 && two_steps_ok(steps[0], steps[1]);
   FewSteps few = {};
   std::copy_n(steps, step_count, few.at);
   few.count = step_count;
@@ -556,7 +549,7 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
   };
   bool low = true;
   for (int k = 0; k < step_count && e == hipSuccess;) {
-    const int together = steps_from(k), next = k + together;
+    const int together = k == 0 && two_first ? 2 : 1, next = k + together;
     const OrthoStep& p = steps[k];
     symmetric(kOfX, {0, 0, 0, 0.0f, 0.0f, 0.0f});
     symmetric(kOfOne, {1, 0, 0, p.b, 0.0f, p.c});
@@ -571,7 +564,7 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
       u.of_x = p.a * q.a;
     }
     // A last step for itself takes the operand alone as X: 2^-11 of it at most, which no step makes larger.
-    u.low_out = low = !(next + 1 == step_count) || steps_from(next) == 2;
+    u.low_out = low = next + 1 != step_count;
     if (e == hipSuccess) e = t.small ? launch_ortho_small_update(t, kPair, turn, u, st) : launch_ortho_tiles_update(t, kPair, turn, u, st);
     turn ^= 1;
     k = next;
@@ -581,10 +574,7 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
 
 }  // namespace
 
-bool ortho_steps_ok(const OrthoStep* steps, int count) {
-  double before[kOrthoMostSteps];
-  return singular_bounds(steps, count, before);
-}
+bool ortho_steps_ok(const OrthoStep* steps, int count) { return singular_values_stay(steps, count); }
 
 size_t ortho_workspace_bytes(const OrthoItem* items, int64_t count) {
   size_t most = round_up(kWsDataOffset, 256) + kPartialBytes;

@@ -72,7 +72,7 @@ struct Table {
   int total_partials, total_blocks, total_tiles[3];
   int size[3];  // of the tiles of A, B and X
   float epsilon;
-  bool twos;   // two steps at once
+  bool twos;   // the first two steps at once
   bool small;  // the small matrices' kernels, which keep X^T as well
 };
 

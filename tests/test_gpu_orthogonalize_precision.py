@@ -1,0 +1,121 @@
+"""How exact Newton-Schulz products are at the sizes of layers, where the kernels' own choices are those
+that a program gets, against products in float64 on the GPU.
+
+Tolerance: a result's rounding to its type, measured on the float64 result, and twice what a model of the
+operands' roundings is off (steps one by one, and the first two at once, whichever is more).  The two
+are independent of each other, so that their squares add: a value's place between two bfloat16
+ones says nothing about the error that it has.  Errors of a million elements and more spread
+over the norms of several hundred directions, so that the kernel's and the model's are within a few
+percent of each other if they have the same roundings; twice is for what differs (the order of sums
+that are rounded to operands), and 1% for the first."""
+
+import functools
+import math
+
+import pytest
+import torch
+
+import paper_1802_01561_amd as vt
+from oracle import parameters as op
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def matrix(seed, m, n, dtype, kind="strong"):
+    """A few strong directions above noise, or noise."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((m, n), generator=g, device="cuda")
+    if kind == "strong":
+        r = max(1, min(m, n) // 16)
+        x = torch.randn((m, r), generator=g, device="cuda") @ torch.randn((r, n), generator=g, device="cuda") / math.sqrt(r) + 0.3 * x
+    return (1e-3 * x).to(dtype)
+
+
+def _turned(x):
+    return x.t().contiguous() if x.shape[0] > x.shape[1] else x
+
+
+def _start(g):
+    x = _turned(g.double())
+    return x / torch.linalg.vector_norm(x)
+
+
+def _steps(steps):
+    return [[float(torch.tensor(v)) for v in s] for s in steps]
+
+
+def exact(g, steps):
+    x = _start(g)
+    for a, b, c in _steps(steps):
+        s = x @ x.t().contiguous()
+        x = a * x + (b * s + c * (s @ s)) @ x
+    return x.t() if g.shape[0] > g.shape[1] else x
+
+
+def _operand(x, scale):
+    return (x * scale).half().double() / scale
+
+
+class _Symmetric:
+    """The diagonal in float32, the rest as an operand."""
+
+    def __init__(self, off, diagonal):
+        self.diagonal = diagonal.float().double()
+        self.off = _operand(off - torch.diag(torch.diagonal(off)), 8192.0)
+
+
+def _combine(m, n, of_m, of_n, of_mn):
+    oo = m.off @ n.off
+    dm, dn = m.diagonal[:, None], n.diagonal[None, :]
+    off = of_m * m.off + of_n * n.off + of_mn * (dm * n.off + m.off * dn + oo)
+    return _Symmetric(off, of_m * m.diagonal + of_n * n.diagonal + of_mn * (m.diagonal * n.diagonal + torch.diagonal(oo)))
+
+
+def rounded(g, steps, together):
+    """bfloat16 matrices: float16 operands, and sums without rounding, which is far less."""
+    x, k, steps = _start(g), 0, _steps(steps)
+    while k < len(steps):
+        a, b, c = steps[k]
+        xs = _operand(x, 4096.0)
+        gram = xs @ xs.t().contiguous()
+        m = _Symmetric(gram, torch.diagonal(gram))
+        p = _combine(m, m, b, 0.0, c)
+        k += 1
+        if together == 2 and k == 1 and k < len(steps):
+            a2, b2, c2 = steps[k]
+            t = _combine(m, p, a, 0.0, 1.0)
+            m = _combine(t, p, a, 0.0, 1.0)
+            p = _combine(_combine(m, m, b2, 0.0, c2), p, a, a2, 1.0)
+            a *= a2
+            k += 1
+        x = (a + p.diagonal)[:, None] * x + p.off @ xs
+    return x.t() if g.shape[0] > g.shape[1] else x
+
+
+def _norm(x):
+    return torch.linalg.vector_norm(x).item()
+
+
+@functools.lru_cache(maxsize=None)
+def _model(seed, m, n, kind, steps):
+    g = matrix(seed, m, n, BF16, kind)
+    ref = exact(g, steps)
+    return g, ref, max(_norm(rounded(g, steps, k) - ref) for k in (1, 2)), _norm(ref.to(BF16).double() - ref)
+
+
+STEPS = (op.QUINTIC,) * 5
+
+
+@pytest.mark.parametrize("m,n,kind", [(2048, 2048, "strong"), (2048, 2048, "normal"), (4096, 1024, "strong"), (4096, 4096, "strong")])
+@pytest.mark.parametrize("kernel", [None, "ortho_128x2", "ortho_256x1", "ortho_256x2"])
+def test_bfloat16_layers(m, n, kind, kernel, monkeypatch):
+    monkeypatch.delenv("VTRACE_KERNEL", raising=False)
+    if kernel:
+        monkeypatch.setenv("VTRACE_KERNEL", kernel)
+    g, ref, off, rounding = _model(m + n, m, n, kind, STEPS)
+    got, = vt.vtrace_orthogonalize([g])
+    err = _norm(got.double() - ref)
+    print(f"[case] {m} x {n} {kind} {kernel}: {err / _norm(ref):.3e}, rounding {rounding / _norm(ref):.3e}, model {off / _norm(ref):.3e}", flush=True)
+    assert err <= math.hypot(1.01 * rounding, 2.0 * off)
