@@ -92,8 +92,7 @@ def _combine(m, n, of_m, of_n, of_mn, parts):
 
 def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.0, parts=1, together=1):
     """orthogonalize() with the roundings of the operands, of the sums of products and of what is
-    kept between the products: X float32 (in a last step for itself, of one part: the operand),
-    operands float16 in one part or two, diagonals apart.
+    kept between the products: X float32, operands float16 in one part or two, diagonals apart.
     together 2: the first two steps at once, the second's matrices from the first's."""
     single = lambda y: _f64(np.asarray(y).astype(np.float32))  # noqa: E731
     x = single(_start(g, epsilon))
@@ -115,7 +114,5 @@ def orthogonalize_rounded(g, coefficients=(QUINTIC,) * 5, epsilon=1e-7, scale=1.
             p = _combine(q, p, a, a2, 1.0, parts)
             a = float(np.float32(a * a2))
             k += 1
-        elif parts == 1 and k == len(coefficients):
-            x = xs[0]
         x = single(single(a + p.diagonal)[:, None] * x + _product(p.operand, xs))
     return scale * (x.T if tall else x)

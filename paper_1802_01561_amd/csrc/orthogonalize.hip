@@ -547,13 +547,12 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
     e = t.small ? launch_ortho_small_symmetric(t, of, kPair, turn, p, later && first ? &few : nullptr, st) : launch_ortho_tiles_symmetric(t, of, kPair, turn, p, st);
     first = false;
   };
-  bool low = true;
   for (int k = 0; k < step_count && e == hipSuccess;) {
     const int together = k == 0 && two_first ? 2 : 1, next = k + together;
     const OrthoStep& p = steps[k];
     symmetric(kOfX, {0, 0, 0, 0.0f, 0.0f, 0.0f});
     symmetric(kOfOne, {1, 0, 0, p.b, 0.0f, p.c});
-    Update u = {1, p.a, next == step_count, low, false};
+    Update u = {1, p.a, next == step_count};
     if (together == 2) {
       const OrthoStep& q = steps[k + 1];
       symmetric(kOfTwo, {2, 0, 1, p.a, 0.0f, 1.0f});
@@ -563,8 +562,6 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
       u.by = 0;
       u.of_x = p.a * q.a;
     }
-    // A last step for itself takes the operand alone as X: 2^-11 of it at most, which no step makes larger.
-    u.low_out = low = next + 1 != step_count;
     if (e == hipSuccess) e = t.small ? launch_ortho_small_update(t, kPair, turn, u, st) : launch_ortho_tiles_update(t, kPair, turn, u, st);
     turn ^= 1;
     k = next;

@@ -271,11 +271,10 @@ __device__ __forceinline__ void store_results(Out* p, const float (&y)[2][4], in
 
 // The launches of one translation unit each: a symmetric matrix, or X <- of_x X + C X with the
 // symmetric matrix numbered `by`.  `pair`: float32 matrices.
-// Of bfloat16 ones, low_in and low_out: whether X's remainder beside the operand is read, and written.
 struct Update {
   int by;
   float of_x;
-  bool last, low_in, low_out;
+  bool last;
 };
 hipError_t launch_ortho_tiles_symmetric(const Table& t, int of, bool pair, int turn, const Product& p, hipStream_t s);
 hipError_t launch_ortho_tiles_update(const Table& t, bool pair, int turn, const Update& u, hipStream_t s);

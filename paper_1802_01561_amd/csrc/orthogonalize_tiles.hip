@@ -344,8 +344,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           x[n % kBuffers][m + 1] = *reinterpret_cast<const f32x4*>(p.x + from + 4);
         } else {
           part[n % kBuffers][0][m / 2] = *reinterpret_cast<const v4u*>(p.from[0] + from);
-          part[n % kBuffers][1][m / 2] = v4u{};
-          if (f.low_in) part[n % kBuffers][1][m / 2] = *reinterpret_cast<const v4u*>(p.low + from);
+          part[n % kBuffers][1][m / 2] = *reinterpret_cast<const v4u*>(p.low + from);
         }
       }
     };
@@ -409,7 +408,7 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_up
           auto both = [](v2u u, v2u v) { return v4u{u[0], u[1], v[0], v[1]}; };
           *reinterpret_cast<v4u*>(p.to[0] + to) = both(high[0], high[1]);
           if constexpr (kPair) *reinterpret_cast<v4u*>(p.to[1] + to) = both(low4(y[0], high[0]), low4(y[1], high[1]));
-          else if (f.low_out) *reinterpret_cast<v4u*>(p.low + to) = both(left4(y[0], high[0]), left4(y[1], high[1]));
+          else *reinterpret_cast<v4u*>(p.low + to) = both(left4(y[0], high[0]), left4(y[1], high[1]));
         }
       }
       __builtin_amdgcn_sched_barrier(0);

@@ -119,3 +119,22 @@ def test_bfloat16_layers(m, n, kind, kernel, monkeypatch):
     err = _norm(got.double() - ref)
     print(f"[case] {m} x {n} {kind} {kernel}: {err / _norm(ref):.3e}, rounding {rounding / _norm(ref):.3e}, model {off / _norm(ref):.3e}", flush=True)
     assert err <= math.hypot(1.01 * rounding, 2.0 * off)
+
+
+@pytest.mark.parametrize("m,n", [(90, 100), (400, 300), (1100, 1030)])
+@pytest.mark.parametrize("steps", [1, 2, 3, 5])
+@pytest.mark.parametrize("kernel", [None] + [f"ortho_{size}x{together}" for size in (64, 128, 256) for together in (1, 2)])
+def test_bfloat16_matrices_keep_22_bits_from_step_to_step(m, n, steps, kernel, monkeypatch):
+    """Steps that change nothing give G / |G| rounded once.  X is float32 behind each step and then two
+    float16 parts, the second at most half a step of the first, 2^-11, and so off by 2^-22 at most; where
+    the first leaves float16's range the second's step is 2^-24 2^-11 of X 2^12.  Twice for the float32 operations'
+    2^-24, a step more for the start.  A single part, 2^-11, is an eighth of bfloat16's half step."""
+    monkeypatch.delenv("VTRACE_KERNEL", raising=False)
+    if kernel:
+        monkeypatch.setenv("VTRACE_KERNEL", kernel)
+    g = matrix(m + steps, m, n, BF16)
+    got, = vt.vtrace_orthogonalize([g], steps=steps, coefficients=(1.0, 0.0, 0.0))
+    ref = g.double() / torch.linalg.vector_norm(g.double())
+    half_step = torch.exp2(torch.floor(torch.log2(ref.abs().clamp(min=1e-30))) - 8)
+    tol = half_step + 2.0 * (steps + 1) * (2.0 ** -22 * ref.abs() + 2.0 ** -47)
+    assert ((got.double() - ref).abs() <= tol).all()
