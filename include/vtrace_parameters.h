@@ -56,7 +56,7 @@ vtrace_status vtrace_vocab_embed(
  *                written, rows of tokens that no step has with zeros; otherwise
  *                rows of tokens that steps have are added to, and no other is touched
  *   workspace    vtrace_vocab_embed_grad_workspace_bytes(T,B,V,H) bytes, 16-byte aligned,
- *                cleared once by vtrace_workspace_init
+ *                cleared once by vtrace_workspace_init.  No smaller T*B, V and H need more
  * Everything else as above.  Sums are float32 over up to 128 steps of a token and float64
  * beyond, in an order that depends on the tokens alone; scaled and added in float32,
  * rounded once.  A token that is neither in the vocabulary nor VTRACE_NO_TOKEN adds

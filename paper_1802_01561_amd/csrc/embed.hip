@@ -13,6 +13,8 @@
 #include "embed.hpp"
 #include "wave_ops.hpp"
 
+#include <algorithm>
+
 namespace vtrace {
 namespace {
 
@@ -354,6 +356,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_move_kernel(EmbedArgs a, i
 // ---- Sums. ----
 
 constexpr int kLeastChunk = 4, kMostChunk = 128;
+constexpr int kWorkgroups = 1024;  // least, where chunks are longer than the shortest
 constexpr int kBatch = 8;  // rows of a chunk in flight
 constexpr int kFillRows = 256;  // most rows of a workgroup that fills
 constexpr int64_t kFillBytes = 65536;
@@ -587,10 +590,13 @@ hipError_t launch_sums(const EmbedArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-int passes_of(int64_t V, int* bits) {
+int token_bits(int64_t V) {
   int all = 1;  // keys are 0 .. V
   while ((V >> all) != 0) ++all;
-  const int passes = (all + kMostDigitBits - 1) / kMostDigitBits;
+  return all;
+}
+int passes_of(int64_t V, int* bits) {
+  const int all = token_bits(V), passes = (all + kMostDigitBits - 1) / kMostDigitBits;
   *bits = (all + passes - 1) / passes;
   return passes;
 }
@@ -647,7 +653,7 @@ EmbedPlan plan_embed_grad(int64_t N, int64_t V, int64_t H) {
   const int lanes = row_lanes_log2(H, 8);
   const int64_t slabs = ceil_div(H / kUnit, kThreads), groups = kThreads >> lanes;
   p.chunk = kLeastChunk;
-  while (p.chunk < kMostChunk && N * slabs / (groups * p.chunk * 2) >= 1024) p.chunk *= 2;
+  while (p.chunk < kMostChunk && N * slabs / (groups * p.chunk * 2) >= kWorkgroups) p.chunk *= 2;
   size_t at = kWsDataOffset;
   auto take = [&](size_t bytes) {
     const size_t begin = at;
@@ -659,12 +665,14 @@ EmbedPlan plan_embed_grad(int64_t N, int64_t V, int64_t H) {
     p.keys_at[b] = take(N * 4);
     p.steps_at[b] = take(N * 4);
   }
-  if (!p.ranks) {
-    int bits = 0;
-    passes_of(V, &bits);
-    p.counts_at = take((ceil_div(N, kSortItems) << bits) * 4);
-  }
-  p.partials_at = take(ceil_div(N, p.chunk) * 2 * H * 4);
+  // What is taken is enough for fewer steps, fewer tokens and shorter rows too, so that the bytes for
+  // the largest call serve all of them.  Fewer tokens may be sorted in fewer passes of more bits.
+  if (!p.ranks) p.counts_at = take((ceil_div(N, kSortItems) << std::min(token_bits(V), kMostDigitBits)) * 4);
+  // Chunks that are twice as long halve the partial sums, and fewer steps have more of them: chunks that
+  // are not of kMostChunk are less than 2 kWorkgroups groups / slabs, whose rows have at most kThreads kUnit slabs /
+  // groups elements (and one row for the chunk that is not whole).
+  const int64_t least = ceil_div(N, kLeastChunk) * H, most = int64_t(2) * kWorkgroups * kThreads * kUnit + H;
+  p.partials_at = take(std::max({ceil_div(N, p.chunk) * H, ceil_div(N, kMostChunk) * H, std::min(least, most)}) * 2 * 4);
   p.bytes = at;
   return p;
 }

@@ -35,7 +35,8 @@ QUINTIC = (3.4445, -4.7750, 2.0315)
 
 
 class EmbedWorkspace(_CallWorkspace):
-    """Workspace of vtrace_vocab_embed_grad (and of vtrace_vocab_embed, for its flag)."""
+    """Workspace of vtrace_vocab_embed_grad (and of vtrace_vocab_embed, for its flag), for calls
+    of so many steps, tokens and elements of a row, or fewer."""
 
     def __init__(self, T: int, B: int, V: int, H: int, device=None, stream=None):
         n = vtrace_vocab_embed_grad_workspace_bytes(T, B, V, H)

@@ -186,3 +186,19 @@ def test_python_binding_validates_before_calling():
                  lambda: vt.vtrace_orthogonalize([m.half()])):
         with pytest.raises(TypeError):
             call()
+
+
+def test_embed_grad_workspace_for_more_serves_less(L):
+    """Around where chunks become longer, sorts begin and digits get another width, and in between."""
+    n = L.vtrace_vocab_embed_grad_workspace_bytes
+    steps = sorted({max(1, s + d) for s in [1 << k for k in range(26)] + [5000, 20000, 40000, 300000] for d in (-1, 0, 1) if s + d <= 1 << 25})
+    for H in (8, 64, 72, 1000, 1024, 1032, 2048, 2056, 4096):
+        sizes = [n(s, 1, 131072, H) for s in steps]
+        assert all(0 < a <= b for a, b in zip(sizes, sizes[1:])), H
+    for N in (1, 1000, 16384, 16385, 65536, 1 << 20):
+        sizes = [n(N, 1, (1 << k) + d, 64) for k in range(1, 24) for d in (-1, 0, 1)]
+        assert all(0 < a <= b for a, b in zip(sizes, sizes[1:])), N
+        sizes = [n(N, 1, 1000, H) for H in range(8, 4104, 8)]
+        assert all(0 < a <= b for a, b in zip(sizes, sizes[1:])), N
+    # a learner's batches of other lengths with the workspace of the longest
+    assert all(n(N, 1, 131072, 2048) <= n(65536, 1, 131072, 2048) for N in (65535, 40000, 32768, 20000, 8191, 100))
