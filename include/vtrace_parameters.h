@@ -93,7 +93,8 @@ vtrace_status vtrace_vocab_embed_grad(
  *                 bring singular values from 0.01 |G| on into 0.68 .. 1.21
  *   epsilon       finite, > 0; a matrix of zeros gives zeros
  *   workspace     vtrace_orthogonalize_workspace_bytes(count, rows, columns, dtypes) bytes, 16-byte
- *                 aligned, cleared once by vtrace_workspace_init; 0 for an invalid list
+ *                 aligned, cleared once by vtrace_workspace_init; 0 for an invalid list.  Any list of
+ *                 some of the matrices, in any order, needs as many or fewer
  * Numerics: norms are float64.  Matrices of at most 32 rows or columns are float64 up to the
  * result's rounding (as long as the coefficients a multiply to at most 8192 over the steps).
  * Otherwise X has 22 bits (bfloat16 matrices) or is float32 from step to step, sums of

@@ -30,6 +30,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
+#include <functional>
+#include <numeric>
 #include <string>
 
 namespace vtrace {
@@ -240,7 +242,8 @@ int64_t tiles_in(const Entry& e, int kind, int size) {
 // pieces of 13 steps take as long as one of 64, 20 to store and 12 a piece to join; six of 43 150 less
 // than one of 256).  A of 4 matrices of 4096 x 4096 and 2 of 4096 x 16384, which has 16 of 272 long tiles too
 // many: 1030 -> 780 us.  `split`: into so many wherever there are as many steps.
-double tiles_cost(const Table& t, int kind, int size, int passes, int split, Units* units) {
+// `room`: bytes for the pieces' sums.
+double tiles_cost(const Table& t, int kind, int size, int passes, int split, int64_t room, Units* units) {
   double all = 0.0;
   for (int i = 0; i < t.count; ++i) all += static_cast<double>(tiles_in(t.at[i], kind, size));
   const bool alone = size == kSmallTile && all <= kCus;
@@ -260,6 +263,7 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
   const double to_store = size == kTile ? 20.0 : 10.0, to_join = size == kTile ? 12.0 : 6.0;
   *units = {};
   int splits = 0;
+  int64_t sums = room / (size * size * static_cast<int64_t>(sizeof(float)));  // pieces that there is room for
   double us = 0.0, open_us = 0.0;
   for (int i = 0; i < t.count;) {
     auto steps_of = [&](int k) { return (kind == 0 ? t.at[k].pc : t.at[k].pr) / kTileK; };
@@ -278,6 +282,7 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
     const double work = step(left) * k;
     int64_t pieces = std::min<int64_t>((slots - left + own) / own, split ? std::min(split, steps) : steps / 4);
     if (!split) pieces = std::min(pieces, std::max<int64_t>(1, std::lround(std::sqrt(work / to_join))));
+    pieces = std::min(pieces, sums / own);
     if (pieces < 2) continue;
     const int64_t there = left + own * (pieces - 1);
     const double then = step(there) * k / static_cast<double>(pieces) + to_store + to_join * static_cast<double>(pieces);
@@ -285,6 +290,7 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
     units->begin[splits] = static_cast<int>(at - own);
     units->end[splits] = static_cast<int>(at);
     units->pieces[splits++] = static_cast<int>(pieces);
+    sums -= own * pieces;
     open = there;
     open_us = std::max(before, then + beside(there));
     if (open == slots) {
@@ -299,11 +305,6 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, Uni
     else units->total += (units->end[k] - units->begin[k]) * (units->pieces[k] - 1);
   }
   return us + open_us;
-}
-int64_t sums_bytes(const Units& u, int size) {
-  int64_t slots = 0;
-  for (int k = 0; k < Units::kSplits; ++k) slots += static_cast<int64_t>(u.end[k] - u.begin[k]) * u.pieces[k];
-  return slots * size * size * static_cast<int64_t>(sizeof(float));
 }
 
 // The same in the small matrices' kernels' tiles of 64 or 32: a launch, and the tile that has a CU for
@@ -345,8 +346,27 @@ Forced forced_kernel() {
   return f;
 }
 
-// The entries of a group of matrices, all of one type, and the workspace's bytes for them.
-Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_t* bytes) {
+// A matrix's share of the workspace, whatever it is worked on with: its pieces, and spare bytes that hold
+// X^T (the small matrices' kernels), or those of all matrices the sums of split tiles.  So the bytes for a
+// list serve every list of some of its matrices, whose tiles may be others: of nine bfloat16 512 x
+// 2048 tiles of 128, of eight of them tiles of 64.
+// Where an X^T has more than that, tiles of 128 or 256 cost less than small ones in any list.
+constexpr int64_t kMostSpare = int64_t(1) << 28;
+int64_t transposed_of_entry(const Entry& e, bool pair) { return pair ? transposed_bytes<true>(e.c, e.pr) : transposed_bytes<false>(e.c, e.pr); }
+int64_t spare_of(const Entry& e, bool pair) { return round_up(std::min(transposed_of_entry(e, pair), kMostSpare), 256); }
+int64_t pieces_bytes(const Entry& e, bool pair) {
+  return round_up(pair ? piece_bytes<true>(e.r, e.pr, e.pc) : piece_bytes<false>(e.r, e.pr, e.pc), 256);
+}
+int64_t few_bytes(const Entry& e) { return few_chunks(e.c) * static_cast<int64_t>(kFewRows * kFewRows * sizeof(double)); }
+int64_t share_of(const Entry& e, bool pair) {
+  const int64_t tiles = pieces_bytes(e, pair) + spare_of(e, pair);
+  return e.r <= kFewRows ? std::max(tiles, few_bytes(e)) : tiles;
+}
+// For forced pieces as well: as many as a launch may have.
+int64_t forced_spare() { return forced_kernel().split ? 2 * kCus * kTile * kTile * static_cast<int64_t>(sizeof(float)) : 0; }
+
+// The entries of a group of matrices, all of one type.
+Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws) {
   Table t = {};
   const bool pair = !items[0].bf16;
   const Forced forced = forced_kernel();
@@ -358,8 +378,12 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
   t.few = static_cast<int>(std::count_if(t.at, t.at + count, few));
   count -= t.few;
   t.count = count;
+  int64_t room = forced_spare();
+  bool small_fits = true;
   for (int i = 0; i < count; ++i) {
     Entry& e = t.at[i];
+    room += spare_of(e, pair);
+    small_fits = small_fits && transposed_of_entry(e, pair) <= kMostSpare;
     const int64_t elements = static_cast<int64_t>(e.r) * e.c;
     e.first_partial = t.total_partials;
     e.partials = static_cast<int32_t>((elements + norm_chunk(elements) - 1) / norm_chunk(elements));
@@ -374,8 +398,8 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     for (int kind = 0; kind < 3; ++kind) {
       Units units;
       t.size[kind] = kTile;
-      tiles[kind] = tiles_cost(t, kind, kTile, passes, 0, &t.units[kind]);
-      const double of_small = tiles_cost(t, kind, kSmallTile, passes, 0, &units);
+      tiles[kind] = tiles_cost(t, kind, kTile, passes, 0, room, &t.units[kind]);
+      const double of_small = tiles_cost(t, kind, kSmallTile, passes, 0, room, &units);
       if (of_small < tiles[kind]) {
         t.size[kind] = kSmallTile;
         tiles[kind] = of_small;
@@ -387,7 +411,7 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     // The first two steps: A and X twice, or once and three products more of B's size.
     auto one_by_one = [](const double (&us)[3]) { return 2.0 * (us[0] + us[1] + us[2]); };
     auto together = [](const double (&us)[3]) { return us[0] + 5.0 * us[1] + us[2]; };
-    t.small = std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
+    t.small = small_fits && std::min(one_by_one(small), together(small)) < std::min(one_by_one(tiles), together(tiles));
     if (t.small) std::copy_n(small_size, 3, t.size);
     // The few rows' results go with the others' X, or with their first A if that takes as long as they do (five
     // float32 matrices of 16 to 513 rows 198 -> 191 us; beside a 64 x 64 matrix's A two 67 -> 69).
@@ -395,11 +419,12 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     t.twos = t.small ? together(small) < one_by_one(small) : together(tiles) < one_by_one(tiles);
   }
   if (forced.size) {
-    t.small = forced.size < kSmallTile;
+    const int size = small_fits ? forced.size : std::max(forced.size, kSmallTile);
+    t.small = size < kSmallTile;
     t.few_later = false;
-    std::fill_n(t.size, 3, forced.size);
+    std::fill_n(t.size, 3, size);
     for (int kind = 0; kind < 3 && !t.small; ++kind) {
-      tiles_cost(t, kind, forced.size, pair ? 3 : 1, forced.split, &t.units[kind]);
+      tiles_cost(t, kind, size, pair ? 3 : 1, forced.split, room, &t.units[kind]);
     }
   }
   if (forced.together) t.twos = forced.together == 2;
@@ -408,8 +433,8 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
   for (int i = 0; i < count; ++i) {
     Entry& e = t.at[i];
     e.base = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
-    at += round_up(pair ? piece_bytes<true>(e.r, e.pr, e.pc) : piece_bytes<false>(e.r, e.pr, e.pc), 256);
-    if (t.small) at += round_up(pair ? transposed_bytes<true>(e.c, e.pr) : transposed_bytes<false>(e.c, e.pr), 256);
+    at += pieces_bytes(e, pair);
+    if (t.small) at += spare_of(e, pair);
     for (int kind = 0; kind < 3; ++kind) {
       e.first_tile[kind] = t.total_tiles[kind];
       t.total_tiles[kind] += static_cast<int32_t>(tiles_in(e, kind, t.size[kind]));
@@ -417,9 +442,7 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
   }
   t.counters = reinterpret_cast<unsigned*>(reinterpret_cast<uintptr_t>(ws) + kWsHeaderBytes);
   t.sums = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
-  int64_t sums = 0;
-  for (int kind = 0; kind < 3 && count > 0 && !t.small; ++kind) sums = std::max(sums, sums_bytes(t.units[kind], t.size[kind]));
-  at += sums;
+  if (!t.small) at += room;
   // Every workgroup forms its Q, about 5 us: one tile each, then more (256 columns each, always: one float32
   // 32 x 4096 matrix 32 us, so 25; eight of 2 x 300 29 and 21).
   auto few_blocks = [&](int64_t block) {
@@ -433,13 +456,12 @@ Table table_of(const OrthoItem* items, int count, bool few_rows, char* ws, size_
     Entry& e = t.at[i];
     e.base = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(ws) + static_cast<uintptr_t>(at));
     e.partials = static_cast<int32_t>(few_chunks(e.c));
-    at += e.partials * static_cast<int64_t>(kFewRows * kFewRows * sizeof(double));
+    at += few_bytes(e);
     e.first_partial = t.few_chunks;
     t.few_chunks += e.partials;
     e.first_block = t.few_blocks;
     t.few_blocks += (e.c + t.few_block - 1) / t.few_block;
   }
-  *bytes = static_cast<size_t>(at);
   return t;
 }
 
@@ -523,8 +545,7 @@ bool few_rows_ok(const OrthoStep* steps, int count) {
 template <typename T, bool kPair>
 hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
                         hipStream_t st) {
-  size_t bytes;
-  Table t = table_of(items, count, few_rows_ok(steps, step_count), ws, &bytes);
+  Table t = table_of(items, count, few_rows_ok(steps, step_count), ws);
   t.epsilon = epsilon;
   const bool two_first = t.twos && step_count > 1 && two_steps_ok(steps[0], steps[1]);
   FewSteps few = {};
@@ -574,18 +595,20 @@ hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* step
 bool ortho_steps_ok(const OrthoStep* steps, int count) { return singular_values_stay(steps, count); }
 
 size_t ortho_workspace_bytes(const OrthoItem* items, int64_t count) {
-  size_t most = round_up(kWsDataOffset, 256) + kPartialBytes;
+  // The largest shares of a table, but not more than a group of several matrices may have: 32 bytes an
+  // element of float32, and what the pitches add to 38 of 2^28 elements, less than 9 2^28 (half of both of
+  // bfloat16).
+  int64_t most = 0;
   for (const bool bf16 : {true, false}) {
-    const std::vector<OrthoItem> of = of_type(items, count, bf16);
-    for_groups(of, [&](size_t first, size_t last) {
-      for (const bool few_rows : {true, false}) {
-        size_t bytes;
-        table_of(of.data() + first, static_cast<int>(last - first), few_rows, nullptr, &bytes);
-        most = std::max(most, bytes);
-      }
-    });
+    std::vector<int64_t> shares;
+    for (int64_t i = 0; i < count; ++i)
+      if (items[i].bf16 == bf16) shares.push_back(share_of(entry_for(items[i]), !bf16));
+    std::sort(shares.begin(), shares.end(), std::greater<int64_t>());
+    if (shares.size() > static_cast<size_t>(Table::kMost)) shares.resize(Table::kMost);
+    const int64_t all = std::accumulate(shares.begin(), shares.end(), int64_t(0));
+    if (!shares.empty()) most = std::max({most, shares[0], std::min(all, kGroupElements * (bf16 ? 21 : 42))});
   }
-  return most;
+  return round_up(kWsDataOffset, 256) + kPartialBytes + static_cast<size_t>(most + forced_spare());
 }
 
 hipError_t launch_orthogonalize(const OrthoItem* items, int64_t count, const OrthoStep* steps, int step_count, float epsilon,

@@ -46,7 +46,7 @@ class EmbedWorkspace(_CallWorkspace):
 
 
 class OrthogonalWorkspace(_CallWorkspace):
-    """Workspace of vtrace_orthogonalize, for matrices of these shapes and types in this order."""
+    """Workspace of vtrace_orthogonalize, for matrices of these shapes and types, or some of them."""
 
     def __init__(self, matrices: Sequence[torch.Tensor], device=None, stream=None):
         matrices = list(matrices)

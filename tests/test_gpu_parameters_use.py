@@ -498,3 +498,26 @@ def test_few_rows_beside_others(dtype, long):
     alone = vt.vtrace_orthogonalize([g.cuda() for g in few], 0.5)
     _same([o for i, o in enumerate(got) if i not in (1, 4)], alone)
     _same(vt.vtrace_orthogonalize(on, 0.5, out=on, workspace=ws), got)
+
+
+@pytest.mark.parametrize("dtype,shapes,fewer", [
+    (BF16, [(512, 2048)] * 9, (8, 5, 1)), (BF16, [(2048, 512)] * 11, (10,)), (F32, [(512, 512)] * 15, (14, 3)),
+    (F32, [(700, 2100), (90, 100), (20, 500), (700, 2100), (33, 64), (640, 640)] * 7, (41, 39, 20)),
+    (BF16, [(4096, 4096)] * 2 + [(4096, 16384)], (2, 1))])
+def test_a_workspace_for_all_matrices_serves_some_of_them(dtype, shapes, fewer):
+    """The last ones alone, whose tiles are others than those of all: what they get in a workspace of their own, and
+    nothing behind the workspace's bytes is written."""
+    gs = [(1e-3 * torch.randn(s, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda")).to(dtype) for i, s in enumerate(shapes)]
+    ws = vt.OrthogonalWorkspace(gs)
+    ws.tensor = torch.full((ws.nbytes + 65536,), 0xFF, dtype=torch.uint8, device="cuda")
+    ws.tensor[:4352] = 0
+    whole = vt.vtrace_orthogonalize(gs, workspace=ws)
+    for k in fewer:
+        own = vt.OrthogonalWorkspace(gs[-k:])
+        assert own.nbytes <= ws.nbytes
+        own.tensor = torch.full((own.nbytes + 65536,), 0xFF, dtype=torch.uint8, device="cuda")
+        own.tensor[:4352] = 0
+        _same(vt.vtrace_orthogonalize(gs[-k:], workspace=ws), vt.vtrace_orthogonalize(gs[-k:], workspace=own))
+        assert (own.tensor[own.nbytes:] == 0xFF).all()
+    _same(vt.vtrace_orthogonalize(gs, workspace=ws), whole)
+    assert (ws.tensor[ws.nbytes:] == 0xFF).all()

@@ -5,6 +5,7 @@ dereferenced."""
 import ctypes
 import math
 import os
+import random
 import re
 
 import pytest
@@ -202,3 +203,27 @@ def test_embed_grad_workspace_for_more_serves_less(L):
         assert all(0 < a <= b for a, b in zip(sizes, sizes[1:])), N
     # a learner's batches of other lengths with the workspace of the longest
     assert all(n(N, 1, 131072, 2048) <= n(65536, 1, 131072, 2048) for N in (65535, 40000, 32768, 20000, 8191, 100))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_orthogonalize_workspace_for_more_serves_less(L, dtype):
+    """Also where some of a list's matrices have other tiles than all of them, are put into launches with
+    others, or fewer of them into one."""
+    def size(shapes):
+        n = _ortho_bytes(L, [m for m, _ in shapes], [n for _, n in shapes], [dtype] * len(shapes))
+        assert n > 0
+        return n
+
+    for shape in ((512, 2048), (512, 512), (2048, 512), (1024, 1024), (64, 64), (20, 500), (33, 40), (4096, 4096), (1000, 30000)):
+        sizes = [size([shape] * k) for k in range(1, 80)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), shape
+    r = random.Random(dtype)
+    for _ in range(300):
+        shapes = []
+        for _ in range(r.randint(1, 5)):
+            shapes += [(int(2 ** r.uniform(0, 13)), int(2 ** r.uniform(0, 13)))] * r.randint(1, 30)
+        r.shuffle(shapes)
+        whole = size(shapes)
+        for _ in range(10):
+            assert size([s for s in shapes if r.random() < 0.7] or shapes[:1]) <= whole
+        assert size(shapes[1:] or shapes) <= whole and size(shapes[::-1]) == whole
