@@ -187,6 +187,11 @@ def vtrace_vocab_embed_grad(d_embedded, tokens, vocab_size: int, scale: float = 
     return given
 
 
+def _is_number(x) -> bool:
+    """One value and no sequence: tensors and arrays of no dimension have a length that raises."""
+    return not hasattr(x, "__len__") or getattr(x, "ndim", 1) == 0
+
+
 _quintic = {}  # steps -> the table of QUINTIC for so many
 
 
@@ -195,9 +200,9 @@ def _coefficients(coefficients, steps: int):
     if coefficients is QUINTIC and steps in _quintic:
         return _quintic[steps]
     rows = list(coefficients)
-    if len(rows) == 3 and not any(hasattr(r, "__len__") for r in rows):
+    if len(rows) == 3 and all(_is_number(r) for r in rows):
         rows = [rows] * steps
-    if len(rows) != steps or any(len(r) != 3 for r in rows):
+    if len(rows) != steps or any(_is_number(r) or len(r) != 3 for r in rows):
         raise ValueError(f"coefficients must be a triple, or {steps} of them")
     table = (ctypes.c_float * (3 * steps))(*(float(x) for r in rows for x in r))
     if coefficients is QUINTIC:
@@ -233,12 +238,12 @@ def vtrace_orthogonalize(matrices: Sequence[torch.Tensor], scale: Union[float, S
                                         workspace.tensor, workspace.nbytes, device, fast.stream(device))
             if r is not None:
                 return list(_outputs(r))
-    if hasattr(scale, "__len__"):
+    if _is_number(scale):
+        scales = (ctypes.c_float * n)(*([float(scale)] * n))
+    else:
         if len(scale) != n:
             raise ValueError(f"{len(scale)} scales for {n} matrices")
         scales = (ctypes.c_float * n)(*(float(x) for x in scale))
-    else:
-        scales = (ctypes.c_float * n)(*([float(scale)] * n))
     rows, columns, dtypes = _shapes(matrices)
     dev = matrices[0].device
     if dev.type != "cuda":

@@ -521,3 +521,10 @@ def test_a_workspace_for_all_matrices_serves_some_of_them(dtype, shapes, fewer):
         assert (own.tensor[own.nbytes:] == 0xFF).all()
     _same(vt.vtrace_orthogonalize(gs, workspace=ws), whole)
     assert (ws.tensor[ws.nbytes:] == 0xFF).all()
+
+
+def test_scales_as_tensors():
+    gs = _mixed(25)
+    expect = vt.vtrace_orthogonalize(gs, 0.5)
+    for scale in (torch.tensor(0.5), torch.tensor(0.5, device="cuda"), torch.full((len(gs),), 0.5), np.array(0.5)):
+        _same(vt.vtrace_orthogonalize(gs, scale), expect)

@@ -2,6 +2,7 @@
 
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -79,3 +80,23 @@ def test_workspaces_of_other_calls_and_types_are_not_native(monkeypatch):
     with pytest.raises(ValueError, match="one or the other"):
         vt.vtrace_vocab_embed_grad(d, t, 5, accumulate_into=w, out=w)
     assert len(seen) == 1
+
+
+@pytest.mark.parametrize("scale", [torch.tensor(0.5), np.array(0.5), np.float32(0.5), 1, [0.5, 2.0], torch.tensor([0.5, 2.0])])
+def test_scales_of_updates_as_numbers_tensors_and_arrays(monkeypatch, scale):
+    """One, of no dimension, or one for each matrix: past the checks, to where the library is called."""
+    g = [torch.ones(3, 4), torch.ones(4, 2)]
+    with pytest.raises(ValueError, match="GPU"):
+        vt.vtrace_orthogonalize(g, scale)
+    with pytest.raises(ValueError, match="3 scales for 2"):
+        vt.vtrace_orthogonalize(g, [1.0, 2.0, 3.0])
+
+
+@pytest.mark.parametrize("given", [torch.tensor([1.5, -0.5, 0.25]), np.array([1.5, -0.5, 0.25]), torch.tensor([[1.5, -0.5, 0.25]] * 3)])
+def test_coefficients_as_tensors_and_arrays(given):
+    assert list(parameters._coefficients(given, 3)) == [1.5, -0.5, 0.25] * 3
+    if given.ndim == 1:
+        assert list(parameters._coefficients(given, 2)) == [1.5, -0.5, 0.25] * 2
+        for short in (given[:2], [given[0], given[1]], [1.5, given], given[0:1]):
+            with pytest.raises(ValueError, match="coefficients"):
+                parameters._coefficients(short, len(short))
