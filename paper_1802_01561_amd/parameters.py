@@ -98,16 +98,17 @@ def _tokens_shape(tokens, device):
 
 def vtrace_vocab_embed(vocab_weight, tokens, scale: float = 1.0, *, out_dtype=None, workspace=None,
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """scale * vocab_weight[tokens]: [T,B,H] of ``out_dtype`` (float32 or bfloat16; None: the
-    table's) from a table [V,H] of either type; zeros for NO_TOKEN, NaN for a token that is
-    not in the vocabulary.
+    """scale * vocab_weight[tokens]: [T,B,H] of ``out_dtype`` (float32 or bfloat16; None: that
+    of ``out`` or of the table) from a table [V,H] of either type; zeros for NO_TOKEN, NaN
+    for a token that is not in the vocabulary.
 
     ``workspace`` (any of this library's) is there for its error flag alone."""
     # As in tokens.py, native code takes the ordinary call, or declines.
     if stream is None and type(scale) is float and (workspace is None or isinstance(workspace, _CallWorkspace)):
         fast = _fast_call(vocab_weight)
         if fast:
-            wanted = out.dtype if type(out) is torch.Tensor else out_dtype or vocab_weight.dtype
+            given = out if type(out) is torch.Tensor else vocab_weight
+            wanted = given.dtype if out_dtype is None else out_dtype
             if wanted in _DTYPES:
                 device = fast.device()
                 r = fast.call_vocab_embed(fast.vocab_embed, vocab_weight, tokens, scale, wanted is torch.bfloat16, out,
@@ -121,7 +122,10 @@ def vtrace_vocab_embed(vocab_weight, tokens, scale: float = 1.0, *, out_dtype=No
         raise ValueError("vocab_weight must be [V, H]")
     V, H = vocab_weight.shape
     dev = vocab_weight.device
-    out_dtype = out.dtype if out is not None else vocab_weight.dtype if out_dtype is None else out_dtype
+    if out_dtype is None:
+        out_dtype = (vocab_weight if out is None else out).dtype
+    elif out is not None and out.dtype != out_dtype:
+        raise TypeError(f"out has dtype {out.dtype}, expected {out_dtype}")
     codes = _dtype_code(vocab_weight.dtype, "vocab_weight.dtype"), _dtype_code(out_dtype, "out_dtype")
     if dev.type != "cuda":
         raise ValueError("inputs must be on a GPU device")
@@ -145,9 +149,10 @@ def vtrace_vocab_embed_grad(d_embedded, tokens, vocab_size: int, scale: float = 
     """The table's gradient [V,H] from those of vtrace_vocab_embed's rows, [T,B,H] (float32 or
     bfloat16): the sum over each token's steps, times ``scale``.
 
-    ``accumulate_into`` [V,H], whose type then decides, is added to in place (rows of tokens
-    that steps have; the others are not touched) and returned; otherwise all of a tensor
-    of ``grad_dtype`` is written, rows that no step has with zeros."""
+    ``accumulate_into`` [V,H] is added to in place (rows of tokens that steps have; the others
+    are not touched) and returned; otherwise all of ``out`` or a new tensor is written, rows
+    that no step has with zeros.  ``grad_dtype`` is a new tensor's: that of ``accumulate_into``
+    or ``out`` decides otherwise."""
     if accumulate_into is not None and out is not None:
         raise ValueError("out and accumulate_into are one or the other")
     given = accumulate_into if out is None else out

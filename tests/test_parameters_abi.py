@@ -227,3 +227,14 @@ def test_orthogonalize_workspace_for_more_serves_less(L, dtype):
         for _ in range(10):
             assert size([s for s in shapes if r.random() < 0.7] or shapes[:1]) <= whole
         assert size(shapes[1:] or shapes) <= whole and size(shapes[::-1]) == whole
+
+
+def test_an_output_of_another_type_than_asked_for_is_refused():
+    w, t = torch.zeros(10, 64), torch.zeros(2, 3, dtype=torch.int32)
+    for dtype, other in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        out = torch.empty(2, 3, 64, dtype=dtype)
+        with pytest.raises(TypeError, match="out has dtype"):
+            vt.vtrace_vocab_embed(w, t, out_dtype=other, out=out)
+        for given in (None, dtype):
+            with pytest.raises(ValueError, match="GPU"):
+                vt.vtrace_vocab_embed(w, t, out_dtype=given, out=out)

@@ -100,3 +100,16 @@ def test_coefficients_as_tensors_and_arrays(given):
         for short in (given[:2], [given[0], given[1]], [1.5, given], given[0:1]):
             with pytest.raises(ValueError, match="coefficients"):
                 parameters._coefficients(short, len(short))
+
+
+def test_the_type_asked_for_reaches_native_code(monkeypatch):
+    """Which declines an output of another."""
+    seen = []
+    monkeypatch.setattr(parameters, "_fast_call", lambda first: _declines(seen))
+    t, w = torch.zeros((2, 3), dtype=torch.int32), torch.zeros(5, 8)
+    out = torch.zeros(2, 3, 8)
+    with pytest.raises(TypeError, match="out has dtype"):
+        vt.vtrace_vocab_embed(w, t, out_dtype=torch.bfloat16, out=out)
+    with pytest.raises(ValueError, match="GPU"):
+        vt.vtrace_vocab_embed(w, t, out=out.bfloat16())
+    assert [args[4] for args in seen] == [True, True]
