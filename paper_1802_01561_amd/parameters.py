@@ -120,6 +120,8 @@ def vtrace_vocab_embed(vocab_weight, tokens, scale: float = 1.0, *, out_dtype=No
         raise TypeError("vocab_weight must be a torch.Tensor")
     if vocab_weight.dim() != 2:
         raise ValueError("vocab_weight must be [V, H]")
+    if out is not None and not isinstance(out, torch.Tensor):
+        raise TypeError("out must be a torch.Tensor")
     V, H = vocab_weight.shape
     dev = vocab_weight.device
     if out_dtype is None:

@@ -238,3 +238,11 @@ def test_an_output_of_another_type_than_asked_for_is_refused():
         for given in (None, dtype):
             with pytest.raises(ValueError, match="GPU"):
                 vt.vtrace_vocab_embed(w, t, out_dtype=given, out=out)
+
+
+@pytest.mark.parametrize("out", [1.0, [torch.zeros(2, 3, 64)], "out"])
+def test_an_output_of_the_lookup_is_a_tensor(out):
+    w, t = torch.zeros(10, 64), torch.zeros(2, 3, dtype=torch.int32)
+    for out_dtype in (None, torch.float32):
+        with pytest.raises(TypeError, match="out must be a torch.Tensor"):
+            vt.vtrace_vocab_embed(w, t, out_dtype=out_dtype, out=out)
