@@ -17,6 +17,7 @@ import torch
 
 import paper_1802_01561_amd as vt
 from oracle import parameters as op
+from test_gpu_orthogonalize import check
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +139,56 @@ def test_bfloat16_matrices_keep_22_bits_from_step_to_step(m, n, steps, kernel, m
     half_step = torch.exp2(torch.floor(torch.log2(ref.abs().clamp(min=1e-30))) - 8)
     tol = half_step + 2.0 * (steps + 1) * (2.0 ** -22 * ref.abs() + 2.0 ** -47)
     assert ((got.double() - ref).abs() <= tol).all()
+
+
+def _half_steps(ref, dtype):
+    """Half the distance between the values of `dtype` around each element."""
+    return torch.exp2(torch.floor(torch.log2(ref.abs().clamp(min=1e-30))) - (8 if dtype is BF16 else 24))
+
+
+@pytest.mark.parametrize("m,n", [(1, 1), (2, 2), (4, 4), (3, 5), (1, 257), (300, 1), (16, 192), (31, 33), (32, 32), (256, 32), (32, 4096),
+                                 (20, 65536)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["strong", "normal"])
+@pytest.mark.parametrize("coefficients", [STEPS, ((1.5, -0.5, 0.0),) * 12])
+def test_few_rows_are_float64_up_to_one_rounding(m, n, dtype, kind, coefficients, monkeypatch):
+    """All steps of up to 32 rows in float64.  An entry of a 32 x 32 product has a rounding error of 32 2^-53
+    of the sizes that are summed, 12 at most: 2^-44.4.  Those of A beside small eigenvalues grow by a^2 with
+    each step that follows, 3.4445^8 = 2^14.3 until the last of five (the cubic's 1.5^22 = 2^12.9), and P
+    has |b| + 2 |c| t, at most 9, of them: 2^-27 of the result's norm, twice for what the earlier steps' add.
+    Then comes the result's own rounding, to one bit more where that carries it over a power of two."""
+    monkeypatch.delenv("VTRACE_KERNEL", raising=False)
+    g = matrix(m + n, m, n, dtype, kind)
+    got, = vt.vtrace_orthogonalize([g], steps=len(coefficients), coefficients=coefficients)
+    ref = exact(g, coefficients)
+    more, half_steps = 2.0 ** -26 * _norm(ref), _half_steps(ref, dtype)
+    near = _half_steps(ref.abs() + more, dtype)
+    err = (got.double() - ref).abs()
+    assert (err <= torch.maximum(half_steps, near) + more).all()
+    assert _norm(err) <= 1.01 * _norm(torch.maximum(half_steps, near)) + more
+
+
+@pytest.mark.parametrize("m,n", [(65536, 32768), (65536, 5000), (4000, 65536)])
+def test_both_parts_of_the_largest_float32_matrices(m, n, monkeypatch):
+    """A small matrix's rows and columns among zeros, from the first to the last: the same result there and zeros
+    elsewhere.  With either part of an operand lost or from elsewhere it would be off by 2^-12 and more;
+    the bound is that of the small matrix, whose sums' terms are the same (each of them is added by itself,
+    no more than 200 roundings of 2^-24, for which the bound has 15)."""
+    monkeypatch.delenv("VTRACE_KERNEL", raising=False)
+    steps = STEPS[:3]
+    small = matrix(m + n, 200, 150, F32, "strong")
+    g = torch.Generator(device="cuda").manual_seed(n)
+
+    def places(size, count):
+        p = torch.randperm(size - 2, generator=g, device="cuda")[:count - 2] + 1
+        return torch.cat([torch.tensor([0, size - 1], device="cuda"), p]).sort().values
+
+    rows, columns = places(m, 200), places(n, 150)
+    large = torch.zeros((m, n), device="cuda")
+    large[rows[:, None], columns[None, :]] = small
+    ws = vt.OrthogonalWorkspace([large])
+    vt.vtrace_orthogonalize([large], steps=3, out=[large], workspace=ws)
+    got = large[rows[:, None], columns[None, :]]
+    check(small, got, steps=steps)
+    large[rows[:, None], columns[None, :]] = 0.0
+    assert all(int(torch.count_nonzero(large[at:at + 8192])) == 0 for at in range(0, m, 8192))
