@@ -175,7 +175,7 @@ def test_nan_and_infinity_stay_in_their_rows():
     assert torch.isnan(got[1, 3]) and torch.isinf(got[3, 4]) and torch.isfinite(got).sum() == got.numel() - 2
 
 
-@pytest.mark.parametrize("most,lengths,H", [(8192, (8191, 5000, 8192, 3), 2048), (20000, (16385, 16384, 19999, 700), 264)])
+@pytest.mark.parametrize("most,lengths,H", [(8192, (8191, 5000, 8192, 3), 2048), (20000, (16385, 16384, 19999, 700, 12289, 12288), 264)])
 def test_a_workspace_for_the_longest_batch_serves_the_others(most, lengths, H):
     """Batches whose chunks are shorter, and their partial sums as many or more; ranked and sorted ones."""
     V = 300
@@ -188,10 +188,12 @@ def test_a_workspace_for_the_longest_batch_serves_the_others(most, lengths, H):
         check_grad(d[:N], tokens[:N].cpu().numpy(), V, 1.0, got)
 
 
+@pytest.mark.parametrize("N", [12288, 16384])
 @pytest.mark.parametrize("V", [40, 511, 512, 70001])
-def test_ranked_and_sorted_steps_are_in_the_same_order(V):
-    """One step more, without a token, is sorted in another way into the same order: the same sums, bit for bit."""
-    N, H = 16384, 16
+def test_ranked_and_sorted_steps_are_in_the_same_order(N, V):
+    """Where one step more, without a token, is sorted in another way, it is into the same order: the same
+    sums, bit for bit."""
+    H = 16
     d = _normal(V, (N + 1, 1, H), F32).cuda()
     t = torch.from_numpy(_tokens(V, N + 1, V, "text", 0.0)).cuda().view(N + 1, 1)
     t[N] = vt.NO_TOKEN
