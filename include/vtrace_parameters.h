@@ -71,7 +71,8 @@ vtrace_status vtrace_vocab_embed_grad(
 
 /*
  * Newton-Schulz products that leave a matrix's singular vectors and bring its singular
- * values near 1, for each matrix G of a list on its own:
+ * values near 1 (the iteration of Bjorck and Bowie, 1971, with the quintic's coefficients of
+ * Jordan et al., "Muon", 2024), for each matrix G of a list on its own:
  *   X = G / max(|G|, epsilon), |G| = sqrt(sum of squares);
  *   `steps` times, with coefficients a, b, c of that step:
  *     A = X X^T,  X <- a X + (b A + c A A) X   (a singular value s becomes a s + b s^3 + c s^5);
@@ -80,7 +81,7 @@ vtrace_status vtrace_vocab_embed_grad(
  *   count         0 .. 2^16 matrices; matrices, outputs, rows, columns, dtypes and scales are
  *                 HOST arrays of that length, coefficients one of 3*steps floats, all
  *                 read during the call
- *   matrices      device pointers to rows[i] x columns[i] (each 0 .. 65536, together up to 2^31)
+ *   matrices      device pointers to rows[i] x columns[i] (each 0 .. 65536, their product up to 2^31)
  *                 contiguous elements of dtypes[i] (VTRACE_F32 or VTRACE_BF16), element-aligned
  *                 (NULL if there are none)
  *   outputs       where the results go, of the same sizes and types.  An output may be its own
@@ -99,14 +100,17 @@ vtrace_status vtrace_vocab_embed_grad(
  * result's rounding (as long as the coefficients a multiply to at most 8192 over the steps).
  * Otherwise X has 22 bits (bfloat16 matrices) or is float32 from step to step, sums of
  * products are float32, products take float16 operands of a fixed scale, for float32 matrices
- * in two parts (22 bits) each, and the diagonals of the symmetric matrices are float32.  Against
- * products in 64 bits results of bfloat16 matrices are off by little more than their own
- * rounding (1.7e-3 to 2.3e-3 for 5 steps of the quintic), and those of float32 matrices by up
- * to 1.3e-6, in relation to their norm, down to norms of epsilon: far below it, where singular
- * values stay small, results of bfloat16 matrices are off by up to 2^-36 each.  Where terms are
- * all alike (matrices of a few values in large blocks) roundings do not cancel: up to 9e-3 and,
- * beyond 2048 x 2048, 3.5e-4.  NaN or Inf in a matrix makes all of its result NaN, and that of no
- * other matrix.
+ * in two parts (22 bits) each, and the diagonals of the symmetric matrices are float32.  In
+ * relation to their norm, against products in 64 bits and for 5 steps of the quintic, results of
+ * bfloat16 matrices are off by little more than their own rounding (1.67e-3 to 1.85e-3, and where
+ * one size is some 30 and the other thousands 1.96e-3; the rounding is 1.66e-3), and those of
+ * float32 matrices by 3e-7 to 9e-7 (2.4e-6 measured where all but the largest singular values are
+ * a hundredth of those).  That holds down to norms of epsilon: far below it, where singular values
+ * stay small, results of bfloat16 matrices are off by up to 2^-36 each.  Where terms are all
+ * alike (matrices of a few values in large blocks) roundings do not cancel, and results are off by
+ * up to 2e-2 (bfloat16); float32 2e-5 where sizes are some hundreds, 3e-4 for thousands and 1.1e-3
+ * for 65536 x 32768.  NaN or Inf in a matrix makes all of its result NaN, and that of no other
+ * matrix.
  */
 size_t vtrace_orthogonalize_workspace_bytes(int64_t count, const int64_t* rows, const int64_t* columns,
                                             const int32_t* dtypes);

@@ -14,14 +14,19 @@
 // are kept out of the operands, in float32:
 //   with A = D + O:  B = b (D + O) + c (D D + D O + O D + O O),   B X = diag(B) X + offdiag(B) X,
 // where only O O and offdiag(B) X are products on the matrix cores (with the diagonals in the
-// operands 1.7e-3 to 2.8e-3 off, without 2e-4 to 7e-4, and one rounding to bfloat16 is 1.7e-3:
-// results of 33 rows and more are 1.7e-3 to 2.3e-3 off).
-// Float32 matrices have operands in two parts, high + low, and three products for each: 4e-7
-// to 1.3e-6 off, from the float32 sums (a library's float32 products 2e-6 to 7e-5: small singular
-// values grow by 3.44 a step, and rounding errors beside the largest with them).  Of matrices of a few
-// values in large blocks, whose roundings do not cancel, results are up to 9e-3 (bfloat16) and, in tiles
-// of 256 or 128, 3.5e-4 off (a library's 3e-3); sums over 256 k apiece, which tiles of 64 and 32 have
-// (8e-6), would leave 256 x 256 no registers, and tiles of 128 take 24% longer for 4096 x 4096.
+// operands 1.7e-3 to 2.8e-3 off, without 2e-4 to 7e-4, and one rounding to bfloat16 is 1.66e-3:
+// results of 33 rows and more are 1.67e-3 to 1.85e-3 off, of 34 x 3194 1.96e-3).
+// Float32 matrices have operands in two parts, high + low, and three products for each: 3e-7
+// to 9e-7 off, from X's own rounding and the float32 sums (a library's float32 products 1.6e-6 to 3.6e-6:
+// small singular values grow by 3.44 a step, and rounding errors beside the largest with them; where most
+// are a hundredth of the largest, 2048 x 2048, 2.4e-6 and the library's 1.9e-5).
+//
+// Of matrices of a few values in large blocks the roundings are alike and do not cancel: results of bfloat16
+// ones are up to 8.8e-3 off (steps one by one) and 1.9e-2 (the first two at once).  Of float32 ones tiles
+// of 64 and 32, whose sums are over 256 k apiece, up to 1.8e-5, the others 1.9e-4 for 2048 x 2048, 3.2e-4 for 4096 x
+// 8192 and 1.1e-3 for 65536 x 32768 (a library's products 8e-5 for 1024 x 1024, 5e-4 for 4096 x 4096, where this
+// has 2.5e-6 and 3.4e-5).  Such sums in tiles of 256 have no registers; in tiles of 128 half of them go
+// to scratch memory, and 4096 x 4096 takes 46% longer.
 //
 // A and B are symmetric: their tiles on and below the diagonal are computed, and stored twice.
 #include "orthogonalize_few.hpp"
@@ -230,18 +235,20 @@ int64_t tiles_in(const Entry& e, int kind, int size) {
 }
 
 // What a launch of one kind takes (us) in tiles of 256 or 128: rounds of as many as there is room for.
-// Fewer than that take less a step: 72 tiles of 256 1.0 (float32 1.15), 256 of them 1.56; of 128 one a
-// CU 0.8, two 1.0.  What a tile costs beside its steps is its fill and its stores.  bfloat16, x1 / x2
-// (steps one by one, two at once) in tiles of 64, 128, 256, us: 16 of 1024 x 1024 999 / -, 666 / 794,
-// 647 / 749; 2 of 2048 x 2048 774 / -, 542 / 617, 848 / 995; 2 of 3000 x 3000 2675 / -, 1613 / 1780, 1499 /
-// 1540; 8 of 1024 x 4096 1751 / -, 887 / 756, 1123 / 1041; float32 2 of 2048 x 2048 2058 / -, 1453 / 1659,
-// 2059 / 2530.
+// Fewer than that take less a step, gradually (A of 64 and 128 steps, us a step): 36 to 72 tiles of 256 1.1
+// (float32 1.2 to 1.35), 100 to 144 1.35 (1.45 to 1.5), 160 1.4 to 1.55 (1.65), 250 1.55 to 1.8 (1.75 to
+// 1.85); of 128 36 to 144 0.45 to 0.5, 252 to 272 0.5 to 0.65, 360 to 410 0.85 to 0.9, 470 1.0.  Two values
+// of each stand for that here, with the border between.  What a tile costs beside its steps is its fill
+// and its stores.  bfloat16, x1 / x2 (steps one by one, the first two at once) in tiles of 64, 128, 256, us: 16 of
+// 1024 x 1024 1063 / 1122, 728 / 785, 690 / 728; 2 of 2048 x 2048 812 / 853, 577 / 610, 851 / 924; 2 of 3000 x 3000
+// 2699 / 2707, 1692 / 1783, 1602 / 1623; 8 of 1024 x 4096 1759 / 1575, 949 / 896, 1182 / 1132; float32 2 of 2048 x
+// 2048 2132 / 2219, 1494 / 1600, 2195 / 2404.
 //
 // Tiles of equal steps that would leave a round behind theirs mostly empty are split along k, into up to
 // as many pieces as fill it, if that is a fifth less with what their sums cost (us, of tiles of 256: five
 // pieces of 13 steps take as long as one of 64, 20 to store and 12 a piece to join; six of 43 150 less
 // than one of 256).  A of 4 matrices of 4096 x 4096 and 2 of 4096 x 16384, which has 16 of 272 long tiles too
-// many: 1030 -> 780 us.  `split`: into so many wherever there are as many steps.
+// many: 1030 -> 790 us.  `split`: into so many wherever there are as many steps.
 // `room`: bytes for the pieces' sums.
 double tiles_cost(const Table& t, int kind, int size, int passes, int split, int64_t room, Units* units) {
   double all = 0.0;
@@ -309,8 +316,8 @@ double tiles_cost(const Table& t, int kind, int size, int passes, int split, int
 
 // The same in the small matrices' kernels' tiles of 64 or 32: a launch, and the tile that has a CU for
 // itself, or all rounds of them.
-// 1024 x 1024, us with tiles of 32, 64, 128: one bfloat16 matrix 189, 153, 322, four 503, 353, 304,
-// eight 927, 573, 393; float32 268, 246, 635, two 421, 458, 642, four 735, 756, 655.
+// 1024 x 1024, us with tiles of 32, 64, 128: one bfloat16 matrix 192, 159, 279, four 511, 360, 301,
+// eight 940, 587, 377; float32 270, 248, 625, two 439, 466, 633, four 758, 775, 651.
 double small_cost(const Table& t, int kind, int size, bool pair) {
   double work = 0.0, longest = 0.0, tiles = 0.0;
   for (int i = 0; i < t.count; ++i) {
@@ -541,7 +548,8 @@ bool few_rows_ok(const OrthoStep* steps, int count) {
 // The first two steps alone.  Their X is of norm 1, so that most singular values are small and Q with
 // them, and the rounding errors are those of steps one by one (2048 x 2048 bfloat16 1.70e-3 off, of which
 // one rounding is 1.66e-3).  Later most are near 1, Q is near -a a', and a result has its errors in full:
-// with the last two of five at once as well 1.97e-3, of 4096 x 4096 2.28e-3 where this has 1.69e-3.
+// with the last two of five at once as well 1.97e-3, of 4096 x 4096 2.28e-3 where this has 1.69e-3 (and 5 to 8%
+// less time).  One layer of hidden size 4096 13.5 ms, one by one 14.15; 24 matrices of hidden size 1024 1565 us, 1665.
 template <typename T, bool kPair>
 hipError_t launch_group(const OrthoItem* items, int count, const OrthoStep* steps, int step_count, float epsilon, char* ws,
                         hipStream_t st) {

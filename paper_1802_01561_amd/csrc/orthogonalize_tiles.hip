@@ -82,10 +82,10 @@ __device__ __forceinline__ s16x4 transposed_read(const char* lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec)lds);
 }
 
-// Float16 products on the matrix cores bound these kernels where k is long: A of 4 matrices of 4096 x 4096
-// and 2 of 4096 x 16384 takes 780 us (1.06 PFLOP/s of the halves that are asked for, whose diagonal
-// tiles are computed whole), A A 470 (0.88), A A of 24 matrices of hidden size 1024 47 (0.55: one round
-// of 16 steps, 25 us, beside a tile's fill and stores, 21).
+// Float16 products on the matrix cores and the operands' copies bound these kernels where k is long: A of 4
+// matrices of 4096 x 4096 and 2 of 4096 x 16384 takes 790 us (1.04 PFLOP/s of the halves that are asked for,
+// whose diagonal tiles are computed whole; matrix units busy 52%), A A 475 (0.87, 42%), A A of 24 matrices
+// of hidden size 1024 55 (0.47, 23%: one round of 16 steps, 25 us, beside a tile's fill and stores).
 //
 // A symmetric matrix: the tiles (i, j), j <= i, of M N, rows of both "along".  A lane of the MFMA
 // layout holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
@@ -268,9 +268,9 @@ __global__ __launch_bounds__(kGemmThreads, kSize == kTile ? 1 : 2) void ortho_sy
   __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy into LDS outlives the workgroup
 }
 
-// 4 of 4096 x 4096 and 2 of 4096 x 16384 1485 us (1.11 PFLOP/s), 24 matrices of hidden size 1024 160
-// (0.64: X's 8 bytes an element beside 16 steps of products; four columns a lane, 8-byte loads and stores, took
-// 1630 and 193; rows fetched further ahead, and workgroups that start at different times, gain nothing).
+// 4 of 4096 x 4096 and 2 of 4096 x 16384 1500 us (1.10 PFLOP/s, matrix units busy 52%), 24 matrices of hidden size
+// 1024 166 (0.62, 27%: X's 8 bytes an element beside 16 steps of products; four columns a lane, 8-byte loads and
+// stores, took 9 and 20% more; rows fetched further ahead, and workgroups that start at different times, gain nothing).
 // X <- a X + B X, or of the last step the result: m runs along X's columns (X "across"), n along
 // its rows (B "along").  A lane holds columns j + 8 g + 32 (m / 2) + 4 (m % 2) + 0..3 of row i + 16 n + s.
 template <typename Out, bool kPair, bool kLast, int kSize>

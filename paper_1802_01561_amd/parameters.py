@@ -29,7 +29,7 @@ __all__ = [
     "vtrace_vocab_embed_grad_workspace_bytes",
 ]
 
-# Coefficients of the Newton-Schulz steps: s -> a s + b s^3 + c s^5 with the steepest slope at
+# Coefficients of the Newton-Schulz steps (Jordan et al., "Muon", 2024): s -> a s + b s^3 + c s^5 with the steepest slope at
 # 0 for which singular values near 1 stay there.
 QUINTIC = (3.4445, -4.7750, 2.0315)
 
